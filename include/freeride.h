@@ -578,6 +578,131 @@ int fr_stage_set_filler(fr_stage* s, void* stream, uint32_t workgroups, uint64_t
    *n_out = their number. */
 int fr_stage_op_times(fr_stage* s, uint64_t* ns_host, size_t cap, size_t* n_out);
 
+/* ------------------------------------------------------------------ text generation as a side task */
+/*
+ * What one step of generating text needs beside matrix products (fr_gemm_bf16): keys and values appended to a cache of
+ * pages with the position rotation on the way, attention of a batch whose sequences share a prefix, and the choice of a
+ * token.  A step is one token for every sequence: short, of known length, resumable - the shape of work a bubble takes
+ * (examples/generate_in_bubbles.py runs it as a side task).  All calls are asynchronous on `stream`, allocate nothing and
+ * keep nothing between calls, so they can be captured in a HIP graph; all pointers are device pointers of the current
+ * device.  Numbers on the device (lengths, page ids, slots, positions) are not seen by the host: the kernels bound them
+ * as stated at each, so that no value of theirs leads outside the arrays.
+ */
+#define FR_DTYPE_BF16 0
+#define FR_DTYPE_F16  1
+#define FR_DTYPE_F32  2
+
+/* A cache of keys and values in pages of page_size slots.  Element (page, head, slot, i) of K lies at
+   k[page * page_stride + head * head_stride + slot * slot_stride + i], of V likewise: pages of a head side by side, heads of
+   a slot side by side, K and V in one array are all views of that.  Strides are in elements, multiples of 8, not negative;
+   k and v are 16-byte aligned. */
+typedef struct fr_kv_pages {
+    void*    k;
+    void*    v;
+    int64_t  n_pages;              /* 1 .. 2^31 - 1                                                           */
+    int64_t  page_stride, head_stride, slot_stride;
+    int32_t  n_kv_heads;           /* 1 .. 1024                                                               */
+    int32_t  head_dim;             /* 64 or 128                                                               */
+    int32_t  page_size;            /* a power of two, 1 .. 4096                                               */
+    int32_t  dtype;                /* FR_DTYPE_BF16 or FR_DTYPE_F16                                           */
+} fr_kv_pages;
+
+#define FR_ROTARY_HALVES 0         /* element i turns with element i + rotary_dim / 2                         */
+#define FR_ROTARY_PAIRS  1         /* element 2 i turns with element 2 i + 1                                  */
+/*
+ * fr_kv_append: K[slot[t]] = rotated k[t], V[slot[t]] = v[t], q_out[t] = rotated q[t] for tokens t < n_tokens.
+ * A rotation takes (a, b) to (a c - b s, b c + a s) with c = rotary[position[t]][i], s = rotary[position[t]][rotary_dim / 2 + i],
+ * in 32 bits, rounded once to the cache's type; elements from rotary_dim on are copied.  Values are copied bit by bit.
+ * A token whose slot is negative or beyond the cache is padding: nothing is stored for it (its q_out is written).  A
+ * position below 0 or from n_positions on counts as the nearest one that the table has.
+ */
+typedef struct fr_kv_append_desc {
+    fr_kv_pages cache;
+    const void* k;                 /* [n_tokens][n_kv_heads][head_dim], k_stride elements from token to token */
+    const void* v;
+    const void* q;                 /* [n_tokens][n_q_heads][head_dim]; NULL: no queries (n_q_heads 0)         */
+    void*       q_out;             /* may be q itself with the same stride                                    */
+    int64_t     k_stride, v_stride, q_stride, q_out_stride;   /* elements, multiples of 8; rows of a call are apart */
+    const int64_t* slot;           /* page * page_size + slot of the page; distinct where not negative        */
+    const int32_t* position;       /* NULL: not rotated (rotary_dim 0)                                        */
+    const float*   rotary;         /* [n_positions][rotary_dim]: cosines, then sines; 16-byte aligned         */
+    int32_t     n_positions, rotary_dim;      /* rotary_dim: a multiple of 16 up to head_dim                  */
+    int32_t     style;             /* FR_ROTARY_*                                                             */
+    int32_t     n_tokens;          /* 0: nothing to do                                                        */
+    int32_t     n_q_heads;         /* 0 .. 1024                                                               */
+    int32_t     reserved;
+} fr_kv_append_desc;
+int fr_kv_append(const fr_kv_append_desc* d, void* stream);
+
+/*
+ * fr_attend_shared: attention of a batch of sequences behind one shared prefix.  The sequences' tokens lie one after the
+ * other, those of sequence b at q_begin[b] .. q_begin[b + 1]; they are the last of its own_len[b] own keys.  Its token i of
+ * t sees the prefix_len shared keys and its first own_len[b] - t + 1 + i own ones (all of it counted from 0; with more
+ * tokens than own keys the first tokens see the prefix only).  With scores x_j = scale <q, k_j> over the keys it sees,
+ *     out = sum_j exp(x_j) v_j / sum_j exp(x_j),    lse = log sum_j exp(x_j);
+ * a token that sees nothing gets zeros and -infinity.  Query head h reads key head h / (n_q_heads / n_kv_heads).  Slots
+ * behind a length are never used, whatever they hold; neither does a key that a token may not see change its result.
+ * Scores, softmax and sums are held in 32 bits; the weights exp(x_j - max) are rounded to the cache's type for the
+ * product with v, as is the result.
+ * Bounds on the device's numbers: a page id outside the cache counts as the nearest one inside, own_len is cut to
+ * 0 .. max_own_len, q_begin to 0 .. n_tokens, a sequence's tokens beyond max_q are not computed.
+ */
+typedef struct fr_attend_desc {
+    fr_kv_pages cache;
+    const void* q;                 /* [n_tokens][n_q_heads][head_dim] of the cache's type                     */
+    void*       out;               /* as q; not q itself                                                      */
+    float*      lse;               /* [n_tokens][n_q_heads], or NULL                                          */
+    int64_t     q_stride, out_stride;         /* elements from token to token, multiples of 8                 */
+    const int32_t* q_begin;        /* [n_seqs + 1] ascending; NULL: one token each (n_tokens = n_seqs)        */
+    const int32_t* prefix_pages;   /* page ids of the prefix; NULL if prefix_len is 0                         */
+    const int32_t* pages;          /* [n_seqs], pages_stride apart: page ids of the own keys; NULL if max_own_len is 0 */
+    const int32_t* own_len;        /* [n_seqs]; NULL if max_own_len is 0                                      */
+    int64_t     pages_stride;      /* >= ceil(max_own_len / page_size)                                        */
+    int32_t     n_tokens, n_seqs;  /* 0: nothing to do                                                        */
+    int32_t     n_q_heads;         /* a multiple of n_kv_heads, up to 1024                                    */
+    int32_t     max_q;             /* upper bound of a sequence's tokens in this call, >= 1                   */
+    int32_t     prefix_len, max_own_len;      /* >= 0, together below 2^31 - 4096                             */
+    float       scale;             /* positive and finite                                                     */
+    int32_t     reserved;
+    void*       workspace;         /* fr_attend_shared_workspace_bytes of it, 256-byte aligned; free again when
+                                      the call's work on the stream is done                                   */
+    uint64_t    workspace_bytes;
+} fr_attend_desc;
+/* Reads the sizes of d only (no pointer), so that a program can ask for its largest call. */
+int fr_attend_shared_workspace_bytes(const fr_attend_desc* d, uint64_t* bytes_out);
+int fr_attend_shared(const fr_attend_desc* d, void* stream);
+
+/*
+ * fr_sample: one token for every row of logits, from a given random number.  With m the row's largest logit (NaN counts
+ * as -infinity): the weight of entry i is w_i = exp((l_i - m) * (1 / temperature)), 1 where l_i = m, 0 where l_i is
+ * -infinity, its mass the integer floor(w_i 2^43).  Entries are ordered by falling logit, equal ones by rising index; kept are
+ *   the first top_k (all, if top_k <= 0), of these
+ *   the shortest prefix that holds at least ceil(top_p * their mass), one entry at least (all, unless top_p < 1), of these
+ *   all but those with w_i < min_p (min_p above 1 counts as 1);
+ * the token is the lowest index i such that the kept masses up to i exceed floor(uniform * the kept mass).  Masses being
+ * integers, the token does not depend on the order in which they are added up.  temperature <= 0 (or NaN) takes the largest
+ * logit, the lowest index of equals.  A row without any logit above -infinity gives -1.
+ */
+typedef struct fr_sample_desc {
+    const void*    logits;         /* [n_rows], row_stride elements apart; aligned to its type                */
+    int64_t        row_stride;     /* >= n_vocab                                                              */
+    int32_t        dtype;          /* FR_DTYPE_BF16, _F16 or _F32                                             */
+    int32_t        n_rows;         /* 0: nothing to do                                                        */
+    int32_t        n_vocab;        /* 1 .. 2^19                                                               */
+    int32_t        reserved;
+    const float*   temperature;    /* [n_rows]; NULL: 1                                                       */
+    const int32_t* top_k;          /* [n_rows]; NULL: off                                                     */
+    const float*   top_p;          /* [n_rows]; NULL: off                                                     */
+    const float*   min_p;          /* [n_rows]; NULL: off                                                     */
+    const float*   uniform;        /* [n_rows] in [0, 1); below 0 or NaN counts as 0, 1 and above as just below 1 */
+    int32_t*       token;          /* [n_rows]                                                                */
+    void*          workspace;      /* fr_sample_workspace_bytes of it, 256-byte aligned; NULL if that is 0    */
+    uint64_t       workspace_bytes;
+} fr_sample_desc;
+/* Reads dtype, n_rows and n_vocab of d only. */
+int fr_sample_workspace_bytes(const fr_sample_desc* d, uint64_t* bytes_out);
+int fr_sample(const fr_sample_desc* d, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

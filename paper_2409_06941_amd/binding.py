@@ -12,6 +12,8 @@ FR_EV_INIT, FR_EV_CHUNK, FR_EV_IDLE, FR_EV_MISS, FR_EV_OVERRUN, FR_EV_REFUSED = 
 FR_PR_SEG_VERTEX, FR_PR_SEG_SCATTER, FR_PR_SEG_GATHER, FR_PR_SEG_FINISH = 0, 1, 2, 3
 FR_LOAD_BUSYWAIT, FR_LOAD_GPT = 0, 1
 FR_SCHED_1F1B, FR_SCHED_GPIPE, FR_SCHED_INTERLEAVED = 0, 1, 2
+FR_DTYPE_BF16, FR_DTYPE_F16, FR_DTYPE_F32 = 0, 1, 2
+FR_ROTARY_HALVES, FR_ROTARY_PAIRS = 0, 1
 
 _ERR_NAMES = {0: "FR_OK", -1: "FR_ERR_ARG", -2: "FR_ERR_STATE", -3: "FR_ERR_NOMEM", -4: "FR_ERR_OOM",
               -5: "FR_ERR_OVERRUN", -6: "FR_ERR_HIP"}
@@ -122,6 +124,35 @@ class fr_epoch_result(C.Structure):
                 ("n_bubbles", C.c_uint32), ("overruns", C.c_uint32), ("reserved", C.c_uint32)]
 
 
+class fr_kv_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int64), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("slot_stride", C.c_int64), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("dtype", C.c_int32)]
+
+
+class fr_kv_append_desc(C.Structure):
+    _fields_ = [("cache", fr_kv_pages), ("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("q_out", C.c_void_p),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_stride", C.c_int64), ("q_out_stride", C.c_int64),
+                ("slot", C.c_void_p), ("position", C.c_void_p), ("rotary", C.c_void_p), ("n_positions", C.c_int32),
+                ("rotary_dim", C.c_int32), ("style", C.c_int32), ("n_tokens", C.c_int32), ("n_q_heads", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class fr_attend_desc(C.Structure):
+    _fields_ = [("cache", fr_kv_pages), ("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("q_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("q_begin", C.c_void_p), ("prefix_pages", C.c_void_p), ("pages", C.c_void_p),
+                ("own_len", C.c_void_p), ("pages_stride", C.c_int64), ("n_tokens", C.c_int32), ("n_seqs", C.c_int32),
+                ("n_q_heads", C.c_int32), ("max_q", C.c_int32), ("prefix_len", C.c_int32), ("max_own_len", C.c_int32),
+                ("scale", C.c_float), ("reserved", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class fr_sample_desc(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("row_stride", C.c_int64), ("dtype", C.c_int32), ("n_rows", C.c_int32),
+                ("n_vocab", C.c_int32), ("reserved", C.c_int32), ("temperature", C.c_void_p), ("top_k", C.c_void_p),
+                ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("uniform", C.c_void_p), ("token", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
 # name -> (restype, argtypes); every symbol the header declares
 SIGNATURES = {
     "fr_create": (C.c_int, [C.POINTER(fr_config), C.POINTER(C.c_void_p)]),
@@ -174,6 +205,11 @@ SIGNATURES = {
     "fr_stage_run_epoch": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(fr_epoch_result)]),
     "fr_stage_set_filler": (C.c_int, [C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint64]),
     "fr_stage_op_times": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64), C.c_size_t, C.POINTER(C.c_size_t)]),
+    "fr_kv_append": (C.c_int, [C.POINTER(fr_kv_append_desc), C.c_void_p]),
+    "fr_attend_shared_workspace_bytes": (C.c_int, [C.POINTER(fr_attend_desc), C.POINTER(C.c_uint64)]),
+    "fr_attend_shared": (C.c_int, [C.POINTER(fr_attend_desc), C.c_void_p]),
+    "fr_sample_workspace_bytes": (C.c_int, [C.POINTER(fr_sample_desc), C.POINTER(C.c_uint64)]),
+    "fr_sample": (C.c_int, [C.POINTER(fr_sample_desc), C.c_void_p]),
 }
 
 _lib = None
@@ -517,3 +553,139 @@ class Stage:
         if self.handle:
             _check(lib().fr_stage_destroy(self.handle), "fr_stage_destroy")
             self.handle = C.c_void_p()
+
+
+def _dtype(x):
+    """FR_DTYPE_* of a torch tensor."""
+    name = str(x.dtype)
+    if name not in ("torch.bfloat16", "torch.float16", "torch.float32"):
+        raise TypeError("%s: the library takes bfloat16, float16 and float32" % name)
+    return {"torch.bfloat16": FR_DTYPE_BF16, "torch.float16": FR_DTYPE_F16, "torch.float32": FR_DTYPE_F32}[name]
+
+
+def _typed(x, name, what, like=None):
+    """A tensor whose elements lie side by side and are of a type the C side cannot see."""
+    if x is None:
+        return None
+    if str(x.dtype) != "torch." + what or x.stride(-1) != 1 and x.shape[-1] > 1:
+        raise TypeError("%s: %s elements side by side are needed" % (name, what))
+    if like is not None and tuple(x.shape) != tuple(like):
+        raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(like), tuple(x.shape)))
+    return x
+
+
+def _rows(x, name, shape, dtype):
+    """Stride between tokens of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
+    if tuple(x.shape) != tuple(shape):
+        raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(shape), tuple(x.shape)))
+    if _dtype(x) != dtype:
+        raise TypeError("%s: not of the cache's type" % name)
+    if x.numel() and (x.shape[2] > 1 and x.stride(2) != 1 or x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise ValueError("%s: heads of a token have to lie side by side" % name)
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
+class KvPages:
+    """fr_kv_pages of two torch tensors [n_pages, n_kv_heads, page_size, head_dim] with the same strides (views are fine)."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v: [n_pages, n_kv_heads, page_size, head_dim], alike in shape, strides and type")
+        if k.stride(3) != 1:
+            raise ValueError("the elements of a head have to lie side by side")
+        d = fr_kv_pages()
+        d.k, d.v = _ptr(k), _ptr(v)
+        d.n_pages, d.n_kv_heads, d.page_size, d.head_dim = k.shape
+        d.page_stride, d.head_stride, d.slot_stride = k.stride()[:3]
+        d.dtype = _dtype(k)
+        self.desc = d
+        self._keep = (k, v)
+
+
+def fr_kv_append(cache, k, v, slot, q=None, q_out=None, position=None, rotary=None, style=FR_ROTARY_HALVES, stream=None):
+    d = fr_kv_append_desc()
+    c = d.cache = cache.desc
+    T = k.shape[0]
+    d.n_tokens = T
+    d.k_stride, d.v_stride = (_rows(x, n, (T, c.n_kv_heads, c.head_dim), c.dtype) for x, n in ((k, "k"), (v, "v")))
+    d.k, d.v = _ptr(k), _ptr(v)
+    if q is not None:
+        d.n_q_heads = q.shape[1]
+        d.q_stride = _rows(q, "q", (T, d.n_q_heads, c.head_dim), c.dtype)
+        d.q_out_stride = _rows(q_out, "q_out", (T, d.n_q_heads, c.head_dim), c.dtype)
+        d.q, d.q_out = _ptr(q), _ptr(q_out)
+    d.slot = _ptr(_typed(slot, "slot", "int64", (T,)))
+    if rotary is not None:
+        d.n_positions, d.rotary_dim = rotary.shape
+        if not rotary.is_contiguous():
+            raise ValueError("rotary: rows have to lie side by side")
+        d.rotary = _ptr(_typed(rotary, "rotary", "float32"))
+        d.position = _ptr(_typed(position, "position", "int32", (T,)))
+    d.style = style
+    return _check(lib().fr_kv_append(C.byref(d), _stream(stream)), "fr_kv_append")
+
+
+def _attend_sizes(cache, q, n_seqs, prefix_len, max_own_len, max_q):
+    d = fr_attend_desc()
+    d.cache = cache.desc
+    d.n_tokens, d.n_q_heads = q.shape[0], q.shape[1]
+    d.n_seqs, d.prefix_len, d.max_own_len, d.max_q = n_seqs, prefix_len, max_own_len, max_q
+    return d
+
+
+def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, max_q=1):
+    """q: a tensor of the call's shape (only its shape is read)."""
+    d, out = _attend_sizes(cache, q, n_seqs, prefix_len, max_own_len, max_q), C.c_uint64()
+    _check(lib().fr_attend_shared_workspace_bytes(C.byref(d), C.byref(out)), "fr_attend_shared_workspace_bytes")
+    return out.value
+
+
+def fr_attend_shared(cache, q, out, pages, own_len, scale, prefix_len=0, max_own_len=0, prefix_pages=None, q_begin=None,
+                     max_q=1, lse=None, workspace=None, stream=None):
+    c = cache.desc
+    n_seqs = q.shape[0] if q_begin is None else q_begin.shape[0] - 1
+    d = _attend_sizes(cache, q, n_seqs, prefix_len, max_own_len, max_q)
+    d.q_stride, d.out_stride = (_rows(x, n, (q.shape[0], q.shape[1], c.head_dim), c.dtype) for x, n in ((q, "q"), (out, "out")))
+    d.q, d.out, d.scale = _ptr(q), _ptr(out), scale
+    d.lse = _ptr(_typed(lse, "lse", "float32", (q.shape[0], q.shape[1])))
+    if lse is not None and not lse.is_contiguous():
+        raise ValueError("lse: rows have to lie side by side")
+    d.q_begin = _ptr(_typed(q_begin, "q_begin", "int32"))
+    if prefix_pages is not None:
+        if prefix_pages.numel() * c.page_size < prefix_len:
+            raise ValueError("prefix_pages: too few for prefix_len")
+        d.prefix_pages = _ptr(_typed(prefix_pages, "prefix_pages", "int32"))
+    if pages is not None:
+        if pages.dim() != 2 or pages.shape[0] != n_seqs or pages.shape[1] * c.page_size < max_own_len:
+            raise ValueError("pages: [n_seqs, at least max_own_len / page_size] is needed")
+        d.pages, d.pages_stride = _ptr(_typed(pages, "pages", "int32")), (pages.stride(0) if n_seqs > 1 else pages.shape[1])
+        d.own_len = _ptr(_typed(own_len, "own_len", "int32", (n_seqs,)))
+    d.workspace, d.workspace_bytes = _ptr(workspace), (workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    return _check(lib().fr_attend_shared(C.byref(d), _stream(stream)), "fr_attend_shared")
+
+
+def _sample_sizes(logits):
+    d = fr_sample_desc()
+    d.n_rows, d.n_vocab = logits.shape
+    d.dtype = _dtype(logits)
+    return d
+
+
+def fr_sample_workspace_bytes(logits):
+    """logits: a tensor of the call's shape and type (only these are read)."""
+    d, out = _sample_sizes(logits), C.c_uint64()
+    _check(lib().fr_sample_workspace_bytes(C.byref(d), C.byref(out)), "fr_sample_workspace_bytes")
+    return out.value
+
+
+def fr_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, stream=None):
+    d = _sample_sizes(logits)
+    n = d.n_rows
+    if logits.shape[1] > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: the entries of a row have to lie side by side")
+    d.logits, d.row_stride = _ptr(logits), (logits.stride(0) if n > 1 else d.n_vocab)
+    for name, x, what in (("temperature", temperature, "float32"), ("top_k", top_k, "int32"), ("top_p", top_p, "float32"),
+                          ("min_p", min_p, "float32"), ("uniform", uniform, "float32"), ("token", token, "int32")):
+        setattr(d, name, _ptr(_typed(x, name, what, (n,))))
+    d.workspace, d.workspace_bytes = _ptr(workspace), (workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    return _check(lib().fr_sample(C.byref(d), _stream(stream)), "fr_sample")
