@@ -1,11 +1,26 @@
 // Attention of a batch of sequences behind a shared prefix, keys and values in a cache of pages.
 
+#include <algorithm>
 #include <cmath>
 
 #include "common.h"
 #include "lm_types.h"
 
 namespace {
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short i16x4;
+typedef __attribute__((address_space(3))) char* LdsBytes;
+__device__ __forceinline__ LdsBytes lds_at(uint32_t address) { return reinterpret_cast<LdsBytes>(address); }
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kXcds = 8, kThreads = 256, kWaves = 4;
+constexpr int kRows = 32;                  // query rows of a wavefront: the columns of its MFMA blocks
+constexpr float kSlack = 8.0f;             // a running maximum may lag behind by a factor of 2^8 in the weights
+
+struct Segment {                           // the work of one of the two kinds of workgroups
+    int32_t row_tiles, splits, split_len, first_part, items;
+};
 
 struct AttendArgs {
     fr_kv_pages c;
@@ -16,64 +31,564 @@ struct AttendArgs {
     const int32_t *q_begin, *prefix_pages, *pages, *own_len;
     int32_t n_tokens, n_seqs, n_q_heads, max_q, prefix_len, max_own_len, page_shift, group;
     float scale;
+    int32_t own_from;                      // the sequences' workgroups take keys from here on: 0, or prefix_len
+    Segment prefix, own;
+    int32_t parts;                         // 1: results go to `out`, else to part_*
+    float* part_o;                         // [parts][n_tokens * n_q_heads][head_dim], relative to 2^m
+    float2* part_ml;                       // [parts][n_tokens * n_q_heads]: m in powers of 2, sum
 };
 
 __device__ __forceinline__ int32_t within(int32_t x, int32_t lo, int32_t hi) { return x < lo ? lo : x > hi ? hi : x; }
-
-// One wavefront per token and query head: keys in rounds of 64, a lane each.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void k_attend(AttendArgs a)
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(kLeft) : "memory"); }
+// Global memory to LDS without passing through registers, 16 bytes (or 4) a lane: lane l's go to LDS address lds + 16 l (4 l).
+// Written as assembly so that the compiler does not wait for every load in flight before each read of LDS; which loads have to be
+// here is counted by hand.
+__device__ __forceinline__ void load16_to_lds(uint32_t lds, const void* g)
 {
-    const int lane = threadIdx.x, head = blockIdx.y, kv = head / a.group, b = blockIdx.z, i = blockIdx.x;
-    const int t0 = a.q_begin ? within(a.q_begin[b], 0, a.n_tokens) : b, t1 = a.q_begin ? within(a.q_begin[b + 1], t0, a.n_tokens) : b + 1;
-    if (i >= t1 - t0) return;
-    const int own = a.max_own_len ? within(a.own_len[b], 0, a.max_own_len) : 0;
-    int seen = own - (t1 - t0) + 1 + i;
-    seen = a.prefix_len + (seen < 0 ? 0 : seen);
-    const int token = t0 + i;
-    const uint16_t* q = a.q + token * a.q_stride + (int64_t)head * D;
-    auto at = [&](int j) {
-        const int32_t x = j < a.prefix_len ? j : j - a.prefix_len;
-        const int32_t id = j < a.prefix_len ? a.prefix_pages[x >> a.page_shift] : a.pages[b * a.pages_stride + (x >> a.page_shift)];
-        return within(id, 0, (int32_t)a.c.n_pages - 1) * a.c.page_stride + kv * a.c.head_stride + (x & (a.c.page_size - 1)) * a.c.slot_stride;
-    };
-    float m = -INFINITY, total = 0.0f, acc[D / 64];
-    for (int x = 0; x < D / 64; ++x) acc[x] = 0.0f;
-    for (int j0 = 0; j0 < seen; j0 += 64) {
-        const int n = seen - j0 < 64 ? seen - j0 : 64;
-        const int64_t mine = at(lane < n ? j0 + lane : j0);
-        float s = -INFINITY;
-        if (lane < n) {
-            const uint16_t* k = static_cast<const uint16_t*>(a.c.k) + mine;
-            s = 0.0f;
-            for (int x = 0; x < D; ++x) s += T::up(q[x]) * T::up(k[x]);
-            s *= a.scale;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory");
+}
+__device__ __forceinline__ void load4_to_lds(uint32_t lds, const void* g)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(g) : "memory");
+}
+__device__ __forceinline__ float of_both_halves(float x)          // the larger of lane l's and lane l ^ 32's
+{
+    typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u2;
+    const u2 r = __builtin_bit_cast(u2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_of_both_halves(float x)
+{
+    typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u2;
+    const u2 r = __builtin_bit_cast(u2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <typename T> __device__ __forceinline__ f32x16 mfma(typename T::x8 a, typename T::x8 b, f32x16 c);
+template <> __device__ __forceinline__ f32x16 mfma<Bf16>(Bf16::x8 a, Bf16::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+template <> __device__ __forceinline__ f32x16 mfma<F16>(F16::x8 a, F16::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// What a workgroup works on: query rows (token and head of a group, the group's heads side by side) against a run of keys.
+struct Item {
+    int32_t kv, token0, rows, row0;        // key head; first token; rows there are; first row of this workgroup
+    int32_t k0, k1;                        // keys, counted through the prefix and then the sequence's own
+    int32_t seen0, seen_step;              // a row of token i sees the keys below max(prefix, seen0 + i * seen_step)
+    int32_t part;
+    const int32_t* own_pages;
+};
+
+// Where a row's result goes.
+template <int D> struct Rows {
+    const AttendArgs& a;
+    const Item& w;
+    __device__ __forceinline__ int32_t token(int r) const { return w.token0 + r / a.group; }
+    __device__ __forceinline__ int32_t head(int r) const { return w.kv * a.group + r % a.group; }
+    __device__ __forceinline__ int32_t seen(int r) const { return max(a.prefix_len, w.seen0 + r / a.group * w.seen_step); }
+};
+
+// LDS of a workgroup: tiles of keys and values (rows of head_dim elements, 16-byte chunk c of row r at place c ^ f(r)), page ids.
+// f: K is read 16 bytes a lane, lanes along rows; V 8 bytes a lane, four rows by 64 bytes at a time, transposed on the way.
+template <int D> struct Lds {
+    static constexpr uint32_t kRow = D * 2, kChunks = D / 8, kRowsALoad = 1024 / kRow;
+    static constexpr uint32_t kBytes = 512 * D;                   // 64 KB at D = 128: two workgroups share a compute unit
+    static __device__ __forceinline__ uint32_t fk(uint32_t r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+    static __device__ __forceinline__ uint32_t fv(uint32_t r) { return D == 128 ? (r & 3) * 4 : (r & 2) * 2; }
+};
+
+// The state of 32 query rows in a wavefront: lane l holds row l % 32 (keys of its half of every block), the result transposed.
+template <typename T, int D> struct Softmax {
+    f32x16 o[D / 32];
+    float m, l;                            // running maximum of the scores (before the scale), sum of this half's weights
+    typename T::x8 q[D / 16];
+
+    __device__ __forceinline__ void start()
+    {
+        m = -INFINITY;
+        l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    }
+
+    // Scores of kBlocks x 32 keys to weights: the blocks' key of element i is 8 (i / 4) + 4 (lane / 32) + i % 4.
+    template <int kBlocks>
+    __device__ __forceinline__ void weigh(f32x16 (&s)[kBlocks], float c, int first, int end, int lane)
+    {
+        if (first + 32 * kBlocks > end) {  // (end: keys that the row sees, at most the workgroup's last)
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (first + b * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= end) s[b][i] = -INFINITY;
         }
-        float top = s;
-        for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-        top = fmaxf(top, m);
-        const float base = top == -INFINITY ? 0.0f : top, p = expf(s - base), old = expf(m - base);
-        float sum = p;
-        for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
-        total = total * old + sum;
-        m = top;
-        for (int x = 0; x < D / 64; ++x) acc[x] *= old;
-        for (int j = 0; j < n; ++j) {
-            const float w = __shfl(p, j);
-            const int64_t where = __shfl(mine, j);
-            for (int x = 0; x < D / 64; ++x) acc[x] += w * T::up(static_cast<const uint16_t*>(a.c.v)[where + x * 64 + lane]);
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        top = of_both_halves(top);
+        if (__any((top - m) * c > kSlack)) {                       // (m = -infinity: the first keys a row sees)
+            const float now = fmaxf(top, m), old = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * c);
+            m = now;
+            l *= old;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= old;
+        }
+        const float base = m == -INFINITY ? 0.0f : m * c;
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -base));
+                sum[i % 4] += s[b][i];
+            }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+
+    // The eight keys a lane's fragment of P holds are four and four neighbours (16 x + 4 h + .., 16 x + 8 + 4 h + ..), as they come
+    // out of the scores; a transposed read of V takes four neighbouring keys, so that it has the same order.
+    static __device__ __forceinline__ typename T::x8 weights(const f32x16& s, int half)
+    {
+        const uint4 x = make_uint4(T::pack(s[8 * half], s[8 * half + 1]), T::pack(s[8 * half + 2], s[8 * half + 3]),
+                                   T::pack(s[8 * half + 4], s[8 * half + 5]), T::pack(s[8 * half + 6], s[8 * half + 7]));
+        return __builtin_bit_cast(typename T::x8, x);
+    }
+};
+
+// Fragment of K: lane l has row l % 32, elements 16 s + 8 (l / 32) .. + 7.
+template <typename T, int D> __device__ __forceinline__ typename T::x8 k_fragment(uint32_t tile, int s, int lane)
+{
+    typedef const __attribute__((address_space(3))) typename T::x8* Fragment;
+    const uint32_t r = lane & 31;
+    return *reinterpret_cast<Fragment>(lds_at(tile + r * Lds<D>::kRow + (((uint32_t)(2 * s + (lane >> 5))) ^ Lds<D>::fk(r)) * 16));
+}
+
+// Fragment of V transposed: lane l has element 32 d + l % 32 of the keys 16 x + 4 (l / 32) .. + 3 and 16 x + 8 + 4 (l / 32) .. + 3.
+template <typename T, int D> __device__ __forceinline__ typename T::x8 v_fragment(uint32_t tile, int x, int d, int lane)
+{
+    typedef __attribute__((address_space(3))) i16x4* Quad;
+    const uint32_t i = lane & 15, r = 16 * x + 4 * (lane >> 5) + (i >> 2), chunk = d * 4 + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+    const uint32_t at = tile + r * Lds<D>::kRow + (chunk ^ Lds<D>::fv(r)) * 16 + (i & 1) * 8;      // (fv(r + 8) = fv(r))
+    struct { i16x4 lo, hi; } y = {__builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<Quad>(lds_at(at))),
+                                  __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<Quad>(lds_at(at + 8 * Lds<D>::kRow)))};
+    return __builtin_bit_cast(typename T::x8, y);
+}
+
+// One workgroup: four wavefronts.  kWide: 128 rows, 32 a wavefront, which share tiles of 64 keys; else 32 rows, and every
+// wavefront takes every fourth tile of 32 keys for itself, the four results being joined at the end.
+template <typename T, int D, bool kWide>
+__device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char* lds_array, int32_t* ids_array)
+{
+    typedef Lds<D> L;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds = (uint32_t)reinterpret_cast<uintptr_t>((LdsBytes)lds_array), ids = (uint32_t)reinterpret_cast<uintptr_t>((LdsBytes)(char*)ids_array);
+    asm volatile("" ::"s"(lds), "s"(ids) : "memory");       // (both arrays are written behind the compiler's back)
+    const Rows<D> rows{a, w};
+    const float c = a.scale * kLog2e;
+
+    // the wavefront's rows
+    const int row_first = w.row0 + (kWide ? wave * kRows : 0), row = row_first + (lane & 31);
+    const bool idle = row_first >= w.rows;
+    const int row_here = min(row, w.rows - 1);
+    const int end = min(rows.seen(row_here), w.k1);
+    Softmax<T, D> x;
+    x.start();
+    {
+        const uint16_t* q = a.q + rows.token(row_here) * a.q_stride + (int64_t)rows.head(row_here) * D + (lane >> 5) * 8;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) x.q[s] = __builtin_bit_cast(typename T::x8, *reinterpret_cast<const uint4*>(q + s * 16));
+    }
+
+    // page ids of n keys from `first` on, a lane each, to LDS; keys behind the last stand for the last
+    auto ask_ids = [&](uint32_t to, int first, int n) {
+        const int j = min(first + (lane & (n - 1)), w.k1 - 1), own = j - a.prefix_len;
+        const int32_t* g = own < 0 ? a.prefix_pages + (j >> a.page_shift) : w.own_pages + (own >> a.page_shift);
+        load4_to_lds(to, g);
+    };
+    // offset of the 16 bytes that this lane loads of key row r (counted from `first`, whose ids stand at `from`)
+    auto offset = [&](uint32_t from, int first, uint32_t r) -> int64_t {
+        const int j = min(first + (int)r, w.k1 - 1), in = j < a.prefix_len ? j : j - a.prefix_len;
+        const int32_t id = within(*reinterpret_cast<const __attribute__((address_space(3))) int32_t*>(lds_at(from + r * 4)), 0, (int32_t)a.c.n_pages - 1);
+        return (int64_t)id * a.c.page_stride + (int64_t)(in & (a.c.page_size - 1)) * a.c.slot_stride;
+    };
+    const uint16_t* gk = static_cast<const uint16_t*>(a.c.k) + w.kv * a.c.head_stride;
+    const uint16_t* gv = static_cast<const uint16_t*>(a.c.v) + w.kv * a.c.head_stride;
+    const uint32_t load_row = lane / L::kChunks, place = lane % L::kChunks;
+
+    if (w.k0 < w.k1) {
+        if constexpr (kWide) {
+            constexpr int kTile = 64, kLoads = 16 / L::kRowsALoad;         // a wavefront loads 16 rows of each
+            constexpr uint32_t kHalf = kTile * L::kRow, kStage = 2 * kHalf;
+            const int tiles = (w.k1 - w.k0 + kTile - 1) / kTile;
+            const uint32_t my_ids = ids + wave * 512;       // (64 lanes write 256 bytes at a time)
+            auto first_of = [&](int t) { return w.k0 + t * kTile + wave * 16; };
+            auto ask = [&](int t) {
+                const uint32_t to = lds + (t & 1) * kStage + wave * 16 * L::kRow, from = my_ids + (t & 1) * 256;
+#pragma unroll
+                for (int x = 0; x < kLoads; ++x) {
+                    const uint32_t r = x * L::kRowsALoad + load_row;
+                    const int64_t at = offset(from, first_of(t), r);
+                    load16_to_lds(to + x * 1024, gk + at + (place ^ L::fk(r)) * 8);
+                    load16_to_lds(to + kHalf + x * 1024, gv + at + (place ^ L::fv(r)) * 8);
+                }
+            };
+            ask_ids(my_ids, first_of(0), 16);
+            ask_ids(my_ids + 256, first_of(1), 16);
+            wait_loads<0>();
+            ask(0);
+            for (int t = 0; t < tiles; ++t) {
+                wait_loads<0>();
+                __syncthreads();                         // tile t is here, and everybody is done with tile t - 1
+                if (t + 1 < tiles) {
+                    ask(t + 1);
+                    wait_lds();
+                    ask_ids(my_ids + (t & 1) * 256, first_of(t + 2), 16);
+                }
+                if (idle) continue;
+                const uint32_t k = lds + (t & 1) * kStage, v = k + kHalf;
+                f32x16 s[2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+                for (int f = 0; f < D / 16; ++f)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) s[b] = mfma<T>(k_fragment<T, D>(k + b * 32 * L::kRow, f, lane), x.q[f], s[b]);
+                x.template weigh<2>(s, c, w.k0 + t * kTile, end, lane);
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    const typename T::x8 p = Softmax<T, D>::weights(s[f / 2], f % 2);
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma<T>(v_fragment<T, D>(v, f, d, lane), p, x.o[d]);
+                }
+            }
+        } else {
+            constexpr int kTile = 32, kLoads = kTile / L::kRowsALoad;
+            constexpr uint32_t kHalf = kTile * L::kRow;
+            const int all = (w.k1 - w.k0 + kTile - 1) / kTile, tiles = (all - wave + kWaves - 1) / kWaves;
+            const uint32_t k = lds + wave * 2 * kHalf, v = k + kHalf, my_ids = ids + wave * 512;
+            auto first_of = [&](int t) { return w.k0 + (t * kWaves + wave) * kTile; };
+            int64_t at[kLoads];
+            auto ask_k = [&](int t) {
+#pragma unroll
+                for (int x = 0; x < kLoads; ++x) {
+                    const uint32_t r = x * L::kRowsALoad + load_row;
+                    at[x] = offset(my_ids + (t & 1) * 256, first_of(t), r);
+                    load16_to_lds(k + x * 1024, gk + at[x] + (place ^ L::fk(r)) * 8);
+                }
+            };
+            auto ask_v = [&] {
+#pragma unroll
+                for (int x = 0; x < kLoads; ++x) load16_to_lds(v + x * 1024, gv + at[x] + (place ^ L::fv(x * L::kRowsALoad + load_row)) * 8);
+            };
+            if (tiles > 0) {
+                ask_ids(my_ids, first_of(0), kTile);
+                ask_ids(my_ids + 256, first_of(1), kTile);
+                wait_loads<0>();
+                ask_k(0);
+                ask_v();
+            }
+            for (int t = 0; t < tiles; ++t) {
+                // in flight: K and V of tile t, in this order
+                const bool more = t + 1 < tiles;
+                wait_loads<kLoads>();
+                typename T::x8 kf[D / 16];
+#pragma unroll
+                for (int f = 0; f < D / 16; ++f) kf[f] = k_fragment<T, D>(k, f, lane);
+                wait_lds();
+                if (more) {
+                    ask_ids(my_ids + (t & 1) * 256, first_of(t + 2), kTile);
+                    ask_k(t + 1);
+                }
+                f32x16 s[1];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
+#pragma unroll
+                for (int f = 0; f < D / 16; ++f) s[0] = mfma<T>(kf[f], x.q[f], s[0]);
+                x.template weigh<1>(s, c, first_of(t), end, lane);
+                if (more) wait_loads<kLoads + 1>();
+                else wait_loads<0>();
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const typename T::x8 p = Softmax<T, D>::weights(s[0], f);
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma<T>(v_fragment<T, D>(v, f, d, lane), p, x.o[d]);
+                }
+                wait_lds();
+                if (more) ask_v();
+            }
+        }
+
+        // A weight of 0 for a key that a row does not see, times a value that is not finite, is not 0: where rows of a workgroup see
+        // different keys and a result is not finite, the row's sum is made again from the keys it sees, one after the other.
+        bool bad = false;
+        if (w.seen_step) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) bad |= !(fabsf(x.o[d][i]) < INFINITY);
+        }
+        if (__any(bad && !idle) && !idle) {
+            const float base = x.m == -INFINITY ? 0.0f : x.m * c;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x.o[d][i] = 0.0f;
+            for (int j = w.k0; j < end; ++j) {
+                if (!kWide && (j - w.k0) / 32 % kWaves != wave) continue;
+                const int in = j < a.prefix_len ? j : j - a.prefix_len;
+                const int32_t id = within(j < a.prefix_len ? a.prefix_pages[in >> a.page_shift] : w.own_pages[in >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
+                const int64_t at = (int64_t)id * a.c.page_stride + (int64_t)(in & (a.c.page_size - 1)) * a.c.slot_stride;
+                const uint16_t* q = a.q + rows.token(row_here) * a.q_stride + (int64_t)rows.head(row_here) * D;
+                float s = 0.0f;
+                for (int e = 0; e < D; ++e) s = fmaf(T::up(q[e]), T::up(gk[at + e]), s);
+                const float p = T::up((uint16_t)T::pack(__builtin_amdgcn_exp2f(fmaf(s, c, -base)), 0.0f));
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x.o[d][i] = fmaf(p, T::up(gv[at + d * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4]), x.o[d][i]);
+            }
         }
     }
-    for (int x = 0; x < D / 64; ++x)
-        a.out[token * a.out_stride + (int64_t)head * D + x * 64 + lane] = (uint16_t)T::pack(seen ? acc[x] / total : 0.0f, 0.0f);
-    if (a.lse && lane == 0) a.lse[(int64_t)token * a.n_q_heads + head] = seen ? m + logf(total) : -INFINITY;
+    x.l = sum_of_both_halves(x.l);
+
+    // results through LDS, so that rows are written whole: a wavefront's 32 rows of D floats, 16-byte chunk c of row r at c ^ r
+    __shared__ float2 row_ml[kWaves][kRows];
+    typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+    typedef __attribute__((address_space(3))) f32x4* LdsFloats;
+    constexpr uint32_t kFloatRow = D * 4, kFloatChunks = D / 4;
+    __syncthreads();                                     // tiles are done with
+    const float m2 = x.m * c;                            // (-infinity stays: c is positive)
+    float mine = 1.0f;
+    if (lane < 32) row_ml[wave][lane] = make_float2(m2, x.l);
+    if constexpr (!kWide) {
+        __syncthreads();
+        float top = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < kWaves; ++y) top = fmaxf(top, row_ml[y][lane & 31].x);
+        mine = __builtin_amdgcn_exp2f(m2 - (top == -INFINITY ? 0.0f : top));
+    }
+    const uint32_t region = lds + wave * kRows * kFloatRow;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const uint32_t r = lane & 31, chunk = d * 8 + 2 * (i / 4) + (lane >> 5);
+            *reinterpret_cast<LdsFloats>(lds_at(region + r * kFloatRow + (chunk ^ (r & (kFloatChunks - 1))) * 16)) =
+                f32x4{x.o[d][i] * mine, x.o[d][i + 1] * mine, x.o[d][i + 2] * mine, x.o[d][i + 3] * mine};
+        }
+    __syncthreads();
+    // a thread takes eight elements of a row: two chunks
+    constexpr int kPieces = D / 8, kOutRows = kWide ? kWaves * kRows : kRows;
+    for (int y = tid; y < kOutRows * kPieces; y += kThreads) {
+        const int r = y / kPieces, piece = y % kPieces, from = w.row0 + r;
+        if (from >= w.rows) continue;
+        f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+        float top, sum;
+        const int in = r % kRows;
+        auto chunk = [&](int wv, int e) { return *reinterpret_cast<LdsFloats>(lds_at(lds + (wv * kRows + in) * kFloatRow + ((uint32_t)(2 * piece + e) ^ (in & (kFloatChunks - 1))) * 16)); };
+        if constexpr (kWide) {
+            lo = chunk(r / kRows, 0), hi = chunk(r / kRows, 1);
+            top = row_ml[r / kRows][in].x, sum = row_ml[r / kRows][in].y;
+        } else {
+            top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int wv = 0; wv < kWaves; ++wv) top = fmaxf(top, row_ml[wv][in].x);
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int wv = 0; wv < kWaves; ++wv) {
+                lo += chunk(wv, 0), hi += chunk(wv, 1);
+                sum += row_ml[wv][in].y * __builtin_amdgcn_exp2f(row_ml[wv][in].x - base);
+            }
+        }
+        const int64_t token = rows.token(from), head = rows.head(from);
+        if (a.parts == 1) {
+            const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+            *reinterpret_cast<uint4*>(a.out + token * a.out_stride + head * D + piece * 8) =
+                make_uint4(T::pack(lo[0] * f, lo[1] * f), T::pack(lo[2] * f, lo[3] * f), T::pack(hi[0] * f, hi[1] * f), T::pack(hi[2] * f, hi[3] * f));
+            if (a.lse && piece == 0) a.lse[token * a.n_q_heads + head] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
+        } else {
+            const int64_t to = ((int64_t)w.part * a.n_tokens + token) * a.n_q_heads + head;
+            *reinterpret_cast<f32x4*>(a.part_o + to * D + piece * 8) = lo;
+            *reinterpret_cast<f32x4*>(a.part_o + to * D + piece * 8 + 4) = hi;
+            if (piece == 0) a.part_ml[to] = make_float2(top, sum);
+        }
+    }
+}
+
+// Workgroups are dealt round-robin over the XCDs: every XCD gets a contiguous run of items, of which neighbours read the same keys.
+__device__ __forceinline__ int item_of(int block, int items)
+{
+    const int xcd = block % kXcds, q = items / kXcds, r = items % kXcds;
+    return xcd * q + min(xcd, r) + block / kXcds;
+}
+
+// Rows of all tokens against a part of the prefix.
+template <typename T, int D, bool kWide>
+__global__ __launch_bounds__(kThreads, 2) void k_attend_prefix(AttendArgs a)
+{
+    __shared__ __align__(1024) char lds[Lds<D>::kBytes];
+    __shared__ __align__(1024) int32_t ids[kWaves * 128];
+    const int item = item_of(blockIdx.x, a.prefix.items), tile = item % a.prefix.row_tiles, rest = item / a.prefix.row_tiles;
+    Item w;
+    w.kv = rest / a.prefix.splits;
+    w.part = rest % a.prefix.splits;
+    w.token0 = 0;
+    w.rows = a.n_tokens * a.group;
+    w.row0 = tile * (kWide ? kWaves * kRows : kRows);
+    w.k0 = w.part * a.prefix.split_len;
+    w.k1 = min(a.prefix_len, w.k0 + a.prefix.split_len);
+    w.seen0 = a.prefix_len;
+    w.seen_step = 0;
+    w.own_pages = nullptr;
+    attend<T, D, kWide>(a, w, lds, ids);
+}
+
+// Rows of one sequence against a part of its keys, or of the prefix and its keys.
+template <typename T, int D, bool kWide>
+__global__ __launch_bounds__(kThreads, 2) void k_attend_own(AttendArgs a)
+{
+    __shared__ __align__(1024) char lds[Lds<D>::kBytes];
+    __shared__ __align__(1024) int32_t ids[kWaves * 128];
+    const int item = item_of(blockIdx.x, a.own.items), tile = item % a.own.row_tiles;
+    int rest = item / a.own.row_tiles;
+    const int split = rest % a.own.splits;
+    rest /= a.own.splits;
+    Item w;
+    w.kv = rest % a.c.n_kv_heads;
+    const int b = rest / a.c.n_kv_heads;
+    const int t0 = a.q_begin ? within(a.q_begin[b], 0, a.n_tokens) : b, t1 = a.q_begin ? within(a.q_begin[b + 1], t0, a.n_tokens) : b + 1;
+    const int t = t1 - t0, own = a.max_own_len ? within(a.own_len[b], 0, a.max_own_len) : 0;
+    w.token0 = t0;
+    w.rows = min(t, a.max_q) * a.group;
+    w.row0 = tile * (kWide ? kWaves * kRows : kRows);
+    if (w.row0 >= w.rows) return;
+    w.seen0 = a.prefix_len + own - t + 1;
+    w.seen_step = t > 1 ? 1 : 0;
+    const int last = min(w.rows, w.row0 + (kWide ? kWaves * kRows : kRows)) - 1;
+    const int seen = max(a.prefix_len, w.seen0 + last / a.group);
+    w.k0 = a.own_from + split * a.own.split_len;
+    w.k1 = min(seen, w.k0 + a.own.split_len);
+    if (w.k0 >= w.k1 && a.parts > 1) return;
+    w.part = a.own.first_part + split;
+    w.own_pages = a.pages + b * a.pages_stride;
+    attend<T, D, kWide>(a, w, lds, ids);
+}
+
+// Joins the parts of a row: eight (four) elements a thread, head_dim / 8 threads a row.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_blocks)
+{
+    constexpr int kPieces = D / 8, kRowsHere = kThreads / kPieces;
+    const int b = blockIdx.x / row_blocks, r = blockIdx.x % row_blocks * kRowsHere + threadIdx.x / kPieces, piece = threadIdx.x % kPieces;
+    const int t0 = a.q_begin ? within(a.q_begin[b], 0, a.n_tokens) : b, t1 = a.q_begin ? within(a.q_begin[b + 1], t0, a.n_tokens) : b + 1;
+    const int t = t1 - t0, i = r / a.n_q_heads, own = a.max_own_len ? within(a.own_len[b], 0, a.max_own_len) : 0;
+    if (i >= min(t, a.max_q)) return;
+    const int seen = max(a.prefix_len, a.prefix_len + own - t + 1 + i);
+    const int of_own = seen > a.own_from ? (seen - a.own_from + a.own.split_len - 1) / a.own.split_len : 0, parts = a.own.first_part + of_own;
+    const int64_t token = t0 + i, head = r % a.n_q_heads, row = token * a.n_q_heads + head, pitch = (int64_t)a.n_tokens * a.n_q_heads;
+    float top = -INFINITY;
+    for (int y = 0; y < parts; ++y) top = fmaxf(top, a.part_ml[y * pitch + row].x);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+    for (int y = 0; y < parts; ++y) {
+        const float2 ml = a.part_ml[y * pitch + row];
+        const float f = __builtin_amdgcn_exp2f(ml.x - base);
+        const float4* p = reinterpret_cast<const float4*>(a.part_o + (y * pitch + row) * D + piece * 8);
+        const float4 lo = p[0], hi = p[1];
+        sum = fmaf(ml.y, f, sum);
+        o[0] = fmaf(lo.x, f, o[0]), o[1] = fmaf(lo.y, f, o[1]), o[2] = fmaf(lo.z, f, o[2]), o[3] = fmaf(lo.w, f, o[3]);
+        o[4] = fmaf(hi.x, f, o[4]), o[5] = fmaf(hi.y, f, o[5]), o[6] = fmaf(hi.z, f, o[6]), o[7] = fmaf(hi.w, f, o[7]);
+    }
+    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+    *reinterpret_cast<uint4*>(a.out + token * a.out_stride + head * D + piece * 8) =
+        make_uint4(T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f), T::pack(o[4] * f, o[5] * f), T::pack(o[6] * f, o[7] * f));
+    if (a.lse && piece == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
 bool sizes_ok(const fr_attend_desc& d)
 {
     if (!kv_pages_shape_ok(d.cache) || d.n_tokens < 0 || d.n_seqs < 0 || d.max_q < 1) return false;
     if (d.n_q_heads < 1 || d.n_q_heads > 1024 || d.n_q_heads % d.cache.n_kv_heads) return false;
+    if ((int64_t)d.n_tokens * d.n_q_heads > 0x7fffffff - 4096) return false;
     return d.prefix_len >= 0 && d.max_own_len >= 0 && (int64_t)d.prefix_len + d.max_own_len < 0x7fffffff - 4096;
+}
+
+// How a call is cut: which keys the prefix' workgroups take, and in how many parts.
+struct Plan {
+    bool shared, wide_prefix, wide_own;
+    Segment prefix{}, own{};
+    int parts = 1;
+    int64_t items = 0;
+};
+
+Plan plan(const fr_attend_desc& d, int units)
+{
+    Plan p;
+    const int64_t group = d.n_q_heads / d.cache.n_kv_heads, heads = d.cache.n_kv_heads, keys = (int64_t)d.prefix_len + d.max_own_len;
+    const int64_t seq_rows = std::min<int64_t>(d.max_q, d.n_tokens) * group, all_rows = d.n_tokens * group;
+    units = std::min(units, 256);
+    auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    p.shared = d.prefix_len > 0 && d.n_seqs > 1 && seq_rows < 128;
+    p.wide_prefix = all_rows > kRows;
+    p.wide_own = seq_rows > kRows;
+    if (p.shared) {
+        p.prefix.row_tiles = (int)up(all_rows, p.wide_prefix ? kWaves * kRows : kRows);
+        const int64_t most = up(d.prefix_len, 256), want = 2 * units / (p.prefix.row_tiles * heads);
+        const int64_t splits = std::max<int64_t>(1, std::min(most, want));
+        p.prefix.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
+        p.prefix.splits = (int)up(d.prefix_len, p.prefix.split_len);
+        p.items += (int64_t)p.prefix.row_tiles * p.prefix.splits * heads;
+        p.prefix.items = (int)std::min<int64_t>(p.items, 0x7fffffff);
+    }
+    p.own.first_part = p.prefix.splits;
+    const int64_t own_keys = p.shared ? d.max_own_len : keys;
+    p.own.row_tiles = (int)up(seq_rows, p.wide_own ? kWaves * kRows : kRows);
+    const int64_t base = (int64_t)d.n_seqs * heads * p.own.row_tiles;
+    // parts of 1024 keys, shorter ones while that leaves units idle
+    int64_t len = 1024;
+    if (base >= 8 * units) len = std::max<int64_t>(own_keys, 1);
+    else
+        while (len > 128 && base * up(own_keys, len) < 4 * units) len /= 2;
+    p.own.split_len = (int)len;
+    p.own.splits = (int)std::max<int64_t>(1, up(own_keys, len));
+    p.parts = p.own.first_part + p.own.splits;
+    const int64_t own_items = own_keys || !p.shared ? base * p.own.splits : 0;
+    if (!own_items) { p.own.splits = 0; p.parts = p.own.first_part; }
+    p.items = std::max({p.items, own_items, (int64_t)d.n_seqs * std::min(d.max_q, d.n_tokens) * d.n_q_heads});      // (the join's grid is smaller)
+    p.own.items = (int)std::min<int64_t>(own_items, 0x7fffffff);
+    return p;
+}
+
+uint64_t part_bytes(const fr_attend_desc& d, const Plan& p)
+{
+    return p.parts > 1 ? (uint64_t)p.parts * d.n_tokens * d.n_q_heads * (d.cache.head_dim * 4 + 8) : 0;
+}
+
+template <typename T, int D>
+int launch(AttendArgs& a, const Plan& p, hipStream_t stream)
+{
+    if (a.prefix.items) {
+        if (p.wide_prefix) hipLaunchKernelGGL((k_attend_prefix<T, D, true>), dim3(a.prefix.items), dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((k_attend_prefix<T, D, false>), dim3(a.prefix.items), dim3(kThreads), 0, stream, a);
+    }
+    if (a.own.items) {
+        if (p.wide_own) hipLaunchKernelGGL((k_attend_own<T, D, true>), dim3(a.own.items), dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((k_attend_own<T, D, false>), dim3(a.own.items), dim3(kThreads), 0, stream, a);
+    }
+    if (p.parts > 1) {
+        const int rows = kThreads / (D / 8), blocks = (int)((std::min<int64_t>(a.max_q, a.n_tokens) * a.n_q_heads + rows - 1) / rows);
+        hipLaunchKernelGGL((k_attend_join<T, D>), dim3((unsigned)(a.n_seqs * (int64_t)blocks)), dim3(kThreads), 0, stream, a, blocks);
+    }
+    return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
 }
 
 }  // namespace
@@ -84,6 +599,8 @@ int fr_attend_shared_workspace_bytes(const fr_attend_desc* d, uint64_t* bytes_ou
 {
     if (!d || !bytes_out || !sizes_ok(*d)) return FR_ERR_ARG;
     *bytes_out = 0;
+    if (d->n_tokens == 0 || d->n_seqs == 0) return FR_OK;
+    *bytes_out = part_bytes(*d, plan(*d, 256));
     return FR_OK;
 }
 
@@ -102,17 +619,21 @@ int fr_attend_shared(const fr_attend_desc* d, void* stream)
     if (d->max_own_len && (!d->pages || !d->own_len || d->pages_stride < ((int64_t)d->max_own_len + c.page_size - 1) / c.page_size || d->pages_stride > most))
         return FR_ERR_ARG;
     AttendArgs a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->prefix_pages,
-                    d->pages, d->own_len, d->n_tokens, d->n_seqs, d->n_q_heads, d->max_q, d->prefix_len, d->max_own_len, __builtin_ctz(c.page_size),
-                    d->n_q_heads / c.n_kv_heads, d->scale};
-    const dim3 grid((unsigned)d->max_q, (unsigned)d->n_q_heads, (unsigned)d->n_seqs);
-    if (c.dtype == FR_DTYPE_BF16) {
-        if (c.head_dim == 64) hipLaunchKernelGGL((k_attend<Bf16, 64>), grid, dim3(64), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((k_attend<Bf16, 128>), grid, dim3(64), 0, (hipStream_t)stream, a);
-    } else {
-        if (c.head_dim == 64) hipLaunchKernelGGL((k_attend<F16, 64>), grid, dim3(64), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((k_attend<F16, 128>), grid, dim3(64), 0, (hipStream_t)stream, a);
-    }
-    return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
+                    d->pages, d->own_len, d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->prefix_len, d->max_own_len,
+                    __builtin_ctz(c.page_size), d->n_q_heads / c.n_kv_heads, d->scale};
+    const Plan p = plan(*d, (int)fr_stream_cus((hipStream_t)stream));
+    if (p.items > 0x7fffffff) return FR_ERR_ARG;
+    const uint64_t need = part_bytes(*d, p), asked = part_bytes(*d, plan(*d, 256));
+    if (asked && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < asked || need > asked)) return FR_ERR_ARG;
+    a.own_from = p.shared ? d->prefix_len : 0;
+    a.prefix = p.prefix;
+    a.own = p.own;
+    a.parts = p.parts;
+    a.part_o = (float*)d->workspace;
+    a.part_ml = (float2*)((char*)d->workspace + (uint64_t)p.parts * d->n_tokens * d->n_q_heads * c.head_dim * 4);
+    hipStream_t s = (hipStream_t)stream;
+    if (c.dtype == FR_DTYPE_BF16) return c.head_dim == 64 ? launch<Bf16, 64>(a, p, s) : launch<Bf16, 128>(a, p, s);
+    return c.head_dim == 64 ? launch<F16, 64>(a, p, s) : launch<F16, 128>(a, p, s);
 }
 
 }  // extern "C"
