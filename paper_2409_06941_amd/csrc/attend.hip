@@ -19,8 +19,10 @@ constexpr int kRows = 32;                  // query rows of a wavefront: the col
 constexpr float kSlack = 8.0f;             // a running maximum may lag behind by a factor of 2^8 in the weights
 
 struct Segment {                           // the work of one of the two kinds of workgroups
-    int32_t row_tiles, splits, split_len, first_part, items;
+    int32_t row_tiles, splits, split_len, first_part, groups, units;
 };
+
+enum Kind { kNone, kFewRows, kWideRows };
 
 struct AttendArgs {
     fr_kv_pages c;
@@ -422,23 +424,25 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
     }
 }
 
-// Workgroups are dealt round-robin over the XCDs: every XCD gets a contiguous run of items, of which neighbours read the same keys.
-__device__ __forceinline__ int item_of(int block, int items)
+// Workgroups are dealt round-robin over the XCDs.  Those that read the same keys (the row tiles of a group: one key head, one run
+// of keys) follow one another on one XCD, through its L2; groups go round the XCDs, so that long sequences spread.  `unit` counts
+// rounds of eight workgroups, one on every XCD.
+__device__ __forceinline__ bool group_of(const Segment& s, int unit, int xcd, int& group, int& tile)
 {
-    const int xcd = block % kXcds, q = items / kXcds, r = items % kXcds;
-    return xcd * q + min(xcd, r) + block / kXcds;
+    tile = unit % s.row_tiles;
+    group = unit / s.row_tiles * kXcds + xcd;
+    return group < s.groups;
 }
 
 // Rows of all tokens against a part of the prefix.
 template <typename T, int D, bool kWide>
-__global__ __launch_bounds__(kThreads, 2) void k_attend_prefix(AttendArgs a)
+__device__ __forceinline__ void attend_prefix(const AttendArgs& a, int unit, int xcd, char* lds, int32_t* ids)
 {
-    __shared__ __align__(1024) char lds[Lds<D>::kBytes];
-    __shared__ __align__(1024) int32_t ids[kWaves * 128];
-    const int item = item_of(blockIdx.x, a.prefix.items), tile = item % a.prefix.row_tiles, rest = item / a.prefix.row_tiles;
+    int group, tile;
+    if (!group_of(a.prefix, unit, xcd, group, tile)) return;
     Item w;
-    w.kv = rest / a.prefix.splits;
-    w.part = rest % a.prefix.splits;
+    w.kv = group / a.prefix.splits;
+    w.part = group % a.prefix.splits;
     w.token0 = 0;
     w.rows = a.n_tokens * a.group;
     w.row0 = tile * (kWide ? kWaves * kRows : kRows);
@@ -452,12 +456,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_prefix(AttendArgs a)
 
 // Rows of one sequence against a part of its keys, or of the prefix and its keys.
 template <typename T, int D, bool kWide>
-__global__ __launch_bounds__(kThreads, 2) void k_attend_own(AttendArgs a)
+__device__ __forceinline__ void attend_own(const AttendArgs& a, int unit, int xcd, char* lds, int32_t* ids)
 {
-    __shared__ __align__(1024) char lds[Lds<D>::kBytes];
-    __shared__ __align__(1024) int32_t ids[kWaves * 128];
-    const int item = item_of(blockIdx.x, a.own.items), tile = item % a.own.row_tiles;
-    int rest = item / a.own.row_tiles;
+    int rest, tile;
+    if (!group_of(a.own, unit, xcd, rest, tile)) return;
     const int split = rest % a.own.splits;
     rest /= a.own.splits;
     Item w;
@@ -481,25 +483,43 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_own(AttendArgs a)
     attend<T, D, kWide>(a, w, lds, ids);
 }
 
-// Joins the parts of a row: eight (four) elements a thread, head_dim / 8 threads a row.
-template <typename T, int D>
+// Both kinds of work in one launch, mixed evenly: the prefix' workgroups keep the matrix cores busy, the sequences' the memory.
+template <typename T, int D, Kind kPrefix, Kind kOwn>
+__global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a)
+{
+    __shared__ __align__(1024) char lds[Lds<D>::kBytes];
+    __shared__ __align__(1024) int32_t ids[kWaves * 128];
+    const int unit = blockIdx.x / kXcds, xcd = blockIdx.x % kXcds;
+    if constexpr (kPrefix != kNone) {
+        const int64_t all = a.prefix.units + a.own.units;
+        const int before = (int)(unit * (int64_t)a.prefix.units / all), after = (int)((unit + 1) * (int64_t)a.prefix.units / all);
+        if (after > before) attend_prefix<T, D, kPrefix == kWideRows>(a, before, xcd, lds, ids);
+        else attend_own<T, D, kOwn == kWideRows>(a, unit - before, xcd, lds, ids);
+    } else {
+        attend_own<T, D, kOwn == kWideRows>(a, unit, xcd, lds, ids);
+    }
+}
+
+// Joins the parts of a row: eight elements a thread, kLanes threads for every eight, each with every kLanes-th part.
+template <typename T, int D, int kLanes>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_blocks)
 {
-    constexpr int kPieces = D / 8, kRowsHere = kThreads / kPieces;
-    const int b = blockIdx.x / row_blocks, r = blockIdx.x % row_blocks * kRowsHere + threadIdx.x / kPieces, piece = threadIdx.x % kPieces;
+    constexpr int kPieces = D / 8, kRowsHere = kThreads / kPieces / kLanes;
+    const int piece = threadIdx.x % kPieces, mine = threadIdx.x / kPieces % kLanes;
+    const int b = blockIdx.x / row_blocks, r = blockIdx.x % row_blocks * kRowsHere + threadIdx.x / kPieces / kLanes;
     const int t0 = a.q_begin ? within(a.q_begin[b], 0, a.n_tokens) : b, t1 = a.q_begin ? within(a.q_begin[b + 1], t0, a.n_tokens) : b + 1;
     const int t = t1 - t0, i = r / a.n_q_heads, own = a.max_own_len ? within(a.own_len[b], 0, a.max_own_len) : 0;
-    if (i >= min(t, a.max_q)) return;
+    const bool there = i < min(t, a.max_q);
     const int seen = max(a.prefix_len, a.prefix_len + own - t + 1 + i);
-    const int of_own = seen > a.own_from ? (seen - a.own_from + a.own.split_len - 1) / a.own.split_len : 0, parts = a.own.first_part + of_own;
+    const int of_own = seen > a.own_from ? (seen - a.own_from + a.own.split_len - 1) / a.own.split_len : 0, parts = there ? a.own.first_part + of_own : 0;
     const int64_t token = t0 + i, head = r % a.n_q_heads, row = token * a.n_q_heads + head, pitch = (int64_t)a.n_tokens * a.n_q_heads;
     float top = -INFINITY;
-    for (int y = 0; y < parts; ++y) top = fmaxf(top, a.part_ml[y * pitch + row].x);
-    const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o[8];
+    for (int y = mine; y < parts; y += kLanes) top = fmaxf(top, a.part_ml[y * pitch + row].x);
+    float base = top == -INFINITY ? 0.0f : top, sum = 0.0f, o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-    for (int y = 0; y < parts; ++y) {
+#pragma unroll 4
+    for (int y = mine; y < parts; y += kLanes) {
         const float2 ml = a.part_ml[y * pitch + row];
         const float f = __builtin_amdgcn_exp2f(ml.x - base);
         const float4* p = reinterpret_cast<const float4*>(a.part_o + (y * pitch + row) * D + piece * 8);
@@ -508,6 +528,28 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_
         o[0] = fmaf(lo.x, f, o[0]), o[1] = fmaf(lo.y, f, o[1]), o[2] = fmaf(lo.z, f, o[2]), o[3] = fmaf(lo.w, f, o[3]);
         o[4] = fmaf(hi.x, f, o[4]), o[5] = fmaf(hi.y, f, o[5]), o[6] = fmaf(hi.z, f, o[6]), o[7] = fmaf(hi.w, f, o[7]);
     }
+    if constexpr (kLanes > 1) {
+        __shared__ float of[10][kThreads];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) of[e][threadIdx.x] = o[e];
+        of[8][threadIdx.x] = sum;
+        of[9][threadIdx.x] = top;
+        __syncthreads();
+        if (mine) return;
+        for (int y = 1; y < kLanes; ++y) top = fmaxf(top, of[9][threadIdx.x + y * kPieces]);
+        base = top == -INFINITY ? 0.0f : top;
+        sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+        for (int y = 0; y < kLanes; ++y) {
+            const int x = threadIdx.x + y * kPieces;
+            const float f = __builtin_amdgcn_exp2f(of[9][x] - base);
+            sum = fmaf(of[8][x], f, sum);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(of[e][x], f, o[e]);
+        }
+    }
+    if (!there) return;
     const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
     *reinterpret_cast<uint4*>(a.out + token * a.out_stride + head * D + piece * 8) =
         make_uint4(T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f), T::pack(o[4] * f, o[5] * f), T::pack(o[6] * f, o[7] * f));
@@ -524,47 +566,55 @@ bool sizes_ok(const fr_attend_desc& d)
 
 // How a call is cut: which keys the prefix' workgroups take, and in how many parts.
 struct Plan {
-    bool shared, wide_prefix, wide_own;
+    Kind of_prefix = kNone, of_own = kFewRows;
     Segment prefix{}, own{};
     int parts = 1;
-    int64_t items = 0;
+    int64_t blocks = 0;                    // of the larger grid
 };
 
-Plan plan(const fr_attend_desc& d, int units)
+Plan plan(const fr_attend_desc& d, int cus)
 {
     Plan p;
-    const int64_t group = d.n_q_heads / d.cache.n_kv_heads, heads = d.cache.n_kv_heads, keys = (int64_t)d.prefix_len + d.max_own_len;
-    const int64_t seq_rows = std::min<int64_t>(d.max_q, d.n_tokens) * group, all_rows = d.n_tokens * group;
-    units = std::min(units, 256);
     auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
-    p.shared = d.prefix_len > 0 && d.n_seqs > 1 && seq_rows < 128;
-    p.wide_prefix = all_rows > kRows;
-    p.wide_own = seq_rows > kRows;
-    if (p.shared) {
-        p.prefix.row_tiles = (int)up(all_rows, p.wide_prefix ? kWaves * kRows : kRows);
-        const int64_t most = up(d.prefix_len, 256), want = 2 * units / (p.prefix.row_tiles * heads);
+    const int64_t group = d.n_q_heads / d.cache.n_kv_heads, heads = d.cache.n_kv_heads;
+    const int64_t tokens_a_seq = std::min(d.max_q, d.n_tokens), seq_rows = tokens_a_seq * group, all_rows = d.n_tokens * group;
+    constexpr int64_t kWideTile = kWaves * kRows;
+    cus = std::min(cus, 256);
+    auto finish = [&](Segment& s, int64_t groups) {
+        s.groups = (int)std::min<int64_t>(groups, 0x7fffffff);
+        const int64_t units = up(groups, kXcds) * s.row_tiles;
+        s.units = (int)std::min<int64_t>(units, 0x7fffffff);
+        p.blocks += units * kXcds;
+    };
+    if (d.prefix_len > 0 && d.n_seqs > 1 && seq_rows < kWideTile && (int64_t)d.n_seqs * d.prefix_len >= 8192) {
+        p.of_prefix = all_rows > kRows ? kWideRows : kFewRows;
+        Segment& s = p.prefix;
+        s.row_tiles = (int)up(all_rows, p.of_prefix == kWideRows ? kWideTile : kRows);
+        const int64_t most = up(d.prefix_len, 256), want = 2 * cus / (s.row_tiles * heads);
         const int64_t splits = std::max<int64_t>(1, std::min(most, want));
-        p.prefix.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
-        p.prefix.splits = (int)up(d.prefix_len, p.prefix.split_len);
-        p.items += (int64_t)p.prefix.row_tiles * p.prefix.splits * heads;
-        p.prefix.items = (int)std::min<int64_t>(p.items, 0x7fffffff);
+        s.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
+        s.splits = (int)up(d.prefix_len, s.split_len);
+        finish(s, heads * s.splits);
     }
-    p.own.first_part = p.prefix.splits;
-    const int64_t own_keys = p.shared ? d.max_own_len : keys;
-    p.own.row_tiles = (int)up(seq_rows, p.wide_own ? kWaves * kRows : kRows);
-    const int64_t base = (int64_t)d.n_seqs * heads * p.own.row_tiles;
-    // parts of 1024 keys, shorter ones while that leaves units idle
-    int64_t len = 1024;
-    if (base >= 8 * units) len = std::max<int64_t>(own_keys, 1);
-    else
-        while (len > 128 && base * up(own_keys, len) < 4 * units) len /= 2;
-    p.own.split_len = (int)len;
-    p.own.splits = (int)std::max<int64_t>(1, up(own_keys, len));
-    p.parts = p.own.first_part + p.own.splits;
-    const int64_t own_items = own_keys || !p.shared ? base * p.own.splits : 0;
-    if (!own_items) { p.own.splits = 0; p.parts = p.own.first_part; }
-    p.items = std::max({p.items, own_items, (int64_t)d.n_seqs * std::min(d.max_q, d.n_tokens) * d.n_q_heads});      // (the join's grid is smaller)
-    p.own.items = (int)std::min<int64_t>(own_items, 0x7fffffff);
+    Segment& s = p.own;
+    const int64_t keys = (p.of_prefix == kNone ? d.prefix_len : 0) + (int64_t)d.max_own_len;
+    p.of_own = seq_rows > kRows ? kWideRows : kFewRows;
+    s.first_part = p.prefix.splits;
+    s.row_tiles = (int)up(seq_rows, p.of_own == kWideRows ? kWideTile : kRows);
+    s.split_len = 1;
+    if (keys || p.of_prefix == kNone) {
+        // parts of 1024 keys, shorter ones while that leaves units idle, whole sequences where there are enough of them
+        const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
+        int64_t len = 1024;
+        if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
+        else
+            while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
+        s.split_len = (int)len;
+        s.splits = (int)std::max<int64_t>(1, up(keys, len));
+        finish(s, (int64_t)d.n_seqs * heads * s.splits);
+    }
+    p.parts = p.prefix.splits + s.splits;
+    p.blocks = std::max(p.blocks, d.n_seqs * tokens_a_seq * d.n_q_heads);        // (the join's grid is not larger)
     return p;
 }
 
@@ -574,19 +624,26 @@ uint64_t part_bytes(const fr_attend_desc& d, const Plan& p)
 }
 
 template <typename T, int D>
-int launch(AttendArgs& a, const Plan& p, hipStream_t stream)
+int launch(const AttendArgs& a, const Plan& p, hipStream_t stream)
 {
-    if (a.prefix.items) {
-        if (p.wide_prefix) hipLaunchKernelGGL((k_attend_prefix<T, D, true>), dim3(a.prefix.items), dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((k_attend_prefix<T, D, false>), dim3(a.prefix.items), dim3(kThreads), 0, stream, a);
-    }
-    if (a.own.items) {
-        if (p.wide_own) hipLaunchKernelGGL((k_attend_own<T, D, true>), dim3(a.own.items), dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((k_attend_own<T, D, false>), dim3(a.own.items), dim3(kThreads), 0, stream, a);
+    const dim3 grid((unsigned)(a.prefix.units + a.own.units) * kXcds);
+    if (p.of_prefix == kNone) {
+        if (p.of_own == kFewRows) hipLaunchKernelGGL((k_attend<T, D, kNone, kFewRows>), grid, dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((k_attend<T, D, kNone, kWideRows>), grid, dim3(kThreads), 0, stream, a);
+    } else if (p.of_prefix == kFewRows) {              // (so few rows in all, so few of a sequence)
+        hipLaunchKernelGGL((k_attend<T, D, kFewRows, kFewRows>), grid, dim3(kThreads), 0, stream, a);
+    } else {
+        if (p.of_own == kFewRows) hipLaunchKernelGGL((k_attend<T, D, kWideRows, kFewRows>), grid, dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((k_attend<T, D, kWideRows, kWideRows>), grid, dim3(kThreads), 0, stream, a);
     }
     if (p.parts > 1) {
-        const int rows = kThreads / (D / 8), blocks = (int)((std::min<int64_t>(a.max_q, a.n_tokens) * a.n_q_heads + rows - 1) / rows);
-        hipLaunchKernelGGL((k_attend_join<T, D>), dim3((unsigned)(a.n_seqs * (int64_t)blocks)), dim3(kThreads), 0, stream, a, blocks);
+        // a thread for every eight elements where a row has few parts, up to 16 threads where it has many
+        const int lanes = p.parts <= 4 ? 1 : p.parts <= 16 ? 4 : 16, rows = kThreads / (D / 8) / lanes;
+        const int64_t blocks = (std::min<int64_t>(a.max_q, a.n_tokens) * a.n_q_heads + rows - 1) / rows;
+        const dim3 joins((unsigned)(a.n_seqs * blocks));
+        if (lanes == 1) hipLaunchKernelGGL((k_attend_join<T, D, 1>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
+        else if (lanes == 4) hipLaunchKernelGGL((k_attend_join<T, D, 4>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
+        else hipLaunchKernelGGL((k_attend_join<T, D, 16>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
     }
     return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
 }
@@ -622,10 +679,10 @@ int fr_attend_shared(const fr_attend_desc* d, void* stream)
                     d->pages, d->own_len, d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->prefix_len, d->max_own_len,
                     __builtin_ctz(c.page_size), d->n_q_heads / c.n_kv_heads, d->scale};
     const Plan p = plan(*d, (int)fr_stream_cus((hipStream_t)stream));
-    if (p.items > 0x7fffffff) return FR_ERR_ARG;
+    if (p.blocks > 0x7fffffff) return FR_ERR_ARG;
     const uint64_t need = part_bytes(*d, p), asked = part_bytes(*d, plan(*d, 256));
     if (asked && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < asked || need > asked)) return FR_ERR_ARG;
-    a.own_from = p.shared ? d->prefix_len : 0;
+    a.own_from = p.of_prefix == kNone ? 0 : d->prefix_len;
     a.prefix = p.prefix;
     a.own = p.own;
     a.parts = p.parts;
