@@ -1,10 +1,19 @@
 // One token for every row of logits, from a given random number: temperature, top-k, top-p and min-p.
 //
-// The entries kept are a prefix of the row in falling order, so nothing is sorted: the prefix' end is searched for, digit by
-// digit, by histograms of the entries' counts and masses.  Masses are 64-bit integers, whose sums do not depend on the order of
-// the additions.  The first digit is a step of 1/64 on the scale of (m - l) / temperature, over which a language model's logits
-// spread evenly (equal digits of a float's bits would put thousands of entries on one counter); the rest are digits of the
-// logit's bits, in an order that rises with the logit.
+// The entries kept are a prefix of the row in falling order, so nothing is sorted: the prefix' end is searched for by histograms of
+// the entries' counts and masses.  Masses are 64-bit integers, whose sums do not depend on the order of the additions.  A
+// histogram's digit is a step of 1/64 on the scale of (m - l) / temperature, over which a language model's logits spread evenly
+// (digits of a float's bits would put thousands of entries on one counter).
+//
+// A workgroup takes a row, and reads it twice:
+//   first for the largest logit, of the row and of every thread's share;
+//   then, for rows that are cut by count or mass, to put the entries that can be kept into LDS.  The rank-th largest of the threads'
+//   own largest logits has at least `rank` entries above it, and seldom many more: with rank = top_k all of the first top_k are
+//   among them; for a cut by mass rank is 640, and the pass adds up the mass of the whole row, which says whether what is in LDS
+//   holds enough of it.  What is left happens in LDS.
+//   Rows that are not cut, or by weight alone, need the masses of runs of 64 lanes' entries instead, and one run again.
+// Rows that none of this fits (many thousands of entries that can be kept, or as many equal ones, infinities) go through the row
+// for every digit of the search.
 
 #include <cmath>
 
@@ -15,7 +24,6 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2 * kThreads, kMostVocab = 1 << 19;
 constexpr float kMassOne = 8796093022208.0f;           // 2^43: the sum over 2^19 entries stays below 2^63
-constexpr uint32_t kMinusInf = 0x007fffffu;            // key of -infinity
 
 struct SampleArgs {
     const void* logits;
@@ -52,40 +60,132 @@ struct Scale {
 
 struct Found { uint32_t digit, count_before, count; uint64_t mass_before, mass; };
 
+constexpr int kCandidates = 4096, kList = 1024, kRank = 640;
+constexpr uint32_t kNoMass = 1909;                     // from this digit on (29.83 and more below the top) masses are 0: 43 ln 2 = 29.81
+
+// A row of any alignment in pieces of 16 bytes: `head` entries up to the first such piece, `pieces` of kEach, `tail` entries.
+template <typename T> struct Row {
+    static constexpr int kEach = 16 / (int)sizeof(typename T::Bits);
+    const typename T::Bits* p;
+    int head, pieces, tail, n;
+    __device__ __forceinline__ Row(const typename T::Bits* row, int V) : p(row), n(V)
+    {
+        head = min(V, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(typename T::Bits));
+        pieces = (V - head) / kEach;
+        tail = V - head - pieces * kEach;
+    }
+    __device__ __forceinline__ float at(int i) const { return T::up(p[i]); }
+    struct Piece { float x[kEach]; };
+    __device__ __forceinline__ Piece piece(int v) const
+    {
+        const uint4 b = *reinterpret_cast<const uint4*>(p + head + v * kEach);
+        const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+        Piece y;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            if constexpr (kEach == 4) y.x[e] = __uint_as_float(w[e]);
+            else y.x[e] = T::up((typename T::Bits)(w[e / 2] >> (16 * (e % 2))));
+        }
+        return y;
+    }
+    // every entry once: f(index, value)
+    template <typename F> __device__ __forceinline__ void each(int tid, F f) const
+    {
+        int v = tid;
+        for (; v + 3 * kThreads < pieces; v += 4 * kThreads) {
+            Piece y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = piece(v + q * kThreads);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) f(head + (v + q * kThreads) * kEach + e, y[q].x[e]);
+        }
+        for (; v < pieces; v += kThreads) {
+            const Piece y = piece(v);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) f(head + v * kEach + e, y.x[e]);
+        }
+        if (tid < head) f(tid, at(tid));
+        if (tid < tail) f(n - tail + tid, at(n - tail + tid));
+    }
+};
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 {
-    __shared__ uint64_t mass[kBins > kMostVocab / 64 ? kBins : kMostVocab / 64];
+    // (the slow path's masses of 64 entries each take the room of histogram, candidates and list)
+    __shared__ __align__(16) uint64_t room[kMostVocab / 64];
     __shared__ uint32_t count[kBins];
-    __shared__ uint64_t wave_mass[kWaves], wave_key[kWaves];
+    __shared__ uint64_t wave_mass[kWaves];
     __shared__ uint32_t wave_count[kWaves];
+    __shared__ float wave_top[kWaves];
     __shared__ Found found;
-    __shared__ uint32_t shared_index;
+    __shared__ uint64_t shared_key, shared_mass;
+    __shared__ uint32_t shared_index, filled;
+    uint64_t* mass = room;                                                         // [kBins]
+    float* cand_value = reinterpret_cast<float*>(room + kBins);                    // [kCandidates]
+    uint32_t* cand_index = reinterpret_cast<uint32_t*>(cand_value + kCandidates);  // [kCandidates]
+    uint64_t* list_key = reinterpret_cast<uint64_t*>(cand_index + kCandidates);    // [kList]
+    uint64_t* list_mass = list_key + kList;
+    static_assert(8 * kBins + 8 * kCandidates + 16 * kList <= (int)sizeof(room), "");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.n_vocab;
     const int64_t r = blockIdx.x;
-    const typename T::Bits* row = static_cast<const typename T::Bits*>(a.logits) + r * a.row_stride;
-    auto at = [&](int i) { return cleaned(T::up(row[i])); };
+    const Row<T> row(static_cast<const typename T::Bits*>(a.logits) + r * a.row_stride, V);
+    auto at = [&](int i) { return cleaned(row.at(i)); };
 
-    // the largest logit, the lowest index of equals
-    uint64_t best = 0;
-    for (int i = tid; i < V; i += kThreads) {
-        const uint64_t x = (uint64_t)key_of(at(i)) << 32 | (uint32_t)~i;
-        best = x > best ? x : best;
-    }
-    for (int x = 1; x < 64; x *= 2) { const uint64_t y = __shfl_xor(best, x); best = y > best ? y : best; }
-    if (lane == 0) wave_key[wave] = best;
+    float top = -INFINITY;
+    row.each(tid, [&](int, float x) { top = fmaxf(top, x); });                     // (fmaxf passes NaN over)
+    const float my_top = top;
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    if (lane == 0) wave_top[wave] = top;
+    if (tid == 0) shared_index = 0xffffffffu;
     __syncthreads();
-    for (int w = 0; w < kWaves; ++w) best = wave_key[w] > best ? wave_key[w] : best;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_top[w]);
     const float temperature = a.temperature ? a.temperature[r] : 1.0f;
-    if ((uint32_t)(best >> 32) <= kMinusInf || !(temperature > 0.0f)) {
-        if (tid == 0) a.token[r] = (uint32_t)(best >> 32) <= kMinusInf ? -1 : (int32_t)~(uint32_t)best;
+    if (top == -INFINITY) {
+        if (tid == 0) a.token[r] = -1;
         return;
     }
-    const Scale scale = {value_of((uint32_t)(best >> 32)), 1.0f / temperature};
+    if (!(temperature > 0.0f)) {
+        uint32_t lowest = 0xffffffffu;
+        if (my_top == top) row.each(tid, [&](int i, float x) { if (x == top) lowest = min(lowest, (uint32_t)i); });
+        if (my_top == top) atomicMin(&shared_index, lowest);
+        __syncthreads();
+        if (tid == 0) a.token[r] = (int32_t)shared_index;
+        return;
+    }
+    const Scale scale = {top, 1.0f / temperature};
     const int k = a.top_k && a.top_k[r] > 0 && a.top_k[r] < V ? a.top_k[r] : V;
     const float p = a.top_p ? a.top_p[r] : 1.0f;
     float min_p = a.min_p ? a.min_p[r] : 0.0f;
     min_p = min_p > 1.0f ? 1.0f : min_p;
+    const float u = a.uniform[r];
+    auto mass_passed = [&](uint64_t total) -> uint64_t {                            // floor(u total), below total
+        if (!(u > 0.0f)) return 0;
+        const double want = floor((double)u * (double)total);
+        const uint64_t x = want < (double)total ? (uint64_t)want : total;
+        return x < total ? x : total - 1;
+    };
+    auto mass_needed = [&](uint64_t total) -> uint64_t {                            // ceil(p total), 1 at least
+        const double want = ceil((double)p * (double)total);
+        return want >= 1.0 ? (uint64_t)want : 1;
+    };
+    // the sum over the workgroup; ends behind a barrier
+    auto add_up = [&](uint64_t x) {
+        for (int y = 1; y < 64; y *= 2) x += __shfl_xor(x, y);
+        __syncthreads();
+        if (lane == 0) wave_mass[wave] = x;
+        __syncthreads();
+        x = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x += wave_mass[w];
+        return x;
+    };
+    const bool plain = top < INFINITY && scale.per_t > 0.0f && scale.per_t < INFINITY;
+    // mass of an entry as a float that is a whole number (the floor is exact: from 2^24 on all are whole); 0 for NaN
+    auto whole_mass = [&](float x) { return fmaxf(floorf(expf((x - top) * scale.per_t) * kMassOne), 0.0f); };
 
     // first digit at which the running count (by_mass: mass) of the histogram reaches `need`; ends behind a barrier
     auto search = [&](bool by_mass, uint64_t need) {
@@ -124,6 +224,190 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         atomicAdd(&count[digit], 1u);
         atomicAdd((unsigned long long*)&mass[digit], (unsigned long long)scale.mass(scale.weight(x)));
     };
+    if (plain && k == V && !(p < 1.0f)) {
+        // not cut: masses of runs of 64 pieces; head and tail are runs of their own
+        constexpr int kEach = Row<T>::kEach;
+        const int runs = (row.pieces + 63) / 64, all = runs + 2;
+        auto amount = [&](float x) -> double {
+            const float w = expf((x - top) * scale.per_t);
+            return w < min_p ? 0.0f : fmaxf(floorf(w * kMassOne), 0.0f);
+        };
+        auto lane_sum = [&](int s, double (&m)[kEach]) {                            // entries of run s: what a lane has of it
+            double sum = 0.0;
+            const int v = (s - 1) * 64 + lane;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) m[e] = 0.0;
+            if (s == 0 || s == all - 1) {
+                const int n = s ? row.tail : row.head, i = s ? V - row.tail + lane : lane;
+                if (lane < n) m[0] = amount(row.at(i));
+            } else if (v < row.pieces) {
+                const typename Row<T>::Piece y = row.piece(v);
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) m[e] = amount(y.x[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) sum += m[e];
+            return sum;
+        };
+        double m[kEach];
+        uint64_t sum = 0;
+        for (int s = wave; s < all; s += kWaves) {
+            double x = lane_sum(s, m);                                              // (whole numbers below 2^53: exact)
+            for (int y = 1; y < 64; y *= 2) x += __shfl_xor(x, y);
+            if (lane == 0) room[s] = (uint64_t)x;
+            sum += lane == 0 ? (uint64_t)x : 0;
+        }
+        const uint64_t need = mass_passed(add_up(sum)) + 1;
+        if (wave == 0) {
+            uint64_t before = 0;
+            for (int s0 = 0; s0 < all; s0 += 64) {
+                uint64_t x = s0 + lane < all ? room[s0 + lane] : 0;
+                for (int y = 1; y < 64; y *= 2) { const uint64_t z = __shfl_up(x, y); if (lane >= y) x += z; }
+                const uint64_t hit = __ballot(before + x >= need);
+                if (hit) {
+                    const int f = __ffsll((unsigned long long)hit) - 1, s = s0 + f;
+                    if (f) before += __shfl(x, f - 1);
+                    uint64_t mine = (uint64_t)lane_sum(s, m), z = mine;
+                    for (int y = 1; y < 64; y *= 2) { const uint64_t q = __shfl_up(z, y); if (lane >= y) z += q; }
+                    const uint64_t here = __ballot(before + z >= need);
+                    if (lane == __ffsll((unsigned long long)here) - 1) {
+                        before += z - mine;
+                        int e = 0;
+                        if (s != 0 && s != all - 1)
+                            for (; e < kEach - 1; ++e) {
+                                before += (uint64_t)m[e];
+                                if (before >= need) break;
+                            }
+                        a.token[r] = s == 0 ? lane : s == all - 1 ? V - row.tail + lane : row.head + ((s - 1) * 64 + lane) * kEach + e;
+                    }
+                    break;
+                }
+                before += __shfl(x, 63);
+            }
+        }
+        return;
+    }
+    // The element of `digit` at which the running count or mass of the list's keys, the largest first, reaches `need`: its key, and
+    // the mass up to it; false if the digit has more entries than the list has room for.
+    auto resolve = [&](int n, uint32_t digit, bool by_mass, uint64_t need, auto digit_of, auto key_at, auto mass_at) {
+        __syncthreads();
+        if (tid == 0) filled = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kThreads)
+            if (digit_of(i) == digit) {
+                const uint64_t m = mass_at(i);
+                const uint32_t to = atomicAdd(&filled, 1u);
+                if (to < kList) { list_key[to] = key_at(i); list_mass[to] = m; }
+            }
+        __syncthreads();
+        const int here = (int)filled;
+        if (here > kList) return false;
+        if (tid < here) {
+            const uint64_t key = list_key[tid], mine = list_mass[tid];
+            uint64_t before = 0, above = 0;
+            for (int j = 0; j < here; ++j)
+                if (list_key[j] > key) { before += list_mass[j]; ++above; }
+            const uint64_t x = by_mass ? before : above, y = by_mass ? mine : 1;
+            if (x < need && x + y >= need) { shared_key = key; shared_mass = before + mine; }
+        }
+        __syncthreads();
+        return true;
+    };
+    bool fast = plain && (k == V || k <= kThreads || V <= kCandidates);
+    if (fast) {
+        // digits up to `last` can be kept
+        uint32_t last = kNoMass - 1;
+        if (V > kCandidates) {
+            for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; }
+            __syncthreads();
+            if (my_top > -INFINITY) atomicAdd(&count[scale.bin(my_top)], 1u);
+            if (tid == 0) found = {kBins, 0, 0, 0, 0};
+            last = min(last, search(false, (uint64_t)(k < V ? k : kRank)).digit);
+        }
+        if (tid == 0) filled = 0;
+        __syncthreads();
+        const float edge = (float)(last + 1);
+        uint64_t total = 0;
+        auto take = [&](int i, float x) {
+            if ((top - x) * scale.per_t * 64.0f < edge) {                            // (false for NaN)
+                const uint32_t to = atomicAdd(&filled, 1u);
+                if (to < kCandidates) { cand_value[to] = x + 0.0f; cand_index[to] = (uint32_t)i; }
+            }
+        };
+        if (k < V) {
+            row.each(tid, take);
+        } else {
+            double sum = 0.0;                          // (whole numbers, at most 512 of 2^43: exact)
+            row.each(tid, [&](int i, float x) { sum += (double)whole_mass(x); take(i, x); });
+            total = add_up((uint64_t)sum);
+        }
+        __syncthreads();
+        const int n = (int)filled;
+        fast = n <= kCandidates;
+        if (fast) {
+            auto digit_of = [&](int i) { return scale.bin(cand_value[i]); };
+            auto key_at = [&](int i) { return (uint64_t)key_of(cand_value[i]) << 32 | (uint32_t)~cand_index[i]; };
+            auto mass_at = [&](int i) { return (uint64_t)whole_mass(cand_value[i]); };
+            clear();
+            for (int i = tid; i < n; i += kThreads) put(digit_of(i), cand_value[i]);
+            // kept: digits before `digit`, and of it the keys from `key` on
+            uint32_t digit = kBins;
+            uint64_t key = 0;
+            if (k < n) {
+                const Found f = search(false, (uint64_t)k);
+                const uint64_t need = (uint64_t)k - f.count_before;
+                digit = f.digit;
+                total = f.mass_before + f.mass;
+                if (need < f.count) {
+                    fast = resolve(n, digit, false, need, digit_of, key_at, mass_at);
+                    if (fast) { key = shared_key; total = f.mass_before + shared_mass; }
+                }
+            } else if (k < V) {                        // (fewer entries with a mass than top_k)
+                uint64_t sum = 0;
+                for (int i = tid; i < n; i += kThreads) sum += mass_at(i);
+                total = add_up(sum);
+            }
+            if (fast && p < 1.0f) {
+                const uint64_t need = mass_needed(total);
+                __syncthreads();
+                if (tid == 0) found = {kBins, 0, 0, 0, 0};
+                const Found f = search(true, need);
+                fast = f.digit < kBins;                // (else the candidates hold too little)
+                if (fast) {
+                    digit = f.digit;
+                    key = 0;
+                    fast = resolve(n, digit, true, need - f.mass_before, digit_of, key_at, mass_at);
+                    if (fast) key = shared_key;
+                }
+            }
+            if (fast) {
+                auto kept = [&](int i) -> uint64_t {
+                    const uint32_t d = digit_of(i);
+                    if (d > digit || (d == digit && key_at(i) < key)) return 0;
+                    if (expf((cand_value[i] - top) * scale.per_t) < min_p) return 0;
+                    return mass_at(i);
+                };
+                // the same search along the index: 2048 runs of the vocabulary
+                int shift = 0;
+                while (((V - 1) >> shift) >= kBins) ++shift;
+                clear();
+                uint64_t sum = 0;
+                for (int i = tid; i < n; i += kThreads) {
+                    const uint64_t m = kept(i);
+                    if (m) atomicAdd((unsigned long long*)&mass[cand_index[i] >> shift], (unsigned long long)m);
+                    sum += m;
+                }
+                const uint64_t need = mass_passed(add_up(sum)) + 1;
+                const Found f = search(true, need);
+                fast = resolve(n, f.digit, true, need - f.mass_before, [&](int i) { return cand_index[i] >> shift; },
+                               [&](int i) { return (uint64_t)(uint32_t)~cand_index[i]; }, kept);
+                if (fast) {
+                    if (tid == 0) a.token[r] = (int32_t)~(uint32_t)shared_key;
+                    return;
+                }
+            }
+        }
+    }
     // the end of a prefix: all of the bins before `bin`, and of it all (whole) or the keys above `key` and `ties` entries of it
     struct End { uint32_t bin, key, ties, equal; bool whole; uint64_t mass; };
     End end = {kBins - 1, 0, 0, 0, true, 0};
@@ -162,16 +446,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         end.bin = in_k.digit;
         bool cut_k = (uint64_t)k - in_k.count_before < in_k.count;
         if (p < 1.0f && !cut_k) {
-            const double want = ceil((double)p * (double)total);
-            need = want >= 1.0 ? (uint64_t)want : 1;
+            need = mass_needed(total);
             in_p = search(true, need);
         }
         if (cut_k) {
             end = descend(false, in_k, (uint64_t)k - in_k.count_before);
             total = end.mass;
             if (p < 1.0f) {
-                const double want = ceil((double)p * (double)total);
-                need = want >= 1.0 ? (uint64_t)want : 1;
+                need = mass_needed(total);
                 clear();
                 for (int i = tid; i < V; i += kThreads) { const float x = at(i); put(scale.bin(x), x); }
                 in_p = search(true, need);
@@ -233,13 +515,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     __syncthreads();
     total = 0;
     for (int w = 0; w < kWaves; ++w) total += wave_mass[w];
-    const float u = a.uniform[r];
-    uint64_t passed = 0;
-    if (u > 0.0f) {
-        const double want = floor((double)u * (double)total);
-        passed = want < (double)total ? (uint64_t)want : total - 1;
-        if (passed >= total) passed = total - 1;
-    }
+    const uint64_t passed = mass_passed(total);
     const uint32_t token = lowest(passed + 1, kept);
     if (tid == 0) a.token[r] = (int32_t)token;
 }
