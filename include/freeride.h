@@ -594,7 +594,7 @@ int fr_stage_op_times(fr_stage* s, uint64_t* ns_host, size_t cap, size_t* n_out)
 
 /* A cache of keys and values in pages of page_size slots.  Element (page, head, slot, i) of K lies at
    k[page * page_stride + head * head_stride + slot * slot_stride + i], of V likewise: pages of a head side by side, heads of
-   a slot side by side, K and V in one array are all views of that.  Strides are in elements, multiples of 8, not negative;
+   a slot side by side, K and V in one array are all views of that.  Strides are in elements, multiples of 8 from 0 to 2^31;
    k and v are 16-byte aligned. */
 typedef struct fr_kv_pages {
     void*    k;

@@ -2,6 +2,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "lm_types.h"
@@ -22,6 +23,9 @@ struct Segment {                           // the work of one of the two kinds o
     int32_t row_tiles, splits, split_len, first_part, groups, units;
 };
 
+typedef std::integral_constant<uint32_t, 0> Even;
+typedef std::integral_constant<uint32_t, 1> Odd;
+
 enum Kind { kNone, kFewRows, kWideRows };
 
 struct AttendArgs {
@@ -40,6 +44,8 @@ struct AttendArgs {
     float2* part_ml;                       // [parts][n_tokens * n_q_heads]: m in powers of 2, sum
 };
 
+// The instruction scheduler keeps what stands on either side of this apart.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
 __device__ __forceinline__ int32_t within(int32_t x, int32_t lo, int32_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(kLeft) : "memory"); }
@@ -96,90 +102,88 @@ template <int D> struct Lds {
     static constexpr uint32_t kBytes = 512 * D;                   // 64 KB at D = 128: two workgroups share a compute unit
     static __device__ __forceinline__ uint32_t fk(uint32_t r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
     static __device__ __forceinline__ uint32_t fv(uint32_t r) { return D == 128 ? (r & 3) * 4 : (r & 2) * 2; }
+    // the chunk that a lane loads in load y of rows y * kRowsALoad + lane / kChunks: the one whose place is its own
+    static __device__ __forceinline__ uint32_t k_piece(uint32_t lane, int y) { return (lane % kChunks) ^ fk(y * kRowsALoad + lane / kChunks); }
+    static __device__ __forceinline__ uint32_t v_piece(uint32_t lane, int y) { return (lane % kChunks) ^ fv(y * kRowsALoad + lane / kChunks); }
 };
 
 // The state of 32 query rows in a wavefront: lane l holds row l % 32 (keys of its half of every block), the result transposed.
 template <typename T, int D> struct Softmax {
     f32x16 o[D / 32];
-    float m, l;                            // running maximum of the scores (before the scale), sum of this half's weights
+    float m, l, l1;                        // running maximum of the scores (before the scale); sums of this half's weights, even and odd keys
     typename T::x8 q[D / 16];
 
     __device__ __forceinline__ void start()
     {
         m = -INFINITY;
-        l = 0.0f;
+        l = l1 = 0.0f;
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     }
 
-    // Scores of kBlocks x 32 keys to weights: the blocks' key of element i is 8 (i / 4) + 4 (lane / 32) + i % 4.
-    template <int kBlocks>
-    __device__ __forceinline__ void weigh(f32x16 (&s)[kBlocks], float c, int first, int end, int lane)
+    // Scores of kBlocks x 32 keys: element i of a block is key 8 (i / 4) + 4 (lane / 32) + i % 4.  Keys from `end` on are not seen.
+    template <int kBlocks> static __device__ __forceinline__ void hide(f32x16 (&s)[kBlocks], int first, int end, int lane)
     {
-        if (first + 32 * kBlocks > end) {  // (end: keys that the row sees, at most the workgroup's last)
+        if (first + 32 * kBlocks > end) {
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (first + b * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= end) s[b][i] = -INFINITY;
         }
-        float top = s[0][0];
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = of_both_halves(top);
-        if (__any((top - m) * c > kSlack)) {                       // (m = -infinity: the first keys a row sees)
+    }
+    // A larger maximum, if the one in use lags behind by more than kSlack (m = -infinity: the first keys a row sees).
+    __device__ __forceinline__ void grow(float top, float c)
+    {
+        if (__any((top - m) * c > kSlack)) {
             const float now = fmaxf(top, m), old = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * c);
             m = now;
             l *= old;
+            l1 *= old;
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= old;
         }
-        const float base = m == -INFINITY ? 0.0f : m * c;
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -base));
-                sum[i % 4] += s[b][i];
-            }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
-
+    __device__ __forceinline__ float base(float c) const { return m == -INFINITY ? 0.0f : m * c; }
+    // Two weights for the product with the values, rounded to the type (the matrix cores take 16 bits: half an ulp of a weight is
+    // what the result's own rounding costs); their sum is of the weights as they are.
+    __device__ __forceinline__ uint32_t weigh(float s0, float s1, float c, float base)
+    {
+        const float w0 = __builtin_amdgcn_exp2f(fmaf(s0, c, -base)), w1 = __builtin_amdgcn_exp2f(fmaf(s1, c, -base));
+        l += w0;
+        l1 += w1;
+        return T::pack(w0, w1);
+    }
     // The eight keys a lane's fragment of P holds are four and four neighbours (16 x + 4 h + .., 16 x + 8 + 4 h + ..), as they come
     // out of the scores; a transposed read of V takes four neighbouring keys, so that it has the same order.
-    static __device__ __forceinline__ typename T::x8 weights(const f32x16& s, int half)
-    {
-        const uint4 x = make_uint4(T::pack(s[8 * half], s[8 * half + 1]), T::pack(s[8 * half + 2], s[8 * half + 3]),
-                                   T::pack(s[8 * half + 4], s[8 * half + 5]), T::pack(s[8 * half + 6], s[8 * half + 7]));
-        return __builtin_bit_cast(typename T::x8, x);
-    }
+    static __device__ __forceinline__ typename T::x8 fragment(const uint32_t* w) { return __builtin_bit_cast(typename T::x8, make_uint4(w[0], w[1], w[2], w[3])); }
 };
 
-// Fragment of K: lane l has row l % 32, elements 16 s + 8 (l / 32) .. + 7.
-template <typename T, int D> __device__ __forceinline__ typename T::x8 k_fragment(uint32_t tile, int s, int lane)
-{
-    typedef const __attribute__((address_space(3))) typename T::x8* Fragment;
-    const uint32_t r = lane & 31;
-    return *reinterpret_cast<Fragment>(lds_at(tile + r * Lds<D>::kRow + (((uint32_t)(2 * s + (lane >> 5))) ^ Lds<D>::fk(r)) * 16));
-}
-
-// Fragment of V transposed: lane l has element 32 d + l % 32 of the keys 16 x + 4 (l / 32) .. + 3 and 16 x + 8 + 4 (l / 32) .. + 3.
-template <typename T, int D> __device__ __forceinline__ typename T::x8 v_fragment(uint32_t tile, int x, int d, int lane)
-{
+// Where a lane's fragments lie in a tile.  K: lane l has row l % 32, elements 16 f + 8 (l / 32) .. + 7 of fragment f.  V, transposed: lane l
+// has element 32 d + l % 32 of the keys 16 x + 4 (l / 32) .. + 3 and 16 x + 8 + 4 (l / 32) .. + 3.
+template <typename T, int D> struct Fragments {
+    typedef const __attribute__((address_space(3))) typename T::x8* Eight;
     typedef __attribute__((address_space(3))) i16x4* Quad;
-    const uint32_t i = lane & 15, r = 16 * x + 4 * (lane >> 5) + (i >> 2), chunk = d * 4 + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
-    const uint32_t at = tile + r * Lds<D>::kRow + (chunk ^ Lds<D>::fv(r)) * 16 + (i & 1) * 8;      // (fv(r + 8) = fv(r))
-    struct { i16x4 lo, hi; } y = {__builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<Quad>(lds_at(at))),
-                                  __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<Quad>(lds_at(at + 8 * Lds<D>::kRow)))};
-    return __builtin_bit_cast(typename T::x8, y);
-}
+    uint32_t k, v;                         // of the first fragment; the others' chunks differ in bits that f leaves alone (lds on 1024 bytes)
+    __device__ __forceinline__ Fragments(uint32_t lds, int lane)
+    {
+        const uint32_t r = lane & 31, i = lane & 15, rv = 4 * (lane >> 5) + (i >> 2);
+        k = lds + r * Lds<D>::kRow + ((uint32_t)(lane >> 5) ^ Lds<D>::fk(r)) * 16;
+        v = lds + rv * Lds<D>::kRow + ((uint32_t)(((lane >> 4) & 1) * 2 + ((i & 3) >> 1)) ^ Lds<D>::fv(rv)) * 16 + (i & 1) * 8;
+    }
+    __device__ __forceinline__ typename T::x8 of_k(int tile, int f) const { return *reinterpret_cast<Eight>(lds_at(k ^ (uint32_t)(f * 32)) + tile); }
+    __device__ __forceinline__ typename T::x8 of_v(int tile, int x, int d) const
+    {                                      // (rows r + 8 and r + 16 have r's order of chunks)
+        const LdsBytes at = lds_at(v ^ (uint32_t)(d * 64)) + tile + 16 * x * (int)Lds<D>::kRow;
+        struct { i16x4 lo, hi; } y = {__builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<Quad>(at)),
+                                      __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<Quad>(at + 8 * (int)Lds<D>::kRow))};
+        return __builtin_bit_cast(typename T::x8, y);
+    }
+};
 
 // One workgroup: four wavefronts.  kWide: 128 rows, 32 a wavefront, which share tiles of 64 keys; else 32 rows, and every
 // wavefront takes every fourth tile of 32 keys for itself, the four results being joined at the end.
@@ -206,69 +210,126 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         for (int s = 0; s < D / 16; ++s) x.q[s] = __builtin_bit_cast(typename T::x8, *reinterpret_cast<const uint4*>(q + s * 16));
     }
 
+    // (which part of which row a lane loads is made anew from `anew(lane)` for every tile: kept, it holds registers that the loop needs)
+    auto anew = [](int x) { asm volatile("" : "+v"(x)); return (uint32_t)x; };
+
     // page ids of n keys from `first` on, a lane each, to LDS; keys behind the last stand for the last
     auto ask_ids = [&](uint32_t to, int first, int n) {
         const int j = min(first + (lane & (n - 1)), w.k1 - 1), own = j - a.prefix_len;
         const int32_t* g = own < 0 ? a.prefix_pages + (j >> a.page_shift) : w.own_pages + (own >> a.page_shift);
         load4_to_lds(to, g);
     };
-    // offset of the 16 bytes that this lane loads of key row r (counted from `first`, whose ids stand at `from`)
-    auto offset = [&](uint32_t from, int first, uint32_t r) -> int64_t {
-        const int j = min(first + (int)r, w.k1 - 1), in = j < a.prefix_len ? j : j - a.prefix_len;
-        const int32_t id = within(*reinterpret_cast<const __attribute__((address_space(3))) int32_t*>(lds_at(from + r * 4)), 0, (int32_t)a.c.n_pages - 1);
-        return (int64_t)id * a.c.page_stride + (int64_t)(in & (a.c.page_size - 1)) * a.c.slot_stride;
+    // offsets of the rows that this lane loads a part of, rows y * kRowsALoad + its own, counted from `first`, whose ids stand at `from`
+    auto offsets = [&](uint32_t from, int first, auto& where) {
+        constexpr int n = std::extent<std::remove_reference_t<decltype(where)>>::value;
+        const uint32_t load_row = anew(lane) / L::kChunks;
+        uint32_t id[n];
+#pragma unroll
+        for (int y = 0; y < n; ++y) id[y] = *reinterpret_cast<const __attribute__((address_space(3))) uint32_t*>(lds_at(from + (y * L::kRowsALoad + load_row) * 4));
+#pragma unroll
+        for (int y = 0; y < n; ++y) {
+            const int j = min(first + (int)(y * L::kRowsALoad + load_row), w.k1 - 1), in = j < a.prefix_len ? j : j - a.prefix_len;
+            const uint32_t page = (uint32_t)within((int32_t)id[y], 0, (int32_t)a.c.n_pages - 1);
+            where[y] = (int64_t)((uint64_t)page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)(in & (a.c.page_size - 1)) * (uint32_t)a.c.slot_stride);
+        }
     };
     const uint16_t* gk = static_cast<const uint16_t*>(a.c.k) + w.kv * a.c.head_stride;
     const uint16_t* gv = static_cast<const uint16_t*>(a.c.v) + w.kv * a.c.head_stride;
-    const uint32_t load_row = lane / L::kChunks, place = lane % L::kChunks;
-
     if (w.k0 < w.k1) {
         if constexpr (kWide) {
+            // While tile t's scores become weights (vector unit), the matrix cores make those of tile t + 1: K runs a tile ahead of V.
             constexpr int kTile = 64, kLoads = 16 / L::kRowsALoad;         // a wavefront loads 16 rows of each
-            constexpr uint32_t kHalf = kTile * L::kRow, kStage = 2 * kHalf;
+            constexpr uint32_t kHalf = kTile * L::kRow;
             const int tiles = (w.k1 - w.k0 + kTile - 1) / kTile;
             const uint32_t my_ids = ids + wave * 512;       // (64 lanes write 256 bytes at a time)
             auto first_of = [&](int t) { return w.k0 + t * kTile + wave * 16; };
-            auto ask = [&](int t) {
-                const uint32_t to = lds + (t & 1) * kStage + wave * 16 * L::kRow, from = my_ids + (t & 1) * 256;
+            int64_t at[kLoads];                             // of the tile whose V is asked for next
+            auto ask_k = [&](int t, auto odd) {
+                offsets(my_ids + odd * 256, first_of(t), at);
+                const uint32_t l = anew(lane);
 #pragma unroll
-                for (int x = 0; x < kLoads; ++x) {
-                    const uint32_t r = x * L::kRowsALoad + load_row;
-                    const int64_t at = offset(from, first_of(t), r);
-                    load16_to_lds(to + x * 1024, gk + at + (place ^ L::fk(r)) * 8);
-                    load16_to_lds(to + kHalf + x * 1024, gv + at + (place ^ L::fv(r)) * 8);
+                for (int y = 0; y < kLoads; ++y) load16_to_lds(lds + odd * kHalf + wave * 16 * L::kRow + y * 1024, gk + at[y] + L::k_piece(l, y) * 8);
+            };
+            auto ask_v = [&](auto odd) {
+                const uint32_t l = anew(lane);
+#pragma unroll
+                for (int y = 0; y < kLoads; ++y) load16_to_lds(lds + (2 + odd) * kHalf + wave * 16 * L::kRow + y * 1024, gv + at[y] + L::v_piece(l, y) * 8);
+            };
+            constexpr int kSteps = D / 8, kElements = 32 / kSteps;          // MFMAs of the scores, and as many with the values
+            constexpr int kAhead = 4;                                       // fragments read ahead of their MFMA
+            const Even even{};
+            const Odd odd{};
+            Fragments<T, D> fragments(lds, lane);
+            typename T::x8 ahead[kAhead];
+            auto k_of = [&](auto odd, int y) { return fragments.of_k(odd * kHalf + y % 2 * 32 * L::kRow, y / 2); };
+            auto v_of = [&](auto odd, int y) { return fragments.of_v((2 + odd) * kHalf, y / (D / 32), y % (D / 32)); };
+            const f32x16 zero = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            float top = -INFINITY;
+            auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2], int t, auto here, auto other) {      // (here: t modulo 2)
+                wait_loads<0>();
+                __syncthreads();                            // K of t + 1 and V of t are here; K of t and V of t - 1 are done with
+                if (!idle) {
+                    asm volatile("" : "+v"(fragments.k), "+v"(fragments.v));        // (one register each, not one for every fragment)
+#pragma unroll
+                    for (int y = 0; y < kAhead; ++y) ahead[y] = k_of(other, y);
                 }
+                if (t + 1 < tiles) ask_v(other);
+                if (t + 2 < tiles) {
+                    ask_k(t + 2, here);
+                    ask_ids(my_ids + other * 256, first_of(t + 3), 16);
+                }
+                if (idle) return;
+                x.grow(top, c);
+                const float base = x.base(c);
+                uint32_t p[16];
+                keep_order();
+#pragma unroll
+                for (int y = 0; y < kSteps; ++y) {          // (behind the last tile: of what lies there, not used)
+                    next[y % 2] = mfma<T>(ahead[y % kAhead], x.q[y / 2], y < 2 ? zero : next[y % 2]);
+                    ahead[y % kAhead] = y + kAhead < kSteps ? k_of(other, y + kAhead) : v_of(here, y + kAhead - kSteps);
+#pragma unroll
+                    for (int e = y * kElements; e < (y + 1) * kElements; e += 2) {
+                        p[e / 2] = x.weigh(now[e / 16][e % 16], now[e / 16][e % 16 + 1], c, base);
+                        asm volatile("" : "+v"(p[e / 2]), "+v"(x.l), "+v"(x.l1));     // (made here, not where they are used)
+                    }
+                    keep_order();
+                }
+                x.template hide<2>(next, w.k0 + (t + 1) * kTile, end, lane);
+                top = -INFINITY;
+                keep_order();
+#pragma unroll
+                for (int y = 0; y < kSteps; ++y) {
+                    const int f = y / (D / 32), d = y % (D / 32);
+                    x.o[d] = mfma<T>(ahead[y % kAhead], Softmax<T, D>::fragment(p + 4 * f), x.o[d]);
+                    if (y + kAhead < kSteps) ahead[y % kAhead] = v_of(here, y + kAhead);
+#pragma unroll
+                    for (int e = y * kElements; e < (y + 1) * kElements; ++e) top = fmaxf(top, next[e / 16][e % 16]);
+                    keep_order();
+                }
+                top = of_both_halves(top);
             };
             ask_ids(my_ids, first_of(0), 16);
             ask_ids(my_ids + 256, first_of(1), 16);
             wait_loads<0>();
-            ask(0);
-            for (int t = 0; t < tiles; ++t) {
-                wait_loads<0>();
-                __syncthreads();                         // tile t is here, and everybody is done with tile t - 1
-                if (t + 1 < tiles) {
-                    ask(t + 1);
-                    wait_lds();
-                    ask_ids(my_ids + (t & 1) * 256, first_of(t + 2), 16);
-                }
-                if (idle) continue;
-                const uint32_t k = lds + (t & 1) * kStage, v = k + kHalf;
-                f32x16 s[2];
+            ask_k(0, even);
+            wait_loads<0>();
+            __syncthreads();
+            ask_v(even);
+            if (tiles > 1) ask_k(1, odd);
+            wait_lds();
+            ask_ids(my_ids, first_of(2), 16);
+            f32x16 s0[2], s1[2];
+            if (!idle) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int y = 0; y < kSteps; ++y) s0[y % 2] = mfma<T>(k_of(even, y), x.q[y / 2], y < 2 ? zero : s0[y % 2]);
+                x.template hide<2>(s0, w.k0, end, lane);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
-#pragma unroll
-                for (int f = 0; f < D / 16; ++f)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) s[b] = mfma<T>(k_fragment<T, D>(k + b * 32 * L::kRow, f, lane), x.q[f], s[b]);
-                x.template weigh<2>(s, c, w.k0 + t * kTile, end, lane);
-#pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const typename T::x8 p = Softmax<T, D>::weights(s[f / 2], f % 2);
-#pragma unroll
-                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma<T>(v_fragment<T, D>(v, f, d, lane), p, x.o[d]);
-                }
+                for (int e = 0; e < 32; ++e) top = fmaxf(top, s0[e / 16][e % 16]);
+                top = of_both_halves(top);
+            }
+            for (int t = 0; t < tiles; t += 2) {
+                step(s0, s1, t, even, odd);
+                if (t + 1 < tiles) step(s1, s0, t + 1, odd, even);
             }
         } else {
             constexpr int kTile = 32, kLoads = kTile / L::kRowsALoad;
@@ -276,18 +337,18 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
             const int all = (w.k1 - w.k0 + kTile - 1) / kTile, tiles = (all - wave + kWaves - 1) / kWaves;
             const uint32_t k = lds + wave * 2 * kHalf, v = k + kHalf, my_ids = ids + wave * 512;
             auto first_of = [&](int t) { return w.k0 + (t * kWaves + wave) * kTile; };
+            const Fragments<T, D> fragments(k, lane);
             int64_t at[kLoads];
             auto ask_k = [&](int t) {
+                offsets(my_ids + (t & 1) * 256, first_of(t), at);
+                const uint32_t l = anew(lane);
 #pragma unroll
-                for (int x = 0; x < kLoads; ++x) {
-                    const uint32_t r = x * L::kRowsALoad + load_row;
-                    at[x] = offset(my_ids + (t & 1) * 256, first_of(t), r);
-                    load16_to_lds(k + x * 1024, gk + at[x] + (place ^ L::fk(r)) * 8);
-                }
+                for (int y = 0; y < kLoads; ++y) load16_to_lds(k + y * 1024, gk + at[y] + L::k_piece(l, y) * 8);
             };
             auto ask_v = [&] {
+                const uint32_t l = anew(lane);
 #pragma unroll
-                for (int x = 0; x < kLoads; ++x) load16_to_lds(v + x * 1024, gv + at[x] + (place ^ L::fv(x * L::kRowsALoad + load_row)) * 8);
+                for (int y = 0; y < kLoads; ++y) load16_to_lds(v + y * 1024, gv + at[y] + L::v_piece(l, y) * 8);
             };
             if (tiles > 0) {
                 ask_ids(my_ids, first_of(0), kTile);
@@ -302,7 +363,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 wait_loads<kLoads>();
                 typename T::x8 kf[D / 16];
 #pragma unroll
-                for (int f = 0; f < D / 16; ++f) kf[f] = k_fragment<T, D>(k, f, lane);
+                for (int f = 0; f < D / 16; ++f) kf[f] = fragments.of_k(0, f);
                 wait_lds();
                 if (more) {
                     ask_ids(my_ids + (t & 1) * 256, first_of(t + 2), kTile);
@@ -313,15 +374,21 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
 #pragma unroll
                 for (int f = 0; f < D / 16; ++f) s[0] = mfma<T>(kf[f], x.q[f], s[0]);
-                x.template weigh<1>(s, c, first_of(t), end, lane);
+                x.template hide<1>(s, first_of(t), end, lane);
+                float top = s[0][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
+                x.grow(of_both_halves(top), c);
+                const float base = x.base(c);
+                uint32_t p[8];
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) p[i / 2] = x.weigh(s[0][i], s[0][i + 1], c, base);
                 if (more) wait_loads<kLoads + 1>();
                 else wait_loads<0>();
 #pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const typename T::x8 p = Softmax<T, D>::weights(s[0], f);
+                for (int f = 0; f < 2; ++f)
 #pragma unroll
-                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma<T>(v_fragment<T, D>(v, f, d, lane), p, x.o[d]);
-                }
+                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma<T>(fragments.of_v(kHalf, f, d), Softmax<T, D>::fragment(p + 4 * f), x.o[d]);
                 wait_lds();
                 if (more) ask_v();
             }
@@ -337,7 +404,9 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 for (int i = 0; i < 16; ++i) bad |= !(fabsf(x.o[d][i]) < INFINITY);
         }
         if (__any(bad && !idle) && !idle) {
-            const float base = x.m == -INFINITY ? 0.0f : x.m * c;
+            const float base = x.base(c);
+            const int mine = min(row_first + (int)(anew(lane) & 31), w.rows - 1);
+            const uint16_t* q = a.q + rows.token(mine) * a.q_stride + (int64_t)rows.head(mine) * D;
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -347,7 +416,6 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 const int in = j < a.prefix_len ? j : j - a.prefix_len;
                 const int32_t id = within(j < a.prefix_len ? a.prefix_pages[in >> a.page_shift] : w.own_pages[in >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
                 const int64_t at = (int64_t)id * a.c.page_stride + (int64_t)(in & (a.c.page_size - 1)) * a.c.slot_stride;
-                const uint16_t* q = a.q + rows.token(row_here) * a.q_stride + (int64_t)rows.head(row_here) * D;
                 float s = 0.0f;
                 for (int e = 0; e < D; ++e) s = fmaf(T::up(q[e]), T::up(gk[at + e]), s);
                 const float p = T::up((uint16_t)T::pack(__builtin_amdgcn_exp2f(fmaf(s, c, -base)), 0.0f));
@@ -358,7 +426,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
             }
         }
     }
-    x.l = sum_of_both_halves(x.l);
+    x.l = sum_of_both_halves(x.l + x.l1);
 
     // results through LDS, so that rows are written whole: a wavefront's 32 rows of D floats, 16-byte chunk c of row r at c ^ r
     __shared__ float2 row_ml[kWaves][kRows];

@@ -50,8 +50,7 @@ inline bool kv_pages_ok(const fr_kv_pages& c)
 {
     if (!kv_pages_shape_ok(c) || !c.k || !c.v || (((uintptr_t)c.k | (uintptr_t)c.v) & 15)) return false;
     if (c.n_pages < 1 || c.n_pages > 0x7fffffff) return false;
-    const int64_t most = (int64_t)1 << 45;
     for (int64_t s : {c.page_stride, c.head_stride, c.slot_stride})
-        if (s < 0 || s > most || s % 8) return false;
+        if (s < 0 || s > 0x7fffffff || s % 8) return false;
     return true;
 }
