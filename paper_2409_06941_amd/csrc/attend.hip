@@ -15,18 +15,18 @@ typedef __attribute__((address_space(3))) char* LdsBytes;
 __device__ __forceinline__ LdsBytes lds_at(uint32_t address) { return reinterpret_cast<LdsBytes>(address); }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kXcds = 8, kThreads = 256, kWaves = 4;
+constexpr int kXcds = 8, kUnits = 256, kThreads = 256, kWaves = 4;
 constexpr int kRows = 32;                  // query rows of a wavefront: the columns of its MFMA blocks
 constexpr float kSlack = 8.0f;             // a running maximum may lag behind by a factor of 2^8 in the weights
 
 struct Segment {                           // the work of one of the two kinds of workgroups
-    int32_t row_tiles, splits, split_len, first_part, groups, units;
+    int32_t row_tiles, splits, split_len, first_part, items, groups, units;      // (a group: what follows one another on an XCD, its row tiles)
 };
 
 typedef std::integral_constant<uint32_t, 0> Even;
 typedef std::integral_constant<uint32_t, 1> Odd;
 
-enum Kind { kNone, kFewRows, kWideRows };
+enum Kind { kNone, kFewRows, kWaveRows, kWideRows };
 
 struct AttendArgs {
     fr_kv_pages c;
@@ -185,12 +185,15 @@ template <typename T, int D> struct Fragments {
     }
 };
 
-// One workgroup: four wavefronts.  kWide: 128 rows, 32 a wavefront, which share tiles of 64 keys; else 32 rows, and every
-// wavefront takes every fourth tile of 32 keys for itself, the four results being joined at the end.
-template <typename T, int D, bool kWide>
+// One workgroup: four wavefronts.  kWideRows: 128 rows, 32 a wavefront, which share tiles of 64 keys.  kFewRows: 32 rows, and every
+// wavefront takes every fourth tile of 32 keys for itself, the four results being joined at the end.  kWaveRows: every wavefront
+// has an item of its own, 32 rows and all of its keys in tiles of 32, and meets no barrier.
+template <typename T, int D, Kind kKind>
 __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char* lds_array, int32_t* ids_array)
 {
     typedef Lds<D> L;
+    constexpr bool kWide = kKind == kWideRows, kAlone = kKind == kWaveRows;
+    constexpr int kSharers = kAlone ? 1 : kWaves;           // wavefronts that deal tiles of 32 keys out among themselves
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t lds = (uint32_t)reinterpret_cast<uintptr_t>((LdsBytes)lds_array), ids = (uint32_t)reinterpret_cast<uintptr_t>((LdsBytes)(char*)ids_array);
     asm volatile("" ::"s"(lds), "s"(ids) : "memory");       // (both arrays are written behind the compiler's back)
@@ -334,9 +337,9 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         } else {
             constexpr int kTile = 32, kLoads = kTile / L::kRowsALoad;
             constexpr uint32_t kHalf = kTile * L::kRow;
-            const int all = (w.k1 - w.k0 + kTile - 1) / kTile, tiles = (all - wave + kWaves - 1) / kWaves;
+            const int all = (w.k1 - w.k0 + kTile - 1) / kTile, mine = kAlone ? 0 : wave, tiles = (all - mine + kSharers - 1) / kSharers;
             const uint32_t k = lds + wave * 2 * kHalf, v = k + kHalf, my_ids = ids + wave * 512;
-            auto first_of = [&](int t) { return w.k0 + (t * kWaves + wave) * kTile; };
+            auto first_of = [&](int t) { return w.k0 + (t * kSharers + mine) * kTile; };
             const Fragments<T, D> fragments(k, lane);
             int64_t at[kLoads];
             auto ask_k = [&](int t) {
@@ -412,7 +415,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x.o[d][i] = 0.0f;
             for (int j = w.k0; j < end; ++j) {
-                if (!kWide && (j - w.k0) / 32 % kWaves != wave) continue;
+                if (kKind == kFewRows && (j - w.k0) / 32 % kWaves != wave) continue;
                 const int in = j < a.prefix_len ? j : j - a.prefix_len;
                 const int32_t id = within(j < a.prefix_len ? a.prefix_pages[in >> a.page_shift] : w.own_pages[in >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
                 const int64_t at = (int64_t)id * a.c.page_stride + (int64_t)(in & (a.c.page_size - 1)) * a.c.slot_stride;
@@ -433,12 +436,16 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
     typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
     typedef __attribute__((address_space(3))) f32x4* LdsFloats;
     constexpr uint32_t kFloatRow = D * 4, kFloatChunks = D / 4;
-    __syncthreads();                                     // tiles are done with
+    auto meet = [] {
+        if constexpr (!kAlone) __syncthreads();
+        else wait_lds();
+    };
+    meet();                                              // tiles are done with
     const float m2 = x.m * c;                            // (-infinity stays: c is positive)
     float mine = 1.0f;
     if (lane < 32) row_ml[wave][lane] = make_float2(m2, x.l);
-    if constexpr (!kWide) {
-        __syncthreads();
+    if constexpr (kKind == kFewRows) {
+        meet();
         float top = -INFINITY;
 #pragma unroll
         for (int y = 0; y < kWaves; ++y) top = fmaxf(top, row_ml[y][lane & 31].x);
@@ -453,19 +460,23 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
             *reinterpret_cast<LdsFloats>(lds_at(region + r * kFloatRow + (chunk ^ (r & (kFloatChunks - 1))) * 16)) =
                 f32x4{x.o[d][i] * mine, x.o[d][i + 1] * mine, x.o[d][i + 2] * mine, x.o[d][i + 3] * mine};
         }
-    __syncthreads();
+    meet();
     // a thread takes eight elements of a row: two chunks
     constexpr int kPieces = D / 8, kOutRows = kWide ? kWaves * kRows : kRows;
-    for (int y = tid; y < kOutRows * kPieces; y += kThreads) {
+    for (int y = kAlone ? lane : tid; y < kOutRows * kPieces; y += kAlone ? 64 : kThreads) {
         const int r = y / kPieces, piece = y % kPieces, from = w.row0 + r;
-        if (from >= w.rows) continue;
+        if (from >= w.rows) {
+            if (kWide) continue;
+            break;
+        }
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
         float top, sum;
         const int in = r % kRows;
         auto chunk = [&](int wv, int e) { return *reinterpret_cast<LdsFloats>(lds_at(lds + (wv * kRows + in) * kFloatRow + ((uint32_t)(2 * piece + e) ^ (in & (kFloatChunks - 1))) * 16)); };
-        if constexpr (kWide) {
-            lo = chunk(r / kRows, 0), hi = chunk(r / kRows, 1);
-            top = row_ml[r / kRows][in].x, sum = row_ml[r / kRows][in].y;
+        if constexpr (kKind != kFewRows) {
+            const int wv = kAlone ? wave : r / kRows;
+            lo = chunk(wv, 0), hi = chunk(wv, 1);
+            top = row_ml[wv][in].x, sum = row_ml[wv][in].y;
         } else {
             top = -INFINITY, sum = 0.0f;
 #pragma unroll
@@ -503,9 +514,10 @@ __device__ __forceinline__ bool group_of(const Segment& s, int unit, int xcd, in
 }
 
 // Rows of all tokens against a part of the prefix.
-template <typename T, int D, bool kWide>
+template <typename T, int D, Kind kKind>
 __device__ __forceinline__ void attend_prefix(const AttendArgs& a, int unit, int xcd, char* lds, int32_t* ids)
 {
+    constexpr int kTileRows = kKind == kWideRows ? kWaves * kRows : kRows;
     int group, tile;
     if (!group_of(a.prefix, unit, xcd, group, tile)) return;
     Item w;
@@ -513,21 +525,26 @@ __device__ __forceinline__ void attend_prefix(const AttendArgs& a, int unit, int
     w.part = group % a.prefix.splits;
     w.token0 = 0;
     w.rows = a.n_tokens * a.group;
-    w.row0 = tile * (kWide ? kWaves * kRows : kRows);
+    w.row0 = tile * kTileRows;
     w.k0 = w.part * a.prefix.split_len;
     w.k1 = min(a.prefix_len, w.k0 + a.prefix.split_len);
     w.seen0 = a.prefix_len;
     w.seen_step = 0;
     w.own_pages = nullptr;
-    attend<T, D, kWide>(a, w, lds, ids);
+    attend<T, D, kKind>(a, w, lds, ids);
 }
 
 // Rows of one sequence against a part of its keys, or of the prefix and its keys.
-template <typename T, int D, bool kWide>
+template <typename T, int D, Kind kKind>
 __device__ __forceinline__ void attend_own(const AttendArgs& a, int unit, int xcd, char* lds, int32_t* ids)
 {
+    constexpr int kTileRows = kKind == kWideRows ? kWaves * kRows : kRows;
     int rest, tile;
     if (!group_of(a.own, unit, xcd, rest, tile)) return;
+    if constexpr (kKind == kWaveRows) {                    // (four items a workgroup; it has one row tile)
+        rest = rest * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (rest >= a.own.items) return;
+    }
     const int split = rest % a.own.splits;
     rest /= a.own.splits;
     Item w;
@@ -537,18 +554,18 @@ __device__ __forceinline__ void attend_own(const AttendArgs& a, int unit, int xc
     const int t = t1 - t0, own = a.max_own_len ? within(a.own_len[b], 0, a.max_own_len) : 0;
     w.token0 = t0;
     w.rows = min(t, a.max_q) * a.group;
-    w.row0 = tile * (kWide ? kWaves * kRows : kRows);
+    w.row0 = tile * kTileRows;
     if (w.row0 >= w.rows) return;
     w.seen0 = a.prefix_len + own - t + 1;
     w.seen_step = t > 1 ? 1 : 0;
-    const int last = min(w.rows, w.row0 + (kWide ? kWaves * kRows : kRows)) - 1;
+    const int last = min(w.rows, w.row0 + kTileRows) - 1;
     const int seen = max(a.prefix_len, w.seen0 + last / a.group);
     w.k0 = a.own_from + split * a.own.split_len;
     w.k1 = min(seen, w.k0 + a.own.split_len);
     if (w.k0 >= w.k1 && a.parts > 1) return;
     w.part = a.own.first_part + split;
     w.own_pages = a.pages + b * a.pages_stride;
-    attend<T, D, kWide>(a, w, lds, ids);
+    attend<T, D, kKind>(a, w, lds, ids);
 }
 
 // Both kinds of work in one launch, mixed evenly: the prefix' workgroups keep the matrix cores busy, the sequences' the memory.
@@ -561,10 +578,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a)
     if constexpr (kPrefix != kNone) {
         const int64_t all = a.prefix.units + a.own.units;
         const int before = (int)(unit * (int64_t)a.prefix.units / all), after = (int)((unit + 1) * (int64_t)a.prefix.units / all);
-        if (after > before) attend_prefix<T, D, kPrefix == kWideRows>(a, before, xcd, lds, ids);
-        else attend_own<T, D, kOwn == kWideRows>(a, unit - before, xcd, lds, ids);
+        if (after > before) attend_prefix<T, D, kPrefix>(a, before, xcd, lds, ids);
+        else attend_own<T, D, kOwn>(a, unit - before, xcd, lds, ids);
     } else {
-        attend_own<T, D, kOwn == kWideRows>(a, unit, xcd, lds, ids);
+        attend_own<T, D, kOwn>(a, unit, xcd, lds, ids);
     }
 }
 
@@ -647,10 +664,11 @@ Plan plan(const fr_attend_desc& d, int cus)
     const int64_t group = d.n_q_heads / d.cache.n_kv_heads, heads = d.cache.n_kv_heads;
     const int64_t tokens_a_seq = std::min(d.max_q, d.n_tokens), seq_rows = tokens_a_seq * group, all_rows = d.n_tokens * group;
     constexpr int64_t kWideTile = kWaves * kRows;
-    cus = std::min(cus, 256);
-    auto finish = [&](Segment& s, int64_t groups) {
+    cus = std::min(cus, kUnits);
+    auto finish = [&](Segment& s, int64_t items, int64_t at_once) {
+        const int64_t groups = up(items, at_once), units = up(groups, kXcds) * s.row_tiles;
+        s.items = (int)std::min<int64_t>(items, 0x7fffffff);
         s.groups = (int)std::min<int64_t>(groups, 0x7fffffff);
-        const int64_t units = up(groups, kXcds) * s.row_tiles;
         s.units = (int)std::min<int64_t>(units, 0x7fffffff);
         p.blocks += units * kXcds;
     };
@@ -662,7 +680,7 @@ Plan plan(const fr_attend_desc& d, int cus)
         const int64_t splits = std::max<int64_t>(1, std::min(most, want));
         s.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
         s.splits = (int)up(d.prefix_len, s.split_len);
-        finish(s, heads * s.splits);
+        finish(s, heads * s.splits, 1);
     }
     Segment& s = p.own;
     const int64_t keys = (p.of_prefix == kNone ? d.prefix_len : 0) + (int64_t)d.max_own_len;
@@ -671,15 +689,19 @@ Plan plan(const fr_attend_desc& d, int cus)
     s.row_tiles = (int)up(seq_rows, p.of_own == kWideRows ? kWideTile : kRows);
     s.split_len = 1;
     if (keys || p.of_prefix == kNone) {
-        // parts of 1024 keys, shorter ones while that leaves units idle, whole sequences where there are enough of them
         const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
         int64_t len = 1024;
         if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
         else
             while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
+        if (p.of_own == kFewRows && p.of_prefix != kFewRows && base >= 2 * cus) {
+            p.of_own = kWaveRows;
+            len = 256;
+            while (base * up(keys, len) > 16 * cus && len < keys) len *= 2;
+        }
         s.split_len = (int)len;
         s.splits = (int)std::max<int64_t>(1, up(keys, len));
-        finish(s, (int64_t)d.n_seqs * heads * s.splits);
+        finish(s, (int64_t)d.n_seqs * heads * s.splits, p.of_own == kWaveRows ? kWaves : 1);
     }
     p.parts = p.prefix.splits + s.splits;
     p.blocks = std::max(p.blocks, d.n_seqs * tokens_a_seq * d.n_q_heads);        // (the join's grid is not larger)
@@ -695,14 +717,17 @@ template <typename T, int D>
 int launch(const AttendArgs& a, const Plan& p, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.prefix.units + a.own.units) * kXcds);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
     if (p.of_prefix == kNone) {
-        if (p.of_own == kFewRows) hipLaunchKernelGGL((k_attend<T, D, kNone, kFewRows>), grid, dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((k_attend<T, D, kNone, kWideRows>), grid, dim3(kThreads), 0, stream, a);
-    } else if (p.of_prefix == kFewRows) {              // (so few rows in all, so few of a sequence)
-        hipLaunchKernelGGL((k_attend<T, D, kFewRows, kFewRows>), grid, dim3(kThreads), 0, stream, a);
+        if (p.of_own == kFewRows) go(k_attend<T, D, kNone, kFewRows>);
+        else if (p.of_own == kWaveRows) go(k_attend<T, D, kNone, kWaveRows>);
+        else go(k_attend<T, D, kNone, kWideRows>);
+    } else if (p.of_prefix == kFewRows) {              // (few rows in all: few of a sequence, and few sequences)
+        go(k_attend<T, D, kFewRows, kFewRows>);
     } else {
-        if (p.of_own == kFewRows) hipLaunchKernelGGL((k_attend<T, D, kWideRows, kFewRows>), grid, dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((k_attend<T, D, kWideRows, kWideRows>), grid, dim3(kThreads), 0, stream, a);
+        if (p.of_own == kFewRows) go(k_attend<T, D, kWideRows, kFewRows>);
+        else if (p.of_own == kWaveRows) go(k_attend<T, D, kWideRows, kWaveRows>);
+        else go(k_attend<T, D, kWideRows, kWideRows>);
     }
     if (p.parts > 1) {
         // a thread for every eight elements where a row has few parts, up to 16 threads where it has many
@@ -725,7 +750,7 @@ int fr_attend_shared_workspace_bytes(const fr_attend_desc* d, uint64_t* bytes_ou
     if (!d || !bytes_out || !sizes_ok(*d)) return FR_ERR_ARG;
     *bytes_out = 0;
     if (d->n_tokens == 0 || d->n_seqs == 0) return FR_OK;
-    *bytes_out = part_bytes(*d, plan(*d, 256));
+    *bytes_out = part_bytes(*d, plan(*d, kUnits));
     return FR_OK;
 }
 
@@ -746,10 +771,13 @@ int fr_attend_shared(const fr_attend_desc* d, void* stream)
     AttendArgs a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->prefix_pages,
                     d->pages, d->own_len, d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->prefix_len, d->max_own_len,
                     __builtin_ctz(c.page_size), d->n_q_heads / c.n_kv_heads, d->scale};
-    const Plan p = plan(*d, (int)fr_stream_cus((hipStream_t)stream));
+    // cut for the units that the stream may use, in no more parts than the workspace was asked for
+    const Plan whole = plan(*d, kUnits);
+    Plan p = plan(*d, (int)fr_stream_cus((hipStream_t)stream));
+    if (p.parts > whole.parts) p = whole;
     if (p.blocks > 0x7fffffff) return FR_ERR_ARG;
-    const uint64_t need = part_bytes(*d, p), asked = part_bytes(*d, plan(*d, 256));
-    if (asked && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < asked || need > asked)) return FR_ERR_ARG;
+    const uint64_t asked = part_bytes(*d, whole);
+    if (asked && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < asked)) return FR_ERR_ARG;
     a.own_from = p.of_prefix == kNone ? 0 : d->prefix_len;
     a.prefix = p.prefix;
     a.own = p.own;
