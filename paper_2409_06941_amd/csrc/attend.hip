@@ -213,53 +213,54 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         for (int s = 0; s < D / 16; ++s) x.q[s] = __builtin_bit_cast(typename T::x8, *reinterpret_cast<const uint4*>(q + s * 16));
     }
 
-    // (which part of which row a lane loads is made anew from `anew(lane)` for every tile: kept, it holds registers that the loop needs)
+    // What a lane loads is made anew from `anew(lane)` for every tile: kept, it holds registers that the loop needs.
     auto anew = [](int x) { asm volatile("" : "+v"(x)); return (uint32_t)x; };
 
-    // page ids of n keys from `first` on, a lane each, to LDS; keys behind the last stand for the last
-    auto ask_ids = [&](uint32_t to, int first, int n) {
-        const int j = min(first + (lane & (n - 1)), w.k1 - 1), own = j - a.prefix_len;
-        const int32_t* g = own < 0 ? a.prefix_pages + (j >> a.page_shift) : w.own_pages + (own >> a.page_shift);
-        load4_to_lds(to, g);
+    // A wavefront loads kLoadRows rows of a tile.  Where 64 of them (a set: those of two or four tiles) lie is worked out at once, a
+    // lane each: page ids come to LDS, offsets go back there.  Keys behind the last stand for the last.
+    constexpr int kLoadRows = kWide ? 16 : 32, kTilesASet = 64 / kLoadRows, kLoads = kLoadRows / L::kRowsALoad;
+    const uint32_t my_ids = ids + wave * 1536, my_offsets = my_ids + 512;
+    auto key_of = [&](int set) {
+        const int l = (int)anew(lane), tile = set * kTilesASet + l / kLoadRows;
+        return min(w.k0 + (kWide ? tile * 64 + wave * 16 : (kAlone ? tile : tile * kWaves + wave) * 32) + l % kLoadRows, w.k1 - 1);
     };
-    // offsets of the rows that this lane loads a part of, rows y * kRowsALoad + its own, counted from `first`, whose ids stand at `from`
-    auto offsets = [&](uint32_t from, int first, auto& where) {
-        constexpr int n = std::extent<std::remove_reference_t<decltype(where)>>::value;
-        const uint32_t load_row = anew(lane) / L::kChunks;
-        uint32_t id[n];
-#pragma unroll
-        for (int y = 0; y < n; ++y) id[y] = *reinterpret_cast<const __attribute__((address_space(3))) uint32_t*>(lds_at(from + (y * L::kRowsALoad + load_row) * 4));
-#pragma unroll
-        for (int y = 0; y < n; ++y) {
-            const int j = min(first + (int)(y * L::kRowsALoad + load_row), w.k1 - 1), in = j < a.prefix_len ? j : j - a.prefix_len;
-            const uint32_t page = (uint32_t)within((int32_t)id[y], 0, (int32_t)a.c.n_pages - 1);
-            where[y] = (int64_t)((uint64_t)page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)(in & (a.c.page_size - 1)) * (uint32_t)a.c.slot_stride);
-        }
+    auto ask_ids = [&](int set) {
+        const int j = key_of(set), own = j - a.prefix_len;
+        load4_to_lds(my_ids + (set & 1) * 256, own < 0 ? a.prefix_pages + (j >> a.page_shift) : w.own_pages + (own >> a.page_shift));
     };
+    typedef __attribute__((address_space(3))) uint64_t* LdsOffset;
+    auto make_offsets = [&](int set) {
+        const int j = key_of(set), in = j < a.prefix_len ? j : j - a.prefix_len;
+        const int32_t id = *reinterpret_cast<const __attribute__((address_space(3))) int32_t*>(lds_at(my_ids + (set & 1) * 256 + anew(lane) * 4));
+        const uint32_t page = (uint32_t)within(id, 0, (int32_t)a.c.n_pages - 1);
+        *reinterpret_cast<LdsOffset>(lds_at(my_offsets + (set & 1) * 512 + anew(lane) * 8)) =
+            (uint64_t)page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)(in & (a.c.page_size - 1)) * (uint32_t)a.c.slot_stride;
+    };
+    // tile t's rows of K (V) to LDS
+    auto ask = [&](int t, const uint16_t* from, uint32_t to, auto piece) {
+        const uint32_t l = anew(lane), at = my_offsets + (t / kTilesASet & 1) * 512 + (t % kTilesASet) * (kLoadRows * 8) + l / L::kChunks * 8;
+        uint64_t row[kLoads];
+#pragma unroll
+        for (int y = 0; y < kLoads; ++y) row[y] = *reinterpret_cast<LdsOffset>(lds_at(at) + y * (int)L::kRowsALoad * 8);
+#pragma unroll
+        for (int y = 0; y < kLoads; ++y) load16_to_lds(to + y * 1024, from + piece(l, y) * 8 + row[y]);
+    };
+    auto k_piece = [](uint32_t l, int y) { return L::k_piece(l, y); };
+    auto v_piece = [](uint32_t l, int y) { return L::v_piece(l, y); };
     const uint16_t* gk = static_cast<const uint16_t*>(a.c.k) + w.kv * a.c.head_stride;
     const uint16_t* gv = static_cast<const uint16_t*>(a.c.v) + w.kv * a.c.head_stride;
     if (w.k0 < w.k1) {
         if constexpr (kWide) {
             // While tile t's scores become weights (vector unit), the matrix cores make those of tile t + 1: K runs a tile ahead of V.
-            constexpr int kTile = 64, kLoads = 16 / L::kRowsALoad;         // a wavefront loads 16 rows of each
+            constexpr int kTile = 64;
             constexpr uint32_t kHalf = kTile * L::kRow;
             const int tiles = (w.k1 - w.k0 + kTile - 1) / kTile;
-            const uint32_t my_ids = ids + wave * 512;       // (64 lanes write 256 bytes at a time)
-            auto first_of = [&](int t) { return w.k0 + t * kTile + wave * 16; };
-            int64_t at[kLoads];                             // of the tile whose V is asked for next
-            auto ask_k = [&](int t, auto odd) {
-                offsets(my_ids + odd * 256, first_of(t), at);
-                const uint32_t l = anew(lane);
-#pragma unroll
-                for (int y = 0; y < kLoads; ++y) load16_to_lds(lds + odd * kHalf + wave * 16 * L::kRow + y * 1024, gk + at[y] + L::k_piece(l, y) * 8);
-            };
-            auto ask_v = [&](auto odd) {
-                const uint32_t l = anew(lane);
-#pragma unroll
-                for (int y = 0; y < kLoads; ++y) load16_to_lds(lds + (2 + odd) * kHalf + wave * 16 * L::kRow + y * 1024, gv + at[y] + L::v_piece(l, y) * 8);
-            };
-            constexpr int kSteps = D / 8, kElements = 32 / kSteps;          // MFMAs of the scores, and as many with the values
-            constexpr int kAhead = 4;                                       // fragments read ahead of their MFMA
+            auto ask_k = [&](int t, auto odd) { ask(t, gk, lds + odd * kHalf + wave * 16 * L::kRow, k_piece); };
+            auto ask_v = [&](int t, auto odd) { ask(t, gv, lds + (2 + odd) * kHalf + wave * 16 * L::kRow, v_piece); };
+            constexpr int kSteps = D / 8;                   // MFMAs of the scores, and as many with the values
+            constexpr int kAhead = 4;                       // fragments read ahead of their MFMA
+            // 16 pairs of weights: as many beside the scores' MFMAs as they take time, the rest beside the first half of the values'
+            constexpr int kPairsBeside = D == 128 ? 10 : 8;
             const Even even{};
             const Odd odd{};
             Fragments<T, D> fragments(lds, lane);
@@ -276,25 +277,26 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
 #pragma unroll
                     for (int y = 0; y < kAhead; ++y) ahead[y] = k_of(other, y);
                 }
-                if (t + 1 < tiles) ask_v(other);
-                if (t + 2 < tiles) {
-                    ask_k(t + 2, here);
-                    ask_ids(my_ids + other * 256, first_of(t + 3), 16);
-                }
+                if (t + 1 < tiles) ask_v(t + 1, other);
+                if (t + 2 < tiles) ask_k(t + 2, here);
+                // offsets of set s are there when step 4 s - 2 asks for K of tile 4 s
+                if (t % kTilesASet == 0 && t + kTilesASet < tiles) ask_ids(t / kTilesASet + 1);
+                if (t % kTilesASet == 1 && t + kTilesASet - 1 < tiles) make_offsets(t / kTilesASet + 1);
                 if (idle) return;
                 x.grow(top, c);
                 const float base = x.base(c);
                 uint32_t p[16];
+                auto pair = [&](int e) {
+                    p[e] = x.weigh(now[e / 8][2 * e % 16], now[e / 8][2 * e % 16 + 1], c, base);
+                    asm volatile("" : "+v"(p[e]), "+v"(x.l), "+v"(x.l1));             // (made here, not where they are used)
+                };
                 keep_order();
 #pragma unroll
                 for (int y = 0; y < kSteps; ++y) {          // (behind the last tile: of what lies there, not used)
                     next[y % 2] = mfma<T>(ahead[y % kAhead], x.q[y / 2], y < 2 ? zero : next[y % 2]);
                     ahead[y % kAhead] = y + kAhead < kSteps ? k_of(other, y + kAhead) : v_of(here, y + kAhead - kSteps);
 #pragma unroll
-                    for (int e = y * kElements; e < (y + 1) * kElements; e += 2) {
-                        p[e / 2] = x.weigh(now[e / 16][e % 16], now[e / 16][e % 16 + 1], c, base);
-                        asm volatile("" : "+v"(p[e / 2]), "+v"(x.l), "+v"(x.l1));     // (made here, not where they are used)
-                    }
+                    for (int e = y * kPairsBeside / kSteps; e < (y + 1) * kPairsBeside / kSteps; ++e) pair(e);
                     keep_order();
                 }
                 x.template hide<2>(next, w.k0 + (t + 1) * kTile, end, lane);
@@ -302,25 +304,29 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 keep_order();
 #pragma unroll
                 for (int y = 0; y < kSteps; ++y) {
+                    constexpr int kFirst = kSteps / 2, kRest = 16 - kPairsBeside;
                     const int f = y / (D / 32), d = y % (D / 32);
                     x.o[d] = mfma<T>(ahead[y % kAhead], Softmax<T, D>::fragment(p + 4 * f), x.o[d]);
                     if (y + kAhead < kSteps) ahead[y % kAhead] = v_of(here, y + kAhead);
+                    if (y < kFirst) {
 #pragma unroll
-                    for (int e = y * kElements; e < (y + 1) * kElements; ++e) top = fmaxf(top, next[e / 16][e % 16]);
+                        for (int e = y * kRest / kFirst; e < (y + 1) * kRest / kFirst; ++e) pair(kPairsBeside + e);
+                    } else {
+#pragma unroll
+                        for (int e = (y - kFirst) * 32 / kFirst; e < (y - kFirst + 1) * 32 / kFirst; ++e) top = fmaxf(top, next[e / 16][e % 16]);
+                    }
                     keep_order();
                 }
                 top = of_both_halves(top);
             };
-            ask_ids(my_ids, first_of(0), 16);
-            ask_ids(my_ids + 256, first_of(1), 16);
+            ask_ids(0);
             wait_loads<0>();
+            make_offsets(0);
             ask_k(0, even);
             wait_loads<0>();
             __syncthreads();
-            ask_v(even);
+            ask_v(0, even);
             if (tiles > 1) ask_k(1, odd);
-            wait_lds();
-            ask_ids(my_ids, first_of(2), 16);
             f32x16 s0[2], s1[2];
             if (!idle) {
 #pragma unroll
@@ -335,48 +341,47 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 if (t + 1 < tiles) step(s1, s0, t + 1, odd, even);
             }
         } else {
-            constexpr int kTile = 32, kLoads = kTile / L::kRowsALoad;
+            constexpr int kTile = 32;
             constexpr uint32_t kHalf = kTile * L::kRow;
             const int all = (w.k1 - w.k0 + kTile - 1) / kTile, mine = kAlone ? 0 : wave, tiles = (all - mine + kSharers - 1) / kSharers;
-            const uint32_t k = lds + wave * 2 * kHalf, v = k + kHalf, my_ids = ids + wave * 512;
+            const uint32_t k = lds + wave * 2 * kHalf, v = k + kHalf;
             auto first_of = [&](int t) { return w.k0 + (t * kSharers + mine) * kTile; };
             const Fragments<T, D> fragments(k, lane);
-            int64_t at[kLoads];
-            auto ask_k = [&](int t) {
-                offsets(my_ids + (t & 1) * 256, first_of(t), at);
-                const uint32_t l = anew(lane);
-#pragma unroll
-                for (int y = 0; y < kLoads; ++y) load16_to_lds(k + y * 1024, gk + at[y] + L::k_piece(l, y) * 8);
-            };
-            auto ask_v = [&] {
-                const uint32_t l = anew(lane);
-#pragma unroll
-                for (int y = 0; y < kLoads; ++y) load16_to_lds(v + y * 1024, gv + at[y] + L::v_piece(l, y) * 8);
-            };
-            if (tiles > 0) {
-                ask_ids(my_ids, first_of(0), kTile);
-                ask_ids(my_ids + 256, first_of(1), kTile);
-                wait_loads<0>();
-                ask_k(0);
-                ask_v();
-            }
-            for (int t = 0; t < tiles; ++t) {
-                // in flight: K and V of tile t, in this order
-                const bool more = t + 1 < tiles;
-                wait_loads<kLoads>();
-                typename T::x8 kf[D / 16];
+            // LDS is where tiles pass through: K and V of a tile go on into registers as soon as they are here, and the next one's are
+            // asked for, so that every load has a whole round to arrive.
+            typename T::x8 kf[D / 16], vf[2][D / 32];
+            auto take_k = [&] {
 #pragma unroll
                 for (int f = 0; f < D / 16; ++f) kf[f] = fragments.of_k(0, f);
                 wait_lds();
-                if (more) {
-                    ask_ids(my_ids + (t & 1) * 256, first_of(t + 2), kTile);
-                    ask_k(t + 1);
-                }
+            };
+            if (tiles > 0) {
+                ask_ids(0);
+                ask_ids(1);
+                wait_loads<0>();
+                make_offsets(0);
+                ask(0, gk, k, k_piece);
+                ask(0, gv, v, v_piece);
+                wait_loads<kLoads>();
+                take_k();
+                if (tiles > 1) ask(1, gk, k, k_piece);
+            }
+            for (int t = 0; t < tiles; ++t) {
+                // K of tile t is in registers; in flight are V of tile t, K of t + 1 and, for odd t, page ids, in this order
+                const bool more = t + 1 < tiles;
                 f32x16 s[1];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
 #pragma unroll
                 for (int f = 0; f < D / 16; ++f) s[0] = mfma<T>(kf[f], x.q[f], s[0]);
+                if (more) wait_loads<kLoads>();
+                else wait_loads<0>();
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) vf[f][d] = fragments.of_v(kHalf, f, d);
+                wait_lds();
+                if (more) ask(t + 1, gv, v, v_piece);
                 x.template hide<1>(s, first_of(t), end, lane);
                 float top = s[0][0];
 #pragma unroll
@@ -386,14 +391,19 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 uint32_t p[8];
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) p[i / 2] = x.weigh(s[0][i], s[0][i + 1], c, base);
-                if (more) wait_loads<kLoads + 1>();
-                else wait_loads<0>();
+                if (more) {
+                    wait_loads<kLoads>();
+                    take_k();
+                    if (t + 2 < tiles) {
+                        if (t % 2 == 0) make_offsets(t / 2 + 1);
+                        ask(t + 2, gk, k, k_piece);
+                        if (t % 2 == 0) ask_ids(t / 2 + 2);
+                    }
+                }
 #pragma unroll
                 for (int f = 0; f < 2; ++f)
 #pragma unroll
-                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma<T>(fragments.of_v(kHalf, f, d), Softmax<T, D>::fragment(p + 4 * f), x.o[d]);
-                wait_lds();
-                if (more) ask_v();
+                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma<T>(vf[f][d], Softmax<T, D>::fragment(p + 4 * f), x.o[d]);
             }
         }
 
@@ -461,7 +471,9 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 f32x4{x.o[d][i] * mine, x.o[d][i + 1] * mine, x.o[d][i + 2] * mine, x.o[d][i + 3] * mine};
         }
     meet();
-    // a thread takes eight elements of a row: two chunks
+    // a thread takes eight elements of a row: two chunks, neighbours for a result of 16 bits, head_dim / 2 apart for a part (so that
+    // neighbouring threads write neighbouring chunks)
+    const bool whole = a.parts == 1;
     constexpr int kPieces = D / 8, kOutRows = kWide ? kWaves * kRows : kRows;
     for (int y = kAlone ? lane : tid; y < kOutRows * kPieces; y += kAlone ? 64 : kThreads) {
         const int r = y / kPieces, piece = y % kPieces, from = w.row0 + r;
@@ -472,7 +484,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
         float top, sum;
         const int in = r % kRows;
-        auto chunk = [&](int wv, int e) { return *reinterpret_cast<LdsFloats>(lds_at(lds + (wv * kRows + in) * kFloatRow + ((uint32_t)(2 * piece + e) ^ (in & (kFloatChunks - 1))) * 16)); };
+        auto chunk = [&](int wv, int e) { return *reinterpret_cast<LdsFloats>(lds_at(lds + (wv * kRows + in) * kFloatRow + ((uint32_t)(whole ? 2 * piece + e : piece + e * kPieces) ^ (in & (kFloatChunks - 1))) * 16)); };
         if constexpr (kKind != kFewRows) {
             const int wv = kAlone ? wave : r / kRows;
             lo = chunk(wv, 0), hi = chunk(wv, 1);
@@ -489,15 +501,15 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
             }
         }
         const int64_t token = rows.token(from), head = rows.head(from);
-        if (a.parts == 1) {
+        if (whole) {
             const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
             *reinterpret_cast<uint4*>(a.out + token * a.out_stride + head * D + piece * 8) =
                 make_uint4(T::pack(lo[0] * f, lo[1] * f), T::pack(lo[2] * f, lo[3] * f), T::pack(hi[0] * f, hi[1] * f), T::pack(hi[2] * f, hi[3] * f));
             if (a.lse && piece == 0) a.lse[token * a.n_q_heads + head] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
         } else {
             const int64_t to = ((int64_t)w.part * a.n_tokens + token) * a.n_q_heads + head;
-            *reinterpret_cast<f32x4*>(a.part_o + to * D + piece * 8) = lo;
-            *reinterpret_cast<f32x4*>(a.part_o + to * D + piece * 8 + 4) = hi;
+            *reinterpret_cast<f32x4*>(a.part_o + to * D + piece * 4) = lo;
+            *reinterpret_cast<f32x4*>(a.part_o + to * D + D / 2 + piece * 4) = hi;
             if (piece == 0) a.part_ml[to] = make_float2(top, sum);
         }
     }
@@ -573,7 +585,7 @@ template <typename T, int D, Kind kPrefix, Kind kOwn>
 __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a)
 {
     __shared__ __align__(1024) char lds[Lds<D>::kBytes];
-    __shared__ __align__(1024) int32_t ids[kWaves * 128];
+    __shared__ __align__(1024) int32_t ids[kWaves * 384];      // a wavefront: two sets of 64 page ids, two of 64 offsets
     const int unit = blockIdx.x / kXcds, xcd = blockIdx.x % kXcds;
     if constexpr (kPrefix != kNone) {
         const int64_t all = a.prefix.units + a.own.units;
@@ -585,7 +597,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a)
     }
 }
 
-// Joins the parts of a row: eight elements a thread, kLanes threads for every eight, each with every kLanes-th part.
+// Joins the parts of a row: twice four elements a thread, kLanes threads for every eight, each with every kLanes-th part.
 template <typename T, int D, int kLanes>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_blocks)
 {
@@ -607,8 +619,8 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_
     for (int y = mine; y < parts; y += kLanes) {
         const float2 ml = a.part_ml[y * pitch + row];
         const float f = __builtin_amdgcn_exp2f(ml.x - base);
-        const float4* p = reinterpret_cast<const float4*>(a.part_o + (y * pitch + row) * D + piece * 8);
-        const float4 lo = p[0], hi = p[1];
+        const float4* p = reinterpret_cast<const float4*>(a.part_o + (y * pitch + row) * D) + piece;
+        const float4 lo = p[0], hi = p[kPieces];
         sum = fmaf(ml.y, f, sum);
         o[0] = fmaf(lo.x, f, o[0]), o[1] = fmaf(lo.y, f, o[1]), o[2] = fmaf(lo.z, f, o[2]), o[3] = fmaf(lo.w, f, o[3]);
         o[4] = fmaf(hi.x, f, o[4]), o[5] = fmaf(hi.y, f, o[5]), o[6] = fmaf(hi.z, f, o[6]), o[7] = fmaf(hi.w, f, o[7]);
@@ -636,8 +648,9 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_
     }
     if (!there) return;
     const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-    *reinterpret_cast<uint4*>(a.out + token * a.out_stride + head * D + piece * 8) =
-        make_uint4(T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f), T::pack(o[4] * f, o[5] * f), T::pack(o[6] * f, o[7] * f));
+    uint16_t* out = a.out + token * a.out_stride + head * D + piece * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f));
+    *reinterpret_cast<uint2*>(out + D / 2) = make_uint2(T::pack(o[4] * f, o[5] * f), T::pack(o[6] * f, o[7] * f));
     if (a.lse && piece == 0) a.lse[row] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
