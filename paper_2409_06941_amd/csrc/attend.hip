@@ -479,7 +479,9 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         for (int y = 0; y < kWaves; ++y) top = fmaxf(top, row_ml[y][lane % kCols].x);
         mine = __builtin_amdgcn_exp2f(m2 - (top == -INFINITY ? 0.0f : top));
     }
-    const uint32_t region = lds + wave * kCols * kFloatRow;
+    constexpr uint32_t kRegion = 128 * D;                // (what the wavefront's own tiles take: others may still be at theirs)
+    static_assert(kCols * kFloatRow <= kRegion, "");
+    const uint32_t region = lds + wave * kRegion;
 #pragma unroll
     for (int d = 0; d < D / kCols; ++d)
 #pragma unroll
@@ -502,7 +504,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
         float top, sum;
         const int in = r % kCols;
-        auto chunk = [&](int wv, int e) { return *reinterpret_cast<LdsFloats>(lds_at(lds + (wv * kCols + in) * kFloatRow + ((uint32_t)(whole ? 2 * piece + e : piece + e * kPieces) ^ (in & (kFloatChunks - 1))) * 16)); };
+        auto chunk = [&](int wv, int e) { return *reinterpret_cast<LdsFloats>(lds_at(lds + wv * kRegion + in * kFloatRow + ((uint32_t)(whole ? 2 * piece + e : piece + e * kPieces) ^ (in & (kFloatChunks - 1))) * 16)); };
         if constexpr (kKind != kFewRows) {
             const int wv = kAlone ? wave : r / kCols;
             lo = chunk(wv, 0), hi = chunk(wv, 1);

@@ -231,6 +231,17 @@ def test_attend_longer(P, own, new):
     _attend_case("f16", 8, 2, 64, 16, P, own, new, seed=P + 2)
 
 
+@pytest.mark.parametrize("dt,D", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("P,new", [(0, 1), (150, 1), (700, 1), (150, 3)])
+def test_attend_many_short_sequences(dt, D, P, new):
+    # enough of them for a wavefront each: lengths from none to several parts, one and several tokens
+    print("attend many", dt, D, P, new, flush=True)
+    rng = np.random.default_rng(P + new)
+    own = [int(x) for x in rng.integers(0, 40, 66)] + [0, 1, 31, 32, 33, 255, 256, 257, 600]
+    t = [min(x, int(rng.integers(1, new + 1))) if new > 1 else 1 for x in own]
+    _attend_case(dt, 16, 8, D, 16, P, own, t, seed=P + D)
+
+
 @pytest.mark.parametrize("layout", ["slots", "joined"])
 def test_attend_layouts_and_strides(layout):
     print("attend", layout, flush=True)
