@@ -602,7 +602,7 @@ __device__ __forceinline__ void attend_own(const AttendArgs& a, int unit, int xc
 // sequences' workgroups, in the room that is left beside each, keep the memory busy.  (Two a unit at first, or both kinds mixed evenly,
 // take 10 to 15 % longer: 256 sequences with 64 heads behind 4096 keys 96 us, 122 and 114.)
 template <typename T, int D, Kind kPrefix, Kind kOwn>
-__global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a)
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(AttendArgs a)
 {
     __shared__ __align__(1024) char lds[Lds<D, 32>::kBytes];
     __shared__ __align__(1024) int32_t ids[kWaves * 384];      // a wavefront: two sets of 64 page ids, two of 64 offsets
@@ -721,7 +721,7 @@ Plan plan(const fr_attend_desc& d, int cus)
     s.split_len = 1;
     if (keys || p.of_prefix == kNone) {
         const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
-        int64_t len = 1024;
+        int64_t len = 2048;
         if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
         else
             while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
