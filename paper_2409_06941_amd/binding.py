@@ -555,34 +555,51 @@ class Stage:
             self.handle = C.c_void_p()
 
 
+_DTYPE_OF = {"torch.bfloat16": FR_DTYPE_BF16, "torch.float16": FR_DTYPE_F16, "torch.float32": FR_DTYPE_F32}
+_codes = {}                    # torch dtype -> (its name, FR_DTYPE_* or None): these calls are short, and so is what they check
+
+
+def _code(dtype):
+    got = _codes.get(dtype)
+    if got is None:
+        got = _codes[dtype] = (str(dtype)[len("torch."):], _DTYPE_OF.get(str(dtype)))
+    return got
+
+
 def _dtype(x):
     """FR_DTYPE_* of a torch tensor."""
-    name = str(x.dtype)
-    if name not in ("torch.bfloat16", "torch.float16", "torch.float32"):
+    name, code = _code(x.dtype)
+    if code is None:
         raise TypeError("%s: the library takes bfloat16, float16 and float32" % name)
-    return {"torch.bfloat16": FR_DTYPE_BF16, "torch.float16": FR_DTYPE_F16, "torch.float32": FR_DTYPE_F32}[name]
+    return code
 
 
 def _typed(x, name, what, like=None):
-    """A tensor whose elements lie side by side and are of a type the C side cannot see."""
+    """Address of a tensor whose elements lie side by side and are of a type the C side cannot see; None for None."""
     if x is None:
         return None
-    if str(x.dtype) != "torch." + what or x.stride(-1) != 1 and x.shape[-1] > 1:
+    if _code(x.dtype)[0] != what or x.stride(-1) != 1 and x.shape[-1] > 1:
         raise TypeError("%s: %s elements side by side are needed" % (name, what))
-    if like is not None and tuple(x.shape) != tuple(like):
+    if like is not None and x.shape != like:
         raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(like), tuple(x.shape)))
-    return x
+    return x.data_ptr()
 
 
 def _rows(x, name, shape, dtype):
     """Stride between tokens of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
-    if tuple(x.shape) != tuple(shape):
+    if x.shape != shape:
         raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(shape), tuple(x.shape)))
-    if _dtype(x) != dtype:
+    if _code(x.dtype)[1] != dtype:
         raise TypeError("%s: not of the cache's type" % name)
-    if x.numel() and (x.shape[2] > 1 and x.stride(2) != 1 or x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+    tokens, heads, dim = shape
+    t, h, e = x.stride()
+    if (dim > 1 and e != 1 or heads > 1 and h != dim) and x.numel():
         raise ValueError("%s: heads of a token have to lie side by side" % name)
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+    return t if tokens > 1 else heads * dim
+
+
+def _workspace(x):
+    return (None, 0) if x is None else (x.data_ptr(), x.numel() * x.element_size())
 
 
 class KvPages:
@@ -603,39 +620,27 @@ class KvPages:
 
 
 def fr_kv_append(cache, k, v, slot, q=None, q_out=None, position=None, rotary=None, style=FR_ROTARY_HALVES, stream=None):
-    d = fr_kv_append_desc()
-    c = d.cache = cache.desc
+    c = cache.desc
+    dim, dtype = c.head_dim, c.dtype
     T = k.shape[0]
-    d.n_tokens = T
-    d.k_stride, d.v_stride = (_rows(x, n, (T, c.n_kv_heads, c.head_dim), c.dtype) for x, n in ((k, "k"), (v, "v")))
-    d.k, d.v = _ptr(k), _ptr(v)
-    if q is not None:
-        d.n_q_heads = q.shape[1]
-        d.q_stride = _rows(q, "q", (T, d.n_q_heads, c.head_dim), c.dtype)
-        d.q_out_stride = _rows(q_out, "q_out", (T, d.n_q_heads, c.head_dim), c.dtype)
-        d.q, d.q_out = _ptr(q), _ptr(q_out)
-    d.slot = _ptr(_typed(slot, "slot", "int64", (T,)))
-    if rotary is not None:
-        d.n_positions, d.rotary_dim = rotary.shape
-        if not rotary.is_contiguous():
-            raise ValueError("rotary: rows have to lie side by side")
-        d.rotary = _ptr(_typed(rotary, "rotary", "float32"))
-        d.position = _ptr(_typed(position, "position", "int32", (T,)))
-    d.style = style
+    kv, n_q = (T, c.n_kv_heads, dim), 0 if q is None else q.shape[1]
+    of_q = (T, n_q, dim)
+    positions, rotary_dim = (0, 0) if rotary is None else rotary.shape
+    if rotary is not None and not rotary.is_contiguous():
+        raise ValueError("rotary: rows have to lie side by side")
+    d = fr_kv_append_desc(c, k.data_ptr(), v.data_ptr(), q.data_ptr() if n_q else None, q_out.data_ptr() if n_q else None,
+                          _rows(k, "k", kv, dtype), _rows(v, "v", kv, dtype), _rows(q, "q", of_q, dtype) if n_q else 0,
+                          _rows(q_out, "q_out", of_q, dtype) if n_q else 0, _typed(slot, "slot", "int64", (T,)),
+                          _typed(position, "position", "int32", (T,)) if rotary_dim else None, _typed(rotary, "rotary", "float32"),
+                          positions, rotary_dim, style, T, n_q, 0)
     return _check(lib().fr_kv_append(C.byref(d), _stream(stream)), "fr_kv_append")
-
-
-def _attend_sizes(cache, q, n_seqs, prefix_len, max_own_len, max_q):
-    d = fr_attend_desc()
-    d.cache = cache.desc
-    d.n_tokens, d.n_q_heads = q.shape[0], q.shape[1]
-    d.n_seqs, d.prefix_len, d.max_own_len, d.max_q = n_seqs, prefix_len, max_own_len, max_q
-    return d
 
 
 def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, max_q=1):
     """q: a tensor of the call's shape (only its shape is read)."""
-    d, out = _attend_sizes(cache, q, n_seqs, prefix_len, max_own_len, max_q), C.c_uint64()
+    d = fr_attend_desc(cache.desc, n_tokens=q.shape[0], n_seqs=n_seqs, n_q_heads=q.shape[1], max_q=max_q, prefix_len=prefix_len,
+                       max_own_len=max_own_len)
+    out = C.c_uint64()
     _check(lib().fr_attend_shared_workspace_bytes(C.byref(d), C.byref(out)), "fr_attend_shared_workspace_bytes")
     return out.value
 
@@ -643,49 +648,42 @@ def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, 
 def fr_attend_shared(cache, q, out, pages, own_len, scale, prefix_len=0, max_own_len=0, prefix_pages=None, q_begin=None,
                      max_q=1, lse=None, workspace=None, stream=None):
     c = cache.desc
-    n_seqs = q.shape[0] if q_begin is None else q_begin.shape[0] - 1
-    d = _attend_sizes(cache, q, n_seqs, prefix_len, max_own_len, max_q)
-    d.q_stride, d.out_stride = (_rows(x, n, (q.shape[0], q.shape[1], c.head_dim), c.dtype) for x, n in ((q, "q"), (out, "out")))
-    d.q, d.out, d.scale = _ptr(q), _ptr(out), scale
-    d.lse = _ptr(_typed(lse, "lse", "float32", (q.shape[0], q.shape[1])))
+    dtype, page = c.dtype, c.page_size
+    tokens, heads = q.shape[0], q.shape[1]
+    n_seqs = tokens if q_begin is None else q_begin.shape[0] - 1
+    shape = (tokens, heads, c.head_dim)
     if lse is not None and not lse.is_contiguous():
         raise ValueError("lse: rows have to lie side by side")
-    d.q_begin = _ptr(_typed(q_begin, "q_begin", "int32"))
-    if prefix_pages is not None:
-        if prefix_pages.numel() * c.page_size < prefix_len:
-            raise ValueError("prefix_pages: too few for prefix_len")
-        d.prefix_pages = _ptr(_typed(prefix_pages, "prefix_pages", "int32"))
+    if prefix_pages is not None and prefix_pages.numel() * page < prefix_len:
+        raise ValueError("prefix_pages: too few for prefix_len")
+    width = 0
     if pages is not None:
-        if pages.dim() != 2 or pages.shape[0] != n_seqs or pages.shape[1] * c.page_size < max_own_len:
+        if pages.dim() != 2 or pages.shape[0] != n_seqs or pages.shape[1] * page < max_own_len:
             raise ValueError("pages: [n_seqs, at least max_own_len / page_size] is needed")
-        d.pages, d.pages_stride = _ptr(_typed(pages, "pages", "int32")), (pages.stride(0) if n_seqs > 1 else pages.shape[1])
-        d.own_len = _ptr(_typed(own_len, "own_len", "int32", (n_seqs,)))
-    d.workspace, d.workspace_bytes = _ptr(workspace), (workspace.numel() * workspace.element_size()) if workspace is not None else 0
+        width = pages.stride(0) if n_seqs > 1 else pages.shape[1]
+    d = fr_attend_desc(c, q.data_ptr(), out.data_ptr(), _typed(lse, "lse", "float32", shape[:2]), _rows(q, "q", shape, dtype),
+                       _rows(out, "out", shape, dtype), _typed(q_begin, "q_begin", "int32"), _typed(prefix_pages, "prefix_pages", "int32"),
+                       _typed(pages, "pages", "int32"), _typed(own_len, "own_len", "int32", (n_seqs,)) if pages is not None else None,
+                       width, tokens, n_seqs, heads, max_q, prefix_len, max_own_len, scale, 0, *_workspace(workspace))
     return _check(lib().fr_attend_shared(C.byref(d), _stream(stream)), "fr_attend_shared")
-
-
-def _sample_sizes(logits):
-    d = fr_sample_desc()
-    d.n_rows, d.n_vocab = logits.shape
-    d.dtype = _dtype(logits)
-    return d
 
 
 def fr_sample_workspace_bytes(logits):
     """logits: a tensor of the call's shape and type (only these are read)."""
-    d, out = _sample_sizes(logits), C.c_uint64()
+    n, vocab = logits.shape
+    d, out = fr_sample_desc(None, 0, _dtype(logits), n, vocab), C.c_uint64()
     _check(lib().fr_sample_workspace_bytes(C.byref(d), C.byref(out)), "fr_sample_workspace_bytes")
     return out.value
 
 
 def fr_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, stream=None):
-    d = _sample_sizes(logits)
-    n = d.n_rows
-    if logits.shape[1] > 1 and logits.stride(1) != 1:
+    n, vocab = logits.shape
+    stride, entry = logits.stride()
+    if vocab > 1 and entry != 1:
         raise ValueError("logits: the entries of a row have to lie side by side")
-    d.logits, d.row_stride = _ptr(logits), (logits.stride(0) if n > 1 else d.n_vocab)
-    for name, x, what in (("temperature", temperature, "float32"), ("top_k", top_k, "int32"), ("top_p", top_p, "float32"),
-                          ("min_p", min_p, "float32"), ("uniform", uniform, "float32"), ("token", token, "int32")):
-        setattr(d, name, _ptr(_typed(x, name, what, (n,))))
-    d.workspace, d.workspace_bytes = _ptr(workspace), (workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    like = (n,)
+    d = fr_sample_desc(logits.data_ptr(), stride if n > 1 else vocab, _dtype(logits), n, vocab, 0,
+                       _typed(temperature, "temperature", "float32", like), _typed(top_k, "top_k", "int32", like),
+                       _typed(top_p, "top_p", "float32", like), _typed(min_p, "min_p", "float32", like),
+                       _typed(uniform, "uniform", "float32", like), _typed(token, "token", "int32", like), *_workspace(workspace))
     return _check(lib().fr_sample(C.byref(d), _stream(stream)), "fr_sample")
