@@ -35,22 +35,26 @@ struct SampleArgs {
 };
 
 __device__ __forceinline__ float cleaned(float x) { return x == x ? x + 0.0f : -INFINITY; }      // (-0 becomes 0)
-__device__ __forceinline__ uint32_t key_of(float x)
+// The order of entries, the largest first: of its logit (bits in an order that rises with it; 32), then of the index, the lowest first (19).
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t index)
 {
     const uint32_t u = __float_as_uint(x);
-    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+    return (uint64_t)(u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u)) << 19 | (kMostVocab - 1 - index);
 }
-__device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
 
 struct Scale {
     float top, per_t;
+    // the largest logit, the factor and hence every (x - top) per_t of a number x are numbers
+    __device__ __forceinline__ bool usual() const { return top < INFINITY && per_t > 0.0f && per_t < INFINITY; }
     __device__ __forceinline__ float weight(float x) const
     {
         if (x == top) return 1.0f;
         if (x == -INFINITY) return 0.0f;
         return expf((x - top) * per_t);
     }
-    __device__ __forceinline__ uint64_t mass(float w) const { return w > 0.0f ? (uint64_t)(w * kMassOne) : 0; }
+    // the mass as a float that is a whole number (from 2^24 on all floats are); 0 for NaN
+    __device__ __forceinline__ float whole_mass(float x) const { return fmaxf(floorf(weight(x) * kMassOne), 0.0f); }
+    __device__ __forceinline__ uint64_t mass(float x) const { return (uint64_t)whole_mass(x); }
     __device__ __forceinline__ uint32_t bin(float x) const
     {
         if (x == top) return 0;
@@ -60,7 +64,7 @@ struct Scale {
 
 struct Found { uint32_t digit, count_before, count; uint64_t mass_before, mass; };
 
-constexpr int kCandidates = 4096, kList = 1024, kRank = 640;
+constexpr int kCandidates = 4096, kList = 1024, kRank = 896, kMostRuns = kBins;
 constexpr uint32_t kNoMass = 1909;                     // from this digit on (29.83 and more below the top) masses are 0: 43 ln 2 = 29.81
 
 // A row of any alignment in pieces of 16 bytes: `head` entries up to the first such piece, `pieces` of kEach, `tail` entries.
@@ -76,9 +80,9 @@ template <typename T> struct Row {
     }
     __device__ __forceinline__ float at(int i) const { return T::up(p[i]); }
     struct Piece { float x[kEach]; };
-    __device__ __forceinline__ Piece piece(int v) const
+    __device__ __forceinline__ uint4 bits(int v) const { return *reinterpret_cast<const uint4*>(p + head + v * kEach); }
+    static __device__ __forceinline__ Piece unpacked(const uint4& b)
     {
-        const uint4 b = *reinterpret_cast<const uint4*>(p + head + v * kEach);
         const uint32_t w[4] = {b.x, b.y, b.z, b.w};
         Piece y;
 #pragma unroll
@@ -88,54 +92,66 @@ template <typename T> struct Row {
         }
         return y;
     }
-    // every entry once: f(index, value)
-    template <typename F> __device__ __forceinline__ void each(int tid, F f) const
+    __device__ __forceinline__ Piece piece(int v) const { return unpacked(bits(v)); }
+    // every piece once, by(number, piece), and the entries before and behind them, one(index, value)
+    template <int kAtOnce, typename P, typename F> __device__ __forceinline__ void visit(int tid, P by, F one) const
     {
         int v = tid;
-        for (; v + 3 * kThreads < pieces; v += 4 * kThreads) {
-            Piece y[4];
+        for (; v + (kAtOnce - 1) * kThreads < pieces; v += kAtOnce * kThreads) {
+            uint4 b[kAtOnce];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] = piece(v + q * kThreads);
+            for (int q = 0; q < kAtOnce; ++q) b[q] = bits(v + q * kThreads);
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) f(head + (v + q * kThreads) * kEach + e, y[q].x[e]);
+            for (int q = 0; q < kAtOnce; ++q) by(v + q * kThreads, unpacked(b[q]));
         }
-        for (; v < pieces; v += kThreads) {
-            const Piece y = piece(v);
+        if constexpr (kAtOnce > 1)
+            for (; v < pieces; v += kThreads) by(v, piece(v));
+        if (tid < head) one(tid, at(tid));
+        if (tid < tail) one(n - tail + tid, at(n - tail + tid));
+    }
+    // every entry once: f(index, value)
+    template <int kAtOnce = 1, typename F> __device__ __forceinline__ void each(int tid, F f) const
+    {
+        visit<kAtOnce>(tid, [&](int v, const Piece& y) {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) f(head + v * kEach + e, y.x[e]);
-        }
-        if (tid < head) f(tid, at(tid));
-        if (tid < tail) f(n - tail + tid, at(n - tail + tid));
+        }, f);
+    }
+    static __device__ __forceinline__ float top_of(const Piece& y)       // (NaN passed over)
+    {
+        float m = y.x[0];
+#pragma unroll
+        for (int e = 1; e < kEach; ++e) m = fmaxf(m, y.x[e]);
+        return m;
     }
 };
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 {
-    // (the slow path's masses of 64 entries each take the room of histogram, candidates and list)
-    __shared__ __align__(16) uint64_t room[kMostVocab / 64];
-    __shared__ uint32_t count[kBins];
+    constexpr int kEach = Row<T>::kEach;
+    __shared__ uint32_t count[kBins], top_count[kBins];        // histograms: of the entries, of the threads' largest logits
+    __shared__ uint64_t mass[kBins];
+    __shared__ uint64_t run_mass[kMostRuns];                   // masses of runs of the vocabulary
+    __shared__ float cand_value[kCandidates];
+    __shared__ uint32_t cand_index[kCandidates];
+    __shared__ uint64_t list_key[kList], list_mass[kList];
+    __shared__ uint32_t hot[kCandidates];                      // pieces that hold entries which can be kept
     __shared__ uint64_t wave_mass[kWaves];
     __shared__ uint32_t wave_count[kWaves];
     __shared__ float wave_top[kWaves];
+    __shared__ double wave_others[kWaves];
     __shared__ Found found;
     __shared__ uint64_t shared_key, shared_mass;
-    __shared__ uint32_t shared_index, filled;
-    uint64_t* mass = room;                                                         // [kBins]
-    float* cand_value = reinterpret_cast<float*>(room + kBins);                    // [kCandidates]
-    uint32_t* cand_index = reinterpret_cast<uint32_t*>(cand_value + kCandidates);  // [kCandidates]
-    uint64_t* list_key = reinterpret_cast<uint64_t*>(cand_index + kCandidates);    // [kList]
-    uint64_t* list_mass = list_key + kList;
-    static_assert(8 * kBins + 8 * kCandidates + 16 * kList <= (int)sizeof(room), "");
+    __shared__ uint32_t shared_index, filled[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.n_vocab;
     const int64_t r = blockIdx.x;
     const Row<T> row(static_cast<const typename T::Bits*>(a.logits) + r * a.row_stride, V);
-    auto at = [&](int i) { return cleaned(row.at(i)); };
 
     float top = -INFINITY;
-    row.each(tid, [&](int, float x) { top = fmaxf(top, x); });                     // (fmaxf passes NaN over)
+    row.template each<4>(tid, [&](int, float x) { top = fmaxf(top, x); });         // (fmaxf passes NaN over)
+    for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; top_count[x] = 0; run_mass[x] = 0; }
+    if (tid < 8) filled[tid] = 0;
     const float my_top = top;
     for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
     if (lane == 0) wave_top[wave] = top;
@@ -149,19 +165,20 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         return;
     }
     if (!(temperature > 0.0f)) {
-        uint32_t lowest = 0xffffffffu;
-        if (my_top == top) row.each(tid, [&](int i, float x) { if (x == top) lowest = min(lowest, (uint32_t)i); });
-        if (my_top == top) atomicMin(&shared_index, lowest);
+        if (my_top == top) {
+            uint32_t lowest = 0xffffffffu;
+            row.each(tid, [&](int i, float x) { if (x == top) lowest = min(lowest, (uint32_t)i); });
+            atomicMin(&shared_index, lowest);
+        }
         __syncthreads();
         if (tid == 0) a.token[r] = (int32_t)shared_index;
         return;
     }
     const Scale scale = {top, 1.0f / temperature};
     const int k = a.top_k && a.top_k[r] > 0 && a.top_k[r] < V ? a.top_k[r] : V;
-    const float p = a.top_p ? a.top_p[r] : 1.0f;
+    const float p = a.top_p ? a.top_p[r] : 1.0f, u = a.uniform[r];
     float min_p = a.min_p ? a.min_p[r] : 0.0f;
     min_p = min_p > 1.0f ? 1.0f : min_p;
-    const float u = a.uniform[r];
     auto mass_passed = [&](uint64_t total) -> uint64_t {                            // floor(u total), below total
         if (!(u > 0.0f)) return 0;
         const double want = floor((double)u * (double)total);
@@ -183,31 +200,47 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         for (int w = 0; w < kWaves; ++w) x += wave_mass[w];
         return x;
     };
-    const bool plain = top < INFINITY && scale.per_t > 0.0f && scale.per_t < INFINITY;
-    // mass of an entry as a float that is a whole number (the floor is exact: from 2^24 on all are whole); 0 for NaN
-    auto whole_mass = [&](float x) { return fmaxf(floorf(expf((x - top) * scale.per_t) * kMassOne), 0.0f); };
+    auto add_up_row = [&] {                            // (a thread's masses: whole numbers, at most 520 of 2^43: exact in a double)
+        double sum = 0.0;
+        row.template each<2>(tid, [&](int, float x) { sum += (double)scale.whole_mass(x); });
+        return add_up((uint64_t)sum);
+    };
 
-    // first digit at which the running count (by_mass: mass) of the histogram reaches `need`; ends behind a barrier
-    auto search = [&](bool by_mass, uint64_t need) {
+    // Sums of counts and masses up to every digit of a histogram (either may be left out): a thread has two digits.
+    struct Sums { uint32_t c0, c1, before_c, all_c; uint64_t m0, m1, before_m, all_m; };
+    auto scan = [&](const uint32_t* counts, const uint64_t* masses) {
         __syncthreads();
-        const uint32_t c0 = count[2 * tid], c1 = count[2 * tid + 1];
-        const uint64_t m0 = mass[2 * tid], m1 = mass[2 * tid + 1];
-        uint32_t c = c0 + c1;
-        uint64_t m = m0 + m1;
+        Sums b = {counts ? counts[2 * tid] : 0, counts ? counts[2 * tid + 1] : 0, 0, 0, masses ? masses[2 * tid] : 0, masses ? masses[2 * tid + 1] : 0, 0, 0};
+        uint32_t c = b.c0 + b.c1;
+        uint64_t m = b.m0 + b.m1;
+#pragma unroll
         for (int x = 1; x < 64; x *= 2) {
-            const uint32_t cc = __shfl_up(c, x);
-            const uint64_t mm = __shfl_up(m, x);
-            if (lane >= x) { c += cc; m += mm; }
+            if (counts) { const uint32_t cc = __shfl_up(c, x); if (lane >= x) c += cc; }
+            if (masses) { const uint64_t mm = __shfl_up(m, x); if (lane >= x) m += mm; }
         }
         if (lane == 63) { wave_count[wave] = c; wave_mass[wave] = m; }
         __syncthreads();
-        for (int w = 0; w < wave; ++w) { c += wave_count[w]; m += wave_mass[w]; }
-        c -= c0 + c1;
-        m -= m0 + m1;
+        b.before_c = c - b.c0 - b.c1;
+        b.before_m = m - b.m0 - b.m1;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t cw = counts ? wave_count[w] : 0;
+            const uint64_t mw = masses ? wave_mass[w] : 0;
+            if (w < wave) { b.before_c += cw; b.before_m += mw; }
+            b.all_c += cw;
+            b.all_m += mw;
+        }
+        return b;
+    };
+    // The digit at which the running count (by_mass: mass) reaches `need`, which is not more than all of it; ends behind a barrier.
+    auto find = [&](const Sums& b, bool by_mass, uint64_t need) {
+        __syncthreads();
+        uint32_t c = b.before_c;
+        uint64_t m = b.before_m;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const uint32_t cx = x ? c1 : c0;
-            const uint64_t mx = x ? m1 : m0, before = by_mass ? m : c, here = by_mass ? mx : cx;
+            const uint32_t cx = x ? b.c1 : b.c0;
+            const uint64_t mx = x ? b.m1 : b.m0, before = by_mass ? m : c, here = by_mass ? mx : cx;
             if (before < need && before + here >= need) found = {(uint32_t)(2 * tid + x), c, cx, m, mx};
             c += cx;
             m += mx;
@@ -215,92 +248,19 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         __syncthreads();
         return found;
     };
-    auto clear = [&] {
-        __syncthreads();
-        for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; }
-        __syncthreads();
-    };
     auto put = [&](uint32_t digit, float x) {
         atomicAdd(&count[digit], 1u);
-        atomicAdd((unsigned long long*)&mass[digit], (unsigned long long)scale.mass(scale.weight(x)));
+        atomicAdd((unsigned long long*)&mass[digit], (unsigned long long)scale.mass(x));
     };
-    if (plain && k == V && !(p < 1.0f)) {
-        // not cut: masses of runs of 64 pieces; head and tail are runs of their own
-        constexpr int kEach = Row<T>::kEach;
-        const int runs = (row.pieces + 63) / 64, all = runs + 2;
-        auto amount = [&](float x) -> double {
-            const float w = expf((x - top) * scale.per_t);
-            return w < min_p ? 0.0f : fmaxf(floorf(w * kMassOne), 0.0f);
-        };
-        auto lane_sum = [&](int s, double (&m)[kEach]) {                            // entries of run s: what a lane has of it
-            double sum = 0.0;
-            const int v = (s - 1) * 64 + lane;
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) m[e] = 0.0;
-            if (s == 0 || s == all - 1) {
-                const int n = s ? row.tail : row.head, i = s ? V - row.tail + lane : lane;
-                if (lane < n) m[0] = amount(row.at(i));
-            } else if (v < row.pieces) {
-                const typename Row<T>::Piece y = row.piece(v);
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) m[e] = amount(y.x[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) sum += m[e];
-            return sum;
-        };
-        double m[kEach];
-        uint64_t sum = 0;
-        for (int s = wave; s < all; s += kWaves) {
-            double x = lane_sum(s, m);                                              // (whole numbers below 2^53: exact)
-            for (int y = 1; y < 64; y *= 2) x += __shfl_xor(x, y);
-            if (lane == 0) room[s] = (uint64_t)x;
-            sum += lane == 0 ? (uint64_t)x : 0;
-        }
-        const uint64_t need = mass_passed(add_up(sum)) + 1;
-        if (wave == 0) {
-            uint64_t before = 0;
-            for (int s0 = 0; s0 < all; s0 += 64) {
-                uint64_t x = s0 + lane < all ? room[s0 + lane] : 0;
-                for (int y = 1; y < 64; y *= 2) { const uint64_t z = __shfl_up(x, y); if (lane >= y) x += z; }
-                const uint64_t hit = __ballot(before + x >= need);
-                if (hit) {
-                    const int f = __ffsll((unsigned long long)hit) - 1, s = s0 + f;
-                    if (f) before += __shfl(x, f - 1);
-                    uint64_t mine = (uint64_t)lane_sum(s, m), z = mine;
-                    for (int y = 1; y < 64; y *= 2) { const uint64_t q = __shfl_up(z, y); if (lane >= y) z += q; }
-                    const uint64_t here = __ballot(before + z >= need);
-                    if (lane == __ffsll((unsigned long long)here) - 1) {
-                        before += z - mine;
-                        int e = 0;
-                        if (s != 0 && s != all - 1)
-                            for (; e < kEach - 1; ++e) {
-                                before += (uint64_t)m[e];
-                                if (before >= need) break;
-                            }
-                        a.token[r] = s == 0 ? lane : s == all - 1 ? V - row.tail + lane : row.head + ((s - 1) * 64 + lane) * kEach + e;
-                    }
-                    break;
-                }
-                before += __shfl(x, 63);
-            }
-        }
-        return;
-    }
-    // The element of `digit` at which the running count or mass of the list's keys, the largest first, reaches `need`: its key, and
-    // the mass up to it; false if the digit has more entries than the list has room for.
-    auto resolve = [&](int n, uint32_t digit, bool by_mass, uint64_t need, auto digit_of, auto key_at, auto mass_at) {
+    // The list's key, the largest first, at which the running count or mass reaches `need`, to shared_key; the mass up to it to
+    // shared_mass.  Entries are listed with list(which, key, mass); false if there were more than the list has room for.
+    auto list = [&](int which, uint64_t key, uint64_t m) {
+        const uint32_t to = atomicAdd(&filled[which], 1u);
+        if (to < kList) { list_key[to] = key; list_mass[to] = m; }
+    };
+    auto resolve = [&](int which, bool by_mass, uint64_t need) {
         __syncthreads();
-        if (tid == 0) filled = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += kThreads)
-            if (digit_of(i) == digit) {
-                const uint64_t m = mass_at(i);
-                const uint32_t to = atomicAdd(&filled, 1u);
-                if (to < kList) { list_key[to] = key_at(i); list_mass[to] = m; }
-            }
-        __syncthreads();
-        const int here = (int)filled;
+        const int here = (int)filled[which];
         if (here > kList) return false;
         if (tid < here) {
             const uint64_t key = list_key[tid], mine = list_mass[tid];
@@ -313,211 +273,280 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         __syncthreads();
         return true;
     };
-    bool fast = plain && (k == V || k <= kThreads || V <= kCandidates);
-    if (fast) {
+
+    if (scale.usual() && (k < V || p < 1.0f) && (k == V || k <= kThreads || V <= kCandidates)) {
         // digits up to `last` can be kept
         uint32_t last = kNoMass - 1;
         if (V > kCandidates) {
-            for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; }
-            __syncthreads();
-            if (my_top > -INFINITY) atomicAdd(&count[scale.bin(my_top)], 1u);
-            if (tid == 0) found = {kBins, 0, 0, 0, 0};
-            last = min(last, search(false, (uint64_t)(k < V ? k : kRank)).digit);
+            if (my_top > -INFINITY) atomicAdd(&top_count[scale.bin(my_top)], 1u);
+            const Sums tops = scan(top_count, nullptr);
+            const uint32_t rank = k < V ? (uint32_t)k : kRank;
+            if (rank <= tops.all_c) last = min(last, find(tops, false, rank).digit);
         }
-        if (tid == 0) filled = 0;
-        __syncthreads();
-        const float edge = (float)(last + 1);
-        uint64_t total = 0;
+        // entries whose digit can be kept go to LDS; where the mass of the row counts, that of the others is added up roughly: every
+        // weight's error is below 2^-16 of it (products and constant of the exponent: |x| 2^-22 with |x| <= 43, where a weight has a
+        // mass; 2^-23 of each exp; sums of eight in 32 bits), which seldom leaves open where the kept ones end
+        const float edge = (float)(last + 1), low = top - (edge / (64.0f * scale.per_t) * 1.0001f + fabsf(top) * 1e-6f), to_exp2 = scale.per_t * 1.44269504f;
+        double others = 0.0;
+        auto roughly = [&](float x) { return __builtin_amdgcn_exp2f(fmaxf((x - top) * to_exp2, -126.0f)); };      // (NaN: next to nothing)
         auto take = [&](int i, float x) {
             if ((top - x) * scale.per_t * 64.0f < edge) {                            // (false for NaN)
-                const uint32_t to = atomicAdd(&filled, 1u);
+                const uint32_t to = atomicAdd(&filled[0], 1u);
                 if (to < kCandidates) { cand_value[to] = x + 0.0f; cand_index[to] = (uint32_t)i; }
+            } else if (k == V) {
+                others += (double)roughly(x);
             }
         };
-        if (k < V) {
-            row.each(tid, take);
-        } else {
-            double sum = 0.0;                          // (whole numbers, at most 512 of 2^43: exact)
-            row.each(tid, [&](int i, float x) { sum += (double)whole_mass(x); take(i, x); });
-            total = add_up((uint64_t)sum);
+        // (a piece with such an entry is looked into afterwards: nearly every wavefront meets some, few lanes do)
+        row.template visit<4>(tid, [&](int v, const typename Row<T>::Piece& y) {
+            if (Row<T>::top_of(y) >= low) {
+                const uint32_t to = atomicAdd(&filled[7], 1u);
+                if (to < kCandidates) hot[to] = (uint32_t)v;
+            } else if (k == V) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
+                others += (double)sum;
+            }
+        }, take);
+        __syncthreads();
+        const int pieces = min((int)filled[7], kCandidates);
+        for (int i = tid; i < pieces; i += kThreads) {
+            const int v = (int)hot[i];
+            const typename Row<T>::Piece y = row.piece(v);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) take(row.head + v * kEach + e, y.x[e]);
+        }
+        if (k == V) {
+            for (int y = 1; y < 64; y *= 2) others += __shfl_xor(others, y);
+            if (lane == 0) wave_others[wave] = others;
         }
         __syncthreads();
-        const int n = (int)filled;
-        fast = n <= kCandidates;
-        if (fast) {
+        const int n = (int)filled[0];
+        bool fits = n <= kCandidates && (int)filled[7] <= kCandidates;
+        if (fits) {
             auto digit_of = [&](int i) { return scale.bin(cand_value[i]); };
-            auto key_at = [&](int i) { return (uint64_t)key_of(cand_value[i]) << 32 | (uint32_t)~cand_index[i]; };
-            auto mass_at = [&](int i) { return (uint64_t)whole_mass(cand_value[i]); };
-            clear();
+            auto key_at = [&](int i) { return key_of(cand_value[i], cand_index[i]); };
+            auto mass_at = [&](int i) { return scale.mass(cand_value[i]); };
+            auto among = [&](int which, uint32_t digit, bool by_mass, uint64_t need) {
+                for (int i = tid; i < n; i += kThreads)
+                    if (digit_of(i) == digit) list(which, key_at(i), mass_at(i));
+                return resolve(which, by_mass, need);
+            };
             for (int i = tid; i < n; i += kThreads) put(digit_of(i), cand_value[i]);
+            const Sums sums = scan(count, mass);
             // kept: digits before `digit`, and of it the keys from `key` on
             uint32_t digit = kBins;
-            uint64_t key = 0;
+            uint64_t key = 0, least = sums.all_m, most = sums.all_m;                // bounds of the mass that top_p is a share of
             if (k < n) {
-                const Found f = search(false, (uint64_t)k);
+                const Found f = find(sums, false, (uint64_t)k);
                 const uint64_t need = (uint64_t)k - f.count_before;
                 digit = f.digit;
-                total = f.mass_before + f.mass;
+                least = most = f.mass_before + f.mass;
                 if (need < f.count) {
-                    fast = resolve(n, digit, false, need, digit_of, key_at, mass_at);
-                    if (fast) { key = shared_key; total = f.mass_before + shared_mass; }
+                    fits = among(1, digit, false, need);
+                    if (fits) { key = shared_key; least = most = f.mass_before + shared_mass; }
                 }
-            } else if (k < V) {                        // (fewer entries with a mass than top_k)
-                uint64_t sum = 0;
-                for (int i = tid; i < n; i += kThreads) sum += mass_at(i);
-                total = add_up(sum);
+            } else if (k == V) {
+                double sum = 0.0;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) sum += wave_others[w];
+                sum *= (double)kMassOne;
+                const double off = sum * 0x1p-16 + (double)V;                       // (V: what the floors take off)
+                least += sum > off ? (uint64_t)(sum - off) : 0;
+                most += (uint64_t)(sum + off);
             }
-            if (fast && p < 1.0f) {
-                const uint64_t need = mass_needed(total);
-                __syncthreads();
-                if (tid == 0) found = {kBins, 0, 0, 0, 0};
-                const Found f = search(true, need);
-                fast = f.digit < kBins;                // (else the candidates hold too little)
-                if (fast) {
-                    digit = f.digit;
-                    key = 0;
-                    fast = resolve(n, digit, true, need - f.mass_before, digit_of, key_at, mass_at);
-                    if (fast) key = shared_key;
-                }
+            for (int pass = 0; fits && p < 1.0f; ++pass) {
+                const uint64_t need = mass_needed(least);
+                fits = need <= sums.all_m;                                          // (else the candidates hold too little)
+                if (!fits) break;
+                const Found f = find(sums, true, need);
+                fits = among(2 + pass, f.digit, true, need - f.mass_before);
+                if (!fits) break;
+                digit = f.digit;
+                key = shared_key;
+                if (mass_needed(most) <= f.mass_before + shared_mass) break;
+                least = most = add_up_row();           // (it matters: every mass of the row)
             }
-            if (fast) {
+            if (fits) {
                 auto kept = [&](int i) -> uint64_t {
                     const uint32_t d = digit_of(i);
-                    if (d > digit || (d == digit && key_at(i) < key)) return 0;
-                    if (expf((cand_value[i] - top) * scale.per_t) < min_p) return 0;
+                    if (d > digit || (d == digit && key_at(i) < key) || scale.weight(cand_value[i]) < min_p) return 0;
                     return mass_at(i);
                 };
                 // the same search along the index: 2048 runs of the vocabulary
                 int shift = 0;
                 while (((V - 1) >> shift) >= kBins) ++shift;
-                clear();
-                uint64_t sum = 0;
                 for (int i = tid; i < n; i += kThreads) {
                     const uint64_t m = kept(i);
-                    if (m) atomicAdd((unsigned long long*)&mass[cand_index[i] >> shift], (unsigned long long)m);
-                    sum += m;
+                    if (m) atomicAdd((unsigned long long*)&run_mass[cand_index[i] >> shift], (unsigned long long)m);
                 }
-                const uint64_t need = mass_passed(add_up(sum)) + 1;
-                const Found f = search(true, need);
-                fast = resolve(n, f.digit, true, need - f.mass_before, [&](int i) { return cand_index[i] >> shift; },
-                               [&](int i) { return (uint64_t)(uint32_t)~cand_index[i]; }, kept);
-                if (fast) {
-                    if (tid == 0) a.token[r] = (int32_t)~(uint32_t)shared_key;
-                    return;
-                }
+                const Sums runs = scan(nullptr, run_mass);
+                const uint64_t need = mass_passed(runs.all_m) + 1;
+                const Found f = find(runs, true, need);
+                for (int i = tid; i < n; i += kThreads)
+                    if (cand_index[i] >> shift == f.digit) list(4, (uint64_t)~cand_index[i], kept(i));
+                resolve(4, true, need - f.mass_before);                             // (a run has at most 256 entries)
+                if (tid == 0) a.token[r] = (int32_t)~(uint32_t)shared_key;
+                return;
             }
         }
     }
-    // the end of a prefix: all of the bins before `bin`, and of it all (whole) or the keys above `key` and `ties` entries of it
-    struct End { uint32_t bin, key, ties, equal; bool whole; uint64_t mass; };
-    End end = {kBins - 1, 0, 0, 0, true, 0};
-    auto descend = [&](bool by_mass, const Found& in, uint64_t need) {
-        End e = {in.digit, 0, 0, 0, false, in.mass_before};
-        uint32_t above = 0;
-        const int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
-        for (int level = 0; level < 3; ++level) {
+
+    // Through the row for every step: a histogram of all of it, the digits in which the kept entries end looked into.
+    float last_kept = -INFINITY;                       // of the kept entries the last one's logit and index
+    int last_index = V;
+    auto ends_at = [&](uint64_t key) {
+        const uint32_t b = (uint32_t)(key >> 19);
+        last_kept = __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu));
+        last_index = kMostVocab - 1 - (int)(key & (kMostVocab - 1));
+    };
+    auto clear = [&] {
+        __syncthreads();
+        for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; }
+        __syncthreads();
+    };
+    auto histogram = [&] {
+        clear();
+        row.each(tid, [&](int, float x) { x = cleaned(x); put(scale.bin(x), x); });
+        return scan(count, mass);
+    };
+    // as resolve, for a digit of the whole row; the histogram is not there any more afterwards if the list has no room
+    auto among_row = [&](int which, const Found& in, bool by_mass, uint64_t need) {
+        if (in.count <= (uint32_t)kList) {
+            row.each(tid, [&](int i, float x) { x = cleaned(x); if (scale.bin(x) == in.digit) list(which, key_of(x, i), scale.mass(x)); });
+            resolve(which, by_mass, need);
+            return;
+        }
+        uint64_t above = 0, up_to = 0;                 // 51 bits of key in five digits
+        const int shifts[5] = {40, 29, 19, 9, 0}, widths[5] = {11, 11, 10, 10, 9};
+        for (int level = 0; level < 5; ++level) {
             const int shift = shifts[level], width = widths[level];
             const uint32_t ones = (1u << width) - 1;
             clear();
-            for (int i = tid; i < V; i += kThreads) {
-                const float x = at(i);
-                const uint32_t key = key_of(x);
-                if (scale.bin(x) == in.digit && (level == 0 || key >> (shift + width) == above)) put(ones - (key >> shift & ones), x);
-            }
-            const Found f = search(by_mass, need);
+            row.each(tid, [&](int i, float x) {
+                x = cleaned(x);
+                const uint64_t key = key_of(x, i);
+                if (scale.bin(x) == in.digit && (level == 0 || key >> (shift + width) == above)) put(ones - ((uint32_t)(key >> shift) & ones), x);
+            });
+            const Found f = find(scan(count, mass), by_mass, need);
             above = above << width | (ones - f.digit);
             need -= by_mass ? f.mass_before : f.count_before;
-            e.mass += f.mass_before;
-            e.equal = f.count;
+            up_to += f.mass_before + (level == 4 ? f.mass : 0);
         }
-        e.key = above;
-        const uint64_t each = scale.mass(scale.weight(value_of(above)));
-        e.ties = (uint32_t)(by_mass ? (need + each - 1) / each : need);
-        e.mass += e.ties * each;
-        return e;
+        if (tid == 0) { shared_key = above; shared_mass = up_to; }
+        __syncthreads();
     };
-
     if (k < V || p < 1.0f) {
-        clear();
-        for (int i = tid; i < V; i += kThreads) { const float x = at(i); put(scale.bin(x), x); }
-        const Found in_k = search(false, (uint64_t)k);
-        Found in_p = in_k;
-        uint64_t total = in_k.mass_before + in_k.mass, need = 0;
-        end.bin = in_k.digit;
-        bool cut_k = (uint64_t)k - in_k.count_before < in_k.count;
-        if (p < 1.0f && !cut_k) {
-            need = mass_needed(total);
-            in_p = search(true, need);
-        }
-        if (cut_k) {
-            end = descend(false, in_k, (uint64_t)k - in_k.count_before);
-            total = end.mass;
-            if (p < 1.0f) {
-                need = mass_needed(total);
-                clear();
-                for (int i = tid; i < V; i += kThreads) { const float x = at(i); put(scale.bin(x), x); }
-                in_p = search(true, need);
-            }
+        Sums sums = histogram();
+        Found f = find(sums, false, (uint64_t)k);
+        uint64_t total = f.mass_before + f.mass;
+        const uint64_t of_k = (uint64_t)k - f.count_before;
+        if (k < V) {
+            const bool gone = f.count > (uint32_t)kList;
+            among_row(5, f, false, of_k);
+            ends_at(shared_key);
+            total = f.mass_before + shared_mass;
+            if (gone && p < 1.0f) sums = histogram();
         }
         if (p < 1.0f) {
-            end = {in_p.digit, 0, 0, 0, true, 0};
-            if (need - in_p.mass_before < in_p.mass || cut_k) end = descend(true, in_p, need - in_p.mass_before);
+            const uint64_t need = mass_needed(total);
+            f = find(sums, true, need);
+            among_row(6, f, true, need - f.mass_before);
+            ends_at(shared_key);
         }
     }
-    // equal logits of which not all are kept: the index of the first one that is not
-    uint32_t ties_end = (uint32_t)V;
-    const int segments = (V + 63) / 64;
-    auto lowest = [&](uint64_t need, auto amount) -> uint32_t {          // the index at which the running amount reaches `need`
-        __syncthreads();
-        for (int s = wave; s < segments; s += kWaves) {
-            const int i = s * 64 + lane;
-            uint64_t m = i < V ? amount(i) : 0;
-            for (int x = 1; x < 64; x *= 2) m += __shfl_xor(m, x);
-            if (lane == 0) mass[s] = m;
+
+    // Masses of runs of 512 pieces, eight a lane (head and tail of the row are runs of their own), and the run in which the token is
+    // again.
+    constexpr int kLines = 8;
+    const int runs = (row.pieces + 64 * kLines - 1) / (64 * kLines), all = runs + 2;
+    // entries below this have no mass, or less weight than min_p (a little room for the roundings), or are behind the end
+    float low = fmaxf(min_p > 0.0f ? logf(min_p) - 0.001f : -30.0f, -30.0f);
+    if (last_kept > -INFINITY && last_kept < INFINITY) low = fmaxf(low, (last_kept - top) * scale.per_t);
+    const bool usual = scale.usual();
+    auto amount = [&](int i, float x) -> double {
+        const float w = usual ? expf((x - top) * scale.per_t) : scale.weight(cleaned(x));
+        const float m = fmaxf(floorf(w * kMassOne), 0.0f);
+        return (x > last_kept || (x == last_kept && i <= last_index)) && !(w < min_p) ? (double)m : 0.0;
+    };
+    auto ends = [&](int s) -> double {                 // head (run 0) and tail (the last): an entry a lane
+        const int n = s ? row.tail : row.head, i = s ? V - row.tail + lane : lane;
+        return lane < n ? amount(i, row.at(i)) : 0.0;
+    };
+    auto in_piece = [&](int v, const typename Row<T>::Piece& y, double (&m)[kEach]) {      // (whole numbers below 2^53, added up exactly)
+        double sum = 0.0;
+        if (!usual || (Row<T>::top_of(y) - top) * scale.per_t >= low) {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) sum += m[e] = amount(row.head + v * kEach + e, y.x[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) m[e] = 0.0;
         }
-        __syncthreads();
-        if (wave == 0) {
-            uint64_t before = 0;
-            for (int s0 = 0; s0 < segments; s0 += 64) {
-                uint64_t m = s0 + lane < segments ? mass[s0 + lane] : 0;
-                for (int x = 1; x < 64; x *= 2) { const uint64_t y = __shfl_up(m, x); if (lane >= x) m += y; }
-                const uint64_t hit = __ballot(before + m >= need);
-                if (hit) {
-                    const int f = __ffsll((unsigned long long)hit) - 1;
-                    if (f) before += __shfl(m, f - 1);
-                    const int i = (s0 + f) * 64 + lane;
-                    uint64_t y = i < V ? amount(i) : 0;
-                    for (int x = 1; x < 64; x *= 2) { const uint64_t z = __shfl_up(y, x); if (lane >= x) y += z; }
-                    const uint64_t here = __ballot(before + y >= need);
-                    if (lane == 0) shared_index = (uint32_t)((s0 + f) * 64 + __ffsll((unsigned long long)here) - 1);
-                    break;
-                }
-                before += __shfl(m, 63);
+        return sum;
+    };
+    double m[kEach];
+    uint64_t sum = 0;
+    __syncthreads();
+    for (int s = wave; s < all; s += kWaves) {
+        uint64_t x = 0;                                // (512 pieces can pass 2^53)
+        if (s == 0 || s == all - 1) {
+            x = (uint64_t)ends(s);
+        } else {
+            const int v0 = (s - 1) * 64 * kLines + lane;
+            uint4 b[kLines];
+#pragma unroll
+            for (int q = 0; q < kLines; ++q) b[q] = v0 + q * 64 < row.pieces ? row.bits(v0 + q * 64) : make_uint4(0, 0, 0, 0);
+            double y = 0.0;
+#pragma unroll
+            for (int q = 0; q < kLines; ++q)
+                if (v0 + q * 64 < row.pieces) y += in_piece(v0 + q * 64, Row<T>::unpacked(b[q]), m);
+            x = (uint64_t)y;
+        }
+        for (int y = 1; y < 64; y *= 2) x += __shfl_xor(x, y);
+        if (lane == 0) run_mass[s] = x;
+        sum += lane == 0 ? x : 0;
+    }
+    const uint64_t need = mass_passed(add_up(sum)) + 1;
+    if (wave) return;
+    uint64_t before = 0;
+    for (int s0 = 0; s0 < all; s0 += 64) {
+        uint64_t x = s0 + lane < all ? run_mass[s0 + lane] : 0;
+        for (int y = 1; y < 64; y *= 2) { const uint64_t z = __shfl_up(x, y); if (lane >= y) x += z; }
+        const uint64_t hit = __ballot(before + x >= need);
+        if (!hit) {
+            before += __shfl(x, 63);
+            continue;
+        }
+        const int f = __ffsll((unsigned long long)hit) - 1, s = s0 + f;
+        if (f) before += __shfl(x, f - 1);
+        const bool at_end = s == 0 || s == all - 1;
+        for (int q = 0; q < kLines; ++q) {             // the run's lines of 64 pieces
+            const int v = ((s - 1) * kLines + q) * 64 + lane;
+            uint64_t mine = 0;
+            if (at_end) mine = (uint64_t)ends(s);
+            else if (v < row.pieces) mine = (uint64_t)in_piece(v, row.piece(v), m);
+            uint64_t z = mine;
+            for (int y = 1; y < 64; y *= 2) { const uint64_t w = __shfl_up(z, y); if (lane >= y) z += w; }
+            const uint64_t here = __ballot(before + z >= need);
+            if (!here) {
+                before += __shfl(z, 63);
+                continue;
             }
+            if (lane == __ffsll((unsigned long long)here) - 1) {
+                before += z - mine;
+                int e = 0;
+#pragma unroll
+                for (int y = 0; y < kEach - 1; ++y) {
+                    before += (uint64_t)m[y];
+                    if (before < need) e = y + 1;
+                }
+                a.token[r] = s == 0 ? lane : s == all - 1 ? V - row.tail + lane : row.head + v * kEach + e;
+            }
+            break;
         }
-        __syncthreads();
-        return shared_index;
-    };
-    if (!end.whole && end.ties < end.equal)
-        ties_end = lowest(end.ties, [&](int i) { return (uint64_t)(key_of(at(i)) == end.key); }) + 1;
-    auto kept = [&](int i) -> uint64_t {
-        const float x = at(i);
-        const uint32_t b = scale.bin(x), key = key_of(x);
-        if (b > end.bin || (!end.whole && b == end.bin && (key < end.key || (key == end.key && (uint32_t)i >= ties_end)))) return 0;
-        const float w = scale.weight(x);
-        return w < min_p ? 0 : scale.mass(w);
-    };
-    uint64_t total = 0;
-    for (int i = tid; i < V; i += kThreads) total += kept(i);
-    for (int x = 1; x < 64; x *= 2) total += __shfl_xor(total, x);
-    __syncthreads();
-    if (lane == 0) wave_mass[wave] = total;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < kWaves; ++w) total += wave_mass[w];
-    const uint64_t passed = mass_passed(total);
-    const uint32_t token = lowest(passed + 1, kept);
-    if (tid == 0) a.token[r] = (int32_t)token;
+        return;
+    }
 }
 
 bool sizes_ok(const fr_sample_desc& d)
