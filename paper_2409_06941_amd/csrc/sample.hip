@@ -16,6 +16,7 @@
 // for every digit of the search.
 
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "lm_types.h"
@@ -64,7 +65,7 @@ struct Scale {
 
 struct Found { uint32_t digit, count_before, count; uint64_t mass_before, mass; };
 
-constexpr int kCandidates = 4096, kList = 1024, kRank = 896, kMostRuns = kBins;
+constexpr int kCandidates = 4096, kList = 1024, kRank = 960, kMostRuns = kBins;
 constexpr uint32_t kNoMass = 1909;                     // from this digit on (29.83 and more below the top) masses are 0: 43 ln 2 = 29.81
 
 // A row of any alignment in pieces of 16 bytes: `head` entries up to the first such piece, `pieces` of kEach, `tail` entries.
@@ -148,18 +149,54 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     const int64_t r = blockIdx.x;
     const Row<T> row(static_cast<const typename T::Bits*>(a.logits) + r * a.row_stride, V);
 
-    float top = -INFINITY;
-    row.template each<4>(tid, [&](int, float x) { top = fmaxf(top, x); });         // (fmaxf passes NaN over)
+    const float temperature = a.temperature ? a.temperature[r] : 1.0f, per_t = 1.0f / temperature, to_exp2 = per_t * 1.44269504f;
+    const int k = a.top_k && a.top_k[r] > 0 && a.top_k[r] < V ? a.top_k[r] : V;
+    const float p = a.top_p ? a.top_p[r] : 1.0f, u = a.uniform[r];
+    float min_p = a.min_p ? a.min_p[r] : 0.0f;
+    min_p = min_p > 1.0f ? 1.0f : min_p;
+    // First pass: the largest logit of the thread's share; for rows cut by mass alone also the share's mass, roughly, relative to
+    // `from` (which lags behind the largest by up to a factor of 2^8).  The error of a weight in it is below 2^-16 of the weight: of
+    // the exponent's products, differences and constant |x| 5 / 2^24 with |x| <= 43 (where a weight still has a mass), of each exp 2^-23,
+    // of sums of eight in 32 bits 2^-22, of up to six factors where `from` moves 2^-22 each.
+    const bool by_mass = k == V && p < 1.0f && per_t > 0.0f && per_t < INFINITY;
+    float top = -INFINITY, from = -INFINITY;
+    double others = 0.0;
+    auto roughly = [&](float x) { return __builtin_amdgcn_exp2f(fmaxf((x - from) * to_exp2, -126.0f)); };         // (NaN: next to nothing)
+    if (by_mass) {
+        const float slack = 8.0f / to_exp2;
+        auto add = [&](float t, auto sum) {
+            top = fmaxf(top, t);
+            if (t > from + slack) {
+                others *= (double)__builtin_amdgcn_exp2f((from - t) * to_exp2);
+                from = t;
+            }
+            others += (double)sum();
+        };
+        row.template visit<4>(tid, [&](int, const typename Row<T>::Piece& y) {
+            add(Row<T>::top_of(y), [&] {
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
+                return sum;
+            });
+        }, [&](int, float x) { add(fmaxf(x, -INFINITY), [&] { return roughly(x); }); });
+    } else {
+        row.template each<4>(tid, [&](int, float x) { top = fmaxf(top, x); });     // (fmaxf passes NaN over)
+    }
     for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; top_count[x] = 0; run_mass[x] = 0; }
     if (tid < 8) filled[tid] = 0;
     const float my_top = top;
     for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
     if (lane == 0) wave_top[wave] = top;
+    if (by_mass) {                                     // relative to the wavefront's largest
+        double sum = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
+        for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+        if (lane == 0) wave_others[wave] = sum;
+    }
     if (tid == 0) shared_index = 0xffffffffu;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_top[w]);
-    const float temperature = a.temperature ? a.temperature[r] : 1.0f;
     if (top == -INFINITY) {
         if (tid == 0) a.token[r] = -1;
         return;
@@ -167,18 +204,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     if (!(temperature > 0.0f)) {
         if (my_top == top) {
             uint32_t lowest = 0xffffffffu;
-            row.each(tid, [&](int i, float x) { if (x == top) lowest = min(lowest, (uint32_t)i); });
+            row.template each<8>(tid, [&](int i, float x) { if (x == top) lowest = min(lowest, (uint32_t)i); });
             atomicMin(&shared_index, lowest);
         }
         __syncthreads();
         if (tid == 0) a.token[r] = (int32_t)shared_index;
         return;
     }
-    const Scale scale = {top, 1.0f / temperature};
-    const int k = a.top_k && a.top_k[r] > 0 && a.top_k[r] < V ? a.top_k[r] : V;
-    const float p = a.top_p ? a.top_p[r] : 1.0f, u = a.uniform[r];
-    float min_p = a.min_p ? a.min_p[r] : 0.0f;
-    min_p = min_p > 1.0f ? 1.0f : min_p;
+    const Scale scale = {top, per_t};
     auto mass_passed = [&](uint64_t total) -> uint64_t {                            // floor(u total), below total
         if (!(u > 0.0f)) return 0;
         const double want = floor((double)u * (double)total);
@@ -208,9 +241,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 
     // Sums of counts and masses up to every digit of a histogram (either may be left out): a thread has two digits.
     struct Sums { uint32_t c0, c1, before_c, all_c; uint64_t m0, m1, before_m, all_m; };
-    auto scan = [&](const uint32_t* counts, const uint64_t* masses) {
-        __syncthreads();
-        Sums b = {counts ? counts[2 * tid] : 0, counts ? counts[2 * tid + 1] : 0, 0, 0, masses ? masses[2 * tid] : 0, masses ? masses[2 * tid + 1] : 0, 0, 0};
+    auto scan_of = [&](auto counts, auto masses, uint32_t c0, uint32_t c1, uint64_t m0, uint64_t m1) {
+        Sums b = {c0, c1, 0, 0, m0, m1, 0, 0};
         uint32_t c = b.c0 + b.c1;
         uint64_t m = b.m0 + b.m1;
 #pragma unroll
@@ -231,6 +263,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             b.all_m += mw;
         }
         return b;
+    };
+    const std::true_type yes{};
+    const std::false_type no{};
+    auto scan = [&](auto counts, auto masses, const uint32_t* c, const uint64_t* m) {
+        __syncthreads();
+        return scan_of(counts, masses, counts ? c[2 * tid] : 0, counts ? c[2 * tid + 1] : 0, masses ? m[2 * tid] : 0, masses ? m[2 * tid + 1] : 0);
     };
     // The digit at which the running count (by_mass: mass) reaches `need`, which is not more than all of it; ends behind a barrier.
     auto find = [&](const Sums& b, bool by_mass, uint64_t need) {
@@ -274,35 +312,56 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         return true;
     };
 
-    if (scale.usual() && (k < V || p < 1.0f) && (k == V || k <= kThreads || V <= kCandidates)) {
+    if (scale.usual() && (k < V || p < 1.0f || min_p > 0.0f) && (k == V || k <= kThreads || V <= kCandidates)) {
         // digits up to `last` can be kept
         uint32_t last = kNoMass - 1;
-        if (V > kCandidates) {
+        if (k == V && !by_mass) {
+            last = min(last, (uint32_t)fminf(-64.0f * logf(min_p) + 1.0f, (float)last));       // (cut by weight alone)
+        } else if (V > kCandidates) {
             if (my_top > -INFINITY) atomicAdd(&top_count[scale.bin(my_top)], 1u);
-            const Sums tops = scan(top_count, nullptr);
-            const uint32_t rank = k < V ? (uint32_t)k : kRank;
+            const Sums tops = scan(yes, no, top_count, nullptr);
+            uint32_t rank = (uint32_t)k;
+            if (by_mass) {
+                // As many as hold the mass, going by the threads' largest: where c of 1024 threads have theirs above a line, about
+                // -1024 log(1 - c / 1024) entries are above it.  (Too few, and the row takes the long way; too many cost a little.)
+                auto entries = [](uint32_t c) { return -1024.0f * logf(1.0f - fminf((float)c, 1023.5f) / 1024.0f); };
+                const float n0 = entries(tops.before_c), n1 = entries(tops.before_c + tops.c0), n2 = entries(tops.before_c + tops.c0 + tops.c1);
+                const float w0 = expf(-(float)(4 * tid + 1) / 128.0f), w1 = expf(-(float)(4 * tid + 3) / 128.0f);
+                double all = 0.0;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    if (wave_top[w] > -INFINITY) all += wave_others[w] * (double)__builtin_amdgcn_exp2f((wave_top[w] - top) * to_exp2);
+                __syncthreads();
+                const Sums held = scan_of(no, yes, 0, 0, (uint64_t)(fmaxf(n1 - n0, 0.0f) * w0 * 0x1p30f), (uint64_t)(fmaxf(n2 - n1, 0.0f) * w1 * 0x1p30f));
+                const uint64_t want = (uint64_t)fmin((double)p * all * 1.05 * 0x1p30, 0x1p62);
+                rank = kRank;                          // (as many as there is room for, where they seem to hold too little)
+                if (want <= held.all_m) {
+                    last = min(last, find(held, true, want).digit + 4);
+                    rank = V;
+                }
+            }
             if (rank <= tops.all_c) last = min(last, find(tops, false, rank).digit);
         }
-        // entries whose digit can be kept go to LDS; where the mass of the row counts, that of the others is added up roughly: every
-        // weight's error is below 2^-16 of it (products and constant of the exponent: |x| 2^-22 with |x| <= 43, where a weight has a
-        // mass; 2^-23 of each exp; sums of eight in 32 bits), which seldom leaves open where the kept ones end
-        const float edge = (float)(last + 1), low = top - (edge / (64.0f * scale.per_t) * 1.0001f + fabsf(top) * 1e-6f), to_exp2 = scale.per_t * 1.44269504f;
-        double others = 0.0;
-        auto roughly = [&](float x) { return __builtin_amdgcn_exp2f(fmaxf((x - top) * to_exp2, -126.0f)); };      // (NaN: next to nothing)
+        // Entries whose digit can be kept go to LDS.  A thread reads its share again if its largest is among them; the mass of the others
+        // is known roughly, which seldom leaves open where the kept ones end.
+        const float edge = (float)(last + 1), low = top - (edge / (64.0f * scale.per_t) * 1.0001f + fabsf(top) * 1e-6f);
+        others = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
+        if (my_top >= low) others = 0.0;
+        from = top;
         auto take = [&](int i, float x) {
             if ((top - x) * scale.per_t * 64.0f < edge) {                            // (false for NaN)
                 const uint32_t to = atomicAdd(&filled[0], 1u);
                 if (to < kCandidates) { cand_value[to] = x + 0.0f; cand_index[to] = (uint32_t)i; }
-            } else if (k == V) {
+            } else if (by_mass) {
                 others += (double)roughly(x);
             }
         };
         // (a piece with such an entry is looked into afterwards: nearly every wavefront meets some, few lanes do)
-        row.template visit<4>(tid, [&](int v, const typename Row<T>::Piece& y) {
+        if (my_top >= low) row.template visit<8>(tid, [&](int v, const typename Row<T>::Piece& y) {
             if (Row<T>::top_of(y) >= low) {
                 const uint32_t to = atomicAdd(&filled[7], 1u);
                 if (to < kCandidates) hot[to] = (uint32_t)v;
-            } else if (k == V) {
+            } else if (by_mass) {
                 float sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
@@ -317,7 +376,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 #pragma unroll
             for (int e = 0; e < kEach; ++e) take(row.head + v * kEach + e, y.x[e]);
         }
-        if (k == V) {
+        if (by_mass) {
             for (int y = 1; y < 64; y *= 2) others += __shfl_xor(others, y);
             if (lane == 0) wave_others[wave] = others;
         }
@@ -334,7 +393,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 return resolve(which, by_mass, need);
             };
             for (int i = tid; i < n; i += kThreads) put(digit_of(i), cand_value[i]);
-            const Sums sums = scan(count, mass);
+            const Sums sums = scan(yes, yes, count, mass);
             // kept: digits before `digit`, and of it the keys from `key` on
             uint32_t digit = kBins;
             uint64_t key = 0, least = sums.all_m, most = sums.all_m;                // bounds of the mass that top_p is a share of
@@ -347,7 +406,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                     fits = among(1, digit, false, need);
                     if (fits) { key = shared_key; least = most = f.mass_before + shared_mass; }
                 }
-            } else if (k == V) {
+            } else if (by_mass) {
                 double sum = 0.0;
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) sum += wave_others[w];
@@ -381,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                     const uint64_t m = kept(i);
                     if (m) atomicAdd((unsigned long long*)&run_mass[cand_index[i] >> shift], (unsigned long long)m);
                 }
-                const Sums runs = scan(nullptr, run_mass);
+                const Sums runs = scan(no, yes, nullptr, run_mass);
                 const uint64_t need = mass_passed(runs.all_m) + 1;
                 const Found f = find(runs, true, need);
                 for (int i = tid; i < n; i += kThreads)
@@ -408,13 +467,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     };
     auto histogram = [&] {
         clear();
-        row.each(tid, [&](int, float x) { x = cleaned(x); put(scale.bin(x), x); });
-        return scan(count, mass);
+        row.template each<2>(tid, [&](int, float x) { x = cleaned(x); put(scale.bin(x), x); });
+        return scan(yes, yes, count, mass);
     };
     // as resolve, for a digit of the whole row; the histogram is not there any more afterwards if the list has no room
     auto among_row = [&](int which, const Found& in, bool by_mass, uint64_t need) {
         if (in.count <= (uint32_t)kList) {
-            row.each(tid, [&](int i, float x) { x = cleaned(x); if (scale.bin(x) == in.digit) list(which, key_of(x, i), scale.mass(x)); });
+            row.template each<2>(tid, [&](int i, float x) { x = cleaned(x); if (scale.bin(x) == in.digit) list(which, key_of(x, i), scale.mass(x)); });
             resolve(which, by_mass, need);
             return;
         }
@@ -429,7 +488,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 const uint64_t key = key_of(x, i);
                 if (scale.bin(x) == in.digit && (level == 0 || key >> (shift + width) == above)) put(ones - ((uint32_t)(key >> shift) & ones), x);
             });
-            const Found f = find(scan(count, mass), by_mass, need);
+            const Found f = find(scan(yes, yes, count, mass), by_mass, need);
             above = above << width | (ones - f.digit);
             need -= by_mass ? f.mass_before : f.count_before;
             up_to += f.mass_before + (level == 4 ? f.mass : 0);
@@ -465,9 +524,11 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     float low = fmaxf(min_p > 0.0f ? logf(min_p) - 0.001f : -30.0f, -30.0f);
     if (last_kept > -INFINITY && last_kept < INFINITY) low = fmaxf(low, (last_kept - top) * scale.per_t);
     const bool usual = scale.usual();
+    const bool uncut = usual && last_kept == -INFINITY && !(min_p > 0.0f);
     auto amount = [&](int i, float x) -> double {
         const float w = usual ? expf((x - top) * scale.per_t) : scale.weight(cleaned(x));
         const float m = fmaxf(floorf(w * kMassOne), 0.0f);
+        if (uncut) return (double)m;
         return (x > last_kept || (x == last_kept && i <= last_index)) && !(w < min_p) ? (double)m : 0.0;
     };
     auto ends = [&](int s) -> double {                 // head (run 0) and tail (the last): an entry a lane
