@@ -487,6 +487,63 @@ def test_sample_strides_offsets_and_a_flat_row():
                     assert abs(int(j) - int(at)) <= 4 and abs(int(got[r]) - int(index[r][at])) <= 64
 
 
+def _both_ways(logits, uniform, k, p, m, T):
+    """The same rows, once as they are and once with a limit on the count that only leaves out an entry without mass: a limit beyond
+    1024 of a large vocabulary sends a row through every step of the long way."""
+    n, V = logits.shape
+    a = _sample(logits, uniform, temperature=T, top_k=k, top_p=p, min_p=m)
+    b = _sample(logits, uniform, temperature=T, top_k=[x if x else V - 1 for x in k], top_p=p, min_p=m)
+    assert np.array_equal(a, b), [(r, k[r], p[r], m[r], T[r], a[r], b[r]) for r in np.flatnonzero(a != b)][:5]
+    return a
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [6000, 50021, 131072, 300001])
+def test_sample_by_every_way_gives_the_same(dt, V):
+    print("sample ways", dt, V, flush=True)
+    rng = np.random.default_rng(V + 1)
+    n = 40
+    fall = rng.uniform(0.0, 3.0, (n, 1))                               # from flat rows to steep ones
+    x = 12.0 - fall * np.log1p(np.stack([rng.permutation(V) for _ in range(n)])) + 0.3 * rng.standard_normal((n, V))
+    x[rng.random((n, V)) < 0.002] = np.nan
+    x[5] = np.round(x[5])                                              # many equal ones
+    x[6] = np.sort(x[6])                                               # the largest side by side
+    x[7, : V // 2] = -60.0
+    x[:, V // 3] = -np.inf
+    logits = torch.from_numpy(x).to(DT[dt]).cuda()
+    for rounds in range(3):
+        p = [float(np.float32(y)) for y in rng.choice([1.0, 0.3, 0.7, 0.9, 0.95, 0.99, 0.9999], n)]
+        m = [float(np.float32(y)) for y in rng.choice([0.0, 0.0, 0.02, 0.3], n)]
+        T = [float(np.float32(y)) for y in rng.choice([1.0, 0.3, 0.7, 1.5, 20.0], n)]
+        u = list(rng.random(n))
+        got = _both_ways(logits, u, [0] * n, p, m, T)
+        assert got.min() >= 0 and not np.any(np.isnan(x[np.arange(n), got]))
+        # and where the kept entries end exactly at an entry, as nearly as 32 bits of p can say
+        q = []
+        for r in range(n):
+            w, y = oracle.weights(_f64(logits[r]), T[r])
+            run = np.cumsum(np.sort(w)[::-1])
+            q.append(float(np.float32(run[min(int(rng.integers(0, 400)), V - 1)] / run[-1])))
+        _both_ways(logits, [0.999999] * n, [0] * n, q, [0.0] * n, T)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_sample_counts_beyond_a_thousand_and_equal_entries_at_the_end(dt):
+    print("sample counts", dt, flush=True)
+    rng = np.random.default_rng(9)
+    V, n = 70001, 12
+    x = 8.0 - 1.1 * np.log1p(np.stack([rng.permutation(V) for _ in range(n)]))
+    x[:, 100:30000] = 2.0                                              # a third of the entries are equal
+    logits = torch.from_numpy(x).to(DT[dt]).cuda()
+    x = _f64(logits)
+    K = [1, 2, 50, 1000, 1024, 1025, 3000, 20000, 40000, 70000, 70001, 0]
+    for u in (0.0, 0.9999999):
+        got = _sample(logits, [u] * n, temperature=[50.0] * n, top_k=K)
+        for r in range(n):                              # nearly equal weights: the first and the last of the kept indices
+            index, _ = oracle.kept(x[r], 50.0, K[r])
+            assert got[r] == (index[0] if u == 0.0 else index[-1]), (r, K[r])
+
+
 # ---------------------------------------------------------------- graphs
 
 def test_a_captured_step_replays():
