@@ -97,18 +97,18 @@ template <typename T> struct Row {
     // every piece once, by(number, piece), and the entries before and behind them, one(index, value)
     template <int kAtOnce, typename P, typename F> __device__ __forceinline__ void visit(int tid, P by, F one) const
     {
-        int v = tid;
-        for (; v + (kAtOnce - 1) * kThreads < pieces; v += kAtOnce * kThreads) {
+        for (int v = tid; v < pieces; v += kAtOnce * kThreads) {
             uint4 b[kAtOnce];
 #pragma unroll
-            for (int q = 0; q < kAtOnce; ++q) b[q] = bits(v + q * kThreads);
+            for (int q = 0; q < kAtOnce; ++q) b[q] = bits(min(v + q * kThreads, pieces - 1));
 #pragma unroll
-            for (int q = 0; q < kAtOnce; ++q) by(v + q * kThreads, unpacked(b[q]));
+            for (int q = 0; q < kAtOnce; ++q)
+                if (v + q * kThreads < pieces) by(v + q * kThreads, unpacked(b[q]));
         }
-        if constexpr (kAtOnce > 1)
-            for (; v < pieces; v += kThreads) by(v, piece(v));
-        if (tid < head) one(tid, at(tid));
-        if (tid < tail) one(n - tail + tid, at(n - tail + tid));
+        if (tid < head + tail) {
+            const int i = tid < head ? tid : n - tail - head + tid;
+            one(i, at(i));
+        }
     }
     // every entry once: f(index, value)
     template <int kAtOnce = 1, typename F> __device__ __forceinline__ void each(int tid, F f) const
@@ -134,18 +134,33 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     __shared__ uint32_t count[kBins], top_count[kBins];        // histograms: of the entries, of the threads' largest logits
     __shared__ uint64_t mass[kBins];
     __shared__ uint64_t run_mass[kMostRuns];                   // masses of runs of the vocabulary
-    __shared__ float cand_value[kCandidates];
-    __shared__ uint32_t cand_index[kCandidates];
+    __shared__ uint64_t many[kCandidates];                     // the entries that can be kept, or the keys of a digit's
+    float* const cand_value = reinterpret_cast<float*>(many);
+    uint32_t* const cand_index = reinterpret_cast<uint32_t*>(many) + kCandidates;
     __shared__ uint64_t list_key[kList], list_mass[kList];
     __shared__ uint32_t hot[kCandidates];                      // pieces that hold entries which can be kept
-    __shared__ uint64_t wave_mass[kWaves];
+    __shared__ uint64_t wave_mass[kWaves], wave_low[kWaves];
     __shared__ uint32_t wave_count[kWaves];
     __shared__ float wave_top[kWaves];
     __shared__ double wave_others[kWaves];
     __shared__ Found found;
     __shared__ uint64_t shared_key, shared_mass;
-    __shared__ uint32_t shared_index, filled[8];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.n_vocab;
+    __shared__ uint32_t shared_index, filled[10];
+    const int V = a.n_vocab;
+    int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // (from here on what hangs on them is worked out anew, not kept in registers from one part of the kernel to the next)
+    auto of_lane = [&](auto x, int from) {
+        if constexpr (sizeof(x) == 4) {
+            return __builtin_bit_cast(decltype(x), __builtin_amdgcn_ds_bpermute(4 * from, __builtin_bit_cast(int, x)));
+        } else {
+            const uint64_t b = __builtin_bit_cast(uint64_t, x);
+            const uint32_t low = __builtin_amdgcn_ds_bpermute(4 * from, (int)b), high = __builtin_amdgcn_ds_bpermute(4 * from, (int)(b >> 32));
+            return __builtin_bit_cast(decltype(x), (uint64_t)high << 32 | low);
+        }
+    };
+    auto by_xor = [&](auto x, int mask) { return of_lane(x, lane ^ mask); };
+    auto from_below = [&](auto x, int by) { return of_lane(x, lane - by); };     // (for lanes from `by` on)
+    auto afresh = [&] { asm volatile("" : "+v"(tid)); lane = tid & 63; wave = tid >> 6; };
     const int64_t r = blockIdx.x;
     const Row<T> row(static_cast<const typename T::Bits*>(a.logits) + r * a.row_stride, V);
 
@@ -184,13 +199,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         row.template each<4>(tid, [&](int, float x) { top = fmaxf(top, x); });     // (fmaxf passes NaN over)
     }
     for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; top_count[x] = 0; run_mass[x] = 0; }
-    if (tid < 8) filled[tid] = 0;
+    if (tid < 10) filled[tid] = 0;
     const float my_top = top;
-    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, by_xor(top, x));
     if (lane == 0) wave_top[wave] = top;
     if (by_mass) {                                     // relative to the wavefront's largest
         double sum = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
-        for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+        for (int x = 1; x < 64; x *= 2) sum += by_xor(sum, x);
         if (lane == 0) wave_others[wave] = sum;
     }
     if (tid == 0) shared_index = 0xffffffffu;
@@ -211,6 +226,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         if (tid == 0) a.token[r] = (int32_t)shared_index;
         return;
     }
+    afresh();
     const Scale scale = {top, per_t};
     auto mass_passed = [&](uint64_t total) -> uint64_t {                            // floor(u total), below total
         if (!(u > 0.0f)) return 0;
@@ -224,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     };
     // the sum over the workgroup; ends behind a barrier
     auto add_up = [&](uint64_t x) {
-        for (int y = 1; y < 64; y *= 2) x += __shfl_xor(x, y);
+        for (int y = 1; y < 64; y *= 2) x += by_xor(x, y);
         __syncthreads();
         if (lane == 0) wave_mass[wave] = x;
         __syncthreads();
@@ -247,8 +263,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         uint64_t m = b.m0 + b.m1;
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) {
-            if (counts) { const uint32_t cc = __shfl_up(c, x); if (lane >= x) c += cc; }
-            if (masses) { const uint64_t mm = __shfl_up(m, x); if (lane >= x) m += mm; }
+            if (counts) { const uint32_t cc = from_below(c, x); if (lane >= x) c += cc; }
+            if (masses) { const uint64_t mm = from_below(m, x); if (lane >= x) m += mm; }
         }
         if (lane == 63) { wave_count[wave] = c; wave_mass[wave] = m; }
         __syncthreads();
@@ -315,6 +331,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     if (scale.usual() && (k < V || p < 1.0f || min_p > 0.0f) && (k == V || k <= kThreads || V <= kCandidates)) {
         // digits up to `last` can be kept
         uint32_t last = kNoMass - 1;
+        bool fits = true;
         if (k == V && !by_mass) {
             last = min(last, (uint32_t)fminf(-64.0f * logf(min_p) + 1.0f, (float)last));       // (cut by weight alone)
         } else if (V > kCandidates) {
@@ -334,154 +351,157 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 __syncthreads();
                 const Sums held = scan_of(no, yes, 0, 0, (uint64_t)(fmaxf(n1 - n0, 0.0f) * w0 * 0x1p30f), (uint64_t)(fmaxf(n2 - n1, 0.0f) * w1 * 0x1p30f));
                 const uint64_t want = (uint64_t)fmin((double)p * all * 1.05 * 0x1p30, 0x1p62);
-                rank = kRank;                          // (as many as there is room for, where they seem to hold too little)
                 if (want <= held.all_m) {
                     last = min(last, find(held, true, want).digit + 4);
                     rank = V;
+                } else {
+                    // As many as there is room for, and at once the long way if those will hold too little: if what is missing can be
+                    // entries below every thread's largest (else a thread has several of the largest: seldom, but one row is enough).
+                    const float each = expf(-(float)find(tops, false, tops.all_c).digit / 64.0f) * 0x1p30f;
+                    rank = kRank;
+                    fits = (double)held.all_m >= 0.8 * (double)want || (double)(want - held.all_m) > (double)V * each;
                 }
             }
             if (rank <= tops.all_c) last = min(last, find(tops, false, rank).digit);
         }
-        // Entries whose digit can be kept go to LDS.  A thread reads its share again if its largest is among them; the mass of the others
-        // is known roughly, which seldom leaves open where the kept ones end.
-        const float edge = (float)(last + 1), low = top - (edge / (64.0f * scale.per_t) * 1.0001f + fabsf(top) * 1e-6f);
-        others = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
-        if (my_top >= low) others = 0.0;
-        from = top;
-        auto take = [&](int i, float x) {
-            if ((top - x) * scale.per_t * 64.0f < edge) {                            // (false for NaN)
-                const uint32_t to = atomicAdd(&filled[0], 1u);
-                if (to < kCandidates) { cand_value[to] = x + 0.0f; cand_index[to] = (uint32_t)i; }
-            } else if (by_mass) {
-                others += (double)roughly(x);
-            }
-        };
-        // (a piece with such an entry is looked into afterwards: nearly every wavefront meets some, few lanes do)
-        if (my_top >= low) row.template visit<8>(tid, [&](int v, const typename Row<T>::Piece& y) {
-            if (Row<T>::top_of(y) >= low) {
-                const uint32_t to = atomicAdd(&filled[7], 1u);
-                if (to < kCandidates) hot[to] = (uint32_t)v;
-            } else if (by_mass) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
-                others += (double)sum;
-            }
-        }, take);
-        __syncthreads();
-        const int pieces = min((int)filled[7], kCandidates);
-        for (int i = tid; i < pieces; i += kThreads) {
-            const int v = (int)hot[i];
-            const typename Row<T>::Piece y = row.piece(v);
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) take(row.head + v * kEach + e, y.x[e]);
-        }
-        if (by_mass) {
-            for (int y = 1; y < 64; y *= 2) others += __shfl_xor(others, y);
-            if (lane == 0) wave_others[wave] = others;
-        }
-        __syncthreads();
-        const int n = (int)filled[0];
-        bool fits = n <= kCandidates && (int)filled[7] <= kCandidates;
         if (fits) {
-            auto digit_of = [&](int i) { return scale.bin(cand_value[i]); };
-            auto key_at = [&](int i) { return key_of(cand_value[i], cand_index[i]); };
-            auto mass_at = [&](int i) { return scale.mass(cand_value[i]); };
-            auto among = [&](int which, uint32_t digit, bool by_mass, uint64_t need) {
-                for (int i = tid; i < n; i += kThreads)
-                    if (digit_of(i) == digit) list(which, key_at(i), mass_at(i));
-                return resolve(which, by_mass, need);
+            // Entries whose digit can be kept go to LDS.  A thread reads its share again if its largest is among them; the mass of the others
+            // is known roughly, which seldom leaves open where the kept ones end.
+            const float edge = (float)(last + 1), low = top - (edge / (64.0f * scale.per_t) * 1.0001f + fabsf(top) * 1e-6f);
+            others = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
+            if (my_top >= low) others = 0.0;
+            from = top;
+            auto take = [&](int i, float x) {
+                if ((top - x) * scale.per_t * 64.0f < edge) {                            // (false for NaN)
+                    const uint32_t to = atomicAdd(&filled[0], 1u);
+                    if (to < kCandidates) { cand_value[to] = x + 0.0f; cand_index[to] = (uint32_t)i; }
+                } else if (by_mass) {
+                    others += (double)roughly(x);
+                }
             };
-            for (int i = tid; i < n; i += kThreads) put(digit_of(i), cand_value[i]);
-            const Sums sums = scan(yes, yes, count, mass);
-            // kept: digits before `digit`, and of it the keys from `key` on
-            uint32_t digit = kBins;
-            uint64_t key = 0, least = sums.all_m, most = sums.all_m;                // bounds of the mass that top_p is a share of
-            if (k < n) {
-                const Found f = find(sums, false, (uint64_t)k);
-                const uint64_t need = (uint64_t)k - f.count_before;
-                digit = f.digit;
-                least = most = f.mass_before + f.mass;
-                if (need < f.count) {
-                    fits = among(1, digit, false, need);
-                    if (fits) { key = shared_key; least = most = f.mass_before + shared_mass; }
-                }
-            } else if (by_mass) {
-                double sum = 0.0;
+            // (a piece with such an entry is looked into afterwards: nearly every wavefront meets some, few lanes do)
+            if (my_top >= low) row.template visit<8>(tid, [&](int v, const typename Row<T>::Piece& y) {
+                if (Row<T>::top_of(y) >= low) {
+                    const uint32_t to = atomicAdd(&filled[7], 1u);
+                    if (to < kCandidates) hot[to] = (uint32_t)v;
+                } else if (by_mass) {
+                    float sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) sum += wave_others[w];
-                sum *= (double)kMassOne;
-                const double off = sum * 0x1p-16 + (double)V;                       // (V: what the floors take off)
-                least += sum > off ? (uint64_t)(sum - off) : 0;
-                most += (uint64_t)(sum + off);
-            }
-            for (int pass = 0; fits && p < 1.0f; ++pass) {
-                const uint64_t need = mass_needed(least);
-                fits = need <= sums.all_m;                                          // (else the candidates hold too little)
-                if (!fits) break;
-                const Found f = find(sums, true, need);
-                fits = among(2 + pass, f.digit, true, need - f.mass_before);
-                if (!fits) break;
-                digit = f.digit;
-                key = shared_key;
-                if (mass_needed(most) <= f.mass_before + shared_mass) break;
-                least = most = add_up_row();           // (it matters: every mass of the row)
-            }
-            if (fits) {
-                auto kept = [&](int i) -> uint64_t {
-                    const uint32_t d = digit_of(i);
-                    if (d > digit || (d == digit && key_at(i) < key) || scale.weight(cand_value[i]) < min_p) return 0;
-                    return mass_at(i);
-                };
-                // the same search along the index: 2048 runs of the vocabulary
-                int shift = 0;
-                while (((V - 1) >> shift) >= kBins) ++shift;
-                for (int i = tid; i < n; i += kThreads) {
-                    const uint64_t m = kept(i);
-                    if (m) atomicAdd((unsigned long long*)&run_mass[cand_index[i] >> shift], (unsigned long long)m);
+                    for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
+                    others += (double)sum;
                 }
-                const Sums runs = scan(no, yes, nullptr, run_mass);
-                const uint64_t need = mass_passed(runs.all_m) + 1;
-                const Found f = find(runs, true, need);
-                for (int i = tid; i < n; i += kThreads)
-                    if (cand_index[i] >> shift == f.digit) list(4, (uint64_t)~cand_index[i], kept(i));
-                resolve(4, true, need - f.mass_before);                             // (a run has at most 256 entries)
-                if (tid == 0) a.token[r] = (int32_t)~(uint32_t)shared_key;
-                return;
+            }, take);
+            __syncthreads();
+            const int pieces = min((int)filled[7], kCandidates);
+            for (int i = tid; i < pieces; i += kThreads) {
+                const int v = (int)hot[i];
+                const typename Row<T>::Piece y = row.piece(v);
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) take(row.head + v * kEach + e, y.x[e]);
+            }
+            if (by_mass) {
+                for (int y = 1; y < 64; y *= 2) others += by_xor(others, y);
+                if (lane == 0) wave_others[wave] = others;
+            }
+            __syncthreads();
+            const int n = (int)filled[0];
+            fits = n <= kCandidates && (int)filled[7] <= kCandidates;
+            if (fits) {
+                auto digit_of = [&](int i) { return scale.bin(cand_value[i]); };
+                auto key_at = [&](int i) { return key_of(cand_value[i], cand_index[i]); };
+                auto mass_at = [&](int i) { return scale.mass(cand_value[i]); };
+                auto among = [&](int which, uint32_t digit, bool by_mass, uint64_t need) {
+                    for (int i = tid; i < n; i += kThreads)
+                        if (digit_of(i) == digit) list(which, key_at(i), mass_at(i));
+                    return resolve(which, by_mass, need);
+                };
+                for (int i = tid; i < n; i += kThreads) put(digit_of(i), cand_value[i]);
+                const Sums sums = scan(yes, yes, count, mass);
+                // kept: digits before `digit`, and of it the keys from `key` on
+                uint32_t digit = kBins;
+                uint64_t key = 0, least = sums.all_m, most = sums.all_m;                // bounds of the mass that top_p is a share of
+                if (k < n) {
+                    const Found f = find(sums, false, (uint64_t)k);
+                    const uint64_t need = (uint64_t)k - f.count_before;
+                    digit = f.digit;
+                    least = most = f.mass_before + f.mass;
+                    if (need < f.count) {
+                        fits = among(1, digit, false, need);
+                        if (fits) { key = shared_key; least = most = f.mass_before + shared_mass; }
+                    }
+                } else if (by_mass) {
+                    double sum = 0.0;
+#pragma unroll
+                    for (int w = 0; w < kWaves; ++w) sum += wave_others[w];
+                    sum *= (double)kMassOne;
+                    const double off = sum * 0x1p-16 + (double)V;                       // (V: what the floors take off)
+                    least += sum > off ? (uint64_t)(sum - off) : 0;
+                    most += (uint64_t)(sum + off);
+                }
+                for (int pass = 0; fits && p < 1.0f; ++pass) {
+                    const uint64_t need = mass_needed(least);
+                    fits = need <= sums.all_m;                                          // (else the candidates hold too little)
+                    if (!fits) break;
+                    const Found f = find(sums, true, need);
+                    fits = among(2 + pass, f.digit, true, need - f.mass_before);
+                    if (!fits) break;
+                    digit = f.digit;
+                    key = shared_key;
+                    if (mass_needed(most) <= f.mass_before + shared_mass) break;
+                    least = most = add_up_row();           // (it matters: every mass of the row)
+                }
+                if (fits) {
+                    auto kept = [&](int i) -> uint64_t {
+                        const uint32_t d = digit_of(i);
+                        if (d > digit || (d == digit && key_at(i) < key) || scale.weight(cand_value[i]) < min_p) return 0;
+                        return mass_at(i);
+                    };
+                    // the same search along the index: 2048 runs of the vocabulary
+                    int shift = 0;
+                    while (((V - 1) >> shift) >= kBins) ++shift;
+                    for (int i = tid; i < n; i += kThreads) {
+                        const uint64_t m = kept(i);
+                        if (m) atomicAdd((unsigned long long*)&run_mass[cand_index[i] >> shift], (unsigned long long)m);
+                    }
+                    const Sums runs = scan(no, yes, nullptr, run_mass);
+                    const uint64_t need = mass_passed(runs.all_m) + 1;
+                    const Found f = find(runs, true, need);
+                    for (int i = tid; i < n; i += kThreads)
+                        if (cand_index[i] >> shift == f.digit) list(4, (uint64_t)~cand_index[i], kept(i));
+                    resolve(4, true, need - f.mass_before);                             // (a run has at most 256 entries)
+                    if (tid == 0) a.token[r] = (int32_t)~(uint32_t)shared_key;
+                    return;
+                }
             }
         }
     }
 
+    afresh();
     // Through the row for every step: a histogram of all of it, the digits in which the kept entries end looked into.
     float last_kept = -INFINITY;                       // of the kept entries the last one's logit and index
     int last_index = V;
-    auto ends_at = [&](uint64_t key) {
-        const uint32_t b = (uint32_t)(key >> 19);
-        last_kept = __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu));
-        last_index = kMostVocab - 1 - (int)(key & (kMostVocab - 1));
-    };
     auto clear = [&] {
         __syncthreads();
         for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; }
         __syncthreads();
     };
-    auto histogram = [&] {
+    auto histogram = [&](bool counts) {
         clear();
-        row.template each<2>(tid, [&](int, float x) { x = cleaned(x); put(scale.bin(x), x); });
-        return scan(yes, yes, count, mass);
+        row.template each<2>(tid, [&](int, float x) {
+            x = cleaned(x);
+            const uint32_t digit = scale.bin(x);
+            if (counts) atomicAdd(&count[digit], 1u);
+            if (digit < kNoMass || !scale.usual()) atomicAdd((unsigned long long*)&mass[digit], (unsigned long long)scale.mass(x));
+        });
     };
-    // as resolve, for a digit of the whole row; the histogram is not there any more afterwards if the list has no room
-    auto among_row = [&](int which, const Found& in, bool by_mass, uint64_t need) {
-        if (in.count <= (uint32_t)kList) {
-            row.template each<2>(tid, [&](int i, float x) { x = cleaned(x); if (scale.bin(x) == in.digit) list(which, key_of(x, i), scale.mass(x)); });
-            resolve(which, by_mass, need);
-            return;
-        }
-        uint64_t above = 0, up_to = 0;                 // 51 bits of key in five digits
+    // as resolve, for a digit of the whole row: 51 bits of key in five digits
+    auto descend = [&](const Found& in, bool by_mass, uint64_t need) {
+        uint64_t above = 0, up_to = 0;
         const int shifts[5] = {40, 29, 19, 9, 0}, widths[5] = {11, 11, 10, 10, 9};
         for (int level = 0; level < 5; ++level) {
             const int shift = shifts[level], width = widths[level];
             const uint32_t ones = (1u << width) - 1;
+            afresh();
             clear();
             row.each(tid, [&](int i, float x) {
                 x = cleaned(x);
@@ -496,34 +516,170 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         if (tid == 0) { shared_key = above; shared_mass = up_to; }
         __syncthreads();
     };
-    if (k < V || p < 1.0f) {
-        Sums sums = histogram();
-        Found f = find(sums, false, (uint64_t)k);
-        uint64_t total = f.mass_before + f.mass;
-        const uint64_t of_k = (uint64_t)k - f.count_before;
-        if (k < V) {
-            const bool gone = f.count > (uint32_t)kList;
-            among_row(5, f, false, of_k);
-            ends_at(shared_key);
-            total = f.mass_before + shared_mass;
-            if (gone && p < 1.0f) sums = histogram();
-        }
-        if (p < 1.0f) {
-            const uint64_t need = mass_needed(total);
-            f = find(sums, true, need);
-            among_row(6, f, true, need - f.mass_before);
-            ends_at(shared_key);
-        }
-    }
 
     // Masses of runs of 512 pieces, eight a lane (head and tail of the row are runs of their own), and the run in which the token is
-    // again.
-    constexpr int kLines = 8;
+    // again.  (A thread's sum of whole numbers, 520 of 2^43 at most, is exact in a double.)
+    constexpr int kLines = 8, kBatch = 16 / kEach;
     const int runs = (row.pieces + 64 * kLines - 1) / (64 * kLines), all = runs + 2;
+    const bool usual = scale.usual();
+    auto sum_runs = [&](auto end_of, auto piece_of) {
+        afresh();
+        __syncthreads();
+        for (int s = wave; s < all; s += kWaves) {
+            uint64_t x = 0;                            // (512 pieces can pass 2^53)
+            if (s == 0 || s == all - 1) {
+                x = (uint64_t)end_of(s);
+            } else {
+                const int v0 = (s - 1) * 64 * kLines + lane;
+                double y = 0.0;
+#pragma unroll 1
+                for (int q0 = 0; q0 < kLines; q0 += kBatch) {
+                    uint4 b[kBatch];
+#pragma unroll
+                    for (int q = 0; q < kBatch; ++q) b[q] = row.bits(min(v0 + (q0 + q) * 64, row.pieces - 1));
+#pragma unroll
+                    for (int q = 0; q < kBatch; ++q)
+                        if (v0 + (q0 + q) * 64 < row.pieces) y += piece_of(v0 + (q0 + q) * 64, Row<T>::unpacked(b[q]));
+                }
+                x = (uint64_t)y;
+            }
+            for (int y = 1; y < 64; y *= 2) x += by_xor(x, y);
+            if (lane == 0) run_mass[s] = x;
+        }
+        __syncthreads();
+    };
+    bool summed = false;                               // (the runs)
+    auto value_of = [](uint64_t key) {
+        const uint32_t b = (uint32_t)(key >> 19);
+        return __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xffffffffu));
+    };
+    // As resolve, for `here` keys in `many`: digits of 11 bits of what is left of their range, until there is one (keys are unlike).
+    auto resolve_many = [&](int here, uint32_t* counts, uint64_t* masses, bool by_mass, uint64_t need) {
+        afresh();
+        uint64_t low = ~(uint64_t)0, high = 0, before = 0;
+        for (int i = tid; i < here; i += kThreads) { low = min(low, many[i]); high = max(high, many[i]); }
+        for (int x = 1; x < 64; x *= 2) { low = min(low, (uint64_t)by_xor(low, x)); high = max(high, (uint64_t)by_xor(high, x)); }
+        if (lane == 0) { wave_low[wave] = low; wave_mass[wave] = high; }
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) { low = min(low, wave_low[w]); high = max(high, wave_mass[w]); }
+        for (;;) {
+            const int shift = max(53 - __clzll(high - low | 1), 0);
+            __syncthreads();
+            for (int x = tid; x < kBins; x += kThreads) { counts[x] = 0; masses[x] = 0; }
+            __syncthreads();
+            for (int i = tid; i < here; i += kThreads) {
+                const uint64_t key = many[i];
+                if (key > high || key < low) continue;
+                const uint32_t digit = (uint32_t)((high - key) >> shift);
+                atomicAdd(&counts[digit], 1u);
+                atomicAdd((unsigned long long*)&masses[digit], (unsigned long long)scale.mass(value_of(key)));
+            }
+            const Found f = find(scan(yes, yes, counts, masses), by_mass, need);
+            high -= (uint64_t)f.digit << shift;
+            low = max(low, high - (((uint64_t)1 << shift) - 1));
+            before += f.mass_before;
+            if (f.count == 1) {
+                for (int i = tid; i < here; i += kThreads)
+                    if (many[i] <= high && many[i] >= low) { shared_key = many[i]; shared_mass = before + f.mass; }
+                __syncthreads();
+                return;
+            }
+            need -= by_mass ? f.mass_before : f.count_before;
+        }
+    };
+    // The cut by count, then the one by mass.  The last one's digit is gathered in the pass that adds up the runs.
+    uint64_t total = 0;
+    bool gone = false;                                 // (the histogram)
+    const int first = k < V ? 0 : 1, last_cut = p < 1.0f ? 1 : 0;
+#pragma unroll 1
+    for (int cut = first; cut <= last_cut; ++cut) {
+        const bool by_mass = cut == 1, is_last = cut == last_cut;
+        afresh();
+        uint32_t &pieces = filled[5 + cut], &keys = filled[8 + cut];
+        if (cut == first || gone) histogram(!by_mass);
+        const Sums sums = scan(yes, yes, count, mass);
+        if (cut == first) total = sums.all_m;
+        uint64_t need = by_mass ? mass_needed(total) : (uint64_t)k;
+        const Found in = find(sums, by_mass, need);
+        need -= by_mass ? in.mass_before : in.count_before;
+        const float from_digit = (float)in.digit, behind = in.digit < kBins - 1 ? (float)(in.digit + 1) : NAN;
+        const float low = top - (behind / (64.0f * per_t) * 1.0001f + fabsf(top) * 1e-6f);
+        auto take = [&](int i, float x) {
+            x = cleaned(x);
+            if (scale.bin(x) != in.digit) return;
+            const uint32_t to = atomicAdd(&keys, 1u);
+            if (to < kCandidates) many[to] = key_of(x, i);
+        };
+        // the mass of a piece's entries that are kept for certain; pieces with entries of the digit are looked into afterwards
+        auto look = [&](int v, const typename Row<T>::Piece& y) {
+            double sum = 0.0;
+            bool any = false;
+            if (!usual) {
+#pragma unroll 1
+                for (int e = 0; e < kEach; ++e) {
+                    const float x = cleaned(row.at(row.head + v * kEach + e));
+                    any |= scale.bin(x) == in.digit;
+                    if (scale.bin(x) < in.digit && !(scale.weight(x) < min_p)) sum += (double)scale.whole_mass(x);
+                }
+            } else if (!(Row<T>::top_of(y) < low)) {
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const float d = (top - y.x[e]) * per_t * 64.0f, w = expf((y.x[e] - top) * per_t), m = fmaxf(floorf(w * kMassOne), 0.0f);
+                    any |= !(d < from_digit) && !(d >= behind);
+                    if (d < from_digit && !(w < min_p)) sum += (double)m;
+                }
+            }
+            if (any) {
+                const uint32_t to = atomicAdd(&pieces, 1u);
+                if (to < kCandidates) hot[to] = (uint32_t)v;
+            }
+            return sum;
+        };
+        if (!is_last) {
+            row.template visit<2>(tid, look, take);
+        } else {
+            sum_runs([&](int s) {
+                const int n = s ? row.tail : row.head, i = s ? V - row.tail + lane : lane;
+                if (lane >= n) return 0.0;
+                const float x = cleaned(row.at(i));
+                take(i, x);
+                return scale.bin(x) < in.digit && !(scale.weight(x) < min_p) ? (double)scale.whole_mass(x) : 0.0;
+            }, look);
+        }
+        __syncthreads();
+        afresh();
+        for (int j = tid; j < min((int)pieces, kCandidates) * kEach; j += kThreads) {
+            const int i = row.head + (int)hot[j / kEach] * kEach + j % kEach;
+            take(i, row.at(i));
+        }
+        __syncthreads();
+        if ((int)pieces > kCandidates || (int)keys > kCandidates) {
+            descend(in, by_mass, need);
+            gone = true;
+        } else {
+            const int here = (int)keys;
+            // (the histogram is still needed behind the cut by count, the runs' masses behind the last)
+            resolve_many(here, is_last ? count : top_count, is_last ? mass : run_mass, by_mass, need);
+            if (is_last) {
+                for (int j = tid; j < here; j += kThreads) {
+                    const uint64_t key = many[j];
+                    const int i = kMostVocab - 1 - (int)(key & (kMostVocab - 1)), v = i - row.head;
+                    const float x = value_of(key);
+                    if (key >= shared_key && !(scale.weight(x) < min_p))
+                        atomicAdd((unsigned long long*)&run_mass[v < 0 ? 0 : v >= row.pieces * kEach ? all - 1 : 1 + v / (kEach * 64 * kLines)],
+                                  (unsigned long long)scale.mass(x));
+                }
+                summed = true;
+                __syncthreads();
+            }
+        }
+        last_kept = value_of(shared_key);
+        last_index = kMostVocab - 1 - (int)(shared_key & (kMostVocab - 1));
+        total = in.mass_before + shared_mass;
+    }
     // entries below this have no mass, or less weight than min_p (a little room for the roundings), or are behind the end
     float low = fmaxf(min_p > 0.0f ? logf(min_p) - 0.001f : -30.0f, -30.0f);
     if (last_kept > -INFINITY && last_kept < INFINITY) low = fmaxf(low, (last_kept - top) * scale.per_t);
-    const bool usual = scale.usual();
     const bool uncut = usual && last_kept == -INFINITY && !(min_p > 0.0f);
     auto amount = [&](int i, float x) -> double {
         const float w = usual ? expf((x - top) * scale.per_t) : scale.weight(cleaned(x));
@@ -547,33 +703,16 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         return sum;
     };
     double m[kEach];
+    afresh();
+    if (!summed) sum_runs(ends, [&](int v, const typename Row<T>::Piece& y) { return in_piece(v, y, m); });
     uint64_t sum = 0;
-    __syncthreads();
-    for (int s = wave; s < all; s += kWaves) {
-        uint64_t x = 0;                                // (512 pieces can pass 2^53)
-        if (s == 0 || s == all - 1) {
-            x = (uint64_t)ends(s);
-        } else {
-            const int v0 = (s - 1) * 64 * kLines + lane;
-            uint4 b[kLines];
-#pragma unroll
-            for (int q = 0; q < kLines; ++q) b[q] = v0 + q * 64 < row.pieces ? row.bits(v0 + q * 64) : make_uint4(0, 0, 0, 0);
-            double y = 0.0;
-#pragma unroll
-            for (int q = 0; q < kLines; ++q)
-                if (v0 + q * 64 < row.pieces) y += in_piece(v0 + q * 64, Row<T>::unpacked(b[q]), m);
-            x = (uint64_t)y;
-        }
-        for (int y = 1; y < 64; y *= 2) x += __shfl_xor(x, y);
-        if (lane == 0) run_mass[s] = x;
-        sum += lane == 0 ? x : 0;
-    }
+    for (int s = tid; s < all; s += kThreads) sum += run_mass[s];
     const uint64_t need = mass_passed(add_up(sum)) + 1;
     if (wave) return;
     uint64_t before = 0;
     for (int s0 = 0; s0 < all; s0 += 64) {
         uint64_t x = s0 + lane < all ? run_mass[s0 + lane] : 0;
-        for (int y = 1; y < 64; y *= 2) { const uint64_t z = __shfl_up(x, y); if (lane >= y) x += z; }
+        for (int y = 1; y < 64; y *= 2) { const uint64_t z = from_below(x, y); if (lane >= y) x += z; }
         const uint64_t hit = __ballot(before + x >= need);
         if (!hit) {
             before += __shfl(x, 63);
@@ -588,7 +727,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             if (at_end) mine = (uint64_t)ends(s);
             else if (v < row.pieces) mine = (uint64_t)in_piece(v, row.piece(v), m);
             uint64_t z = mine;
-            for (int y = 1; y < 64; y *= 2) { const uint64_t w = __shfl_up(z, y); if (lane >= y) z += w; }
+            for (int y = 1; y < 64; y *= 2) { const uint64_t w = from_below(z, y); if (lane >= y) z += w; }
             const uint64_t here = __ballot(before + z >= need);
             if (!here) {
                 before += __shfl(z, 63);
