@@ -127,6 +127,36 @@ template <typename T> struct Row {
     }
 };
 
+// What lane 63 gets is the result over all of the wavefront, what lane i gets the one over the lanes up to it: rows of 16 lanes
+// first, then a row's last value goes to the rows behind it.  All 64 lanes have to be there.
+template <int kControl, int kRows, typename X> __device__ __forceinline__ X moved(X x, X none)
+{
+    static_assert(sizeof(X) == 4 || sizeof(X) == 8);
+    if constexpr (sizeof(X) == 4) {
+        return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x), kControl, kRows, 0xf, false));
+    } else {
+        const uint64_t n = __builtin_bit_cast(uint64_t, none), b = __builtin_bit_cast(uint64_t, x);
+        const uint32_t low = __builtin_amdgcn_update_dpp((int)n, (int)b, kControl, kRows, 0xf, false);
+        const uint32_t high = __builtin_amdgcn_update_dpp((int)(n >> 32), (int)(b >> 32), kControl, kRows, 0xf, false);
+        return __builtin_bit_cast(X, (uint64_t)high << 32 | low);
+    }
+}
+template <typename X, typename F> __device__ __forceinline__ X up_to(X x, X none, F f)
+{
+    x = f(x, moved<0x111, 0xf>(x, none));              // row_shr by 1, 2, 4, 8
+    x = f(x, moved<0x112, 0xf>(x, none));
+    x = f(x, moved<0x114, 0xf>(x, none));
+    x = f(x, moved<0x118, 0xf>(x, none));
+    x = f(x, moved<0x142, 0xa>(x, none));              // row_bcast 15, then 31
+    return f(x, moved<0x143, 0xc>(x, none));
+}
+template <typename X> __device__ __forceinline__ X sum_up_to(X x) { return up_to(x, X(0), [](X a, X b) { return a + b; }); }
+// (a value of lane `from`, the same for all of the wavefront)
+__device__ __forceinline__ uint64_t of_lane(uint64_t x, int from)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, from);
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 {
@@ -149,17 +179,6 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     const int V = a.n_vocab;
     int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // (from here on what hangs on them is worked out anew, not kept in registers from one part of the kernel to the next)
-    auto of_lane = [&](auto x, int from) {
-        if constexpr (sizeof(x) == 4) {
-            return __builtin_bit_cast(decltype(x), __builtin_amdgcn_ds_bpermute(4 * from, __builtin_bit_cast(int, x)));
-        } else {
-            const uint64_t b = __builtin_bit_cast(uint64_t, x);
-            const uint32_t low = __builtin_amdgcn_ds_bpermute(4 * from, (int)b), high = __builtin_amdgcn_ds_bpermute(4 * from, (int)(b >> 32));
-            return __builtin_bit_cast(decltype(x), (uint64_t)high << 32 | low);
-        }
-    };
-    auto by_xor = [&](auto x, int mask) { return of_lane(x, lane ^ mask); };
-    auto from_below = [&](auto x, int by) { return of_lane(x, lane - by); };     // (for lanes from `by` on)
     auto afresh = [&] { asm volatile("" : "+v"(tid)); lane = tid & 63; wave = tid >> 6; };
     const int64_t r = blockIdx.x;
     const Row<T> row(static_cast<const typename T::Bits*>(a.logits) + r * a.row_stride, V);
@@ -201,12 +220,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; top_count[x] = 0; run_mass[x] = 0; }
     if (tid < 10) filled[tid] = 0;
     const float my_top = top;
-    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, by_xor(top, x));
+    top = up_to(top, -INFINITY, [](float x, float y) { return fmaxf(x, y); });
+    top = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), 63));
     if (lane == 0) wave_top[wave] = top;
     if (by_mass) {                                     // relative to the wavefront's largest
         double sum = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
-        for (int x = 1; x < 64; x *= 2) sum += by_xor(sum, x);
-        if (lane == 0) wave_others[wave] = sum;
+        sum = sum_up_to(sum);
+        if (lane == 63) wave_others[wave] = sum;
     }
     if (tid == 0) shared_index = 0xffffffffu;
     __syncthreads();
@@ -240,9 +260,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     };
     // the sum over the workgroup; ends behind a barrier
     auto add_up = [&](uint64_t x) {
-        for (int y = 1; y < 64; y *= 2) x += by_xor(x, y);
+        x = sum_up_to(x);
         __syncthreads();
-        if (lane == 0) wave_mass[wave] = x;
+        if (lane == 63) wave_mass[wave] = x;
         __syncthreads();
         x = 0;
 #pragma unroll
@@ -259,13 +279,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     struct Sums { uint32_t c0, c1, before_c, all_c; uint64_t m0, m1, before_m, all_m; };
     auto scan_of = [&](auto counts, auto masses, uint32_t c0, uint32_t c1, uint64_t m0, uint64_t m1) {
         Sums b = {c0, c1, 0, 0, m0, m1, 0, 0};
-        uint32_t c = b.c0 + b.c1;
-        uint64_t m = b.m0 + b.m1;
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) {
-            if (counts) { const uint32_t cc = from_below(c, x); if (lane >= x) c += cc; }
-            if (masses) { const uint64_t mm = from_below(m, x); if (lane >= x) m += mm; }
-        }
+        const uint32_t c = counts ? sum_up_to(b.c0 + b.c1) : 0;
+        const uint64_t m = masses ? sum_up_to(b.m0 + b.m1) : 0;
         if (lane == 63) { wave_count[wave] = c; wave_mass[wave] = m; }
         __syncthreads();
         b.before_c = c - b.c0 - b.c1;
@@ -400,8 +415,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 for (int e = 0; e < kEach; ++e) take(row.head + v * kEach + e, y.x[e]);
             }
             if (by_mass) {
-                for (int y = 1; y < 64; y *= 2) others += by_xor(others, y);
-                if (lane == 0) wave_others[wave] = others;
+                others = sum_up_to(others);
+                if (lane == 63) wave_others[wave] = others;
             }
             __syncthreads();
             const int n = (int)filled[0];
@@ -543,8 +558,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 }
                 x = (uint64_t)y;
             }
-            for (int y = 1; y < 64; y *= 2) x += by_xor(x, y);
-            if (lane == 0) run_mass[s] = x;
+            x = sum_up_to(x);
+            if (lane == 63) run_mass[s] = x;
         }
         __syncthreads();
     };
@@ -558,8 +573,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         afresh();
         uint64_t low = ~(uint64_t)0, high = 0, before = 0;
         for (int i = tid; i < here; i += kThreads) { low = min(low, many[i]); high = max(high, many[i]); }
-        for (int x = 1; x < 64; x *= 2) { low = min(low, (uint64_t)by_xor(low, x)); high = max(high, (uint64_t)by_xor(high, x)); }
-        if (lane == 0) { wave_low[wave] = low; wave_mass[wave] = high; }
+        low = up_to(low, ~(uint64_t)0, [](uint64_t x, uint64_t y) { return min(x, y); });
+        high = up_to(high, (uint64_t)0, [](uint64_t x, uint64_t y) { return max(x, y); });
+        if (lane == 63) { wave_low[wave] = low; wave_mass[wave] = high; }
         __syncthreads();
         for (int w = 0; w < kWaves; ++w) { low = min(low, wave_low[w]); high = max(high, wave_mass[w]); }
         for (;;) {
@@ -711,26 +727,24 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     if (wave) return;
     uint64_t before = 0;
     for (int s0 = 0; s0 < all; s0 += 64) {
-        uint64_t x = s0 + lane < all ? run_mass[s0 + lane] : 0;
-        for (int y = 1; y < 64; y *= 2) { const uint64_t z = from_below(x, y); if (lane >= y) x += z; }
+        const uint64_t x = sum_up_to(s0 + lane < all ? run_mass[s0 + lane] : 0);
         const uint64_t hit = __ballot(before + x >= need);
         if (!hit) {
-            before += __shfl(x, 63);
+            before += of_lane(x, 63);
             continue;
         }
         const int f = __ffsll((unsigned long long)hit) - 1, s = s0 + f;
-        if (f) before += __shfl(x, f - 1);
+        if (f) before += of_lane(x, f - 1);
         const bool at_end = s == 0 || s == all - 1;
         for (int q = 0; q < kLines; ++q) {             // the run's lines of 64 pieces
             const int v = ((s - 1) * kLines + q) * 64 + lane;
             uint64_t mine = 0;
             if (at_end) mine = (uint64_t)ends(s);
             else if (v < row.pieces) mine = (uint64_t)in_piece(v, row.piece(v), m);
-            uint64_t z = mine;
-            for (int y = 1; y < 64; y *= 2) { const uint64_t w = from_below(z, y); if (lane >= y) z += w; }
+            const uint64_t z = sum_up_to(mine);
             const uint64_t here = __ballot(before + z >= need);
             if (!here) {
-                before += __shfl(z, 63);
+                before += of_lane(z, 63);
                 continue;
             }
             if (lane == __ffsll((unsigned long long)here) - 1) {

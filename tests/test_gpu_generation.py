@@ -544,6 +544,34 @@ def test_sample_counts_beyond_a_thousand_and_equal_entries_at_the_end(dt):
             assert got[r] == (index[0] if u == 0.0 else index[-1]), (r, K[r])
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [5000, 70003, 131072])
+def test_sample_flat_rows_of_every_width(dt, V):
+    # From rows of nearly equal entries, of which thousands are a cut's last ones, to rows over a wide range.  A 32-bit weight is off by
+    # less than 2^-20 of itself here ((x - top) by 2^-24 of at most 16, its product by as much, exp by 2^-23), so the place of a number
+    # is off by less than 2^-20 of the mass, and by four entries at the end where a limit falls between them.
+    print("sample widths", dt, V, flush=True)
+    rng = np.random.default_rng(V)
+    width = np.array([0.0, 0.001, 0.015, 0.03, 0.1, 0.3, 1.0, 3.0, 8.0, 16.0])
+    n = len(width)
+    logits = torch.from_numpy(rng.random((n, V)) * width[:, None] - 3.0).to(DT[dt]).cuda()
+    x = _f64(logits)
+    u = [0.1, 0.3, 0.5, 0.7, 0.99] * 2
+    for k, p, m in ((0, 0.9, 0.0), (0, 0.3, 0.0), (V // 2, 1.0, 0.0), (V // 3, 0.8, 0.0), (2000, 1.0, 0.0), (2000, 0.5, 0.0), (0, 0.95, 0.25), (0, 1.0, 0.3),
+                    (V - 1, 0.999, 0.0)):
+        p, m = float(np.float32(p)), float(np.float32(m))
+        got = _sample(logits, u, temperature=[1.0] * n, top_k=[k] * n, top_p=[p] * n, min_p=[m] * n)
+        for r in range(n):
+            w = oracle.weights(x[r], 1.0)[0]
+            index = oracle.kept(x[r], 1.0, k, p, m)[0]
+            run, last = np.cumsum(w[index]), w[index].min()
+            slack, at = 2.0 ** -20 * run[-1] + 4 * last, float(np.float32(u[r])) * run[-1]
+            j = int(np.searchsorted(index, got[r]))
+            before = run[j - 1] if j else 0.0
+            assert before - slack <= at <= before + w[got[r]] + slack, (r, k, p, m, before, at, run[-1])
+            assert w[got[r]] >= last * (1 - 2.0 ** -19), (r, k, p, m)
+
+
 # ---------------------------------------------------------------- graphs
 
 def test_a_captured_step_replays():
