@@ -1,6 +1,7 @@
 """ctypes declarations mirroring include/freeride.h, plus small object wrappers that only marshal arguments."""
 import ctypes as C
 import os
+import struct
 
 from . import build as _build
 
@@ -555,30 +556,34 @@ class Stage:
             self.handle = C.c_void_p()
 
 
-_DTYPE_OF = {"torch.bfloat16": FR_DTYPE_BF16, "torch.float16": FR_DTYPE_F16, "torch.float32": FR_DTYPE_F32}
-_codes = {}                    # torch dtype -> (its name, FR_DTYPE_* or None): these calls are short, and so is what they check
+_DTYPE_OF = {"bfloat16": FR_DTYPE_BF16, "float16": FR_DTYPE_F16, "float32": FR_DTYPE_F32}
 
 
-def _code(dtype):
-    got = _codes.get(dtype)
-    if got is None:
-        got = _codes[dtype] = (str(dtype)[len("torch."):], _DTYPE_OF.get(str(dtype)))
-    return got
+class _Names(dict):            # torch dtype -> its name
+    def __missing__(self, dtype):
+        name = self[dtype] = str(dtype)[len("torch."):]
+        return name
+
+
+# The calls of text generation take about 5 us each, most of it for looking at the tensors: their kernels can be as short, so the
+# checks are written for the usual case, and a descriptor is packed in one go.
+_names = _Names()
+_pack_append, _pack_attend, _pack_sample = struct.Struct("64s4Q4q3Q6i"), struct.Struct("64s3Q2q4Qq6ifi2Q"), struct.Struct("Qq4i6Q2Q")
 
 
 def _dtype(x):
     """FR_DTYPE_* of a torch tensor."""
-    name, code = _code(x.dtype)
+    code = _DTYPE_OF.get(_names[x.dtype])
     if code is None:
-        raise TypeError("%s: the library takes bfloat16, float16 and float32" % name)
+        raise TypeError("%s: the library takes bfloat16, float16 and float32" % _names[x.dtype])
     return code
 
 
 def _typed(x, name, what, like=None):
-    """Address of a tensor whose elements lie side by side and are of a type the C side cannot see; None for None."""
+    """Address of a tensor whose elements lie side by side and are of a type the C side cannot see; 0 for None."""
     if x is None:
-        return None
-    if _code(x.dtype)[0] != what or x.stride(-1) != 1 and x.shape[-1] > 1:
+        return 0
+    if _names[x.dtype] != what or not x.is_contiguous() and x.stride(-1) != 1 and x.shape[-1] > 1:
         raise TypeError("%s: %s elements side by side are needed" % (name, what))
     if like is not None and x.shape != like:
         raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(like), tuple(x.shape)))
@@ -589,9 +594,11 @@ def _rows(x, name, shape, dtype):
     """Stride between tokens of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
     if x.shape != shape:
         raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(shape), tuple(x.shape)))
-    if _code(x.dtype)[1] != dtype:
+    if x.dtype != dtype:
         raise TypeError("%s: not of the cache's type" % name)
     tokens, heads, dim = shape
+    if x.is_contiguous():
+        return heads * dim
     t, h, e = x.stride()
     if (dim > 1 and e != 1 or heads > 1 and h != dim) and x.numel():
         raise ValueError("%s: heads of a token have to lie side by side" % name)
@@ -599,7 +606,7 @@ def _rows(x, name, shape, dtype):
 
 
 def _workspace(x):
-    return (None, 0) if x is None else (x.data_ptr(), x.numel() * x.element_size())
+    return (0, 0) if x is None else (x.data_ptr(), x.nbytes)
 
 
 class KvPages:
@@ -615,24 +622,28 @@ class KvPages:
         d.n_pages, d.n_kv_heads, d.page_size, d.head_dim = k.shape
         d.page_stride, d.head_stride, d.slot_stride = k.stride()[:3]
         d.dtype = _dtype(k)
-        self.desc = d
+        self.desc, self.dtype = d, k.dtype
         self._keep = (k, v)
 
 
 def fr_kv_append(cache, k, v, slot, q=None, q_out=None, position=None, rotary=None, style=FR_ROTARY_HALVES, stream=None):
-    c = cache.desc
-    dim, dtype = c.head_dim, c.dtype
-    T = k.shape[0]
-    kv, n_q = (T, c.n_kv_heads, dim), 0 if q is None else q.shape[1]
-    of_q = (T, n_q, dim)
-    positions, rotary_dim = (0, 0) if rotary is None else rotary.shape
-    if rotary is not None and not rotary.is_contiguous():
-        raise ValueError("rotary: rows have to lie side by side")
-    d = fr_kv_append_desc(c, k.data_ptr(), v.data_ptr(), q.data_ptr() if n_q else None, q_out.data_ptr() if n_q else None,
-                          _rows(k, "k", kv, dtype), _rows(v, "v", kv, dtype), _rows(q, "q", of_q, dtype) if n_q else 0,
-                          _rows(q_out, "q_out", of_q, dtype) if n_q else 0, _typed(slot, "slot", "int64", (T,)),
-                          _typed(position, "position", "int32", (T,)) if rotary_dim else None, _typed(rotary, "rotary", "float32"),
-                          positions, rotary_dim, style, T, n_q, 0)
+    c, dtype = cache.desc, cache.dtype
+    dim, T = c.head_dim, k.shape[0]
+    kv, n_q = (T, c.n_kv_heads, dim), 0
+    q_at = q_out_at = q_stride = q_out_stride = position_at = rotary_at = positions = rotary_dim = 0
+    if q is not None and q.shape[1]:
+        n_q = q.shape[1]
+        of_q = (T, n_q, dim)
+        q_at, q_stride, q_out_at, q_out_stride = q.data_ptr(), _rows(q, "q", of_q, dtype), q_out.data_ptr(), _rows(q_out, "q_out", of_q, dtype)
+    if rotary is not None:
+        if not rotary.is_contiguous():
+            raise ValueError("rotary: rows have to lie side by side")
+        rotary_at, (positions, rotary_dim) = _typed(rotary, "rotary", "float32"), rotary.shape
+        if rotary_dim:
+            position_at = _typed(position, "position", "int32", (T,))
+    d = fr_kv_append_desc.from_buffer_copy(_pack_append.pack(
+        bytes(c), k.data_ptr(), v.data_ptr(), q_at, q_out_at, _rows(k, "k", kv, dtype), _rows(v, "v", kv, dtype), q_stride, q_out_stride,
+        _typed(slot, "slot", "int64", (T,)), position_at, rotary_at, positions, rotary_dim, style, T, n_q, 0))
     return _check(lib().fr_kv_append(C.byref(d), _stream(stream)), "fr_kv_append")
 
 
@@ -647,24 +658,26 @@ def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, 
 
 def fr_attend_shared(cache, q, out, pages, own_len, scale, prefix_len=0, max_own_len=0, prefix_pages=None, q_begin=None,
                      max_q=1, lse=None, workspace=None, stream=None):
-    c = cache.desc
-    dtype, page = c.dtype, c.page_size
-    tokens, heads = q.shape[0], q.shape[1]
+    c, dtype = cache.desc, cache.dtype
+    page = c.page_size
+    tokens, heads, _ = q.shape
     n_seqs = tokens if q_begin is None else q_begin.shape[0] - 1
     shape = (tokens, heads, c.head_dim)
     if lse is not None and not lse.is_contiguous():
         raise ValueError("lse: rows have to lie side by side")
     if prefix_pages is not None and prefix_pages.numel() * page < prefix_len:
         raise ValueError("prefix_pages: too few for prefix_len")
-    width = 0
+    width = own_at = 0
     if pages is not None:
         if pages.dim() != 2 or pages.shape[0] != n_seqs or pages.shape[1] * page < max_own_len:
             raise ValueError("pages: [n_seqs, at least max_own_len / page_size] is needed")
         width = pages.stride(0) if n_seqs > 1 else pages.shape[1]
-    d = fr_attend_desc(c, q.data_ptr(), out.data_ptr(), _typed(lse, "lse", "float32", shape[:2]), _rows(q, "q", shape, dtype),
-                       _rows(out, "out", shape, dtype), _typed(q_begin, "q_begin", "int32"), _typed(prefix_pages, "prefix_pages", "int32"),
-                       _typed(pages, "pages", "int32"), _typed(own_len, "own_len", "int32", (n_seqs,)) if pages is not None else None,
-                       width, tokens, n_seqs, heads, max_q, prefix_len, max_own_len, scale, 0, *_workspace(workspace))
+        own_at = _typed(own_len, "own_len", "int32", (n_seqs,))
+    d = fr_attend_desc.from_buffer_copy(_pack_attend.pack(
+        bytes(c), q.data_ptr(), out.data_ptr(), _typed(lse, "lse", "float32", (tokens, heads)), _rows(q, "q", shape, dtype),
+        _rows(out, "out", shape, dtype), _typed(q_begin, "q_begin", "int32"), _typed(prefix_pages, "prefix_pages", "int32"),
+        _typed(pages, "pages", "int32"), own_at, width, tokens, n_seqs, heads, max_q, prefix_len, max_own_len, scale, 0,
+        *_workspace(workspace)))
     return _check(lib().fr_attend_shared(C.byref(d), _stream(stream)), "fr_attend_shared")
 
 
@@ -682,8 +695,8 @@ def fr_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, 
     if vocab > 1 and entry != 1:
         raise ValueError("logits: the entries of a row have to lie side by side")
     like = (n,)
-    d = fr_sample_desc(logits.data_ptr(), stride if n > 1 else vocab, _dtype(logits), n, vocab, 0,
-                       _typed(temperature, "temperature", "float32", like), _typed(top_k, "top_k", "int32", like),
-                       _typed(top_p, "top_p", "float32", like), _typed(min_p, "min_p", "float32", like),
-                       _typed(uniform, "uniform", "float32", like), _typed(token, "token", "int32", like), *_workspace(workspace))
+    d = fr_sample_desc.from_buffer_copy(_pack_sample.pack(
+        logits.data_ptr(), stride if n > 1 else vocab, _dtype(logits), n, vocab, 0, _typed(temperature, "temperature", "float32", like),
+        _typed(top_k, "top_k", "int32", like), _typed(top_p, "top_p", "float32", like), _typed(min_p, "min_p", "float32", like),
+        _typed(uniform, "uniform", "float32", like), _typed(token, "token", "int32", like), *_workspace(workspace)))
     return _check(lib().fr_sample(C.byref(d), _stream(stream)), "fr_sample")
