@@ -558,7 +558,7 @@ __device__ __forceinline__ void attend_prefix(const AttendArgs& a, int unit, int
     w.rows = a.n_tokens * a.group;
     w.row0 = tile * rows_of(kKind);
     w.k0 = w.part * a.prefix.split_len;
-    w.k1 = min(a.prefix_len, w.k0 + a.prefix.split_len);
+    w.k1 = (int)min((uint32_t)a.prefix_len, (uint32_t)w.k0 + (uint32_t)a.prefix.split_len);
     w.seen0 = a.prefix_len;
     w.seen_step = 0;
     w.own_pages = nullptr;
@@ -591,7 +591,7 @@ __device__ __forceinline__ void attend_own(const AttendArgs& a, int unit, int xc
     const int last = min(w.rows, w.row0 + rows_of(kKind)) - 1;
     const int seen = max(a.prefix_len, w.seen0 + last / a.group);
     w.k0 = a.own_from + split * a.own.split_len;
-    w.k1 = min(seen, w.k0 + a.own.split_len);
+    w.k1 = (int)min((uint32_t)seen, (uint32_t)w.k0 + (uint32_t)a.own.split_len);
     if (w.k0 >= w.k1 && a.parts > 1) return;
     w.part = a.own.first_part + split;
     w.own_pages = a.pages + b * a.pages_stride;
@@ -626,7 +626,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_
     const int t = t1 - t0, i = r / a.n_q_heads, own = a.max_own_len ? within(a.own_len[b], 0, a.max_own_len) : 0;
     const bool there = i < min(t, a.max_q);
     const int seen = max(a.prefix_len, a.prefix_len + own - t + 1 + i);
-    const int of_own = seen > a.own_from ? (seen - a.own_from + a.own.split_len - 1) / a.own.split_len : 0, parts = there ? a.own.first_part + of_own : 0;
+    const int of_own = seen > a.own_from ? (int)(((uint32_t)(seen - a.own_from) + (uint32_t)a.own.split_len - 1) / (uint32_t)a.own.split_len) : 0, parts = there ? a.own.first_part + of_own : 0;
     const int64_t token = t0 + i, head = r % a.n_q_heads, row = token * a.n_q_heads + head, pitch = (int64_t)a.n_tokens * a.n_q_heads;
     float top = -INFINITY;
     for (int y = mine; y < parts; y += kLanes) top = fmaxf(top, a.part_ml[y * pitch + row].x);
@@ -688,6 +688,32 @@ struct Plan {
     int64_t blocks = 0;                    // of the larger grid
 };
 
+// What a call with tiles of 128 rows takes, roughly, in microseconds: enough to tell ways to cut it from one another.  A workgroup
+// needs `one` for a tile of 64 keys where it has a unit to itself and `all` where as many are on the unit as fit, and kStart to begin
+// and end; results of several parts are written, read and joined.
+struct Cost {
+    double one, all;
+    int at_once;
+    explicit Cost(int D) : one(D == 128 ? 1.43 : 0.9), all(D == 128 ? 2.0 : 1.6), at_once(D == 128 ? 2 : 3) {}
+    static constexpr double kStart = 4.0, kJoin = 4.0, kBytesAUs = 4e6;
+    double tile(double a_unit) const { return a_unit <= 1 ? one : one + (all - one) * (std::min(std::ceil(a_unit), (double)at_once) - 1) / (at_once - 1); }
+    double workgroups(double blocks, double tiles, int cus) const
+    {
+        const double a_unit = blocks / cus, full = std::floor(a_unit / at_once), rest = a_unit - full * at_once;
+        return tiles * (full * all + (rest > 0 ? tile(rest) : 0)) + kStart * std::ceil(a_unit / at_once);
+    }
+    // two kinds of workgroups in one launch
+    double both(double blocks0, double tiles0, double blocks1, double tiles1, int cus) const
+    {
+        const double a_unit = (blocks0 + blocks1) / cus, work = (blocks0 * tiles0 + blocks1 * tiles1) * all / at_once / cus;
+        return std::max(work + 0.25 * all * tiles1, tile(a_unit) * std::max(tiles0, tiles1)) + kStart * std::ceil(a_unit / at_once);
+    }
+    static double join(int64_t parts, const fr_attend_desc& d)
+    {
+        return parts < 2 ? 0 : kJoin + (double)parts * d.n_tokens * d.n_q_heads * d.cache.head_dim * (2 * sizeof(float)) / kBytesAUs;
+    }
+};
+
 Plan plan(const fr_attend_desc& d, int cus)
 {
     Plan p;
@@ -703,36 +729,81 @@ Plan plan(const fr_attend_desc& d, int cus)
         s.units = (int)std::min<int64_t>(units, 0x7fffffff);
         p.blocks += units * kXcds;
     };
-    if (d.prefix_len > 0 && d.n_seqs > 1 && seq_rows < rows_of(kWideRows) && (int64_t)d.n_seqs * d.prefix_len >= 8192) {
-        p.of_prefix = all_rows > kMostFew ? kWideRows : kFewRows;
-        Segment& s = p.prefix;
-        s.row_tiles = (int)up(all_rows, rows_of(p.of_prefix));
-        const int64_t most = up(d.prefix_len, 256), want = (d.max_own_len ? 1 : 2) * cus / (s.row_tiles * heads);
-        const int64_t splits = std::max<int64_t>(1, std::min(most, want));
-        s.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
-        s.splits = (int)up(d.prefix_len, s.split_len);
-        finish(s, heads * s.splits, 1);
-    }
-    Segment& s = p.own;
-    const int64_t keys = (p.of_prefix == kNone ? d.prefix_len : 0) + (int64_t)d.max_own_len;
+    // `keys` in parts of a whole number of tiles, two at least: as many as cost(parts, tiles of a part) is least for, of powers of two,
+    // the numbers that give every unit up to four workgroups, and parts of two tiles
+    auto cut = [&](Segment& s, int64_t keys, int64_t blocks, auto cost) {
+        double least = INFINITY;
+        const int64_t most = std::max<int64_t>(up(keys, 128), 1);
+        auto consider = [&](int64_t n) {
+            if (n < 1 || n > most) return;
+            const int64_t len = std::max<int64_t>(up(up(keys, n), 64), 1) * 64, parts = std::max<int64_t>(up(keys, len), 1);
+            const double t = cost(parts, len / 64);
+            if (t < least) { least = t; s.split_len = (int)std::min<int64_t>(len, 0x7fffffc0); s.splits = (int)parts; }
+        };
+        for (int64_t n = 1; n == 1 || n * blocks <= 4 * cus; n *= 2) consider(n);
+        for (int a_unit = 1; a_unit <= 4; ++a_unit) consider(a_unit * cus / blocks);
+        if (most * blocks <= cus) consider(most);
+        return least;
+    };
     p.of_own = seq_rows > kMostFew ? kWideRows : kFewRows;
-    s.first_part = p.prefix.splits;
+    Segment &s = p.own, &shared = p.prefix;
     s.row_tiles = (int)up(seq_rows, rows_of(p.of_own));
-    s.split_len = 1;
-    if (keys || p.of_prefix == kNone) {
+    shared.row_tiles = (int)up(all_rows, rows_of(all_rows > kMostFew ? kWideRows : kFewRows));
+    bool share = d.prefix_len > 0 && d.n_seqs > 1 && (int64_t)d.n_seqs * d.prefix_len >= 8192;
+    if (p.of_own == kWideRows) {
+        // row tiles that hold rows, half of a sequence's last one being empty
+        const Cost cost(d.cache.head_dim);
+        const double tiles = std::min((double)d.n_seqs * s.row_tiles, all_rows / 128.0 + 0.5 * d.n_seqs) * heads;
         const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
-        int64_t len = 2048;
-        if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
-        else
-            while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
-        if (p.of_own == kFewRows && p.of_prefix != kFewRows && base >= 2 * cus) {
-            p.of_own = kWaveRows;
-            len = 256;
-            while (base * up(keys, len) > 16 * cus && len < keys) len *= 2;
+        auto alone = [&](int64_t parts, int64_t t) { return cost.workgroups(tiles * parts, (double)t, cus) + cost.join(parts, d); };
+        share = d.prefix_len > 0 && d.n_seqs > 1;
+        double together = INFINITY;
+        if (share) {
+            if (d.max_own_len) cut(s, d.max_own_len, base, alone);
+            together = cut(shared, d.prefix_len, shared.row_tiles * heads, [&](int64_t parts, int64_t t) {
+                return cost.both((double)shared.row_tiles * heads * parts, (double)t, tiles * s.splits, s.split_len / 64.0, cus) +
+                       cost.join(parts + s.splits, d);
+            });
         }
-        s.split_len = (int)len;
-        s.splits = (int)std::max<int64_t>(1, up(keys, len));
+        const Segment own = s;
+        if (cut(s, (int64_t)d.prefix_len + d.max_own_len, base, alone) <= together) {
+            share = false;
+        } else {
+            s = own;
+        }
+    } else if (share) {
+        const int64_t most = up(d.prefix_len, 256), want = (d.max_own_len ? 1 : 2) * cus / (shared.row_tiles * heads);
+        const int64_t splits = std::max<int64_t>(1, std::min(most, want));
+        shared.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
+        shared.splits = (int)up(d.prefix_len, shared.split_len);
+    }
+    if (share) {
+        p.of_prefix = all_rows > kMostFew ? kWideRows : kFewRows;
+        finish(shared, heads * shared.splits, 1);
+    } else {
+        shared = {};
+    }
+    const int64_t keys = (share ? 0 : d.prefix_len) + (int64_t)d.max_own_len;
+    s.first_part = shared.splits;
+    if (keys || !share) {
+        if (p.of_own == kFewRows) {
+            const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
+            int64_t len = 2048;
+            if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
+            else
+                while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
+            if (p.of_prefix != kFewRows && base >= 2 * cus) {
+                p.of_own = kWaveRows;
+                len = 256;
+                while (base * up(keys, len) > 16 * cus && len < keys) len *= 2;
+            }
+            s.split_len = (int)len;
+            s.splits = (int)std::max<int64_t>(1, up(keys, len));
+        }
         finish(s, (int64_t)d.n_seqs * heads * s.splits, p.of_own == kWaveRows ? kWaves : 1);
+    } else {
+        s.splits = 0;
+        s.split_len = 1;
     }
     p.parts = p.prefix.splits + s.splits;
     p.blocks = std::max(p.blocks, d.n_seqs * tokens_a_seq * d.n_q_heads);        // (the join's grid is not larger)
@@ -804,7 +875,8 @@ int fr_attend_shared(const fr_attend_desc* d, void* stream)
                     __builtin_ctz(c.page_size), d->n_q_heads / c.n_kv_heads, d->scale};
     // cut for the units that the stream may use, in no more parts than the workspace was asked for
     const Plan whole = plan(*d, kUnits);
-    Plan p = plan(*d, (int)fr_stream_cus((hipStream_t)stream));
+    const int cus = (int)fr_stream_cus((hipStream_t)stream);
+    Plan p = cus < kUnits ? plan(*d, cus) : whole;
     if (p.parts > whole.parts) p = whole;
     if (p.blocks > 0x7fffffff) return FR_ERR_ARG;
     const uint64_t asked = part_bytes(*d, whole);
