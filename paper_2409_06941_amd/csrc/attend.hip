@@ -792,10 +792,12 @@ Plan plan(const fr_attend_desc& d, int cus)
             if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
             else
                 while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
-            if (p.of_prefix != kFewRows && base >= 2 * cus) {
+            int64_t wave_len = base < cus ? 128 : 256;
+            while (base * up(keys, wave_len) > (base < cus ? 4 : 16) * cus && wave_len < keys) wave_len *= 2;
+            const bool enough = base >= cus / 2 && base * up(keys, wave_len) >= (base < cus ? 4 : 3) * cus / 2;
+            if (p.of_prefix != kFewRows && enough && keys <= (base < 4 * cus ? 2048 : share ? 512 : 256)) {
                 p.of_own = kWaveRows;
-                len = 256;
-                while (base * up(keys, len) > 16 * cus && len < keys) len *= 2;
+                len = wave_len;
             }
             s.split_len = (int)len;
             s.splits = (int)std::max<int64_t>(1, up(keys, len));
