@@ -348,6 +348,24 @@ def test_attend_in_a_long_cache_beyond_32_bits():
     _check_attend("bf16", q, k[used], v[used], small(prefix_pages[None])[0], small(table), 70, own, np.array([0, 1, 2]), D ** -0.5, out, lse)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("Hq,Hk,D,page,P,own,new", [
+    (4, 1, 128, 16, 8200, [50, 61], [41, 40]),                     # two questions about a long document
+    (4, 1, 64, 16, 2100, [70, 66, 0, 33, 1, 64, 50, 90], [64, 40, 0, 33, 1, 64, 50, 64]),
+    (3, 1, 128, 8, 300, [60] * 12, [50] * 12),                     # many about a short one
+    (8, 2, 64, 32, 3000, [200], [170]),                            # a prompt that goes on
+    (4, 2, 128, 16, 0, [1999, 10, 500], [100, 10, 0]),
+    (2, 2, 64, 16, 4000, [0, 0, 0], [45, 60, 1]),                  # nothing but the document
+    # and where the document is gone through once for all of them
+    (8, 2, 128, 16, 8200, [50, 61], [41, 40]),
+    (8, 2, 64, 16, 2048, [70, 66, 60, 33, 1, 64, 50, 90], [40, 40, 37, 33, 1, 40, 40, 40]),
+    (8, 8, 64, 16, 4000, [0, 0, 0], [45, 60, 1]),
+])
+def test_attend_questions_about_a_document(dt, Hq, Hk, D, page, P, own, new):
+    print("attend questions", dt, Hq, Hk, D, page, P, own, new, flush=True)
+    _attend_case(dt, Hq, Hk, D, page, P, own, new, seed=P + len(own), spoil=math.nan)
+
+
 def test_attend_on_another_stream_masked_and_captured():
     print("attend streams", flush=True)
     side = torch.cuda.Stream()
