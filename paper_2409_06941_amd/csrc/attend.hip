@@ -1,4 +1,21 @@
 // Attention of a batch of sequences behind a shared prefix, keys and values in a cache of pages.
+//
+// A query row q (a token, a head) that sees keys k_j with values v_j gets  out = sum_j w_j v_j / sum_j w_j,  w_j = exp(s_j - m),
+// s_j = scale q . k_j,  and lse = m + log sum_j w_j, for whatever m: the largest score seen so far.  Where m rises, the sums so far
+// are multiplied by exp(m_before - m), so that one pass over the keys is enough, and parts of the keys, each with its own m, are
+// joined in the same way.  Scores, m, both sums and the parts' results are of 32 bits; weights are rounded to the type for the
+// product with the values, and the result is, once.
+//
+// The heads that share a key head, and all tokens of a sequence, are rows of one matrix product with its keys; against the prefix
+// the rows of all sequences are, so the prefix is read once for 128 of them.
+// What bounds it:
+//   Decoding from long caches, the reading: 8 sequences of 20000 to 65536 tokens, 1.62 GB in 285 us, 5.7 TB/s (a kernel that only
+//     reads reaches 6.5).
+//   Prompts, the matrix cores: 16 questions of 300 to 700 tokens about 8192, 32 heads, 1.03 TFLOP in 1.05 ms, 0.98 PFLOP/s (a library
+//     product of 8192 x 8192 matrices 1.25); beside them the vector units make 2 exps and 5 other operations of every two weights.
+//   Decoding behind a prefix, neither: of 64 sequences behind 16384 keys (78 us) the prefix' products alone take 38 us, the own keys'
+//     reading alone 40, and the two kinds of workgroups slow one another down; then the parts are joined, 7 us.
+//   A few short sequences, the launch: 5 us.
 
 #include <algorithm>
 #include <cmath>
@@ -208,6 +225,18 @@ template <typename T, int D, int kCols> struct Fragments {
 };
 
 // The work of one workgroup (kWaveRows: of one wavefront).
+//
+// kWideRows: a wavefront's 32 rows are the columns of 32 x 32 x 16 blocks; scores and results stand in its registers, transposed, and
+// weights go from the one product to the next without passing through LDS.  Tiles of 64 keys come to LDS, two of K and two of V.
+// A tile is 32 MFMAs a wavefront (head_dim 128), 0.5 us, and takes 1.43 us where the workgroup is alone on its unit, 2.0 where there
+// are two: there is a barrier to wait for, 64 fragments are read, and the weights' vector operations take as long as the MFMAs beside
+// which they are issued.  Measured at the 16 questions above, 1.013 ms in a graph: fragments read 6 MFMAs ahead instead of 4 1.021;
+// 8 or 12 pairs of weights beside the scores' MFMAs instead of 10 1.009 and 1.028; loads asked for between the MFMAs instead of before
+// them 1.11; the MFMAs with the values at the usual priority 5 % more.
+//
+// kFewRows and kWaveRows: 16 rows, blocks of 16 x 16 x 32, tiles of 32 keys that pass through LDS (where the values are transposed)
+// into registers while the next ones are on their way: with so few rows the MFMAs are next to nothing, and what counts is the number
+// of bytes asked for ahead, 16 KB a wavefront and 128 KB a unit at head_dim 128.
 template <typename T, int D, Kind kKind>
 __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char* lds_array, int32_t* ids_array)
 {
@@ -615,7 +644,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(AttendArgs
     }
 }
 
-// Joins the parts of a row: twice four elements a thread, kLanes threads for every eight, each with every kLanes-th part.
+// Joins the parts of a row: twice four elements a thread, kLanes threads for every eight, each with every kLanes-th part.  Bound by
+// latency (the launch, the sequence's length, then all parts in one go): 33 sequences of up to 6 tokens with 15 heads 7 us of 22, 64
+// sequences with 32 heads and 22 parts, 23 MB, 7 of 72.  (With the parts' maxima first and then the parts, four at once, by 16 threads
+// from 17 parts on, 1.5 to 2 us more.)
 template <typename T, int D, int kLanes>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_blocks)
 {
@@ -628,20 +660,38 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_
     const int seen = max(a.prefix_len, a.prefix_len + own - t + 1 + i);
     const int of_own = seen > a.own_from ? (int)(((uint32_t)(seen - a.own_from) + (uint32_t)a.own.split_len - 1) / (uint32_t)a.own.split_len) : 0, parts = there ? a.own.first_part + of_own : 0;
     const int64_t token = t0 + i, head = r % a.n_q_heads, row = token * a.n_q_heads + head, pitch = (int64_t)a.n_tokens * a.n_q_heads;
-    float top = -INFINITY;
-    for (int y = mine; y < parts; y += kLanes) top = fmaxf(top, a.part_ml[y * pitch + row].x);
-    float base = top == -INFINITY ? 0.0f : top, sum = 0.0f, o[8];
+    constexpr int kAtOnce = 8;
+    float top = -INFINITY, base, sum = 0.0f, o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-#pragma unroll 4
-    for (int y = mine; y < parts; y += kLanes) {
-        const float2 ml = a.part_ml[y * pitch + row];
-        const float f = __builtin_amdgcn_exp2f(ml.x - base);
-        const float4* p = reinterpret_cast<const float4*>(a.part_o + (y * pitch + row) * D) + piece;
-        const float4 lo = p[0], hi = p[kPieces];
-        sum = fmaf(ml.y, f, sum);
-        o[0] = fmaf(lo.x, f, o[0]), o[1] = fmaf(lo.y, f, o[1]), o[2] = fmaf(lo.z, f, o[2]), o[3] = fmaf(lo.w, f, o[3]);
-        o[4] = fmaf(hi.x, f, o[4]), o[5] = fmaf(hi.y, f, o[5]), o[6] = fmaf(hi.z, f, o[6]), o[7] = fmaf(hi.w, f, o[7]);
+    for (int y0 = mine; y0 < parts; y0 += kAtOnce * kLanes) {    // (nearly always all there are)
+        float2 ml[kAtOnce];
+        float4 lo[kAtOnce], hi[kAtOnce];
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+            const int64_t at = min(y0 + x * kLanes, parts - 1) * pitch + row;
+            const float4* p = reinterpret_cast<const float4*>(a.part_o + at * D) + piece;
+            ml[x] = a.part_ml[at];
+            lo[x] = p[0];
+            hi[x] = p[kPieces];
+        }
+        const float before = top;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x)
+            if (y0 + x * kLanes < parts) top = fmaxf(top, ml[x].x);
+        base = top == -INFINITY ? 0.0f : top;
+        const float g = __builtin_amdgcn_exp2f(before - base);
+        sum *= g;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= g;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+            if (y0 + x * kLanes >= parts) continue;
+            const float f = __builtin_amdgcn_exp2f(ml[x].x - base);
+            sum = fmaf(ml[x].y, f, sum);
+            o[0] = fmaf(lo[x].x, f, o[0]), o[1] = fmaf(lo[x].y, f, o[1]), o[2] = fmaf(lo[x].z, f, o[2]), o[3] = fmaf(lo[x].w, f, o[3]);
+            o[4] = fmaf(hi[x].x, f, o[4]), o[5] = fmaf(hi[x].y, f, o[5]), o[6] = fmaf(hi[x].z, f, o[6]), o[7] = fmaf(hi[x].w, f, o[7]);
+        }
     }
     if constexpr (kLanes > 1) {
         __shared__ float of[10][kThreads];
@@ -690,7 +740,12 @@ struct Plan {
 
 // What a call with tiles of 128 rows takes, roughly, in microseconds: enough to tell ways to cut it from one another.  A workgroup
 // needs `one` for a tile of 64 keys where it has a unit to itself and `all` where as many are on the unit as fit, and kStart to begin
-// and end; results of several parts are written, read and joined.
+// and end; results of several parts are written, read and joined.  (1.43 and 2.0 are measured; those of head_dim 64 are about half of
+// that: with 0.7 and 1.1 three of 36 calls take 6 to 17 % longer, none is faster.)
+// Against parts of 128 to 2048 keys, as many as four workgroups a unit ask for, and the prefix gone through by every sequence from
+// 128 rows a sequence on, of 32 heads with 8 key heads: one sequence's 640 rows behind 8192 keys 70 -> 44 us, 2800 rows behind 512
+// 63 -> 34; 64 sequences' 96 rows against 250 keys 46 -> 24; 8 sequences' 160 rows behind 2048 shared keys 53 -> 33, 32 sequences'
+// 640 rows 322 -> 217; where the prefix is short it stays with the sequences (32 of 640 rows behind 512 keys 84; taken apart 134).
 struct Cost {
     double one, all;
     int at_once;
@@ -720,7 +775,10 @@ Plan plan(const fr_attend_desc& d, int cus)
     auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     const int64_t group = d.n_q_heads / d.cache.n_kv_heads, heads = d.cache.n_kv_heads;
     const int64_t tokens_a_seq = std::min(d.max_q, d.n_tokens), seq_rows = tokens_a_seq * group, all_rows = d.n_tokens * group;
-    constexpr int64_t kMostFew = 32;       // rows up to which tiles of 16 are taken (above, one of 128)
+    // Rows of a sequence up to which tiles of 16 are taken, above, tiles of 128: several of those read the same keys, but do
+    // not wait for one another.  8 key heads, in tiles of 16 and of 128: 32 rows, 256 sequences of 64 keys 23 and 36 us, 4 of 1000 13.5 and 15.4,
+    // 16 of 4000 52 and 52; 64 rows, 64 sequences of 250 keys 21.5 and 22, of 1000 79 and 49, 16 of 1000 28 and 25.
+    constexpr int64_t kMostFew = 32;
     cus = std::min(cus, kUnits);
     auto finish = [&](Segment& s, int64_t items, int64_t at_once) {
         const int64_t groups = up(items, at_once), units = up(groups, kXcds) * s.row_tiles;
@@ -749,6 +807,9 @@ Plan plan(const fr_attend_desc& d, int cus)
     Segment &s = p.own, &shared = p.prefix;
     s.row_tiles = (int)up(seq_rows, rows_of(p.of_own));
     shared.row_tiles = (int)up(all_rows, rows_of(all_rows > kMostFew ? kWideRows : kFewRows));
+    // Few rows a sequence: the prefix is taken apart where reading it for every sequence costs more than two more launches' work and
+    // parts to join.  32 heads, 8 key heads, apart and by every sequence: 16 sequences behind 128 keys 11.8 and 9.4 us, behind 512 14.4
+    // and 14.0, behind 2048 16 and 23; 32 behind 512 16 and 18; 2 behind 2048 10.5 and 11.3, behind 8192 14 and 21.
     bool share = d.prefix_len > 0 && d.n_seqs > 1 && (int64_t)d.n_seqs * d.prefix_len >= 8192;
     if (p.of_own == kWideRows) {
         // row tiles that hold rows, half of a sequence's last one being empty
@@ -772,6 +833,8 @@ Plan plan(const fr_attend_desc& d, int cus)
             s = own;
         }
     } else if (share) {
+        // (one workgroup a unit leaves room for the sequences' own; two, 64 sequences behind 12000 keys 47 instead of 37 us.  Without
+        // own keys two: 256 sequences behind 16384 keys 151 instead of 166)
         const int64_t most = up(d.prefix_len, 256), want = (d.max_own_len ? 1 : 2) * cus / (shared.row_tiles * heads);
         const int64_t splits = std::max<int64_t>(1, std::min(most, want));
         shared.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
@@ -787,11 +850,19 @@ Plan plan(const fr_attend_desc& d, int cus)
     s.first_part = shared.splits;
     if (keys || !share) {
         if (p.of_own == kFewRows) {
+            // Parts of 2048 keys, shorter ones while they give less than four workgroups a unit, none where the sequences alone give
+            // eight.  (8 sequences of up to 65536 keys: parts of 512 310 us, 1024 302, 2048 295, 4096 294.  Two or eight a unit instead of
+            // four: 8 of 10000 57 and 52, with four 52; 32 of 2000 39 and 44, with four 39.5; 1 of 60000 43 and 53, with four 45.)
             const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
             int64_t len = 2048;
             if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
             else
                 while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
+            // Short caches: a wavefront an item, of 256 keys (128 where items are few, more where they are many), if there are items
+            // enough, and up to 2048 keys; where there are many, parts cost more than they give from a few hundred keys on.  8 key heads, a
+            // wavefront and a workgroup an item: 256 sequences of 64 keys 12 and 20 us, 64 of up to 1500 50 and 58, 16 of 1500 19 and 23;
+            // 64 of 4000 147 and 143, 256 of 400 53 and 50, of 1500 211 and 194; behind a prefix, 256 of 512 with 64 heads 95 and 98.
+            // Parts of 128 or 512 keys instead of 256 there: 96 and 92; 64 of up to 1500 behind 16384 73.4 and 77.1, with 256 73.5.
             int64_t wave_len = base < cus ? 128 : 256;
             while (base * up(keys, wave_len) > (base < cus ? 4 : 16) * cus && wave_len < keys) wave_len *= 2;
             const bool enough = base >= cus / 2 && base * up(keys, wave_len) >= (base < cus ? 4 : 3) * cus / 2;
@@ -834,13 +905,12 @@ int launch(const AttendArgs& a, const Plan& p, hipStream_t stream)
         else go(k_attend<T, D, kWideRows, kWideRows>);
     }
     if (p.parts > 1) {
-        // a thread for every eight elements where a row has few parts, up to 16 threads where it has many
-        const int lanes = p.parts <= 4 ? 1 : p.parts <= 16 ? 4 : 16, rows = kThreads / (D / 8) / lanes;
+        // a thread for every eight elements where it has all parts in one go, else four
+        const int lanes = p.parts <= 8 ? 1 : 4, rows = kThreads / (D / 8) / lanes;
         const int64_t blocks = (std::min<int64_t>(a.max_q, a.n_tokens) * a.n_q_heads + rows - 1) / rows;
         const dim3 joins((unsigned)(a.n_seqs * blocks));
         if (lanes == 1) hipLaunchKernelGGL((k_attend_join<T, D, 1>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
-        else if (lanes == 4) hipLaunchKernelGGL((k_attend_join<T, D, 4>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
-        else hipLaunchKernelGGL((k_attend_join<T, D, 16>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
+        else hipLaunchKernelGGL((k_attend_join<T, D, 4>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
     }
     return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
 }
