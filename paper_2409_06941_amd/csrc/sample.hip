@@ -1,19 +1,28 @@
 // One token for every row of logits, from a given random number: temperature, top-k, top-p and min-p.
 //
-// The entries kept are a prefix of the row in falling order, so nothing is sorted: the prefix' end is searched for by histograms of
-// the entries' counts and masses.  Masses are 64-bit integers, whose sums do not depend on the order of the additions.  A
-// histogram's digit is a step of 1/64 on the scale of (m - l) / temperature, over which a language model's logits spread evenly
-// (digits of a float's bits would put thousands of entries on one counter).
+// An entry of logit l has the weight w = exp((l - m) / temperature), m being the row's largest.  Kept are the first top_k in falling
+// order, of those the fewest that hold top_p of their weight, of those the ones with w >= min_p; the token is the first in the
+// vocabulary's order at which the running weight of the kept passes uniform times all of it.  Masses, the weights in 64-bit integers
+// of 2^-43 (every weight is rounded down once, to the 24 bits that it has in 32 anyway), add up to the same sum in any order.
 //
-// A workgroup takes a row, and reads it twice:
-//   first for the largest logit, of the row and of every thread's share;
-//   then, for rows that are cut by count or mass, to put the entries that can be kept into LDS.  The rank-th largest of the threads'
-//   own largest logits has at least `rank` entries above it, and seldom many more: with rank = top_k all of the first top_k are
-//   among them; for a cut by mass rank is 640, and the pass adds up the mass of the whole row, which says whether what is in LDS
-//   holds enough of it.  What is left happens in LDS.
-//   Rows that are not cut, or by weight alone, need the masses of runs of 64 lanes' entries instead, and one run again.
-// Rows that none of this fits (many thousands of entries that can be kept, or as many equal ones, infinities) go through the row
-// for every digit of the search.
+// The entries kept are a prefix of the row in falling order, so nothing is sorted: the prefix' end is searched for by histograms of
+// the entries' counts and masses.  A histogram's digit is a step of 1/64 on the scale of (m - l) / temperature, over which a language
+// model's logits spread evenly (digits of a float's bits would put thousands of entries on one counter).
+//
+// A workgroup of 1024 threads takes a row (112 KB of LDS: one on a unit), and goes through it twice:
+//   first for the largest logit, of the row and of every thread's share, and for rows that are cut by mass alone for the share's mass,
+//   roughly;
+//   then, for rows that are cut by count or mass, to put the entries that can be kept into LDS, of the shares that have any.  The
+//   rank-th largest of the threads' own largest logits has at least `rank` entries above it, and seldom many more: with rank = top_k
+//   all of the first top_k are among them; how far down a cut by mass goes is estimated from the threads' largest logits, and the
+//   rough mass of the others says whether what is in LDS holds enough.  What is left happens in LDS.
+//   Rows that are not cut, or by weight alone, need the masses of runs of 512 pieces instead, and one run again.
+// Rows that none of this fits (many thousands of entries that can be kept, or as many equal ones, infinities) take the long way: a
+// histogram of the whole row, and the masses of runs together with the digit in which the kept entries end.
+//
+// What bounds it, at 256 rows of 131072 in 32 bits, 134 MB: the first pass 24 us, 5.6 TB/s, memory; greedy 28; top-k 50 38 and top-p
+// 0.9 48 the steps in LDS, each behind barriers that nothing fills; no cut 60, of which 35 the vector units at 131072 exps a unit, as
+// in the long way: 143 at temperature 1.3 and top-p 0.98, 117 for a flat row.  One row of 32768: 14 us, the steps one after another.
 
 #include <cmath>
 #include <type_traits>
@@ -65,6 +74,8 @@ struct Scale {
 
 struct Found { uint32_t digit, count_before, count; uint64_t mass_before, mass; };
 
+// kRank: what is tried at most.  960 of 1024 threads have theirs above a line that about 2840 entries are above, so that 4096 have room;
+// top-k of 400, 700, 960: 52, 56, 63 us this way and 97 to 100 the long way; of 1000 it often fails, after 20 us.
 constexpr int kCandidates = 4096, kList = 1024, kRank = 960, kMostRuns = kBins;
 constexpr uint32_t kNoMass = 1909;                     // from this digit on (29.83 and more below the top) masses are 0: 43 ln 2 = 29.81
 
@@ -343,7 +354,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         return true;
     };
 
-    if (scale.usual() && (k < V || p < 1.0f || min_p > 0.0f) && (k == V || k <= kThreads || V <= kCandidates)) {
+    if (scale.usual() && (k < V || p < 1.0f || min_p > 0.0f) && (k == V || k <= kRank || V <= kCandidates)) {
         // digits up to `last` can be kept
         uint32_t last = kNoMass - 1;
         bool fits = true;
@@ -355,7 +366,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             uint32_t rank = (uint32_t)k;
             if (by_mass) {
                 // As many as hold the mass, going by the threads' largest: where c of 1024 threads have theirs above a line, about
-                // -1024 log(1 - c / 1024) entries are above it.  (Too few, and the row takes the long way; too many cost a little.)
+                // -1024 log(1 - c / 1024) entries are above it.  5 % more mass and four digits for what the estimate is off by: too few,
+                // and the row takes the long way, too many cost a little.  (Top-p 0.9: with no room 93 us, as it is 48, with 20 % and 16
+                // digits 67.)
                 auto entries = [](uint32_t c) { return -1024.0f * logf(1.0f - fminf((float)c, 1023.5f) / 1024.0f); };
                 const float n0 = entries(tops.before_c), n1 = entries(tops.before_c + tops.c0), n2 = entries(tops.before_c + tops.c0 + tops.c1);
                 const float w0 = expf(-(float)(4 * tid + 1) / 128.0f), w1 = expf(-(float)(4 * tid + 3) / 128.0f);
@@ -372,6 +385,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 } else {
                     // As many as there is room for, and at once the long way if those will hold too little: if what is missing can be
                     // entries below every thread's largest (else a thread has several of the largest: seldom, but one row is enough).
+                    // Flat rows 117 us; with the attempt 149.
                     const float each = expf(-(float)find(tops, false, tops.all_c).digit / 64.0f) * 0x1p30f;
                     rank = kRank;
                     fits = (double)held.all_m >= 0.8 * (double)want || (double)(want - held.all_m) > (double)V * each;
