@@ -1,7 +1,8 @@
 """ctypes declarations mirroring include/freeride.h, plus small object wrappers that only marshal arguments."""
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import os
-import struct
 
 from . import build as _build
 
@@ -559,54 +560,31 @@ class Stage:
 _DTYPE_OF = {"bfloat16": FR_DTYPE_BF16, "float16": FR_DTYPE_F16, "float32": FR_DTYPE_F32}
 
 
-class _Names(dict):            # torch dtype -> its name
-    def __missing__(self, dtype):
-        name = self[dtype] = str(dtype)[len("torch."):]
-        return name
+_calls = None
 
 
-# The calls of text generation take about 5 us each, most of it for looking at the tensors: their kernels can be as short, so the
-# checks are written for the usual case, and a descriptor is packed in one go.
-_names = _Names()
-_pack_append, _pack_attend, _pack_sample = struct.Struct("64s4Q4q3Q6i"), struct.Struct("64s3Q2q4Qq6ifi2Q"), struct.Struct("Qq4i6Q2Q")
+def _torch_calls():
+    """The module that looks at the tensors of a text-generation call, fills its descriptor and calls the library (csrc/torch_calls.cpp)."""
+    global _calls
+    if _calls is None:
+        L = lib()
+        if not os.path.exists(_build.TORCH_CALLS):
+            _build.build_torch_calls()
+        import torch  # noqa: F401  (its libraries have to be there)
+        loader = importlib.machinery.ExtensionFileLoader("_torch_calls", _build.TORCH_CALLS)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_torch_calls", loader))
+        loader.exec_module(module)
+        module.entries(*(C.cast(f, C.c_void_p).value for f in (L.fr_kv_append, L.fr_attend_shared, L.fr_sample)))
+        _calls = module
+    return _calls
 
 
 def _dtype(x):
     """FR_DTYPE_* of a torch tensor."""
-    code = _DTYPE_OF.get(_names[x.dtype])
-    if code is None:
-        raise TypeError("%s: the library takes bfloat16, float16 and float32" % _names[x.dtype])
-    return code
-
-
-def _typed(x, name, what, like=None):
-    """Address of a tensor whose elements lie side by side and are of a type the C side cannot see; 0 for None."""
-    if x is None:
-        return 0
-    if _names[x.dtype] != what or not x.is_contiguous() and x.stride(-1) != 1 and x.shape[-1] > 1:
-        raise TypeError("%s: %s elements side by side are needed" % (name, what))
-    if like is not None and x.shape != like:
-        raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(like), tuple(x.shape)))
-    return x.data_ptr()
-
-
-def _rows(x, name, shape, dtype):
-    """Stride between tokens of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
-    if x.shape != shape:
-        raise ValueError("%s: shape %s is needed, not %s" % (name, tuple(shape), tuple(x.shape)))
-    if x.dtype != dtype:
-        raise TypeError("%s: not of the cache's type" % name)
-    tokens, heads, dim = shape
-    if x.is_contiguous():
-        return heads * dim
-    t, h, e = x.stride()
-    if (dim > 1 and e != 1 or heads > 1 and h != dim) and x.numel():
-        raise ValueError("%s: heads of a token have to lie side by side" % name)
-    return t if tokens > 1 else heads * dim
-
-
-def _workspace(x):
-    return (0, 0) if x is None else (x.data_ptr(), x.nbytes)
+    name = str(x.dtype)[len("torch."):]
+    if name not in _DTYPE_OF:
+        raise TypeError("%s: the library takes bfloat16, float16 and float32" % name)
+    return _DTYPE_OF[name]
 
 
 class KvPages:
@@ -622,29 +600,12 @@ class KvPages:
         d.n_pages, d.n_kv_heads, d.page_size, d.head_dim = k.shape
         d.page_stride, d.head_stride, d.slot_stride = k.stride()[:3]
         d.dtype = _dtype(k)
-        self.desc, self.dtype = d, k.dtype
+        self.desc = d
         self._keep = (k, v)
 
 
 def fr_kv_append(cache, k, v, slot, q=None, q_out=None, position=None, rotary=None, style=FR_ROTARY_HALVES, stream=None):
-    c, dtype = cache.desc, cache.dtype
-    dim, T = c.head_dim, k.shape[0]
-    kv, n_q = (T, c.n_kv_heads, dim), 0
-    q_at = q_out_at = q_stride = q_out_stride = position_at = rotary_at = positions = rotary_dim = 0
-    if q is not None and q.shape[1]:
-        n_q = q.shape[1]
-        of_q = (T, n_q, dim)
-        q_at, q_stride, q_out_at, q_out_stride = q.data_ptr(), _rows(q, "q", of_q, dtype), q_out.data_ptr(), _rows(q_out, "q_out", of_q, dtype)
-    if rotary is not None:
-        if not rotary.is_contiguous():
-            raise ValueError("rotary: rows have to lie side by side")
-        rotary_at, (positions, rotary_dim) = _typed(rotary, "rotary", "float32"), rotary.shape
-        if rotary_dim:
-            position_at = _typed(position, "position", "int32", (T,))
-    d = fr_kv_append_desc.from_buffer_copy(_pack_append.pack(
-        bytes(c), k.data_ptr(), v.data_ptr(), q_at, q_out_at, _rows(k, "k", kv, dtype), _rows(v, "v", kv, dtype), q_stride, q_out_stride,
-        _typed(slot, "slot", "int64", (T,)), position_at, rotary_at, positions, rotary_dim, style, T, n_q, 0))
-    return _check(lib().fr_kv_append(C.byref(d), _stream(stream)), "fr_kv_append")
+    return _check((_calls or _torch_calls()).kv_append(bytes(cache.desc), k, v, slot, q, q_out, position, rotary, style, stream), "fr_kv_append")
 
 
 def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, max_q=1):
@@ -658,27 +619,8 @@ def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, 
 
 def fr_attend_shared(cache, q, out, pages, own_len, scale, prefix_len=0, max_own_len=0, prefix_pages=None, q_begin=None,
                      max_q=1, lse=None, workspace=None, stream=None):
-    c, dtype = cache.desc, cache.dtype
-    page = c.page_size
-    tokens, heads, _ = q.shape
-    n_seqs = tokens if q_begin is None else q_begin.shape[0] - 1
-    shape = (tokens, heads, c.head_dim)
-    if lse is not None and not lse.is_contiguous():
-        raise ValueError("lse: rows have to lie side by side")
-    if prefix_pages is not None and prefix_pages.numel() * page < prefix_len:
-        raise ValueError("prefix_pages: too few for prefix_len")
-    width = own_at = 0
-    if pages is not None:
-        if pages.dim() != 2 or pages.shape[0] != n_seqs or pages.shape[1] * page < max_own_len:
-            raise ValueError("pages: [n_seqs, at least max_own_len / page_size] is needed")
-        width = pages.stride(0) if n_seqs > 1 else pages.shape[1]
-        own_at = _typed(own_len, "own_len", "int32", (n_seqs,))
-    d = fr_attend_desc.from_buffer_copy(_pack_attend.pack(
-        bytes(c), q.data_ptr(), out.data_ptr(), _typed(lse, "lse", "float32", (tokens, heads)), _rows(q, "q", shape, dtype),
-        _rows(out, "out", shape, dtype), _typed(q_begin, "q_begin", "int32"), _typed(prefix_pages, "prefix_pages", "int32"),
-        _typed(pages, "pages", "int32"), own_at, width, tokens, n_seqs, heads, max_q, prefix_len, max_own_len, scale, 0,
-        *_workspace(workspace)))
-    return _check(lib().fr_attend_shared(C.byref(d), _stream(stream)), "fr_attend_shared")
+    return _check((_calls or _torch_calls()).attend_shared(bytes(cache.desc), q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages,
+                                                           q_begin, max_q, lse, workspace, stream), "fr_attend_shared")
 
 
 def fr_sample_workspace_bytes(logits):
@@ -690,13 +632,4 @@ def fr_sample_workspace_bytes(logits):
 
 
 def fr_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, stream=None):
-    n, vocab = logits.shape
-    stride, entry = logits.stride()
-    if vocab > 1 and entry != 1:
-        raise ValueError("logits: the entries of a row have to lie side by side")
-    like = (n,)
-    d = fr_sample_desc.from_buffer_copy(_pack_sample.pack(
-        logits.data_ptr(), stride if n > 1 else vocab, _dtype(logits), n, vocab, 0, _typed(temperature, "temperature", "float32", like),
-        _typed(top_k, "top_k", "int32", like), _typed(top_p, "top_p", "float32", like), _typed(min_p, "min_p", "float32", like),
-        _typed(uniform, "uniform", "float32", like), _typed(token, "token", "int32", like), *_workspace(workspace)))
-    return _check(lib().fr_sample(C.byref(d), _stream(stream)), "fr_sample")
+    return _check((_calls or _torch_calls()).sample(logits, uniform, token, temperature, top_k, top_p, min_p, workspace, stream), "fr_sample")

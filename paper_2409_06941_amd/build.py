@@ -1,11 +1,14 @@
-"""Builds libfreeride.so (HIP, gfx950) in-tree with hipcc."""
+"""Builds libfreeride.so (HIP, gfx950) in-tree with hipcc, and _torch_calls.so, which calls it with torch tensors, with the host's compiler."""
+import importlib.util
 import os
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfreeride.so")
+TORCH_CALLS = os.path.join(HERE, "_torch_calls.so")
 SOURCES = ["runtime.cpp", "stage.cpp", "pagerank.hip", "pagerank_prep.hip", "sgd.hip", "gemm.hip", "kv_append.hip", "attend.hip", "sample.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -51,5 +54,17 @@ def build(force: bool = True) -> str:
     return LIB
 
 
+def build_torch_calls() -> str:
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    tmp = TORCH_CALLS + ".tmp.%d" % os.getpid()
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"),
+                           "-isystem", os.path.join(torch, "include"), "-isystem", sysconfig.get_paths()["include"],
+                           os.path.join(CSRC, "torch_calls.cpp"), "-o", tmp,
+                           "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, TORCH_CALLS)
+    return TORCH_CALLS
+
+
 if __name__ == "__main__":
     print(build())
+    print(build_torch_calls())

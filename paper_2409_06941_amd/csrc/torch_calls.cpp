@@ -1,0 +1,277 @@
+// The calls of text generation from torch tensors: looks at the tensors, fills the descriptor, calls the library.
+//
+// A step of a few sequences has kernels of 4 to 8 us; looking at seven tensors from Python takes as long (0.1 us for every size, stride or
+// type that is asked for), from here less than one.  What a tensor shows and the C side cannot see is checked here: types, shapes,
+// elements that lie side by side, and that it is on a GPU.  The rest is the library's.
+
+#include <torch/csrc/autograd/python_variable.h>
+
+#include "freeride.h"
+
+namespace {
+
+struct Refused {};                         // (the Python error is set)
+
+template <typename... X> [[noreturn]] void refuse(PyObject* kind, const char* text, X... x)
+{
+    PyErr_Format(kind, text, x...);
+    throw Refused{};
+}
+
+int (*append)(const fr_kv_append_desc*, void*);
+int (*attend)(const fr_attend_desc*, void*);
+int (*sample)(const fr_sample_desc*, void*);
+
+bool given(PyObject* x) { return x != Py_None; }
+
+const at::Tensor& tensor(PyObject* x, const char* name)
+{
+    if (!THPVariable_Check(x)) refuse(PyExc_TypeError, "%s: a torch tensor is needed", name);
+    return THPVariable_Unpack(x);
+}
+
+int64_t whole(PyObject* x, const char* name, int64_t most = INT32_MAX)
+{
+    const long long y = PyLong_AsLongLong(x);
+    if (y == -1 && PyErr_Occurred()) throw Refused{};
+    if (y > most || y < -most - 1) refuse(PyExc_ValueError, "%s: %lld is out of range", name, y);
+    return y;
+}
+
+int32_t number(int64_t x, const char* name)
+{
+    if (x > INT32_MAX) refuse(PyExc_ValueError, "%s: %lld is out of range", name, (long long)x);
+    return (int32_t)x;
+}
+
+void* address(PyObject* stream)
+{
+    if (!given(stream)) return nullptr;
+    PyObject* y = PyLong_Check(stream) ? Py_NewRef(stream) : PyObject_GetAttrString(stream, "cuda_stream");
+    if (!y) throw Refused{};
+    void* p = PyLong_AsVoidPtr(y);
+    Py_DECREF(y);
+    if (!p && PyErr_Occurred()) throw Refused{};
+    return p;
+}
+
+at::ScalarType type_of(int32_t dtype) { return dtype == FR_DTYPE_BF16 ? at::kBFloat16 : dtype == FR_DTYPE_F16 ? at::kHalf : at::kFloat; }
+
+// The tensors of a call, to be looked at once more when everything else is right.
+struct Call {
+    const at::Tensor* seen[16];
+    const char* names[16];
+    int n = 0;
+
+    void* of(const at::Tensor& t, const char* name)
+    {
+        seen[n] = &t;
+        names[n++] = name;
+        return t.data_ptr();
+    }
+    // Elements of a type that the C side cannot see, side by side in the last dimension; shape: sizes that are needed.
+    template <typename P = void> P* typed(PyObject* x, const char* name, at::ScalarType type, std::initializer_list<int64_t> shape = {})
+    {
+        if (!given(x)) return nullptr;
+        const at::Tensor& t = tensor(x, name);
+        if (t.scalar_type() != type || (t.dim() && t.stride(-1) != 1 && t.size(-1) > 1))
+            refuse(PyExc_TypeError, "%s: %s elements side by side are needed", name, c10::toString(type));
+        if (shape.size() && !t.sizes().equals(shape)) refuse(PyExc_ValueError, "%s: another shape is needed", name);
+        return static_cast<P*>(of(t, name));
+    }
+    // [tokens, heads, dim], a token's heads side by side
+    void* rows(PyObject* x, const char* name, int64_t tokens, int64_t heads, int64_t dim, at::ScalarType type, int64_t& stride)
+    {
+        const at::Tensor& t = tensor(x, name);
+        if (!t.sizes().equals({tokens, heads, dim}))
+            refuse(PyExc_ValueError, "%s: shape (%lld, %lld, %lld) is needed", name, (long long)tokens, (long long)heads, (long long)dim);
+        if (t.scalar_type() != type) refuse(PyExc_TypeError, "%s: not of the cache's type", name);
+        if (t.numel() && ((dim > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != dim)))
+            refuse(PyExc_ValueError, "%s: heads of a token have to lie side by side", name);
+        stride = tokens > 1 ? t.stride(0) : heads * dim;
+        return of(t, name);
+    }
+    void workspace(PyObject* x, void*& p, uint64_t& bytes)
+    {
+        if (!given(x)) return;
+        const at::Tensor& t = tensor(x, "workspace");
+        p = of(t, "workspace");
+        bytes = t.nbytes();
+    }
+    void on_gpu() const
+    {
+        for (int i = 0; i < n; ++i)
+            if (!seen[i]->is_cuda()) refuse(PyExc_ValueError, "%s: not on a GPU", names[i]);
+    }
+};
+
+template <typename D> PyObject* made(int (*entry)(const D*, void*), const D& d, const Call& call, PyObject* stream)
+{
+    call.on_gpu();
+    void* s = address(stream);
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = entry(&d, s);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(code);
+}
+
+void cache_of(PyObject* bytes, fr_kv_pages& cache)
+{
+    if (!PyBytes_Check(bytes) || PyBytes_GET_SIZE(bytes) != sizeof(cache)) refuse(PyExc_TypeError, "cache: a KvPages is needed");
+    memcpy(&cache, PyBytes_AS_STRING(bytes), sizeof(cache));
+}
+
+// cache, k, v, slot, q, q_out, position, rotary, style, stream
+PyObject* of_append(PyObject* const* x)
+{
+    fr_kv_append_desc d = {};
+    Call call;
+    cache_of(x[0], d.cache);
+    const int64_t dim = d.cache.head_dim, heads = d.cache.n_kv_heads;
+    const at::ScalarType type = type_of(d.cache.dtype);
+    const at::Tensor& k = tensor(x[1], "k");
+    const int64_t tokens = k.dim() ? k.size(0) : 0;
+    d.n_tokens = number(tokens, "k");
+    d.k = call.rows(x[1], "k", tokens, heads, dim, type, d.k_stride);
+    d.v = call.rows(x[2], "v", tokens, heads, dim, type, d.v_stride);
+    d.slot = call.typed<int64_t>(x[3], "slot", at::kLong, {tokens});
+    if (given(x[4])) {
+        const at::Tensor& q = tensor(x[4], "q");
+        const int64_t n = q.dim() > 1 ? q.size(1) : 0;
+        d.n_q_heads = number(n, "q");
+        if (n) {
+            d.q = call.rows(x[4], "q", tokens, n, dim, type, d.q_stride);
+            d.q_out = call.rows(x[5], "q_out", tokens, n, dim, type, d.q_out_stride);
+        }
+    }
+    if (given(x[7])) {
+        const at::Tensor& t = tensor(x[7], "rotary");
+        if (t.dim() != 2 || !t.is_contiguous()) refuse(PyExc_ValueError, "rotary: [positions, rotary_dim], rows side by side, is needed");
+        d.rotary = call.typed<float>(x[7], "rotary", at::kFloat);
+        d.n_positions = number(t.size(0), "rotary");
+        d.rotary_dim = number(t.size(1), "rotary");
+        if (d.rotary_dim) d.position = call.typed<int32_t>(x[6], "position", at::kInt, {tokens});
+    }
+    d.style = (int32_t)whole(x[8], "style");
+    return made(append, d, call, x[9]);
+}
+
+// cache, q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages, q_begin, max_q, lse, workspace, stream
+PyObject* of_attend(PyObject* const* x)
+{
+    fr_attend_desc d = {};
+    Call call;
+    cache_of(x[0], d.cache);
+    const int64_t dim = d.cache.head_dim, page = d.cache.page_size;
+    const at::ScalarType type = type_of(d.cache.dtype);
+    const at::Tensor& q = tensor(x[1], "q");
+    if (q.dim() != 3) refuse(PyExc_ValueError, "q: [tokens, heads, head_dim] is needed");
+    const int64_t tokens = q.size(0), heads = q.size(1);
+    d.n_tokens = number(tokens, "q");
+    d.n_q_heads = number(heads, "q");
+    d.q = call.rows(x[1], "q", tokens, heads, dim, type, d.q_stride);
+    d.out = call.rows(x[2], "out", tokens, heads, dim, type, d.out_stride);
+    d.prefix_len = (int32_t)whole(x[6], "prefix_len");
+    d.max_own_len = (int32_t)whole(x[7], "max_own_len");
+    d.max_q = (int32_t)whole(x[10], "max_q");
+    d.scale = (float)PyFloat_AsDouble(x[5]);
+    if (PyErr_Occurred()) throw Refused{};
+    int64_t seqs = tokens;
+    if (given(x[9])) {
+        const at::Tensor& t = tensor(x[9], "q_begin");
+        if (t.dim() != 1 || t.size(0) < 1) refuse(PyExc_ValueError, "q_begin: [sequences + 1] is needed");
+        seqs = t.size(0) - 1;
+        d.q_begin = call.typed<int32_t>(x[9], "q_begin", at::kInt);
+    }
+    d.n_seqs = number(seqs, "q_begin");
+    if (given(x[11])) {
+        if (!tensor(x[11], "lse").is_contiguous()) refuse(PyExc_ValueError, "lse: rows have to lie side by side");
+        d.lse = call.typed<float>(x[11], "lse", at::kFloat, {tokens, heads});
+    }
+    if (given(x[8])) {
+        const at::Tensor& t = tensor(x[8], "prefix_pages");
+        if (t.dim() != 1 || t.numel() * page < d.prefix_len) refuse(PyExc_ValueError, "prefix_pages: too few for prefix_len");
+        d.prefix_pages = call.typed<int32_t>(x[8], "prefix_pages", at::kInt);
+    }
+    if (given(x[3])) {
+        const at::Tensor& t = tensor(x[3], "pages");
+        if (t.dim() != 2 || t.size(0) != seqs || t.size(1) * page < d.max_own_len)
+            refuse(PyExc_ValueError, "pages: [n_seqs, at least max_own_len / page_size] is needed");
+        d.pages = call.typed<int32_t>(x[3], "pages", at::kInt);
+        d.pages_stride = seqs > 1 ? t.stride(0) : t.size(1);
+        d.own_len = call.typed<int32_t>(x[4], "own_len", at::kInt, {seqs});
+    }
+    call.workspace(x[12], d.workspace, d.workspace_bytes);
+    return made(attend, d, call, x[13]);
+}
+
+// logits, uniform, token, temperature, top_k, top_p, min_p, workspace, stream
+PyObject* of_sample(PyObject* const* x)
+{
+    fr_sample_desc d = {};
+    Call call;
+    const at::Tensor& t = tensor(x[0], "logits");
+    if (t.dim() != 2) refuse(PyExc_ValueError, "logits: [rows, vocabulary] is needed");
+    const int64_t n = t.size(0), vocab = t.size(1);
+    if (vocab > 1 && t.stride(1) != 1) refuse(PyExc_ValueError, "logits: the entries of a row have to lie side by side");
+    const at::ScalarType type = t.scalar_type();
+    if (type != at::kBFloat16 && type != at::kHalf && type != at::kFloat)
+        refuse(PyExc_TypeError, "logits: the library takes bfloat16, float16 and float32");
+    d.dtype = type == at::kBFloat16 ? FR_DTYPE_BF16 : type == at::kHalf ? FR_DTYPE_F16 : FR_DTYPE_F32;
+    d.n_rows = number(n, "logits");
+    d.n_vocab = number(vocab, "logits");
+    d.row_stride = n > 1 ? t.stride(0) : vocab;
+    d.logits = call.of(t, "logits");
+    d.uniform = call.typed<float>(x[1], "uniform", at::kFloat, {n});
+    d.token = call.typed<int32_t>(x[2], "token", at::kInt, {n});
+    d.temperature = call.typed<float>(x[3], "temperature", at::kFloat, {n});
+    d.top_k = call.typed<int32_t>(x[4], "top_k", at::kInt, {n});
+    d.top_p = call.typed<float>(x[5], "top_p", at::kFloat, {n});
+    d.min_p = call.typed<float>(x[6], "min_p", at::kFloat, {n});
+    call.workspace(x[7], d.workspace, d.workspace_bytes);
+    return made(sample, d, call, x[8]);
+}
+
+// No C++ exception leaves: what was refused has its Python error set, anything else becomes one.
+template <PyObject* (*kCall)(PyObject* const*), int kArguments> PyObject* guarded(PyObject*, PyObject* const* x, Py_ssize_t n)
+{
+    if (n != kArguments) return PyErr_Format(PyExc_TypeError, "%d arguments are needed", kArguments);
+    try {
+        return kCall(x);
+    } catch (const Refused&) {
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown error");
+    }
+    return nullptr;
+}
+
+// the library's entries, as addresses: fr_kv_append, fr_attend_shared, fr_sample
+PyObject* entries(PyObject*, PyObject* const* x, Py_ssize_t n)
+{
+    void* p[3];
+    if (n != 3) return PyErr_Format(PyExc_TypeError, "3 arguments are needed");
+    for (int i = 0; i < 3; ++i)
+        if (!(p[i] = PyLong_AsVoidPtr(x[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "an address is needed");
+    append = reinterpret_cast<decltype(append)>(p[0]);
+    attend = reinterpret_cast<decltype(attend)>(p[1]);
+    sample = reinterpret_cast<decltype(sample)>(p[2]);
+    Py_RETURN_NONE;
+}
+
+template <typename F> PyCFunction method(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f)); }
+
+PyMethodDef methods[] = {
+    {"entries", method(entries), METH_FASTCALL, nullptr},
+    {"kv_append", method(guarded<of_append, 10>), METH_FASTCALL, nullptr},
+    {"attend_shared", method(guarded<of_attend, 14>), METH_FASTCALL, nullptr},
+    {"sample", method(guarded<of_sample, 9>), METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr},
+};
+PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__torch_calls() { return PyModule_Create(&module_def); }

@@ -160,6 +160,30 @@ def test_the_binding_refuses_tensors_the_library_cannot_read():
         fr.fr_sample(torch.zeros(3, 10, dtype=torch.int32), torch.zeros(3), n)
 
 
+def test_calls_refuse_host_memory_other_objects_and_numbers_out_of_range():
+    torch = pytest.importorskip("torch")
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    cache, x, slot = fr.KvPages(k, k.clone()), torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64)
+    q, n = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    pages, logits, u = torch.zeros(3, 1, dtype=torch.int32), torch.zeros(3, 10), torch.zeros(3)
+    for call in (lambda: fr.fr_kv_append(cache, x, x, slot), lambda: fr.fr_attend_shared(cache, q, q.clone(), pages, n, 0.1, max_own_len=8),
+                 lambda: fr.fr_sample(logits, u, n)):
+        with pytest.raises(ValueError, match="not on a GPU"):
+            call()
+    for call in (lambda: fr.fr_kv_append(cache, None, x, slot), lambda: fr.fr_kv_append(cache, x, x, 0), lambda: fr.fr_sample(logits, u, [0, 0, 0]),
+                 lambda: fr.fr_attend_shared(cache, 1, q, pages, n, 0.1), lambda: fr.fr_kv_append(cache, x, x, slot, q=q),
+                 lambda: fr.fr_attend_shared(cache, q, q.clone(), pages, n, "1")):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: fr.fr_attend_shared(cache, q, q.clone(), pages, n, 0.1, prefix_len=1 << 31),
+                 lambda: fr.fr_attend_shared(cache, q, q.clone(), pages, n, 0.1, max_q=-(1 << 40)),
+                 lambda: fr.fr_kv_append(cache, x, x, slot, style=1 << 33), lambda: fr.fr_kv_append(cache, x, x, slot, q=q, q_out=q[:, :3]),
+                 lambda: fr.fr_kv_append(cache, x, x, slot, rotary=torch.zeros(64)),
+                 lambda: fr.fr_attend_shared(cache, q, q.clone(), pages, n, 0.1, q_begin=torch.zeros(0, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_oracle_against_closed_forms():
     # a rotation keeps lengths and turns by the sum of two angles; pairs and halves are the same up to the order
     rng = np.random.default_rng(0)
