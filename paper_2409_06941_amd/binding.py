@@ -1,4 +1,5 @@
-"""ctypes declarations mirroring include/freeride.h, plus small object wrappers that only marshal arguments."""
+"""ctypes declarations mirroring include/freeride.h, plus small object wrappers that only marshal arguments (those of the text-generation
+calls, many tensors in a few microseconds, by way of csrc/torch_calls.cpp)."""
 import ctypes as C
 import importlib.machinery
 import importlib.util
