@@ -10,19 +10,19 @@
 // model's logits spread evenly (digits of a float's bits would put thousands of entries on one counter).
 //
 // A workgroup of 1024 threads takes a row (112 KB of LDS: one on a unit), and goes through it twice:
-//   first for the largest logit, of the row and of every thread's share, and for rows that are cut by mass alone for the share's mass,
-//   roughly;
-//   then, for rows that are cut by count or mass, to put the entries that can be kept into LDS, of the shares that have any.  The
-//   rank-th largest of the threads' own largest logits has at least `rank` entries above it, and seldom many more: with rank = top_k
-//   all of the first top_k are among them; how far down a cut by mass goes is estimated from the threads' largest logits, and the
+//   first for the largest logit, of the row and of every thread's share, the largest outside of the share's piece of 16 bytes that holds
+//   it, and for rows that are cut by mass alone the share's mass, roughly;
+//   then, for rows that are cut by count or mass, to put the entries that can be kept into LDS: for most shares that have any from the
+//   one piece alone.  The rank-th largest of the threads' two values has at least `rank` entries above it, and seldom many more: with
+//   rank = top_k all of the first top_k are among them; how far down a cut by mass goes is estimated from the same values, and the
 //   rough mass of the others says whether what is in LDS holds enough.  What is left happens in LDS.
 //   Rows that are not cut, or by weight alone, need the masses of runs of 512 pieces instead, and one run again.
 // Rows that none of this fits (many thousands of entries that can be kept, or as many equal ones, infinities) take the long way: a
 // histogram of the whole row, and the masses of runs together with the digit in which the kept entries end.
 //
-// What bounds it, at 256 rows of 131072 in 32 bits, 134 MB: the first pass 24 us, 5.6 TB/s, memory; greedy 28; top-k 50 38 and top-p
-// 0.9 48 the steps in LDS, each behind barriers that nothing fills; no cut 60, of which 35 the vector units at 131072 exps a unit, as
-// in the long way: 143 at temperature 1.3 and top-p 0.98, 117 for a flat row.  One row of 32768: 14 us, the steps one after another.
+// What bounds it, at 256 rows of 131072 in 32 bits, 134 MB: greedy 23 us, 5.8 TB/s, memory; top-k 50 31 and top-p 0.9 36 the steps in
+// LDS, each behind barriers that nothing fills; no cut 58, of which 35 the vector units at 131072 exps a unit, as in the long way: 144
+// at temperature 1.3 and top-p 0.98, 116 for a flat row.  One row of 32768: 13 us, the steps one after another.
 
 #include <cmath>
 #include <type_traits>
@@ -74,9 +74,9 @@ struct Scale {
 
 struct Found { uint32_t digit, count_before, count; uint64_t mass_before, mass; };
 
-// kRank: what is tried at most.  960 of 1024 threads have theirs above a line that about 2840 entries are above, so that 4096 have room;
-// top-k of 400, 700, 960: 52, 56, 63 us this way and 97 to 100 the long way; of 1000 it often fails, after 20 us.
-constexpr int kCandidates = 4096, kList = 1024, kRank = 960, kMostRuns = kBins;
+// kRank: what is tried at most.  1740 of the threads' 2048 values are above a line that about 2840 entries are above, so that 4096 have
+// room; top-k of 400, 1000, 1740: 39, 57, 65 us this way and 101 the long way.
+constexpr int kCandidates = 4096, kList = 1024, kRank = 1740, kMostRuns = kBins;
 constexpr uint32_t kNoMass = 1909;                     // from this digit on (29.83 and more below the top) masses are 0: 43 ln 2 = 29.81
 
 // A row of any alignment in pieces of 16 bytes: `head` entries up to the first such piece, `pieces` of kEach, `tail` entries.
@@ -91,6 +91,7 @@ template <typename T> struct Row {
         tail = V - head - pieces * kEach;
     }
     __device__ __forceinline__ float at(int i) const { return T::up(p[i]); }
+    __device__ __forceinline__ int lone(int j) const { return j < head ? j : n - tail - head + j; }      // entries outside of the pieces: head + tail
     struct Piece { float x[kEach]; };
     __device__ __forceinline__ uint4 bits(int v) const { return *reinterpret_cast<const uint4*>(p + head + v * kEach); }
     static __device__ __forceinline__ Piece unpacked(const uint4& b)
@@ -116,10 +117,7 @@ template <typename T> struct Row {
             for (int q = 0; q < kAtOnce; ++q)
                 if (v + q * kThreads < pieces) by(v + q * kThreads, unpacked(b[q]));
         }
-        if (tid < head + tail) {
-            const int i = tid < head ? tid : n - tail - head + tid;
-            one(i, at(i));
-        }
+        if (tid < head + tail) one(lone(tid), at(lone(tid)));
     }
     // every entry once: f(index, value)
     template <int kAtOnce = 1, typename F> __device__ __forceinline__ void each(int tid, F f) const
@@ -199,35 +197,65 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     const float p = a.top_p ? a.top_p[r] : 1.0f, u = a.uniform[r];
     float min_p = a.min_p ? a.min_p[r] : 0.0f;
     min_p = min_p > 1.0f ? 1.0f : min_p;
-    // First pass: the largest logit of the thread's share; for rows cut by mass alone also the share's mass, roughly, relative to
+    // First pass: the largest logit of the thread's share, the piece that it is in and the largest of the other pieces (an entry before
+    // or behind the pieces counts as one); for rows cut by mass alone also the share's mass, roughly, apart for that piece, relative to
     // `from` (which lags behind the largest by up to a factor of 2^8).  The error of a weight in it is below 2^-16 of the weight: of
     // the exponent's products, differences and constant |x| 5 / 2^24 with |x| <= 43 (where a weight still has a mass), of each exp 2^-23,
     // of sums of eight in 32 bits 2^-22, of up to six factors where `from` moves 2^-22 each.
     const bool by_mass = k == V && p < 1.0f && per_t > 0.0f && per_t < INFINITY;
-    float top = -INFINITY, from = -INFINITY;
+    float top = -INFINITY, second = -INFINITY, from = -INFINITY, top_mass = 0.0f;
+    int top_piece = -1;
     double others = 0.0;
     auto roughly = [&](float x) { return __builtin_amdgcn_exp2f(fmaxf((x - from) * to_exp2, -126.0f)); };         // (NaN: next to nothing)
+    auto note = [&](int v, float t) {
+        const bool more = t > top;                     // (NaN: passed over)
+        second = fmaxf(second, more ? top : t);
+        if (more) { top = t; top_piece = v; }
+        return more;
+    };
     if (by_mass) {
         const float slack = 8.0f / to_exp2;
-        auto add = [&](float t, auto sum) {
-            top = fmaxf(top, t);
+        auto add = [&](int v, float t, auto sum_of) {
             if (t > from + slack) {
-                others *= (double)__builtin_amdgcn_exp2f((from - t) * to_exp2);
+                const float f = __builtin_amdgcn_exp2f((from - t) * to_exp2);
+                others *= (double)f;
+                top_mass *= f;
                 from = t;
             }
-            others += (double)sum();
+            const float sum = sum_of();
+            const bool more = note(v, t);
+            others += (double)(more ? top_mass : sum);
+            if (more) top_mass = sum;
         };
-        row.template visit<4>(tid, [&](int, const typename Row<T>::Piece& y) {
-            add(Row<T>::top_of(y), [&] {
+        row.template visit<4>(tid, [&](int v, const typename Row<T>::Piece& y) {
+            add(v, Row<T>::top_of(y), [&] {
                 float sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
                 return sum;
             });
-        }, [&](int, float x) { add(fmaxf(x, -INFINITY), [&] { return roughly(x); }); });
+        }, [&](int, float x) { add(row.pieces + tid, x, [&] { return roughly(x); }); });
     } else {
-        row.template each<4>(tid, [&](int, float x) { top = fmaxf(top, x); });     // (fmaxf passes NaN over)
+        row.template visit<4>(tid, [&](int v, const typename Row<T>::Piece& y) { note(v, Row<T>::top_of(y)); }, [&](int, float x) { note(row.pieces + tid, x); });
     }
+    // room for n of every lane's: one addition a wavefront, all lanes there
+    auto room_for = [&](uint32_t& counter, uint32_t n) {
+        const uint32_t up_to_here = sum_up_to(n);
+        uint32_t to = 0;
+        if (lane == 63 && up_to_here) to = atomicAdd(&counter, up_to_here);
+        return (uint32_t)__builtin_amdgcn_readlane((int)to, 63) + up_to_here - n;
+    };
+    // f(index, value) for the entries of a piece; from row.pieces on a piece is an entry before or behind the others
+    auto look_into = [&](int v, auto f) {
+        if (v < row.pieces) {
+            const typename Row<T>::Piece y = row.piece(v);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) f(row.head + v * kEach + e, y.x[e]);
+        } else {
+            const int i = row.lone(v - row.pieces);
+            f(i, row.at(i));
+        }
+    };
     for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; top_count[x] = 0; run_mass[x] = 0; }
     if (tid < 10) filled[tid] = 0;
     const float my_top = top;
@@ -235,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     top = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), 63));
     if (lane == 0) wave_top[wave] = top;
     if (by_mass) {                                     // relative to the wavefront's largest
-        double sum = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
+        double sum = from > -INFINITY ? (others + (double)top_mass) * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
         sum = sum_up_to(sum);
         if (lane == 63) wave_others[wave] = sum;
     }
@@ -249,8 +277,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     }
     if (!(temperature > 0.0f)) {
         if (my_top == top) {
-            uint32_t lowest = 0xffffffffu;
-            row.template each<8>(tid, [&](int i, float x) { if (x == top) lowest = min(lowest, (uint32_t)i); });
+            uint32_t lowest = 0xffffffffu;             // (a share's pieces come in rising order, but for the lone entry)
+            look_into(top_piece, [&](int i, float x) { if (x == top) lowest = min(lowest, (uint32_t)i); });
+            if (tid < row.head + row.tail && row.at(row.lone(tid)) == top) lowest = min(lowest, (uint32_t)row.lone(tid));
             atomicMin(&shared_index, lowest);
         }
         __syncthreads();
@@ -361,21 +390,29 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         if (k == V && !by_mass) {
             last = min(last, (uint32_t)fminf(-64.0f * logf(min_p) + 1.0f, (float)last));       // (cut by weight alone)
         } else if (V > kCandidates) {
+            // (the largest in the lower half of a counter, the second pieces' in the upper)
             if (my_top > -INFINITY) atomicAdd(&top_count[scale.bin(my_top)], 1u);
+            if (second > -INFINITY) atomicAdd(&top_count[scale.bin(second)], 0x10000u);
             const Sums tops = scan(yes, no, top_count, nullptr);
+            auto noted = [](uint32_t c) { return (c & 0xffff) + (c >> 16); };
+            Sums both = tops;
+            both.c0 = noted(tops.c0), both.c1 = noted(tops.c1), both.before_c = noted(tops.before_c), both.all_c = noted(tops.all_c);
             uint32_t rank = (uint32_t)k;
             if (by_mass) {
-                // As many as hold the mass, going by the threads' largest: where c of 1024 threads have theirs above a line, about
-                // -1024 log(1 - c / 1024) entries are above it.  5 % more mass and four digits for what the estimate is off by: too few,
-                // and the row takes the long way, too many cost a little.  (Top-p 0.9: with no room 93 us, as it is 48, with 20 % and 16
-                // digits 67.)
-                auto entries = [](uint32_t c) { return -1024.0f * logf(1.0f - fminf((float)c, 1023.5f) / 1024.0f); };
+                // As many as hold the mass, going by the threads' values: where c of 1024 threads have their largest above a line, about
+                // -1024 log(1 - c / 1024) entries are above it, and as many as there are values above it at least.  5 % more mass and four
+                // digits for what the estimate is off by: too few, and the row takes the long way, too many cost a little.  (With the
+                // largest alone, where a thread may have two that count, top-p 0.9 took 48 us instead of 36; with no room 93, with 20 %
+                // and 16 digits 67.)
+                auto entries = [&](uint32_t c) {
+                    return fmaxf(-1024.0f * 0.69314718f * __builtin_amdgcn_logf(1.0f - fminf((float)(c & 0xffff), 1023.5f) / 1024.0f), (float)noted(c));
+                };
                 const float n0 = entries(tops.before_c), n1 = entries(tops.before_c + tops.c0), n2 = entries(tops.before_c + tops.c0 + tops.c1);
-                const float w0 = expf(-(float)(4 * tid + 1) / 128.0f), w1 = expf(-(float)(4 * tid + 3) / 128.0f);
-                double all = 0.0;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w)
-                    if (wave_top[w] > -INFINITY) all += wave_others[w] * (double)__builtin_amdgcn_exp2f((wave_top[w] - top) * to_exp2);
+                const float w0 = __builtin_amdgcn_exp2f(-(float)(4 * tid + 1) * (1.44269504f / 128.0f)), w1 = w0 * 0.98449644f;      // (of a digit's middle; exp(-1/64))
+                static_assert(kWaves == 16);
+                const float of_wave = wave_top[lane % kWaves];
+                const double in_wave = of_wave > -INFINITY ? wave_others[lane % kWaves] * (double)__builtin_amdgcn_exp2f((of_wave - top) * to_exp2) : 0.0;
+                const double all = __builtin_bit_cast(double, of_lane(__builtin_bit_cast(uint64_t, sum_up_to(in_wave)), 15));
                 __syncthreads();
                 const Sums held = scan_of(no, yes, 0, 0, (uint64_t)(fmaxf(n1 - n0, 0.0f) * w0 * 0x1p30f), (uint64_t)(fmaxf(n2 - n1, 0.0f) * w1 * 0x1p30f));
                 const uint64_t want = (uint64_t)fmin((double)p * all * 1.05 * 0x1p30, 0x1p62);
@@ -384,49 +421,81 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                     rank = V;
                 } else {
                     // As many as there is room for, and at once the long way if those will hold too little: if what is missing can be
-                    // entries below every thread's largest (else a thread has several of the largest: seldom, but one row is enough).
-                    // Flat rows 117 us; with the attempt 149.
-                    const float each = expf(-(float)find(tops, false, tops.all_c).digit / 64.0f) * 0x1p30f;
+                    // entries below all values (else a thread has several of the largest: seldom, but one row is enough).  Flat rows
+                    // 116 us; with the attempt 149.
+                    const float each = expf(-(float)find(both, false, both.all_c).digit / 64.0f) * 0x1p30f;
                     rank = kRank;
                     fits = (double)held.all_m >= 0.8 * (double)want || (double)(want - held.all_m) > (double)V * each;
                 }
             }
-            if (rank <= tops.all_c) last = min(last, find(tops, false, rank).digit);
+            if (rank <= both.all_c) last = min(last, find(both, false, rank).digit);
         }
         if (fits) {
             // Entries whose digit can be kept go to LDS.  A thread reads its share again if its largest is among them; the mass of the others
             // is known roughly, which seldom leaves open where the kept ones end.
             const float edge = (float)(last + 1), low = top - (edge / (64.0f * scale.per_t) * 1.0001f + fabsf(top) * 1e-6f);
-            others = from > -INFINITY ? others * (double)__builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0;
-            if (my_top >= low) others = 0.0;
+            const float scaled = from > -INFINITY ? __builtin_amdgcn_exp2f((from - top) * to_exp2) : 0.0f;
+            others *= (double)scaled;
             from = top;
-            auto take = [&](int i, float x) {
-                if ((top - x) * scale.per_t * 64.0f < edge) {                            // (false for NaN)
-                    const uint32_t to = atomicAdd(&filled[0], 1u);
-                    if (to < kCandidates) { cand_value[to] = x + 0.0f; cand_index[to] = (uint32_t)i; }
-                } else if (by_mass) {
-                    others += (double)roughly(x);
+            const bool is_hot = top_piece >= 0 && my_top >= low;
+            // The pieces that are looked into: those with the shares' largest, and all of a share whose second is among them too, or
+            // where that is too many, those that hold any, for which such shares are read again.
+            const bool all_of_it = is_hot && second >= low, lone = tid < row.head + row.tail;
+            const int share = (row.pieces - tid + kThreads - 1) / kThreads, n_hot = all_of_it ? max(share, 0) + (lone ? 1 : 0) : is_hot ? 1 : 0;
+            const int to = (int)room_for(filled[7], (uint32_t)n_hot);
+            if (to + n_hot <= kCandidates) {
+                if (all_of_it) {
+                    for (int j = 0; j < share; ++j) hot[to + j] = (uint32_t)(tid + j * kThreads);
+                    if (lone) hot[to + n_hot - 1] = (uint32_t)(row.pieces + tid);
+                } else if (is_hot) {
+                    hot[to] = (uint32_t)top_piece;
                 }
-            };
-            // (a piece with such an entry is looked into afterwards: nearly every wavefront meets some, few lanes do)
-            if (my_top >= low) row.template visit<8>(tid, [&](int v, const typename Row<T>::Piece& y) {
-                if (Row<T>::top_of(y) >= low) {
+            }
+            __syncthreads();
+            const bool many = (int)filled[7] > kCandidates;
+            if (!is_hot) others += (double)(top_mass * scaled);
+            else if (many || all_of_it) others = 0.0;
+            if (many) {
+                __syncthreads();
+                if (tid == 0) filled[7] = 0;
+                __syncthreads();
+                auto mark = [&](int v) {
                     const uint32_t to = atomicAdd(&filled[7], 1u);
                     if (to < kCandidates) hot[to] = (uint32_t)v;
-                } else if (by_mass) {
-                    float sum = 0.0f;
+                };
+                if (is_hot) row.template visit<8>(tid, [&](int v, const typename Row<T>::Piece& y) {
+                    if (Row<T>::top_of(y) >= low) {
+                        mark(v);
+                    } else if (by_mass) {
+                        float sum = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
-                    others += (double)sum;
-                }
-            }, take);
-            __syncthreads();
+                        for (int e = 0; e < kEach; ++e) sum += roughly(y.x[e]);
+                        others += (double)sum;
+                    }
+                }, [&](int, float) { mark(row.pieces + tid); });
+                __syncthreads();
+            }
             const int pieces = min((int)filled[7], kCandidates);
-            for (int i = tid; i < pieces; i += kThreads) {
-                const int v = (int)hot[i];
-                const typename Row<T>::Piece y = row.piece(v);
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) take(row.head + v * kEach + e, y.x[e]);
+            for (int i0 = 0; i0 < pieces; i0 += kThreads) {
+                const bool here = i0 + tid < pieces;
+                const int v = here ? (int)hot[i0 + tid] : 0;
+                float sum = 0.0f;
+                uint32_t bits = 0, bit = 1;
+                if (here) look_into(v, [&](int, float x) {
+                    if ((top - x) * scale.per_t * 64.0f < edge) bits |= bit;             // (false for NaN)
+                    else if (by_mass) sum += roughly(x);
+                    bit <<= 1;
+                });
+                others += (double)sum;
+                uint32_t to = room_for(filled[0], (uint32_t)__popc(bits));
+                bit = 1;
+                if (bits) look_into(v, [&](int j, float x) {
+                    if (bits & bit) {
+                        if (to < kCandidates) { cand_value[to] = x + 0.0f; cand_index[to] = (uint32_t)j; }
+                        ++to;
+                    }
+                    bit <<= 1;
+                });
             }
             if (by_mass) {
                 others = sum_up_to(others);
