@@ -21,8 +21,8 @@
 // histogram of the whole row, and the masses of runs together with the digit in which the kept entries end.
 //
 // What bounds it, at 256 rows of 131072 in 32 bits, 134 MB: greedy 23 us, 5.8 TB/s, memory; top-k 50 31 and top-p 0.9 36 the steps in
-// LDS, each behind barriers that nothing fills; no cut 58, of which 35 the vector units at 131072 exps a unit, as in the long way: 144
-// at temperature 1.3 and top-p 0.98, 116 for a flat row.  One row of 32768: 13 us, the steps one after another.
+// LDS, each behind barriers that nothing fills; no cut 51, of which 28 the vector units at 131072 exps a unit, as in the long way: 128
+// at temperature 1.3 and top-p 0.98, 108 for a flat row.  One row of 32768: 13 us, the steps one after another.
 
 #include <cmath>
 #include <type_traits>
@@ -62,9 +62,13 @@ struct Scale {
         if (x == -INFINITY) return 0.0f;
         return expf((x - top) * per_t);
     }
+    // the same of a row as usual, whose exponents are numbers or -infinity (NaN for NaN)
+    __device__ __forceinline__ float usual_weight(float x) const { return expf((x - top) * per_t); }
     // the mass as a float that is a whole number (from 2^24 on all floats are); 0 for NaN
-    __device__ __forceinline__ float whole_mass(float x) const { return fmaxf(floorf(weight(x) * kMassOne), 0.0f); }
+    static __device__ __forceinline__ float whole(float weight) { return fmaxf(floorf(weight * kMassOne), 0.0f); }
+    __device__ __forceinline__ float whole_mass(float x) const { return whole(weight(x)); }
     __device__ __forceinline__ uint64_t mass(float x) const { return (uint64_t)whole_mass(x); }
+    __device__ __forceinline__ uint64_t usual_mass(float x) const { return (uint64_t)whole(usual_weight(x)); }
     __device__ __forceinline__ uint32_t bin(float x) const
     {
         if (x == top) return 0;
@@ -75,7 +79,7 @@ struct Scale {
 struct Found { uint32_t digit, count_before, count; uint64_t mass_before, mass; };
 
 // kRank: what is tried at most.  1740 of the threads' 2048 values are above a line that about 2840 entries are above, so that 4096 have
-// room; top-k of 400, 1000, 1740: 39, 57, 65 us this way and 101 the long way.
+// room; top-k of 400, 1000, 1740: 39, 57, 65 us this way and 95 to 101 the long way.
 constexpr int kCandidates = 4096, kList = 1024, kRank = 1740, kMostRuns = kBins;
 constexpr uint32_t kNoMass = 1909;                     // from this digit on (29.83 and more below the top) masses are 0: 43 ln 2 = 29.81
 
@@ -311,7 +315,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     };
     auto add_up_row = [&] {                            // (a thread's masses: whole numbers, at most 520 of 2^43: exact in a double)
         double sum = 0.0;
-        row.template each<2>(tid, [&](int, float x) { sum += (double)scale.whole_mass(x); });
+        row.template each<2>(tid, [&](int, float x) { sum += (double)Scale::whole(scale.usual_weight(x)); });
         return add_up((uint64_t)sum);
     };
 
@@ -400,10 +404,11 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             uint32_t rank = (uint32_t)k;
             if (by_mass) {
                 // As many as hold the mass, going by the threads' values: where c of 1024 threads have their largest above a line, about
-                // -1024 log(1 - c / 1024) entries are above it, and as many as there are values above it at least.  5 % more mass and four
-                // digits for what the estimate is off by: too few, and the row takes the long way, too many cost a little.  (With the
-                // largest alone, where a thread may have two that count, top-p 0.9 took 48 us instead of 36; with no room 93, with 20 %
-                // and 16 digits 67.)
+                // -1024 log(1 - c / 1024) entries are above it, and as many as there are values above it at least.  5 % more mass (but
+                // 30 % less left out, at most) and four digits for what the estimate is off by: too few, and the row takes the long way,
+                // too many cost a little.  (With the largest alone, where a thread may have two that count, top-p 0.9 took 48 us instead
+                // of 36; with no room 93, with 20 % and 16 digits 67.  Top-p 0.96 and 0.98: with 5 % more always 68 us, 10 % less left out
+                // 53 and 81, 30 % 52 and 50, 50 % 53 and 48, and 64 bf16 rows 23, 24, 31.)
                 auto entries = [&](uint32_t c) {
                     return fmaxf(-1024.0f * 0.69314718f * __builtin_amdgcn_logf(1.0f - fminf((float)(c & 0xffff), 1023.5f) / 1024.0f), (float)noted(c));
                 };
@@ -415,14 +420,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 const double all = __builtin_bit_cast(double, of_lane(__builtin_bit_cast(uint64_t, sum_up_to(in_wave)), 15));
                 __syncthreads();
                 const Sums held = scan_of(no, yes, 0, 0, (uint64_t)(fmaxf(n1 - n0, 0.0f) * w0 * 0x1p30f), (uint64_t)(fmaxf(n2 - n1, 0.0f) * w1 * 0x1p30f));
-                const uint64_t want = (uint64_t)fmin((double)p * all * 1.05 * 0x1p30, 0x1p62);
+                const uint64_t want = (uint64_t)(fmin((double)p * 1.05, 1.0 - 0.7 * (1.0 - (double)p)) * all * 0x1p30);
                 if (want <= held.all_m) {
                     last = min(last, find(held, true, want).digit + 4);
                     rank = V;
                 } else {
                     // As many as there is room for, and at once the long way if those will hold too little: if what is missing can be
                     // entries below all values (else a thread has several of the largest: seldom, but one row is enough).  Flat rows
-                    // 116 us; with the attempt 149.
+                    // 108 us; with the attempt 33 more.
                     const float each = expf(-(float)find(both, false, both.all_c).digit / 64.0f) * 0x1p30f;
                     rank = kRank;
                     fits = (double)held.all_m >= 0.8 * (double)want || (double)(want - held.all_m) > (double)V * each;
@@ -507,7 +512,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             if (fits) {
                 auto digit_of = [&](int i) { return scale.bin(cand_value[i]); };
                 auto key_at = [&](int i) { return key_of(cand_value[i], cand_index[i]); };
-                auto mass_at = [&](int i) { return scale.mass(cand_value[i]); };
+                auto mass_at = [&](int i) { return scale.usual_mass(cand_value[i]); };
                 auto among = [&](int which, uint32_t digit, bool by_mass, uint64_t need) {
                     for (int i = tid; i < n; i += kThreads)
                         if (digit_of(i) == digit) list(which, key_at(i), mass_at(i));
@@ -551,7 +556,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 if (fits) {
                     auto kept = [&](int i) -> uint64_t {
                         const uint32_t d = digit_of(i);
-                        if (d > digit || (d == digit && key_at(i) < key) || scale.weight(cand_value[i]) < min_p) return 0;
+                        if (d > digit || (d == digit && key_at(i) < key) || scale.usual_weight(cand_value[i]) < min_p) return 0;
                         return mass_at(i);
                     };
                     // the same search along the index: 2048 runs of the vocabulary
@@ -583,13 +588,22 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         for (int x = tid; x < kBins; x += kThreads) { count[x] = 0; mass[x] = 0; }
         __syncthreads();
     };
+    const bool usual = scale.usual();
     auto histogram = [&](bool counts) {
         clear();
         row.template each<2>(tid, [&](int, float x) {
-            x = cleaned(x);
-            const uint32_t digit = scale.bin(x);
+            uint32_t digit;
+            uint64_t m;
+            if (usual) {                               // (NaN and -infinity in the last digit, without mass)
+                digit = (uint32_t)fminf((top - x) * per_t * 64.0f, (float)(kBins - 1));
+                m = scale.usual_mass(x);
+            } else {
+                x = cleaned(x);
+                digit = scale.bin(x);
+                m = scale.mass(x);
+            }
             if (counts) atomicAdd(&count[digit], 1u);
-            if (digit < kNoMass || !scale.usual()) atomicAdd((unsigned long long*)&mass[digit], (unsigned long long)scale.mass(x));
+            if (m) atomicAdd((unsigned long long*)&mass[digit], (unsigned long long)m);
         });
     };
     // as resolve, for a digit of the whole row: 51 bits of key in five digits
@@ -619,7 +633,6 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     // again.  (A thread's sum of whole numbers, 520 of 2^43 at most, is exact in a double.)
     constexpr int kLines = 8, kBatch = 16 / kEach;
     const int runs = (row.pieces + 64 * kLines - 1) / (64 * kLines), all = runs + 2;
-    const bool usual = scale.usual();
     auto sum_runs = [&](auto end_of, auto piece_of) {
         afresh();
         __syncthreads();
@@ -723,9 +736,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             } else if (!(Row<T>::top_of(y) < low)) {
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) {
-                    const float d = (top - y.x[e]) * per_t * 64.0f, w = expf((y.x[e] - top) * per_t), m = fmaxf(floorf(w * kMassOne), 0.0f);
+                    const float d = (top - y.x[e]) * per_t * 64.0f, w = scale.usual_weight(y.x[e]), m = Scale::whole(w);
                     any |= !(d < from_digit) && !(d >= behind);
-                    if (d < from_digit && !(w < min_p)) sum += (double)m;
+                    sum += (double)(d < from_digit && !(w < min_p) ? m : 0.0f);
                 }
             }
             if (any) {
@@ -780,21 +793,22 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     float low = fmaxf(min_p > 0.0f ? logf(min_p) - 0.001f : -30.0f, -30.0f);
     if (last_kept > -INFINITY && last_kept < INFINITY) low = fmaxf(low, (last_kept - top) * scale.per_t);
     const bool uncut = usual && last_kept == -INFINITY && !(min_p > 0.0f);
-    auto amount = [&](int i, float x) -> double {
-        const float w = usual ? expf((x - top) * scale.per_t) : scale.weight(cleaned(x));
-        const float m = fmaxf(floorf(w * kMassOne), 0.0f);
-        if (uncut) return (double)m;
-        return (x > last_kept || (x == last_kept && i <= last_index)) && !(w < min_p) ? (double)m : 0.0;
+    auto amount = [&](int i, float x) -> float {
+        const float w = usual ? scale.usual_weight(x) : scale.weight(cleaned(x));
+        return (x > last_kept || (x == last_kept && i <= last_index)) && !(w < min_p) ? Scale::whole(w) : 0.0f;
     };
     auto ends = [&](int s) -> double {                 // head (run 0) and tail (the last): an entry a lane
         const int n = s ? row.tail : row.head, i = s ? V - row.tail + lane : lane;
-        return lane < n ? amount(i, row.at(i)) : 0.0;
+        return lane < n ? (double)amount(i, row.at(i)) : 0.0;
     };
     auto in_piece = [&](int v, const typename Row<T>::Piece& y, double (&m)[kEach]) {      // (whole numbers below 2^53, added up exactly)
         double sum = 0.0;
-        if (!usual || (Row<T>::top_of(y) - top) * scale.per_t >= low) {
+        if (uncut) {
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) sum += m[e] = amount(row.head + v * kEach + e, y.x[e]);
+            for (int e = 0; e < kEach; ++e) sum += m[e] = (double)Scale::whole(scale.usual_weight(y.x[e]));
+        } else if (!usual || (Row<T>::top_of(y) - top) * scale.per_t >= low) {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) sum += m[e] = (double)amount(row.head + v * kEach + e, y.x[e]);
         } else {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) m[e] = 0.0;
