@@ -748,9 +748,9 @@ struct Plan {
 // 640 rows 322 -> 217; where the prefix is short it stays with the sequences (32 of 640 rows behind 512 keys 84; taken apart 134).
 struct Cost {
     double one, all;
-    int at_once;
-    explicit Cost(int D) : one(D == 128 ? 1.43 : 0.9), all(D == 128 ? 2.0 : 1.6), at_once(D == 128 ? 2 : 3) {}
-    static constexpr double kStart = 4.0, kJoin = 4.0, kBytesAUs = 4e6;
+    int at_once, dim;
+    explicit Cost(int D) : one(D == 128 ? 1.43 : 0.9), all(D == 128 ? 2.0 : 1.6), at_once(D == 128 ? 2 : 3), dim(D) {}
+    static constexpr double kStart = 4.0, kJoin = 4.0, kBytesAUs = 4e6, kRound = 0.6, kStartFew = 3.0, kBytesAgain = 12e6;
     double tile(double a_unit) const { return a_unit <= 1 ? one : one + (all - one) * (std::min(std::ceil(a_unit), (double)at_once) - 1) / (at_once - 1); }
     double workgroups(double blocks, double tiles, int cus) const
     {
@@ -763,6 +763,14 @@ struct Cost {
         const double a_unit = (blocks0 + blocks1) / cus, work = (blocks0 * tiles0 + blocks1 * tiles1) * all / at_once / cus;
         return std::max(work + 0.25 * all * tiles1, tile(a_unit) * std::max(tiles0, tiles1)) + kStart * std::ceil(a_unit / at_once);
     }
+    // Workgroups of four wavefronts with 16 rows, which take 32 keys each in a round: kRound us where a unit's memory keeps up, and no
+    // faster than memory is, or the caches for keys that every sequence reads again.
+    double few(double blocks, double tiles, double own_keys, double again, int cus) const
+    {
+        const double rounds = tiles / 2 * kRound;
+        return kStartFew + 0.5 * rounds + std::max(rounds * std::ceil(blocks / (at_once * cus)), reading(own_keys, cus) + again * dim * 4 / kBytesAgain);
+    }
+    double reading(double keys, int cus) const { return keys * dim * 4 / std::min(5.7e6, cus * 40e3); }
     static double join(int64_t parts, const fr_attend_desc& d)
     {
         return parts < 2 ? 0 : kJoin + (double)parts * d.n_tokens * d.n_q_heads * d.cache.head_dim * (2 * sizeof(float)) / kBytesAUs;
@@ -780,6 +788,7 @@ Plan plan(const fr_attend_desc& d, int cus)
     // 16 of 4000 52 and 52; 64 rows, 64 sequences of 250 keys 21.5 and 22, of 1000 79 and 49, 16 of 1000 28 and 25.
     constexpr int64_t kMostFew = 32;
     cus = std::min(cus, kUnits);
+    const Cost cost(d.cache.head_dim);
     auto finish = [&](Segment& s, int64_t items, int64_t at_once) {
         const int64_t groups = up(items, at_once), units = up(groups, kXcds) * s.row_tiles;
         s.items = (int)std::min<int64_t>(items, 0x7fffffff);
@@ -807,17 +816,12 @@ Plan plan(const fr_attend_desc& d, int cus)
     Segment &s = p.own, &shared = p.prefix;
     s.row_tiles = (int)up(seq_rows, rows_of(p.of_own));
     shared.row_tiles = (int)up(all_rows, rows_of(all_rows > kMostFew ? kWideRows : kFewRows));
-    // Few rows a sequence: the prefix is taken apart where reading it for every sequence costs more than two more launches' work and
-    // parts to join.  32 heads, 8 key heads, apart and by every sequence: 16 sequences behind 128 keys 11.8 and 9.4 us, behind 512 14.4
-    // and 14.0, behind 2048 16 and 23; 32 behind 512 16 and 18; 2 behind 2048 10.5 and 11.3, behind 8192 14 and 21.
-    bool share = d.prefix_len > 0 && d.n_seqs > 1 && (int64_t)d.n_seqs * d.prefix_len >= 8192;
+    bool share = d.prefix_len > 0 && d.n_seqs > 1;
+    const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
     if (p.of_own == kWideRows) {
         // row tiles that hold rows, half of a sequence's last one being empty
-        const Cost cost(d.cache.head_dim);
         const double tiles = std::min((double)d.n_seqs * s.row_tiles, all_rows / 128.0 + 0.5 * d.n_seqs) * heads;
-        const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
         auto alone = [&](int64_t parts, int64_t t) { return cost.workgroups(tiles * parts, (double)t, cus) + cost.join(parts, d); };
-        share = d.prefix_len > 0 && d.n_seqs > 1;
         double together = INFINITY;
         if (share) {
             if (d.max_own_len) cut(s, d.max_own_len, base, alone);
@@ -839,6 +843,17 @@ Plan plan(const fr_attend_desc& d, int cus)
         const int64_t splits = std::max<int64_t>(1, std::min(most, want));
         shared.split_len = (int)(up(up(d.prefix_len, splits), 64) * 64);
         shared.splits = (int)up(d.prefix_len, shared.split_len);
+        // Few rows a sequence: taken apart, the prefix is read once, but there are parts to join.  The estimate against 8192 or more keys
+        // in all, 32 heads with 8 key heads and 8 with one: 32 sequences behind 300 keys 15.5 -> 8.6 and 13.5 -> 8.3 us, 128 behind 300
+        // 22.5 either way and 14.5 -> 8.4, 4 behind 2000 11.7 -> 10.3 and 9.8 either way; of 64 behind 5000 (taken apart) 26 and 18, by
+        // every sequence 67 and 22.
+        const double tiles = shared.split_len / 64.0, own = (double)base * d.max_own_len;
+        const double together = (all_rows > kMostFew ? Cost::kStart + tiles * cost.tile((double)shared.row_tiles * heads * shared.splits / cus)
+                                                     : cost.few((double)heads * shared.row_tiles * shared.splits, tiles, (double)heads * d.prefix_len, 0, cus)) +
+                                cost.reading(own, cus) + cost.join(shared.splits + (own > 0 ? 1 : 0), d);
+        share = together < cut(s, (int64_t)d.prefix_len + d.max_own_len, base, [&](int64_t parts, int64_t t) {
+            return cost.few((double)base * parts, (double)t, own, (double)base * d.prefix_len, cus) + cost.join(parts, d);
+        });
     }
     if (share) {
         p.of_prefix = all_rows > kMostFew ? kWideRows : kFewRows;
@@ -850,28 +865,25 @@ Plan plan(const fr_attend_desc& d, int cus)
     s.first_part = shared.splits;
     if (keys || !share) {
         if (p.of_own == kFewRows) {
-            // Parts of 2048 keys, shorter ones while they give less than four workgroups a unit, none where the sequences alone give
-            // eight.  (8 sequences of up to 65536 keys: parts of 512 310 us, 1024 302, 2048 295, 4096 294.  Two or eight a unit instead of
-            // four: 8 of 10000 57 and 52, with four 52; 32 of 2000 39 and 44, with four 39.5; 1 of 60000 43 and 53, with four 45.)
-            const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
-            int64_t len = 2048;
-            if (base >= 8 * cus) len = std::max<int64_t>(keys, 1);
-            else
-                while (len > 128 && base * up(keys, len) < 4 * cus) len /= 2;
-            // Short caches: a wavefront an item, of 256 keys (128 where items are few, more where they are many), if there are items
-            // enough, and up to 2048 keys; where there are many, parts cost more than they give from a few hundred keys on.  8 key heads, a
-            // wavefront and a workgroup an item: 256 sequences of 64 keys 12 and 20 us, 64 of up to 1500 50 and 58, 16 of 1500 19 and 23;
-            // 64 of 4000 147 and 143, 256 of 400 53 and 50, of 1500 211 and 194; behind a prefix, 256 of 512 with 64 heads 95 and 98.
-            // Parts of 128 or 512 keys instead of 256 there: 96 and 92; 64 of up to 1500 behind 16384 73.4 and 77.1, with 256 73.5.
+            // (Against parts that give four workgroups a unit, of 128 keys at least: 8 sequences of 200 to 300 keys 8.9 -> 6.6 us, 12 of 2000
+            // 25 -> 21, 1 of 60000 47 -> 43, 128 of 4000 278 -> 261.)
+            cut(s, keys, base, [&](int64_t parts, int64_t t) {
+                return cost.few((double)base * parts, (double)t, (double)base * d.max_own_len, share ? 0 : (double)base * d.prefix_len, cus) +
+                       cost.join(parts + shared.splits, d);
+            });
+            // Short caches: a wavefront an item.  By themselves, where each unit has four of up to 256 keys: 256 sequences of 64 keys with 8 key
+            // heads 12 us, a workgroup an item 20, 128 of 200 17 and 19; of 400 50 either way, 64 of 200 12 and 10, of 800 28 and 25.
+            // Behind a prefix, whose workgroups take half of a unit, items of 256 keys (128 where they are few, more where they are many),
+            // if there are enough, of up to 2048 keys, 512 where there are many: 16 of 1500 20 and 23, 64 of 400 25 and 27, 256 of 64 30
+            // and 38, of 512 with 64 heads 95 and 98; 256 of 800 137 and 130.  64 of up to 1500 behind 16384: 73.5; in parts of 512 77.1.
             int64_t wave_len = base < cus ? 128 : 256;
             while (base * up(keys, wave_len) > (base < cus ? 4 : 16) * cus && wave_len < keys) wave_len *= 2;
             const bool enough = base >= cus / 2 && base * up(keys, wave_len) >= (base < cus ? 4 : 3) * cus / 2;
-            if (p.of_prefix != kFewRows && enough && keys <= (base < 4 * cus ? 2048 : share ? 512 : 256)) {
+            if (share ? p.of_prefix == kWideRows && enough && keys <= (base < 4 * cus ? 2048 : 512) : base >= 4 * cus && keys <= 256) {
                 p.of_own = kWaveRows;
-                len = wave_len;
+                s.split_len = (int)wave_len;
+                s.splits = (int)std::max<int64_t>(1, up(keys, wave_len));
             }
-            s.split_len = (int)len;
-            s.splits = (int)std::max<int64_t>(1, up(keys, len));
         }
         finish(s, (int64_t)d.n_seqs * heads * s.splits, p.of_own == kWaveRows ? kWaves : 1);
     } else {
