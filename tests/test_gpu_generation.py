@@ -366,6 +366,33 @@ def test_attend_questions_about_a_document(dt, Hq, Hk, D, page, P, own, new):
     _attend_case(dt, Hq, Hk, D, page, P, own, new, seed=P + len(own), spoil=math.nan)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("Hq,Hk,D,page,P,n,most,tokens", [
+    # few rows, a long prefix
+    (8, 8, 128, 16, 6000, 3, 77, 1),
+    (12, 6, 64, 8, 9000, 3, 77, 4),
+    (3, 3, 128, 16, 9000, 3, 0, 1),
+    # more, the prefix' rows in tiles of 128
+    (16, 8, 64, 16, 1500, 40, 200, 1),
+    (15, 5, 64, 8, 5001, 9, 300, 3),
+    (8, 8, 128, 16, 3000, 40, 9, 1),
+    (16, 8, 128, 32, 700, 64, 100, 1),
+    (8, 2, 64, 16, 1200, 70, 300, 2),
+    # many short ones by themselves, behind a few shared keys, and not quite as many
+    (8, 8, 64, 16, 0, 130, 200, 1),
+    (16, 16, 128, 16, 0, 70, 256, 2),
+    (8, 8, 128, 64, 40, 130, 150, 1),
+    (8, 8, 128, 16, 0, 60, 700, 1),
+])
+def test_attend_ways_to_cut_few_rows(dt, Hq, Hk, D, page, P, n, most, tokens):
+    print("attend ways", dt, Hq, Hk, D, page, P, n, most, tokens, flush=True)
+    rng = np.random.default_rng(P + n)
+    own = [int(x) for x in rng.integers(0, most + 1, n)]
+    own[0], own[-1] = most, min(1, most)
+    new = [min(max(1, x) if tokens == 1 else x, tokens) for x in own]
+    _attend_case(dt, Hq, Hk, D, page, P, own, new, seed=n, spoil=math.nan)
+
+
 def test_attend_on_another_stream_masked_and_captured():
     print("attend streams", flush=True)
     side = torch.cuda.Stream()
