@@ -738,12 +738,12 @@ struct Plan {
     int64_t blocks = 0;                    // of the larger grid
 };
 
-// What a call with tiles of 128 rows takes, roughly, in microseconds: enough to tell ways to cut it from one another.  A workgroup
+// What a call takes, roughly, in microseconds: enough to tell ways to cut it from one another.  A workgroup with tiles of 128 rows
 // needs `one` for a tile of 64 keys where it has a unit to itself and `all` where as many are on the unit as fit, and kStart to begin
 // and end; results of several parts are written, read and joined.  (1.43 and 2.0 are measured; those of head_dim 64 are about half of
 // that: with 0.7 and 1.1 three of 36 calls take 6 to 17 % longer, none is faster.)
-// Against parts of 128 to 2048 keys, as many as four workgroups a unit ask for, and the prefix gone through by every sequence from
-// 128 rows a sequence on, of 32 heads with 8 key heads: one sequence's 640 rows behind 8192 keys 70 -> 44 us, 2800 rows behind 512
+// Tiles of 128 rows, against parts of 128 to 2048 keys, as many as four workgroups a unit ask for, and the prefix gone through by every
+// sequence from 128 rows a sequence on, of 32 heads with 8 key heads: one sequence's 640 rows behind 8192 keys 70 -> 44 us, 2800 rows behind 512
 // 63 -> 34; 64 sequences' 96 rows against 250 keys 46 -> 24; 8 sequences' 160 rows behind 2048 shared keys 53 -> 33, 32 sequences'
 // 640 rows 322 -> 217; where the prefix is short it stays with the sequences (32 of 640 rows behind 512 keys 84; taken apart 134).
 struct Cost {
@@ -783,9 +783,9 @@ Plan plan(const fr_attend_desc& d, int cus)
     auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     const int64_t group = d.n_q_heads / d.cache.n_kv_heads, heads = d.cache.n_kv_heads;
     const int64_t tokens_a_seq = std::min(d.max_q, d.n_tokens), seq_rows = tokens_a_seq * group, all_rows = d.n_tokens * group;
-    // Rows of a sequence up to which tiles of 16 are taken, above, tiles of 128: several of those read the same keys, but do
-    // not wait for one another.  8 key heads, in tiles of 16 and of 128: 32 rows, 256 sequences of 64 keys 23 and 36 us, 4 of 1000 13.5 and 15.4,
-    // 16 of 4000 52 and 52; 64 rows, 64 sequences of 250 keys 21.5 and 22, of 1000 79 and 49, 16 of 1000 28 and 25.
+    // Rows of a sequence up to which tiles of 16 are taken, above, tiles of 128: several of those read the same keys, but do not wait
+    // for one another.  8 key heads, in tiles of 16 and of 128: 32 rows, 256 sequences of 64 keys 23 and 36 us, 4 of 1000 13.5 and
+    // 15.4, 16 of 4000 52 and 52; 64 rows, 64 sequences of 250 keys 21.5 and 22, of 1000 79 and 49, 16 of 1000 28 and 25.
     constexpr int64_t kMostFew = 32;
     cus = std::min(cus, kUnits);
     const Cost cost(d.cache.head_dim);
