@@ -457,10 +457,10 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 }
             }
             __syncthreads();
-            const bool many = (int)filled[7] > kCandidates;
+            const bool too_many = (int)filled[7] > kCandidates;
             if (!is_hot) others += (double)(top_mass * scaled);
-            else if (many || all_of_it) others = 0.0;
-            if (many) {
+            else if (too_many || all_of_it) others = 0.0;
+            if (too_many) {
                 __syncthreads();
                 if (tid == 0) filled[7] = 0;
                 __syncthreads();

@@ -100,8 +100,10 @@ struct Call {
     }
     void on_gpu() const
     {
-        for (int i = 0; i < n; ++i)
+        for (int i = 0; i < n; ++i) {
             if (!seen[i]->is_cuda()) refuse(PyExc_ValueError, "%s: not on a GPU", names[i]);
+            if (seen[i]->device() != seen[0]->device()) refuse(PyExc_ValueError, "%s: on another GPU than %s", names[i], names[0]);
+        }
     }
 };
 
