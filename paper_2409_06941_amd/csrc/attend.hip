@@ -296,6 +296,18 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
 #pragma unroll
         for (int y = 0; y < kLoads; ++y) load16_to_lds(to + y * 1024, from + piece(l, y) * 8 + row[y]);
     };
+    // Rows of V that came to LDS for a wavefront, from key `first` on: those behind the last key (which stand for it) become zeros.  Their
+    // weights are 0, but 0 times a value that is not finite is not.
+    typedef __attribute__((address_space(3))) f32x4* LdsFloats;
+    auto blank = [&](uint32_t at, int first) {
+        if (first + kLoadRows <= w.k1) return;
+        const uint32_t l = anew(lane);
+        const float zero = __uint_as_float(anew(0));
+#pragma unroll 1
+        for (int y = 0; y < kLoads; ++y)
+            if (first + y * (int)L::kRowsALoad + (int)(l / L::kChunks) >= w.k1) *reinterpret_cast<LdsFloats>(lds_at(at + l * 16) + y * 1024) = f32x4{zero, zero, zero, zero};
+        wait_lds();
+    };
     auto k_piece = [](uint32_t l, int y) { return L::k_piece(l, y); };
     auto v_piece = [](uint32_t l, int y) { return L::v_piece(l, y); };
     const uint16_t* gk = static_cast<const uint16_t*>(a.c.k) + w.kv * a.c.head_stride;
@@ -322,6 +334,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
             float top = -INFINITY;
             auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2], int t, auto here, auto other) {      // (here: t modulo 2)
                 wait_loads<0>();
+                if (t + 1 == tiles) blank(lds + (2 + here) * kHalf + wave * 16 * L::kRow, w.k0 + t * kTile + wave * 16);
                 __syncthreads();                            // K of t + 1 and V of t are here; K of t and V of t - 1 are done with
                 if (!idle) {
                     asm volatile("" : "+v"(fragments.k), "+v"(fragments.v));        // (one register each, not one for every fragment)
@@ -429,8 +442,12 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
                 for (int f = 0; f < D / 32; ++f)
 #pragma unroll
                     for (int b = 0; b < 2; ++b) s[b] = mfma(kf[b][f], x.q[f], s[b]);
-                if (more) wait_loads<kLoads>();
-                else wait_loads<0>();
+                if (more) {
+                    wait_loads<kLoads>();
+                } else {
+                    wait_loads<0>();
+                    blank(v, first_of(t));
+                }
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) vf[d] = fragments.of_v(kHalf, d);
                 wait_lds();
@@ -491,7 +508,6 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
 
     // results through LDS, so that rows are written whole: a wavefront's rows of D floats, 16-byte chunk c of row r at c ^ r
     __shared__ float2 row_ml[kWaves][kCols];
-    typedef __attribute__((address_space(3))) f32x4* LdsFloats;
     constexpr uint32_t kFloatRow = D * 4, kFloatChunks = D / 4;
     auto meet = [] {
         if constexpr (!kAlone) __syncthreads();

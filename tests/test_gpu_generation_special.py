@@ -1,0 +1,130 @@
+"""Values that are not finite, small weights, tokens outside of a call, large calls and shared workspaces of the text-generation operators."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import paper_2409_06941_amd as fr              # noqa: E402
+from oracle import generation as oracle        # noqa: E402
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+UNIT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}          # half an ulp of 8 and of 11 significant bits
+TINY = {"bf16": 2.0 ** -133, "f16": 2.0 ** -25}        # half the smallest subnormal
+
+
+def _f64(x):
+    return x.detach().double().cpu().numpy()
+
+
+class _Batch:
+    """A cache with sequences of own[b] keys and new[b] tokens behind P shared keys; pages in any order."""
+
+    def __init__(self, dt, Hq, Hk, D, page, P, own, new, seed):
+        g = torch.Generator().manual_seed(seed)
+        self.dt, self.Hq, self.Hk, self.D, self.page, self.P, self.own, self.new = dt, Hq, Hk, D, page, P, own, new
+        prefix_pages, counts = -(-P // page), [-(-x // page) for x in own]
+        pages = prefix_pages + sum(counts) + 2
+        self.k, self.v = (torch.randn((pages, Hk, page, D), generator=g).to(DT[dt]) for _ in range(2))
+        order = torch.randperm(pages, generator=g).to(torch.int32)
+        self.prefix_pages = order[:prefix_pages].contiguous()
+        self.table = torch.zeros((len(own), max(1, max(counts))), dtype=torch.int32)
+        at = prefix_pages
+        for b, c in enumerate(counts):
+            self.table[b, :c] = order[at:at + c]
+            at += c
+        self.begin = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        self.q = torch.randn((int(self.begin[-1]), Hq, D), generator=g).to(DT[dt])
+        self.scale = D ** -0.5
+
+    def place(self, b, j):
+        """Page and slot of key j that sequence b sees (counted through the prefix)."""
+        own = j - self.P
+        return (int(self.prefix_pages[j // self.page]), j % self.page) if own < 0 else (int(self.table[b, own // self.page]), own % self.page)
+
+    def prepare(self):
+        self.gk, self.gv, self.gq = self.k.cuda(), self.v.cuda(), self.q.cuda()
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        self.cache = fr.KvPages(self.gk, self.gv)
+        self.out = torch.full_like(self.gq, 9.0)
+        self.lse = torch.full(self.q.shape[:2], 9.0, device="cuda")
+        self.limits = dict(prefix_len=self.P, max_own_len=max(self.own), max_q=max(max(self.new), 1))
+        need = fr.fr_attend_shared_workspace_bytes(self.cache, self.gq, len(self.own), **self.limits)
+        self.workspace = torch.full((max(need, 1),), 255, dtype=torch.uint8, device="cuda")
+        self.args = (self.table.cuda() if max(self.own) else None, i32(self.own))
+        self.more = dict(prefix_pages=self.prefix_pages.cuda() if self.P else None, q_begin=i32(self.begin))
+        return self
+
+    def call(self):
+        fr.fr_attend_shared(self.cache, self.gq, self.out, *self.args, self.scale, lse=self.lse, workspace=self.workspace,
+                            stream=torch.cuda.current_stream(), **self.more, **self.limits)
+
+    def check(self):
+        """Every row against the oracle: the same infinities, NaN where it has NaN, near it elsewhere."""
+        self.prepare()
+        self.call()
+        torch.cuda.synchronize()
+        q, k, v, out, lse = (_f64(x) for x in (self.q, self.k, self.v, self.out, self.lse))
+        u, G = UNIT[self.dt], self.Hq // self.Hk
+        for b in range(len(self.own)):
+            places = np.array([self.place(b, j) for j in range(self.P + self.own[b])], dtype=np.int64).reshape(-1, 2)
+            for h in range(self.Hq):
+                kk, vv = k[places[:, 0], h // G, places[:, 1]], v[places[:, 0], h // G, places[:, 1]]
+                for i in range(self.new[b]):
+                    n, row = oracle.visible(self.P, self.own[b], self.new[b], i), int(self.begin[b]) + i
+                    with np.errstate(invalid="ignore"):
+                        o, l, _, x = oracle.attend_row(q[row, h], kk[:n], vv[:n], self.scale)
+                        at = (b, i, h, n)
+                        assert np.array_equal(np.isnan(out[row, h]), np.isnan(o)), at
+                        inf = np.isinf(o)
+                        assert np.array_equal(np.isinf(out[row, h]), inf) and np.array_equal(out[row, h][inf], o[inf]), at
+                        there = np.isfinite(o)
+                        if n == 0:
+                            assert not out[row, h].any() and lse[row, h] == -math.inf, at
+                            continue
+                        # scores: sums of D products of 32 bits; a weight is off by that, by a few ulps of exp and by the type's rounding;
+                        # sums of n of them; the result's rounding.  Weights of 16 bits end at half the smallest subnormal.
+                        finite = np.where(np.isfinite(vv[:n]), vv[:n], 0.0)
+                        e = np.exp(self.scale * (kk[:n] @ q[row, h]) - l)
+                        d = (self.D + 4) * 2.0 ** -24 * x + 2.0 ** -20
+                        near = (u + 2 * d + n * 2.0 ** -23) * (e @ np.abs(finite)) + u * np.abs(np.where(there, o, 0.0)) * 1.01 + TINY[self.dt]
+                        near = near + (n * 2.0 ** -25 * np.abs(finite).max() if self.dt == "f16" else 0.0)
+                    assert np.all(np.abs(out[row, h] - o)[there] <= near[there]), at
+                    assert abs(lse[row, h] - l) <= d + n * 2.0 ** -23 + 2.0 ** -20 * (1 + abs(l)), at
+
+
+# the kinds of work that a call is made of: few rows and many, by themselves and behind a prefix, in one part and in several
+KINDS = [
+    (8, 2, 128, 16, 0, [50, 1, 33], [1, 1, 1]),
+    (4, 2, 64, 16, 0, [5001, 70], [1, 1]),
+    (8, 8, 64, 16, 0, [int(x) for x in 1 + np.arange(130) * 7 % 199], [1] * 130),
+    (8, 2, 128, 16, 37, [50, 0, 33], [1, 1, 1]),
+    (8, 8, 128, 16, 6001, [77, 3, 0], [1, 1, 1]),
+    (16, 8, 64, 16, 1501, [int(x) for x in 1 + np.arange(40) * 13 % 197], [1] * 40),
+    (16, 8, 128, 32, 701, [int(x) for x in 1 + np.arange(64) * 7 % 99], [1] * 64),
+    (8, 8, 128, 16, 3001, [0] * 40, [1] * 40),
+    (8, 2, 64, 16, 37, [40, 9, 0], [5, 9, 0]),
+    (6, 2, 128, 16, 0, [130, 70], [130, 70]),
+    (4, 2, 64, 16, 100, [150, 9, 260], [70, 9, 33]),
+    (4, 1, 128, 16, 8203, [50, 61], [41, 40]),
+]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("kind", range(len(KINDS)))
+def test_infinite_values_that_are_seen_stay_what_they_are(dt, kind):
+    Hq, Hk, D, page, P, own, new = KINDS[kind]
+    print("attend infinite", dt, *KINDS[kind][:5], len(own), flush=True)
+    c = _Batch(dt, Hq, Hk, D, page, P, own, new, seed=kind)
+    ends = [(b, P + n - 1) for b, n in enumerate(own) if n] + ([(0, P - 1)] if P else [])
+    for b, j in ends:                                  # the last key of a sequence, and of the prefix
+        page_, slot = c.place(b, j)
+        c.v[page_, :, slot, 3], c.v[page_, :, slot, 5], c.v[page_, :, slot, 40] = math.inf, -math.inf, math.nan
+    first = [(b, 0) for b in range(1)] if P else [(b, 0) for b, n in enumerate(own) if n > 2]
+    for b, j in first:                                 # the first key: the same sign, and another one
+        page_, slot = c.place(b, j)
+        c.v[page_, :, slot, 3], c.v[page_, :, slot, 5], c.v[page_, :, slot, 21] = math.inf, math.inf, -math.inf
+    c.check()
