@@ -303,7 +303,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         if (first + kLoadRows <= w.k1) return;
         const uint32_t l = anew(lane);
         const float zero = __uint_as_float(anew(0));
-#pragma unroll 1
+#pragma unroll
         for (int y = 0; y < kLoads; ++y)
             if (first + y * (int)L::kRowsALoad + (int)(l / L::kChunks) >= w.k1) *reinterpret_cast<LdsFloats>(lds_at(at + l * 16) + y * 1024) = f32x4{zero, zero, zero, zero};
         wait_lds();
@@ -475,32 +475,109 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
             }
         }
 
-        // A weight of 0 for a key that a row does not see, times a value that is not finite, is not 0: where rows of a workgroup see
-        // different keys and a result is not finite, the row's sum is made again from the keys it sees, one after the other.
+        // A weight of 0 for a key that a row does not see, times a value that is not finite, is not 0.  Keys from `hidden` on are not
+        // seen by every row of the workgroup: where a result is not finite and one of them has such a value, the sums are made again,
+        // with zeros for these values, and what they are to the rows that see them is added.  Fragments come straight from memory, V an
+        // element at a time, so that it takes the keys three times as long as the loop above, once; where all that is not finite is seen
+        // by every row, nothing is made again.
+        const int hidden = w.seen_step ? max(w.k0, min(rows.seen(w.row0), w.k1)) : w.k1;
+        auto place_of = [&](int j) {                        // (of a key behind the last: that of the last)
+            j = min(j, w.k1 - 1);
+            const int in = j < a.prefix_len ? j : j - a.prefix_len;
+            const int32_t id = within(j < a.prefix_len ? a.prefix_pages[in >> a.page_shift] : w.own_pages[in >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
+            return (uint64_t)(uint32_t)id * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)(in & (a.c.page_size - 1)) * (uint32_t)a.c.slot_stride;
+        };
+        // keys of j .. j + 63 from `hidden` on with values that are not finite, a bit each
+        auto spoilt = [&](int j) {
+            j += (int)anew(lane);
+            bool any = false;
+            if (j < w.k1) {
+                const uint16_t* y = gv + place_of(j);
+#pragma unroll 1
+                for (int e = 0; e < D; e += 8) {
+                    const uint4 b = *reinterpret_cast<const uint4*>(y + e);
+                    any |= !T::both_finite(b.x) || !T::both_finite(b.y) || !T::both_finite(b.z) || !T::both_finite(b.w);
+                }
+            }
+            return __ballot(any);
+        };
         bool bad = false;
-        if (w.seen_step) {
+        if (hidden < w.k1 && !idle) {
 #pragma unroll
             for (int d = 0; d < D / kCols; ++d)
 #pragma unroll
                 for (int i = 0; i < State::kInBlock; ++i) bad |= !(fabsf(x.o[d][i]) < INFINITY);
         }
-        if (__any(bad && !idle) && !idle) {
+        if (__any(bad)) {
+            bad = false;
+            for (int j = hidden; j < w.k1; j += 64) bad |= spoilt(j) != 0;
+        }
+        if (__any(bad)) {
             const float base = x.base(c);
+            x.clear();
+            constexpr int kBlocks = 32 / kCols, kInRow = 512 / kCols;       // blocks of 32 keys; keys of a fragment of weights
+#pragma unroll 1
+            for (int j0 = w.k0; j0 < w.k1; j0 += 32) {
+                if (kKind == kFewRows && (j0 - w.k0) / 32 % kWaves != wave) continue;
+                typename State::Block s[kBlocks];
+                uint32_t p[8];
+#pragma unroll
+                for (int y = 0; y < kBlocks; ++y) {
+#pragma unroll
+                    for (int i = 0; i < State::kInBlock; ++i) s[y][i] = 0.0f;
+                    const uint16_t* k = gk + place_of(j0 + y * kCols + lane % kCols) + lane / kCols * 8;
+#pragma unroll
+                    for (int f = 0; f < D / kInRow; ++f) s[y] = mfma(__builtin_bit_cast(typename T::x8, *reinterpret_cast<const uint4*>(k + f * kInRow)), x.q[f], s[y]);
+#pragma unroll
+                    for (int i = 0; i < State::kInBlock; i += 2) {
+                        float wt[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) wt[e] = j0 + y * kCols + State::in_block(i + e, lane) < end ? __builtin_amdgcn_exp2f(fmaf(s[y][i + e], c, -base)) : 0.0f;
+                        p[(y * State::kInBlock + i) / 2] = T::pack(wt[0], wt[1]);
+                    }
+                }
+#pragma unroll
+                for (int f = 0; f < 32 / kInRow; ++f) {
+                    uint64_t at[8];
+                    int j[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int r = f * 8 + e;                            // the score's register, through the blocks
+                        j[e] = j0 + r / State::kInBlock * kCols + State::in_block(r % State::kInBlock, lane);
+                        at[e] = place_of(j[e]) + lane % kCols;
+                    }
+#pragma unroll
+                    for (int d = 0; d < D / kCols; ++d) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {
+                            const uint32_t y = (uint32_t)gv[at[e] + d * kCols] | (uint32_t)gv[at[e + 1] + d * kCols] << 16;
+                            v[e / 2] = T::finite_or_0(y, j[e] >= hidden, j[e + 1] >= hidden);
+                        }
+                        x.o[d] = mfma(State::fragment(v), State::fragment(p + 4 * f), x.o[d]);
+                    }
+                }
+            }
             const int mine = min(row_first + (int)(anew(lane) % kCols), w.rows - 1);
             const uint16_t* q = a.q + rows.token(mine) * a.q_stride + (int64_t)rows.head(mine) * D;
-            x.clear();
-            for (int j = w.k0; j < end; ++j) {
-                if (kKind == kFewRows && (j - w.k0) / 32 % kWaves != wave) continue;
-                const int in = j < a.prefix_len ? j : j - a.prefix_len;
-                const int32_t id = within(j < a.prefix_len ? a.prefix_pages[in >> a.page_shift] : w.own_pages[in >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
-                const int64_t at = (int64_t)id * a.c.page_stride + (int64_t)(in & (a.c.page_size - 1)) * a.c.slot_stride;
-                float s = 0.0f;
-                for (int e = 0; e < D; ++e) s = fmaf(T::up(q[e]), T::up(gk[at + e]), s);
-                const float p = T::up((uint16_t)T::pack(__builtin_amdgcn_exp2f(fmaf(s, c, -base)), 0.0f));
+#pragma unroll 1
+            for (int j0 = hidden; j0 < w.k1; j0 += 64) {
+#pragma unroll 1
+                for (uint64_t left = spoilt(j0); left; left &= left - 1) {
+                    const int j = j0 + __ffsll((unsigned long long)left) - 1;
+                    if (kKind == kFewRows && (j - w.k0) / 32 % kWaves != wave) continue;
+                    const uint64_t at = place_of(j);
+                    float s = 0.0f;
+                    for (int e = 0; e < D; ++e) s = fmaf(T::up(q[e]), T::up(gk[at + e]), s);
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s, c, -base));
 #pragma unroll
-                for (int d = 0; d < D / kCols; ++d)
+                    for (int d = 0; d < D / kCols; ++d)
 #pragma unroll
-                    for (int i = 0; i < State::kInBlock; ++i) x.o[d][i] = fmaf(p, T::up(gv[at + d * kCols + State::in_block(i, lane)]), x.o[d][i]);
+                        for (int i = 0; i < State::kInBlock; ++i) {
+                            const float y = T::up(gv[at + d * kCols + State::in_block(i, lane)]);
+                            if (!(fabsf(y) < INFINITY) && j < end) x.o[d][i] = fmaf(p, y, x.o[d][i]);
+                        }
+                }
             }
         }
     }

@@ -8,7 +8,18 @@
 #include "freeride.h"
 
 // Two 16-bit types and float, by the codes of the C ABI: what a kernel loads, and how it goes to 32 bits and back (nearest even).
-struct Bf16 {
+// Two numbers of 16 bits, kOnes being their exponents' bits: whether both are finite; with 0 for one that is not, where asked for.
+template <uint32_t kOnes> struct Finite {
+    static __device__ __forceinline__ bool both_finite(uint32_t w) { return (w & kOnes) != kOnes && (w & kOnes << 16) != kOnes << 16; }
+    static __device__ __forceinline__ uint32_t finite_or_0(uint32_t w, bool lo, bool hi)
+    {
+        if (lo && (w & kOnes) == kOnes) w &= 0xffff0000u;
+        if (hi && (w & kOnes << 16) == kOnes << 16) w &= 0xffffu;
+        return w;
+    }
+};
+
+struct Bf16 : Finite<0x7f80> {
     typedef uint16_t Bits;
     typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 x8;
     static __device__ __forceinline__ float up(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
@@ -21,7 +32,7 @@ struct Bf16 {
     }
 };
 
-struct F16 {
+struct F16 : Finite<0x7c00> {
     typedef uint16_t Bits;
     typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 x8;
     static __device__ __forceinline__ float up(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }

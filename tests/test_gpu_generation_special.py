@@ -128,3 +128,36 @@ def test_infinite_values_that_are_seen_stay_what_they_are(dt, kind):
         page_, slot = c.place(b, j)
         c.v[page_, :, slot, 3], c.v[page_, :, slot, 5], c.v[page_, :, slot, 21] = math.inf, math.inf, -math.inf
     c.check()
+
+
+@pytest.mark.parametrize("D,G,P,t", [(128, 2, 50, 5), (64, 4, 50, 40), (128, 4, 0, 90), (128, 1, 300, 200), (64, 8, 4000, 3)])
+def test_values_that_only_later_tokens_see(D, G, P, t):
+    print("attend later", D, G, P, t, flush=True)
+    c = _Batch("bf16", 2 * G, 2, D, 16, P, [t + 20, 7], [t, 1], seed=t)
+    for back, e, x in ((1, 3, math.inf), (2, 4, math.nan), (3, 3, -math.inf), (t // 2, 9, math.inf), (t, 10, -math.inf), (t + 5, 11, math.inf)):
+        page, slot = c.place(0, P + t + 20 - back)
+        c.v[page, :, slot, e] = x
+    c.check()
+
+
+def test_a_value_that_is_not_finite_does_not_make_a_call_long():
+    # 4 questions about a document that they go through themselves, with one bad value in the document, and one in the questions
+    def us(spoil):
+        c = _Batch("bf16", 16, 4, 128, 16, 4096, [300, 280, 310, 290], [300, 280, 310, 290], seed=2)
+        for b, j in spoil:
+            page, slot = c.place(b, j)
+            c.v[page, :, slot, 17] = math.nan
+        c.prepare()
+        c.call()
+        torch.cuda.synchronize()
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        begin.record()
+        for _ in range(10):
+            c.call()
+        end.record()
+        torch.cuda.synchronize()
+        return begin.elapsed_time(end) * 100
+    clean, document, question = us([]), us([(0, 5)]), us([(1, 4096 + 100)])
+    print("clean %.0f us, a bad value in the document %.0f, in a question %.0f" % (clean, document, question), flush=True)
+    # (keys that not all rows of a tile see are gone through again, at a third of the pace)
+    assert document <= 1.5 * clean + 20 and question <= 4 * clean + 100
