@@ -643,7 +643,7 @@ int fr_kv_append(const fr_kv_append_desc* d, void* stream);
  * a token that sees nothing gets zeros and -infinity.  Query head h reads key head h / (n_q_heads / n_kv_heads).  Slots
  * behind a length are never used, whatever they hold; neither does a key that a token may not see change its result.
  * Scores, softmax and sums are held in 32 bits; the weights exp(x_j - max) are rounded to the cache's type for the
- * product with v, as is the result.
+ * product with v (to its 8 or 11 significant bits; fp16 weights from 2^-21 down to fewer, below 2^-32 to 0), as is the result.
  * Bounds on the device's numbers: a page id outside the cache counts as the nearest one inside, own_len is cut to
  * 0 .. max_own_len, q_begin to 0 .. n_tokens, a sequence's tokens beyond max_q are not computed.
  */

@@ -186,7 +186,11 @@ template <typename T, int D, int kCols> struct Softmax {
                 for (int i = 0; i < kInBlock; ++i) o[d][i] *= old;
         }
     }
-    __device__ __forceinline__ float base(float c) const { return m == -INFINITY ? 0.0f : m * c; }
+    // What weights are relative to, a power of 2: weights of fp16 end at 2^-25, so they are up to 2^7 (with kSlack 2^15 of the type's
+    // nearly 2^16) instead of 1, and those from 2^-32 of the largest on count.
+    static constexpr float kLift = std::is_same_v<T, F16> ? 7.0f : 0.0f;
+    __device__ __forceinline__ float reference(float c) const { return m * c - kLift; }
+    __device__ __forceinline__ float base(float c) const { return m == -INFINITY ? 0.0f : reference(c); }
     // Two weights for the product with the values, rounded to the type (the matrix cores take 16 bits: half an ulp of a weight is
     // what the result's own rounding costs); their sum is of the weights as they are.
     __device__ __forceinline__ uint32_t weigh(float s0, float s1, float c, float base)
@@ -591,7 +595,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         else wait_lds();
     };
     meet();                                              // tiles are done with
-    const float m2 = x.m * c;                            // (-infinity stays: c is positive)
+    const float m2 = x.reference(c);                     // (-infinity stays: c is positive)
     float mine = 1.0f;
     if (lane < kCols) row_ml[wave][lane] = make_float2(m2, x.l);
     if constexpr (kKind == kFewRows) {

@@ -140,6 +140,32 @@ def test_values_that_only_later_tokens_see(D, G, P, t):
     c.check()
 
 
+def test_small_weights_of_many_keys_add_up():
+    # one key far ahead of the others, whose weights of 2^-26 are too small for 16 bits by themselves but not together
+    n, D = 2000, 64
+    for dt in ("f16", "bf16"):
+        for Hk, new in ((8, [40] * 32), (1, [1]), (8, [1] * 200)):
+            print("attend small weights", dt, Hk, len(new), flush=True)
+            c = _Batch(dt, Hk, Hk, D, 16, 0, [n] * len(new), new, seed=1)
+            c.k.zero_()
+            c.v.fill_(256.0)
+            for b in range(len(new)):
+                page, slot = c.place(b, 0)
+                c.k[page, :, slot, 0], c.v[page, :, slot] = 8.0, 0.0
+            c.q.zero_()
+            c.q[:, :, 0] = 1.0
+            c.scale = float(np.float32(26 * math.log(2.0) / 8.0))
+            c.prepare()
+            c.call()
+            torch.cuda.synchronize()
+            w = math.exp(-8.0 * c.scale)
+            for i in (0, new[0] // 2, new[0] - 1):
+                seen = n - new[0] + i
+                want = 256.0 * seen * w / (1 + seen * w)
+                # 2^-7 of a weight (2^-26 but for the rounding of the scale), the sums of n weights in 32 bits, half an ulp of the result
+                assert np.all(np.abs(_f64(c.out)[i::new[0]] - want) <= want * (2.0 ** -7 + n * 2.0 ** -24 + UNIT[dt])), (dt, Hk, len(new), i)
+
+
 def test_a_value_that_is_not_finite_does_not_make_a_call_long():
     # 4 questions about a document that they go through themselves, with one bad value in the document, and one in the questions
     def us(spoil):
