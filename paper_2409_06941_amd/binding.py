@@ -606,7 +606,7 @@ class KvPages:
 
 
 def fr_kv_append(cache, k, v, slot, q=None, q_out=None, position=None, rotary=None, style=FR_ROTARY_HALVES, stream=None):
-    return _check((_calls or _torch_calls()).kv_append(bytes(cache.desc), k, v, slot, q, q_out, position, rotary, style, stream), "fr_kv_append")
+    return _check((_calls or _torch_calls()).kv_append(bytes(cache.desc), *cache._keep, k, v, slot, q, q_out, position, rotary, style, stream), "fr_kv_append")
 
 
 def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, max_q=1):
@@ -620,7 +620,7 @@ def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, 
 
 def fr_attend_shared(cache, q, out, pages, own_len, scale, prefix_len=0, max_own_len=0, prefix_pages=None, q_begin=None,
                      max_q=1, lse=None, workspace=None, stream=None):
-    return _check((_calls or _torch_calls()).attend_shared(bytes(cache.desc), q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages,
+    return _check((_calls or _torch_calls()).attend_shared(bytes(cache.desc), *cache._keep, q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages,
                                                            q_begin, max_q, lse, workspace, stream), "fr_attend_shared")
 
 

@@ -118,18 +118,24 @@ template <typename D> PyObject* made(int (*entry)(const D*, void*), const D& d, 
     return PyLong_FromLong(code);
 }
 
-void cache_of(PyObject* bytes, fr_kv_pages& cache)
+// x: the pages' descriptor, as bytes, and the two tensors that it was made of, which the kernels read and write as well
+fr_kv_pages cache_of(PyObject* const* x, Call& call)
 {
-    if (!PyBytes_Check(bytes) || PyBytes_GET_SIZE(bytes) != sizeof(cache)) refuse(PyExc_TypeError, "cache: a KvPages is needed");
-    memcpy(&cache, PyBytes_AS_STRING(bytes), sizeof(cache));
+    fr_kv_pages cache;
+    if (!PyBytes_Check(x[0]) || PyBytes_GET_SIZE(x[0]) != sizeof(cache)) refuse(PyExc_TypeError, "cache: a KvPages is needed");
+    memcpy(&cache, PyBytes_AS_STRING(x[0]), sizeof(cache));
+    call.of(tensor(x[1], "cache"), "cache k");
+    call.of(tensor(x[2], "cache"), "cache v");
+    return cache;
 }
 
-// cache, k, v, slot, q, q_out, position, rotary, style, stream
+// cache (three), k, v, slot, q, q_out, position, rotary, style, stream
 PyObject* of_append(PyObject* const* x)
 {
     fr_kv_append_desc d = {};
     Call call;
-    cache_of(x[0], d.cache);
+    d.cache = cache_of(x, call);
+    x += 2;
     const int64_t dim = d.cache.head_dim, heads = d.cache.n_kv_heads;
     const at::ScalarType type = type_of(d.cache.dtype);
     const at::Tensor& k = tensor(x[1], "k");
@@ -159,12 +165,13 @@ PyObject* of_append(PyObject* const* x)
     return made(append, d, call, x[9]);
 }
 
-// cache, q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages, q_begin, max_q, lse, workspace, stream
+// cache (three), q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages, q_begin, max_q, lse, workspace, stream
 PyObject* of_attend(PyObject* const* x)
 {
     fr_attend_desc d = {};
     Call call;
-    cache_of(x[0], d.cache);
+    d.cache = cache_of(x, call);
+    x += 2;
     const int64_t dim = d.cache.head_dim, page = d.cache.page_size;
     const at::ScalarType type = type_of(d.cache.dtype);
     const at::Tensor& q = tensor(x[1], "q");
@@ -267,8 +274,8 @@ template <typename F> PyCFunction method(F f) { return reinterpret_cast<PyCFunct
 
 PyMethodDef methods[] = {
     {"entries", method(entries), METH_FASTCALL, nullptr},
-    {"kv_append", method(guarded<of_append, 10>), METH_FASTCALL, nullptr},
-    {"attend_shared", method(guarded<of_attend, 14>), METH_FASTCALL, nullptr},
+    {"kv_append", method(guarded<of_append, 12>), METH_FASTCALL, nullptr},
+    {"attend_shared", method(guarded<of_attend, 16>), METH_FASTCALL, nullptr},
     {"sample", method(guarded<of_sample, 9>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -187,3 +187,16 @@ def test_a_value_that_is_not_finite_does_not_make_a_call_long():
     print("clean %.0f us, a bad value in the document %.0f, in a question %.0f" % (clean, document, question), flush=True)
     # (keys that not all rows of a tile see are gone through again, at a third of the pace)
     assert document <= 1.5 * clean + 20 and question <= 4 * clean + 100
+
+
+def test_a_cache_that_is_not_on_the_gpu_is_refused():
+    print("host cache", flush=True)
+    host = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    there = host.cuda()
+    x, slot = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.arange(3, device="cuda")
+    q, n, pages = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(3, dtype=torch.int32, device="cuda"), torch.zeros(3, 1, dtype=torch.int32, device="cuda")
+    for k, v, name in ((host, host, "cache k"), (host, there, "cache k"), (there, host, "cache v"), (host.to("meta"), there, "cache k")):
+        cache = fr.KvPages(k, v)
+        for call in (lambda: fr.fr_kv_append(cache, x, x, slot), lambda: fr.fr_attend_shared(cache, q, q.clone(), pages, n, 0.1, max_own_len=8)):
+            with pytest.raises(ValueError, match=name + ": not on a GPU"):
+                call()
