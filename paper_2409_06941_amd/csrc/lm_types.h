@@ -50,6 +50,9 @@ struct F32 {
     static __device__ __forceinline__ float up(float x) { return x; }
 };
 
+// Threads of a launch, at most: a dimension of a grid takes less than 2^32 (of more, some workgroups are left out, without an error).
+constexpr int64_t kMostThreads = (int64_t)1 << 31;
+
 // What fr_kv_pages promises, as far as the host can see.
 inline bool kv_pages_shape_ok(const fr_kv_pages& c)
 {

@@ -189,6 +189,18 @@ def test_a_value_that_is_not_finite_does_not_make_a_call_long():
     assert document <= 1.5 * clean + 20 and question <= 4 * clean + 100
 
 
+def test_append_of_more_tokens_than_a_grid_has_threads_for():
+    print("append many", flush=True)
+    T, D = (1 << 24) + 5, 64
+    k = torch.empty((T, 1, D), dtype=torch.int16, device="cuda").random_(-30000, 30000).view(torch.bfloat16)
+    ck, cv = (torch.zeros((-(-T // 16), 1, 16, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    slot = torch.arange(T - 1, -1, -1, device="cuda")
+    fr.fr_kv_append(fr.KvPages(ck, cv), k, k, slot, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for x in (ck, cv):
+        assert torch.equal(x.view(-1, D)[:T].view(torch.int16), k.view(T, D).view(torch.int16).flip(0))
+
+
 def test_a_cache_that_is_not_on_the_gpu_is_refused():
     print("host cache", flush=True)
     host = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
