@@ -201,6 +201,21 @@ def test_append_of_more_tokens_than_a_grid_has_threads_for():
         assert torch.equal(x.view(-1, D)[:T].view(torch.int16), k.view(T, D).view(torch.int16).flip(0))
 
 
+def test_sample_of_more_rows_than_a_grid_has_threads_for():
+    print("sample many", flush=True)
+    n = (1 << 22) + 3
+    r = torch.arange(n, device="cuda")
+    logits = torch.zeros((n, 2), device="cuda")
+    logits[:, 1] = torch.where(r % 11 == 0, -2.0, 0.0)                 # (the second entry has a weight of 0.135 or 1)
+    token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    f32 = lambda x: x.to(torch.float32)
+    fr.fr_sample(logits, f32(torch.where(r % 7 == 0, 0.25, 0.95)), token, temperature=f32(r % 5 != 0), top_k=(r % 5 == 1).int(),
+                 top_p=f32(torch.where(r % 5 == 2, 0.25, 1.0)), min_p=f32(torch.where(r % 5 == 3, 0.5, 0.0)), stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    first = (r % 7 == 0) | (r % 5 <= 2) | ((r % 5 == 3) & (r % 11 == 0))
+    assert torch.equal(token, (~first).int())
+
+
 def test_a_cache_that_is_not_on_the_gpu_is_refused():
     print("host cache", flush=True)
     host = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
