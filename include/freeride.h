@@ -668,7 +668,9 @@ typedef struct fr_attend_desc {
                                       the call's work on the stream is done                                   */
     uint64_t    workspace_bytes;
 } fr_attend_desc;
-/* Reads the sizes of d only (no pointer), so that a program can ask for its largest call. */
+/* Reads the sizes of d only (no pointer), so that a program can ask for its largest call.  FR_ERR_ARG for sizes that the call
+   refuses, too: beside the bounds above, n_seqs times the rows of max_q tokens (n_q_heads each) in tiles of 128, twice as many in
+   parts, is below 2^31. */
 int fr_attend_shared_workspace_bytes(const fr_attend_desc* d, uint64_t* bytes_out);
 int fr_attend_shared(const fr_attend_desc* d, void* stream);
 

@@ -60,6 +60,7 @@ struct AttendArgs {
     int32_t n_tokens, n_seqs, n_q_heads, max_q, prefix_len, max_own_len, page_shift, group;
     float scale;
     int32_t own_from;                      // the sequences' workgroups take keys from here on: 0, or prefix_len
+    int32_t first_unit;                    // of this launch
     Segment prefix, own;
     int32_t parts;                         // 1: results go to `out`, else to part_*
     float* part_o;                         // [parts][n_tokens * n_q_heads][head_dim], relative to 2^m
@@ -732,7 +733,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(AttendArgs
 {
     __shared__ __align__(1024) char lds[Lds<D, 32>::kBytes];
     __shared__ __align__(1024) int32_t ids[kWaves * 384];      // a wavefront: two sets of 64 page ids, two of 64 offsets
-    const int unit = blockIdx.x / kXcds, xcd = blockIdx.x % kXcds;
+    const int unit = a.first_unit + blockIdx.x / kXcds, xcd = blockIdx.x % kXcds;
     if constexpr (kPrefix != kNone) {
         if (unit < a.prefix.units) attend_prefix<T, D, kPrefix>(a, unit, xcd, lds, ids);
         else attend_own<T, D, kOwn>(a, unit - a.prefix.units, xcd, lds, ids);
@@ -746,11 +747,11 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(AttendArgs
 // sequences with 32 heads and 22 parts, 23 MB, 7 of 72.  (With the parts' maxima first and then the parts, four at once, by 16 threads
 // from 17 parts on, 1.5 to 2 us more.)
 template <typename T, int D, int kLanes>
-__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_blocks)
+__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_blocks, int first_block)
 {
     constexpr int kPieces = D / 8, kRowsHere = kThreads / kPieces / kLanes;
     const int piece = threadIdx.x % kPieces, mine = threadIdx.x / kPieces % kLanes;
-    const int b = blockIdx.x / row_blocks, r = blockIdx.x % row_blocks * kRowsHere + threadIdx.x / kPieces / kLanes;
+    const int block = first_block + blockIdx.x, b = block / row_blocks, r = block % row_blocks * kRowsHere + threadIdx.x / kPieces / kLanes;
     const int t0 = a.q_begin ? within(a.q_begin[b], 0, a.n_tokens) : b, t1 = a.q_begin ? within(a.q_begin[b + 1], t0, a.n_tokens) : b + 1;
     const int t = t1 - t0, i = r / a.n_q_heads, own = a.max_own_len ? within(a.own_len[b], 0, a.max_own_len) : 0;
     const bool there = i < min(t, a.max_q);
@@ -832,8 +833,9 @@ struct Plan {
     Kind of_prefix = kNone, of_own = kFewRows;
     Segment prefix{}, own{};
     int parts = 1;
-    int64_t blocks = 0;                    // of the larger grid
+    int64_t blocks = 0;                    // of the attention or the join, whichever are more
 };
+constexpr int64_t kMostBlocks = 0x7fffffff;            // (they are counted in 32 bits)
 
 // What a call takes, roughly, in microseconds: enough to tell ways to cut it from one another.  A workgroup with tiles of 128 rows
 // needs `one` for a tile of 64 keys where it has a unit to itself and `all` where as many are on the unit as fit, and kStart to begin
@@ -873,6 +875,10 @@ struct Cost {
         return parts < 2 ? 0 : kJoin + (double)parts * d.n_tokens * d.n_q_heads * d.cache.head_dim * (2 * sizeof(float)) / kBytesAUs;
     }
 };
+
+// Threads of the join for eight elements of a row, one where it has all parts in one go, else four; rows of its workgroups.
+int join_lanes(int parts) { return parts <= 8 ? 1 : 4; }
+int join_rows(int parts, int head_dim) { return kThreads / (head_dim / 8) / join_lanes(parts); }
 
 Plan plan(const fr_attend_desc& d, int cus)
 {
@@ -988,7 +994,7 @@ Plan plan(const fr_attend_desc& d, int cus)
         s.split_len = 1;
     }
     p.parts = p.prefix.splits + s.splits;
-    p.blocks = std::max(p.blocks, d.n_seqs * tokens_a_seq * d.n_q_heads);        // (the join's grid is not larger)
+    if (p.parts > 1) p.blocks = std::max(p.blocks, d.n_seqs * up(tokens_a_seq * d.n_q_heads, join_rows(p.parts, d.cache.head_dim)));
     return p;
 }
 
@@ -998,10 +1004,14 @@ uint64_t part_bytes(const fr_attend_desc& d, const Plan& p)
 }
 
 template <typename T, int D>
-int launch(const AttendArgs& a, const Plan& p, hipStream_t stream)
+int launch(AttendArgs a, const Plan& p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.prefix.units + a.own.units) * kXcds);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
+    constexpr int kBlocksALaunch = kMostThreads / kThreads;
+    auto go = [&](auto kernel) {
+        const int units = a.prefix.units + a.own.units;
+        for (a.first_unit = 0; a.first_unit < units; a.first_unit += kBlocksALaunch / kXcds)
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(units - a.first_unit, kBlocksALaunch / kXcds) * kXcds), dim3(kThreads), 0, stream, a);
+    };
     if (p.of_prefix == kNone) {
         if (p.of_own == kFewRows) go(k_attend<T, D, kNone, kFewRows>);
         else if (p.of_own == kWaveRows) go(k_attend<T, D, kNone, kWaveRows>);
@@ -1014,12 +1024,13 @@ int launch(const AttendArgs& a, const Plan& p, hipStream_t stream)
         else go(k_attend<T, D, kWideRows, kWideRows>);
     }
     if (p.parts > 1) {
-        // a thread for every eight elements where it has all parts in one go, else four
-        const int lanes = p.parts <= 8 ? 1 : 4, rows = kThreads / (D / 8) / lanes;
-        const int64_t blocks = (std::min<int64_t>(a.max_q, a.n_tokens) * a.n_q_heads + rows - 1) / rows;
-        const dim3 joins((unsigned)(a.n_seqs * blocks));
-        if (lanes == 1) hipLaunchKernelGGL((k_attend_join<T, D, 1>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
-        else hipLaunchKernelGGL((k_attend_join<T, D, 4>), joins, dim3(kThreads), 0, stream, a, (int)blocks);
+        const int rows = join_rows(p.parts, D), blocks = (int)((std::min<int64_t>(a.max_q, a.n_tokens) * a.n_q_heads + rows - 1) / rows);
+        const int64_t all = (int64_t)a.n_seqs * blocks;
+        for (int64_t first = 0; first < all; first += kBlocksALaunch) {
+            const dim3 joins((unsigned)std::min<int64_t>(all - first, kBlocksALaunch));
+            if (join_lanes(p.parts) == 1) hipLaunchKernelGGL((k_attend_join<T, D, 1>), joins, dim3(kThreads), 0, stream, a, blocks, (int)first);
+            else hipLaunchKernelGGL((k_attend_join<T, D, 4>), joins, dim3(kThreads), 0, stream, a, blocks, (int)first);
+        }
     }
     return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
 }
@@ -1033,7 +1044,9 @@ int fr_attend_shared_workspace_bytes(const fr_attend_desc* d, uint64_t* bytes_ou
     if (!d || !bytes_out || !sizes_ok(*d)) return FR_ERR_ARG;
     *bytes_out = 0;
     if (d->n_tokens == 0 || d->n_seqs == 0) return FR_OK;
-    *bytes_out = part_bytes(*d, plan(*d, kUnits));
+    const Plan p = plan(*d, kUnits);
+    if (p.blocks > kMostBlocks) return FR_ERR_ARG;
+    *bytes_out = part_bytes(*d, p);
     return FR_OK;
 }
 
@@ -1058,8 +1071,8 @@ int fr_attend_shared(const fr_attend_desc* d, void* stream)
     const Plan whole = plan(*d, kUnits);
     const int cus = (int)fr_stream_cus((hipStream_t)stream);
     Plan p = cus < kUnits ? plan(*d, cus) : whole;
-    if (p.parts > whole.parts) p = whole;
-    if (p.blocks > 0x7fffffff) return FR_ERR_ARG;
+    if (whole.blocks > kMostBlocks) return FR_ERR_ARG;
+    if (p.parts > whole.parts || p.blocks > kMostBlocks) p = whole;
     const uint64_t asked = part_bytes(*d, whole);
     if (asked && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < asked)) return FR_ERR_ARG;
     a.own_from = p.of_prefix == kNone ? 0 : d->prefix_len;

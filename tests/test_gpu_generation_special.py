@@ -216,6 +216,34 @@ def test_sample_of_more_rows_than_a_grid_has_threads_for():
     assert torch.equal(token, (~first).int())
 
 
+def test_one_long_prompt_beside_many_single_tokens():
+    # sizes at which sequences times the longest prompt are more workgroups than one dimension of a grid takes
+    print("attend ragged", flush=True)
+    n, most, Hq, Hk, D, page = 1024, 4177, 512, 64, 64, 16
+    new = [1] * n
+    new[500] = most
+    own = [int(x) for x in 1 + np.arange(n) * 37 % 60]
+    own[500] = most
+    c = _Batch("bf16", Hq, Hk, D, page, 0, own, new, seed=3)
+    c.prepare()
+    c.call()
+    torch.cuda.synchronize()
+    k, v = _f64(c.k), _f64(c.v)
+    rng = np.random.default_rng(0)
+    for b in [0, 1, 499, 501, n - 1] + [500] * 12:
+        i, h = int(rng.integers(0, new[b])), int(rng.integers(0, Hq))
+        places = np.array([c.place(b, j) for j in range(own[b])])
+        count = oracle.visible(0, own[b], new[b], i)
+        kk, vv = k[places[:count, 0], h // (Hq // Hk), places[:count, 1]], v[places[:count, 0], h // (Hq // Hk), places[:count, 1]]
+        row = int(c.begin[b]) + i
+        o, l, a, x = oracle.attend_row(_f64(c.q[row, h]), kk, vv, c.scale)
+        d = (D + 4) * 2.0 ** -24 * x + 2.0 ** -20
+        near = (UNIT["bf16"] + 2 * d + count * 2.0 ** -23) * a + UNIT["bf16"] * np.abs(o) * 1.01 + TINY["bf16"]
+        assert np.all(np.abs(_f64(c.out[row, h]) - o) <= near), (b, i, h)
+        assert abs(float(c.lse[row, h]) - l) <= d + count * 2.0 ** -23 + 2.0 ** -20 * (1 + abs(l)), (b, i, h)
+    assert bool((c.lse != 9.0).all())
+
+
 def test_a_cache_that_is_not_on_the_gpu_is_refused():
     print("host cache", flush=True)
     host = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
