@@ -664,13 +664,13 @@ typedef struct fr_attend_desc {
     int32_t     prefix_len, max_own_len;      /* >= 0, together below 2^31 - 4096                             */
     float       scale;             /* positive and finite                                                     */
     int32_t     reserved;
-    void*       workspace;         /* fr_attend_shared_workspace_bytes of it, 256-byte aligned; free again when
-                                      the call's work on the stream is done                                   */
+    void*       workspace;         /* fr_attend_shared_workspace_bytes of this or a larger call, 256-byte aligned;
+                                      free again when the call's work on the stream is done                   */
     uint64_t    workspace_bytes;
 } fr_attend_desc;
-/* Reads the sizes of d only (no pointer), so that a program can ask for its largest call.  FR_ERR_ARG for sizes that the call
-   refuses, too: beside the bounds above, n_seqs times the rows of max_q tokens (n_q_heads each) in tiles of 128, twice as many in
-   parts, is below 2^31. */
+/* Reads the sizes of d only (no pointer).  A call of the same heads with no larger n_tokens, n_seqs, max_q, prefix_len and
+   max_own_len needs no more, so that a program can ask for its largest call.  FR_ERR_ARG for sizes that the call refuses, too: those
+   of the fields above, and so many sequences with so many tokens (max_q) that the call would have 2^31 workgroups. */
 int fr_attend_shared_workspace_bytes(const fr_attend_desc* d, uint64_t* bytes_out);
 int fr_attend_shared(const fr_attend_desc* d, void* stream);
 

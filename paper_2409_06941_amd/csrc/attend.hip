@@ -880,16 +880,35 @@ struct Cost {
 int join_lanes(int parts) { return parts <= 8 ? 1 : 4; }
 int join_rows(int parts, int head_dim) { return kThreads / (head_dim / 8) / join_lanes(parts); }
 
-Plan plan(const fr_attend_desc& d, int cus)
+int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
+
+// Rows of results in parts that a call has room for; no call with smaller sizes has more, so that a program can ask once for its
+// largest.  `plan` makes no more than four workgroups a unit by cutting keys (16 where a wavefront takes an item), and two where few
+// rows' prefix is taken apart; what is not cut has one part of every row, of the prefix and of the own keys.
+constexpr int64_t kMostFew = 32;           // rows of a sequence that are few
+constexpr int64_t kMostShared = 1 << 21;   // many rows are not taken apart from there on (2 GB of results; one in a hundred such calls would be)
+int64_t most_part_rows(const fr_attend_desc& d)
+{
+    const int64_t group = d.n_q_heads / d.cache.n_kv_heads, rows = (int64_t)d.n_tokens * d.n_q_heads, parts = up(d.prefix_len, 128) + up(d.max_own_len, 128);
+    const bool few = d.max_q * group <= kMostFew;
+    const int64_t own = few ? 16 * kUnits * std::min<int64_t>(16, d.max_q * group) : 4 * kUnits * 128;
+    const int64_t prefix = few ? 2 * kUnits * std::min<int64_t>(128, d.n_tokens * group) : 4 * kUnits * 128;
+    if (parts < 2) return 0;
+    if (d.prefix_len == 0) return std::min(rows * parts, own);
+    const int64_t of_few = group <= kMostFew ? std::min<int64_t>(d.n_tokens, d.n_seqs * (kMostFew / group)) * d.n_q_heads : 0;
+    const int64_t shared = std::max(of_few, std::min(rows, kMostShared));
+    return std::min(rows * parts, std::max(shared, own) + std::max(shared, prefix));
+}
+
+// `whole`: in one part
+Plan plan(const fr_attend_desc& d, int cus, bool whole = false)
 {
     Plan p;
-    auto up = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     const int64_t group = d.n_q_heads / d.cache.n_kv_heads, heads = d.cache.n_kv_heads;
     const int64_t tokens_a_seq = std::min(d.max_q, d.n_tokens), seq_rows = tokens_a_seq * group, all_rows = d.n_tokens * group;
     // Rows of a sequence up to which tiles of 16 are taken, above, tiles of 128: several of those read the same keys, but do not wait
     // for one another.  8 key heads, in tiles of 16 and of 128: 32 rows, 256 sequences of 64 keys 23 and 36 us, 4 of 1000 13.5 and
     // 15.4, 16 of 4000 52 and 52; 64 rows, 64 sequences of 250 keys 21.5 and 22, of 1000 79 and 49, 16 of 1000 28 and 25.
-    constexpr int64_t kMostFew = 32;
     cus = std::min(cus, kUnits);
     const Cost cost(d.cache.head_dim);
     auto finish = [&](Segment& s, int64_t items, int64_t at_once) {
@@ -903,7 +922,7 @@ Plan plan(const fr_attend_desc& d, int cus)
     // the numbers that give every unit up to four workgroups, and parts of two tiles
     auto cut = [&](Segment& s, int64_t keys, int64_t blocks, auto cost) {
         double least = INFINITY;
-        const int64_t most = std::max<int64_t>(up(keys, 128), 1);
+        const int64_t most = whole ? 1 : std::max<int64_t>(up(keys, 128), 1);
         auto consider = [&](int64_t n) {
             if (n < 1 || n > most) return;
             const int64_t len = std::max<int64_t>(up(up(keys, n), 64), 1) * 64, parts = std::max<int64_t>(up(keys, len), 1);
@@ -919,7 +938,7 @@ Plan plan(const fr_attend_desc& d, int cus)
     Segment &s = p.own, &shared = p.prefix;
     s.row_tiles = (int)up(seq_rows, rows_of(p.of_own));
     shared.row_tiles = (int)up(all_rows, rows_of(all_rows > kMostFew ? kWideRows : kFewRows));
-    bool share = d.prefix_len > 0 && d.n_seqs > 1;
+    bool share = d.prefix_len > 0 && d.n_seqs > 1 && !whole && (p.of_own == kFewRows || (int64_t)d.n_tokens * d.n_q_heads <= kMostShared);
     const int64_t base = (int64_t)d.n_seqs * heads * s.row_tiles;
     if (p.of_own == kWideRows) {
         // row tiles that hold rows, half of a sequence's last one being empty
@@ -981,7 +1000,7 @@ Plan plan(const fr_attend_desc& d, int cus)
             // and 38, of 512 with 64 heads 95 and 98; 256 of 800 137 and 130.  64 of up to 1500 behind 16384: 73.5; in parts of 512 77.1.
             int64_t wave_len = base < cus ? 128 : 256;
             while (base * up(keys, wave_len) > (base < cus ? 4 : 16) * cus && wave_len < keys) wave_len *= 2;
-            const bool enough = base >= cus / 2 && base * up(keys, wave_len) >= (base < cus ? 4 : 3) * cus / 2;
+            const bool enough = !whole && base >= cus / 2 && base * up(keys, wave_len) >= (base < cus ? 4 : 3) * cus / 2;
             if (share ? p.of_prefix == kWideRows && enough && keys <= (base < 4 * cus ? 2048 : 512) : base >= 4 * cus && keys <= 256) {
                 p.of_own = kWaveRows;
                 s.split_len = (int)wave_len;
@@ -994,14 +1013,12 @@ Plan plan(const fr_attend_desc& d, int cus)
         s.split_len = 1;
     }
     p.parts = p.prefix.splits + s.splits;
+    if (p.parts * (int64_t)d.n_tokens * d.n_q_heads > most_part_rows(d) && p.parts > 1) return plan(d, cus, true);     // (most tokens in no sequence)
     if (p.parts > 1) p.blocks = std::max(p.blocks, d.n_seqs * up(tokens_a_seq * d.n_q_heads, join_rows(p.parts, d.cache.head_dim)));
     return p;
 }
 
-uint64_t part_bytes(const fr_attend_desc& d, const Plan& p)
-{
-    return p.parts > 1 ? (uint64_t)p.parts * d.n_tokens * d.n_q_heads * (d.cache.head_dim * 4 + 8) : 0;
-}
+uint64_t part_bytes(const fr_attend_desc& d) { return (uint64_t)most_part_rows(d) * (d.cache.head_dim * 4 + 8); }
 
 template <typename T, int D>
 int launch(AttendArgs a, const Plan& p, hipStream_t stream)
@@ -1046,7 +1063,7 @@ int fr_attend_shared_workspace_bytes(const fr_attend_desc* d, uint64_t* bytes_ou
     if (d->n_tokens == 0 || d->n_seqs == 0) return FR_OK;
     const Plan p = plan(*d, kUnits);
     if (p.blocks > kMostBlocks) return FR_ERR_ARG;
-    *bytes_out = part_bytes(*d, p);
+    *bytes_out = part_bytes(*d);
     return FR_OK;
 }
 
@@ -1073,8 +1090,7 @@ int fr_attend_shared(const fr_attend_desc* d, void* stream)
     Plan p = cus < kUnits ? plan(*d, cus) : whole;
     if (whole.blocks > kMostBlocks) return FR_ERR_ARG;
     if (p.parts > whole.parts || p.blocks > kMostBlocks) p = whole;
-    const uint64_t asked = part_bytes(*d, whole);
-    if (asked && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < asked)) return FR_ERR_ARG;
+    if (whole.parts > 1 && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < part_bytes(*d))) return FR_ERR_ARG;
     a.own_from = p.of_prefix == kNone ? 0 : d->prefix_len;
     a.prefix = p.prefix;
     a.own = p.own;

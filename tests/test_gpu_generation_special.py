@@ -189,6 +189,25 @@ def test_a_value_that_is_not_finite_does_not_make_a_call_long():
     assert document <= 1.5 * clean + 20 and question <= 4 * clean + 100
 
 
+def test_one_workspace_for_the_largest_call_and_smaller_ones():
+    print("attend one workspace", flush=True)
+    sizes = [([4000] * 64, [1] * 64, 0), ([4000] * 8, [1] * 8, 0), ([300] * 16, [70] * 16, 2048), ([300] * 16, [40] * 16, 2048), ([9] * 3, [2] * 3, 2000)]
+    shape = dict(dt="bf16", Hq=8, Hk=2, D=128, page=16)
+    most = torch.empty((16 * 70, 8, 128), dtype=torch.bfloat16, device="cuda")
+    for i, (own, new, P) in enumerate(sizes):
+        c = _Batch(own=own, new=new, P=P, seed=i, **shape)
+        c.prepare()
+        c.call()
+        torch.cuda.synchronize()
+        want = c.out.clone()
+        need = fr.fr_attend_shared_workspace_bytes(c.cache, most, 64, prefix_len=2048, max_own_len=4000, max_q=70)
+        c.workspace = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+        c.out.zero_()
+        c.call()
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, want), i
+
+
 def test_append_of_more_tokens_than_a_grid_has_threads_for():
     print("append many", flush=True)
     T, D = (1 << 24) + 5, 64
