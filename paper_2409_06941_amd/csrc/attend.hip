@@ -102,6 +102,19 @@ __device__ __forceinline__ f32x16 mfma(F16::x8 a, F16::x8 b, f32x16 c) { return 
 __device__ __forceinline__ f32x4 mfma(Bf16::x8 a, Bf16::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mfma(F16::x8 a, F16::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
+// Whether a token is one of the first max_q of a sequence.
+__device__ __forceinline__ bool is_computed(const AttendArgs& a, int token)
+{
+    int b = 0, end = a.n_seqs;
+    while (end - b > 1) {
+        const int middle = b + (end - b) / 2;
+        if (within(a.q_begin[middle], 0, a.n_tokens) <= token) b = middle;
+        else end = middle;
+    }
+    const int t0 = within(a.q_begin[b], 0, a.n_tokens), t1 = within(a.q_begin[b + 1], t0, a.n_tokens);
+    return token >= t0 && token < t1 && token - t0 < a.max_q;
+}
+
 // What a workgroup works on: query rows (token and head of a group, the group's heads side by side) against a run of keys.
 struct Item {
     int32_t kv, token0, rows, row0;        // key head; first token; rows there are; first row of this workgroup
@@ -109,6 +122,7 @@ struct Item {
     int32_t seen0, seen_step;              // a row of token i sees the keys below max(prefix, seen0 + i * seen_step)
     int32_t part;
     const int32_t* own_pages;
+    bool of_all;                           // rows of all tokens, also of those that are in no sequence
 };
 
 // Where a row's result goes.
@@ -590,6 +604,7 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
 
     // results through LDS, so that rows are written whole: a wavefront's rows of D floats, 16-byte chunk c of row r at c ^ r
     __shared__ float2 row_ml[kWaves][kCols];
+    __shared__ bool left_out[rows_of(kKind)];
     constexpr uint32_t kFloatRow = D * 4, kFloatChunks = D / 4;
     auto meet = [] {
         if constexpr (!kAlone) __syncthreads();
@@ -599,6 +614,10 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
     const float m2 = x.reference(c);                     // (-infinity stays: c is positive)
     float mine = 1.0f;
     if (lane < kCols) row_ml[wave][lane] = make_float2(m2, x.l);
+    // (without q_begin every token has a sequence; of parts the join leaves out rows that have none)
+    const bool may_leave_out = !kAlone && w.of_all && a.parts == 1 && a.q_begin;
+    if constexpr (!kAlone)
+        if (may_leave_out && tid < rows_of(kKind)) left_out[tid] = !is_computed(a, rows.token(w.row0 + tid));
     if constexpr (kKind == kFewRows) {
         meet();
         float top = -INFINITY;
@@ -628,6 +647,8 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
             if (kWide) continue;
             break;
         }
+        if constexpr (!kAlone)
+            if (may_leave_out && left_out[r]) continue;
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
         float top, sum;
         const int in = r % kCols;
@@ -689,6 +710,7 @@ __device__ __forceinline__ void attend_prefix(const AttendArgs& a, int unit, int
     w.seen0 = a.prefix_len;
     w.seen_step = 0;
     w.own_pages = nullptr;
+    w.of_all = true;
     attend<T, D, kKind>(a, w, lds, ids);
 }
 
@@ -722,6 +744,7 @@ __device__ __forceinline__ void attend_own(const AttendArgs& a, int unit, int xc
     if (w.k0 >= w.k1 && a.parts > 1) return;
     w.part = a.own.first_part + split;
     w.own_pages = a.pages + b * a.pages_stride;
+    w.of_all = false;
     attend<T, D, kKind>(a, w, lds, ids);
 }
 

@@ -189,6 +189,28 @@ def test_a_value_that_is_not_finite_does_not_make_a_call_long():
     assert document <= 1.5 * clean + 20 and question <= 4 * clean + 100
 
 
+@pytest.mark.parametrize("Hk,G,n,most,P", [(8, 1, 16, 2, 250), (8, 8, 64, 4, 128), (8, 1, 100, 3, 250), (8, 4, 100, 40, 250), (2, 1, 3, 4, 20), (2, 4, 5, 4, 9000)])
+def test_tokens_outside_of_the_sequences_are_not_computed(Hk, G, n, most, P):
+    # tokens before and behind the sequences, a sequence without any, some with more than max_q; no keys but the prefix
+    print("attend outside", Hk, G, n, most, P, flush=True)
+    counts = [1 + b * 5 % (most + 3) for b in range(n)]
+    counts[n // 2] = 0
+    begin = np.concatenate([[2], 2 + np.cumsum(counts)]).astype(np.int32)
+    c = _Batch("bf16", Hk * G, Hk, 128, 16, P, [0] * n, [int(begin[-1]) + 3] + [0] * (n - 1), seed=P)
+    c.prepare()
+    c.limits["max_q"] = most
+    c.more["q_begin"] = torch.from_numpy(begin).cuda()
+    c.workspace = torch.empty(max(1, fr.fr_attend_shared_workspace_bytes(c.cache, c.gq, n, **c.limits)), dtype=torch.uint8, device="cuda")
+    c.call()
+    torch.cuda.synchronize()
+    there = np.zeros(c.q.shape[0], dtype=bool)
+    for b in range(n):
+        there[begin[b]:begin[b] + min(counts[b], most)] = True
+    out, lse = _f64(c.out), _f64(c.lse)
+    assert np.all(out[~there] == 9.0) and np.all(lse[~there] == 9.0)
+    assert np.all(lse[there] != 9.0) and np.all(np.abs(out[there]) < 5.0)
+
+
 def test_one_workspace_for_the_largest_call_and_smaller_ones():
     print("attend one workspace", flush=True)
     sizes = [([4000] * 64, [1] * 64, 0), ([4000] * 8, [1] * 8, 0), ([300] * 16, [70] * 16, 2048), ([300] * 16, [40] * 16, 2048), ([9] * 3, [2] * 3, 2000)]
