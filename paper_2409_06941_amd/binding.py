@@ -571,11 +571,11 @@ def _torch_calls():
         L = lib()
         if not os.path.exists(_build.TORCH_CALLS):
             _build.build_torch_calls()
-        import torch  # noqa: F401  (its libraries have to be there)
+        import torch                                   # (its libraries have to be there)
         loader = importlib.machinery.ExtensionFileLoader("_torch_calls", _build.TORCH_CALLS)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_torch_calls", loader))
         loader.exec_module(module)
-        module.entries(*(C.cast(f, C.c_void_p).value for f in (L.fr_kv_append, L.fr_attend_shared, L.fr_sample)))
+        module.entries(*(C.cast(f, C.c_void_p).value for f in (L.fr_kv_append, L.fr_attend_shared, L.fr_sample)), torch.cuda.current_stream)
         _calls = module
     return _calls
 
@@ -589,7 +589,9 @@ def _dtype(x):
 
 
 class KvPages:
-    """fr_kv_pages of two torch tensors [n_pages, n_kv_heads, page_size, head_dim] with the same strides (views are fine)."""
+    """fr_kv_pages of two torch tensors [n_pages, n_kv_heads, page_size, head_dim] with the same strides (views are fine).
+
+    The calls below take torch tensors, all on one GPU, and without a stream work on torch's current one there."""
 
     def __init__(self, k, v):
         if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
@@ -606,7 +608,7 @@ class KvPages:
 
 
 def fr_kv_append(cache, k, v, slot, q=None, q_out=None, position=None, rotary=None, style=FR_ROTARY_HALVES, stream=None):
-    return _check((_calls or _torch_calls()).kv_append(bytes(cache.desc), *cache._keep, k, v, slot, q, q_out, position, rotary, style, stream), "fr_kv_append")
+    return _check((_calls or _torch_calls()).kv_append(bytes(cache.desc), cache._keep, k, v, slot, q, q_out, position, rotary, style, stream), "fr_kv_append")
 
 
 def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, max_q=1):
@@ -620,7 +622,7 @@ def fr_attend_shared_workspace_bytes(cache, q, n_seqs, prefix_len, max_own_len, 
 
 def fr_attend_shared(cache, q, out, pages, own_len, scale, prefix_len=0, max_own_len=0, prefix_pages=None, q_begin=None,
                      max_q=1, lse=None, workspace=None, stream=None):
-    return _check((_calls or _torch_calls()).attend_shared(bytes(cache.desc), *cache._keep, q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages,
+    return _check((_calls or _torch_calls()).attend_shared(bytes(cache.desc), cache._keep, q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages,
                                                            q_begin, max_q, lse, workspace, stream), "fr_attend_shared")
 
 

@@ -4,6 +4,7 @@
 // type that is asked for), from here less than one.  What a tensor shows and the C side cannot see is checked here: types, shapes,
 // elements that lie side by side, and that it is on a GPU.  The rest is the library's.
 
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "freeride.h"
@@ -21,6 +22,7 @@ template <typename... X> [[noreturn]] void refuse(PyObject* kind, const char* te
 int (*append)(const fr_kv_append_desc*, void*);
 int (*attend)(const fr_attend_desc*, void*);
 int (*sample)(const fr_sample_desc*, void*);
+PyObject* current_stream;                  // (of a device's index: torch's current stream there)
 
 bool given(PyObject* x) { return x != Py_None; }
 
@@ -44,10 +46,12 @@ int32_t number(int64_t x, const char* name)
     return (int32_t)x;
 }
 
-void* address(PyObject* stream)
+void* address(PyObject* stream, c10::Device device)
 {
-    if (!given(stream)) return nullptr;
-    PyObject* y = PyLong_Check(stream) ? Py_NewRef(stream) : PyObject_GetAttrString(stream, "cuda_stream");
+    PyObject* made = given(stream) ? nullptr : PyObject_CallFunction(current_stream, "i", (int)device.index());
+    PyObject* of = given(stream) ? stream : made;
+    PyObject* y = !of ? nullptr : PyLong_Check(of) ? Py_NewRef(of) : PyObject_GetAttrString(of, "cuda_stream");
+    Py_XDECREF(made);
     if (!y) throw Refused{};
     void* p = PyLong_AsVoidPtr(y);
     Py_DECREF(y);
@@ -110,7 +114,8 @@ struct Call {
 template <typename D> PyObject* made(int (*entry)(const D*, void*), const D& d, const Call& call, PyObject* stream)
 {
     call.on_gpu();
-    void* s = address(stream);
+    const c10::DeviceGuard guard(call.seen[0]->device());      // (the null stream is the current device's)
+    void* s = address(stream, call.seen[0]->device());
     int code;
     Py_BEGIN_ALLOW_THREADS
     code = entry(&d, s);
@@ -122,20 +127,21 @@ template <typename D> PyObject* made(int (*entry)(const D*, void*), const D& d, 
 fr_kv_pages cache_of(PyObject* const* x, Call& call)
 {
     fr_kv_pages cache;
-    if (!PyBytes_Check(x[0]) || PyBytes_GET_SIZE(x[0]) != sizeof(cache)) refuse(PyExc_TypeError, "cache: a KvPages is needed");
+    if (!PyBytes_Check(x[0]) || PyBytes_GET_SIZE(x[0]) != sizeof(cache) || !PyTuple_Check(x[1]) || PyTuple_GET_SIZE(x[1]) != 2)
+        refuse(PyExc_TypeError, "cache: a KvPages is needed");
     memcpy(&cache, PyBytes_AS_STRING(x[0]), sizeof(cache));
-    call.of(tensor(x[1], "cache"), "cache k");
-    call.of(tensor(x[2], "cache"), "cache v");
+    call.of(tensor(PyTuple_GET_ITEM(x[1], 0), "cache"), "cache k");
+    call.of(tensor(PyTuple_GET_ITEM(x[1], 1), "cache"), "cache v");
     return cache;
 }
 
-// cache (three), k, v, slot, q, q_out, position, rotary, style, stream
+// cache (two), k, v, slot, q, q_out, position, rotary, style, stream
 PyObject* of_append(PyObject* const* x)
 {
     fr_kv_append_desc d = {};
     Call call;
     d.cache = cache_of(x, call);
-    x += 2;
+    ++x;
     const int64_t dim = d.cache.head_dim, heads = d.cache.n_kv_heads;
     const at::ScalarType type = type_of(d.cache.dtype);
     const at::Tensor& k = tensor(x[1], "k");
@@ -165,13 +171,13 @@ PyObject* of_append(PyObject* const* x)
     return made(append, d, call, x[9]);
 }
 
-// cache (three), q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages, q_begin, max_q, lse, workspace, stream
+// cache (two), q, out, pages, own_len, scale, prefix_len, max_own_len, prefix_pages, q_begin, max_q, lse, workspace, stream
 PyObject* of_attend(PyObject* const* x)
 {
     fr_attend_desc d = {};
     Call call;
     d.cache = cache_of(x, call);
-    x += 2;
+    ++x;
     const int64_t dim = d.cache.head_dim, page = d.cache.page_size;
     const at::ScalarType type = type_of(d.cache.dtype);
     const at::Tensor& q = tensor(x[1], "q");
@@ -257,16 +263,17 @@ template <PyObject* (*kCall)(PyObject* const*), int kArguments> PyObject* guarde
     return nullptr;
 }
 
-// the library's entries, as addresses: fr_kv_append, fr_attend_shared, fr_sample
+// the library's entries, as addresses: fr_kv_append, fr_attend_shared, fr_sample; and what gives torch's current stream of a device
 PyObject* entries(PyObject*, PyObject* const* x, Py_ssize_t n)
 {
     void* p[3];
-    if (n != 3) return PyErr_Format(PyExc_TypeError, "3 arguments are needed");
+    if (n != 4) return PyErr_Format(PyExc_TypeError, "4 arguments are needed");
     for (int i = 0; i < 3; ++i)
         if (!(p[i] = PyLong_AsVoidPtr(x[i]))) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_ValueError, "an address is needed");
     append = reinterpret_cast<decltype(append)>(p[0]);
     attend = reinterpret_cast<decltype(attend)>(p[1]);
     sample = reinterpret_cast<decltype(sample)>(p[2]);
+    Py_XSETREF(current_stream, Py_NewRef(x[3]));
     Py_RETURN_NONE;
 }
 
@@ -274,8 +281,8 @@ template <typename F> PyCFunction method(F f) { return reinterpret_cast<PyCFunct
 
 PyMethodDef methods[] = {
     {"entries", method(entries), METH_FASTCALL, nullptr},
-    {"kv_append", method(guarded<of_append, 12>), METH_FASTCALL, nullptr},
-    {"attend_shared", method(guarded<of_attend, 16>), METH_FASTCALL, nullptr},
+    {"kv_append", method(guarded<of_append, 11>), METH_FASTCALL, nullptr},
+    {"attend_shared", method(guarded<of_attend, 15>), METH_FASTCALL, nullptr},
     {"sample", method(guarded<of_sample, 9>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -296,3 +296,29 @@ def test_a_cache_that_is_not_on_the_gpu_is_refused():
         for call in (lambda: fr.fr_kv_append(cache, x, x, slot), lambda: fr.fr_attend_shared(cache, q, q.clone(), pages, n, 0.1, max_own_len=8)):
             with pytest.raises(ValueError, match=name + ": not on a GPU"):
                 call()
+
+
+def test_calls_without_a_stream_work_on_the_current_one():
+    print("current stream", flush=True)
+    D, n = 64, 40
+    side = torch.cuda.Stream()
+    ck, cv = (torch.zeros(4, 1, 16, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cache = fr.KvPages(ck, cv)
+    k = torch.zeros(n, 1, D, dtype=torch.bfloat16, device="cuda")
+    slot, pages = torch.arange(n, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda")[None]
+    q, out = torch.zeros(1, 2, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, 2, D, dtype=torch.bfloat16, device="cuda")
+    own = torch.tensor([n], dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(1, fr.fr_attend_shared_workspace_bytes(cache, q, 1, 0, n)), dtype=torch.uint8, device="cuda")
+    logits, token = torch.zeros(1, 100, device="cuda"), torch.full((1,), -7, dtype=torch.int32, device="cuda")
+    uniform = torch.zeros(1, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)                 # what follows is still to come when the calls are made
+        k.fill_(3.0)
+        logits[0, 77] = 50.0
+        fr.fr_kv_append(cache, k, k, slot)
+        fr.fr_attend_shared(cache, q, out, pages, own, 0.1, max_own_len=n, workspace=ws)
+        fr.fr_sample(logits, uniform, token)
+        a, b = out.clone(), token.clone()
+    side.synchronize()
+    assert bool((a == 3.0).all()) and int(b) == 77
