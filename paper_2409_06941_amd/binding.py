@@ -569,12 +569,16 @@ def _torch_calls():
     global _calls
     if _calls is None:
         L = lib()
-        if not os.path.exists(_build.TORCH_CALLS):
+        if not os.path.exists(_build.TORCH_CALLS):     # (as the library: an older one is loaded, if its descriptors are laid out alike)
             _build.build_torch_calls()
         import torch                                   # (its libraries have to be there)
         loader = importlib.machinery.ExtensionFileLoader("_torch_calls", _build.TORCH_CALLS)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_torch_calls", loader))
         loader.exec_module(module)
+        want = [x for s in (fr_kv_pages, fr_kv_append_desc, fr_attend_desc, fr_sample_desc)
+                for x in [getattr(s, f[0]).offset for f in s._fields_] + [C.sizeof(s)]]
+        if module.layout() != want:
+            raise RuntimeError("%s was built from another include/freeride.h: build again" % _build.TORCH_CALLS)
         module.entries(*(C.cast(f, C.c_void_p).value for f in (L.fr_kv_append, L.fr_attend_shared, L.fr_sample)), torch.cuda.current_stream)
         _calls = module
     return _calls

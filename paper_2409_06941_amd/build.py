@@ -54,7 +54,16 @@ def build(force: bool = True) -> str:
     return LIB
 
 
-def build_torch_calls() -> str:
+def torch_calls_is_stale() -> bool:
+    if not os.path.exists(TORCH_CALLS):
+        return True
+    t = os.path.getmtime(TORCH_CALLS)
+    return any(os.path.getmtime(d) > t for d in (os.path.join(CSRC, "torch_calls.cpp"), os.path.join(ROOT, "include", "freeride.h")))
+
+
+def build_torch_calls(force: bool = True) -> str:
+    if not force and not torch_calls_is_stale():
+        return TORCH_CALLS
     torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     tmp = TORCH_CALLS + ".tmp.%d" % os.getpid()
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"),

@@ -7,6 +7,9 @@
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstddef>
+#include <vector>
+
 #include "freeride.h"
 
 namespace {
@@ -277,9 +280,42 @@ PyObject* entries(PyObject*, PyObject* const* x, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// Where the fields of the descriptors lie, and their sizes, as this file was compiled: to be compared with the binding's.
+PyObject* layout(PyObject*, PyObject* const*, Py_ssize_t)
+{
+#define AT(S, f) (long)offsetof(S, f)
+    static const std::vector<long> structs[] = {
+#define F(f) AT(fr_kv_pages, f)
+        {F(k), F(v), F(n_pages), F(page_stride), F(head_stride), F(slot_stride), F(n_kv_heads), F(head_dim), F(page_size), F(dtype), sizeof(fr_kv_pages)},
+#undef F
+#define F(f) AT(fr_kv_append_desc, f)
+        {F(cache), F(k), F(v), F(q), F(q_out), F(k_stride), F(v_stride), F(q_stride), F(q_out_stride), F(slot), F(position), F(rotary), F(n_positions),
+         F(rotary_dim), F(style), F(n_tokens), F(n_q_heads), F(reserved), sizeof(fr_kv_append_desc)},
+#undef F
+#define F(f) AT(fr_attend_desc, f)
+        {F(cache), F(q), F(out), F(lse), F(q_stride), F(out_stride), F(q_begin), F(prefix_pages), F(pages), F(own_len), F(pages_stride), F(n_tokens),
+         F(n_seqs), F(n_q_heads), F(max_q), F(prefix_len), F(max_own_len), F(scale), F(reserved), F(workspace), F(workspace_bytes), sizeof(fr_attend_desc)},
+#undef F
+#define F(f) AT(fr_sample_desc, f)
+        {F(logits), F(row_stride), F(dtype), F(n_rows), F(n_vocab), F(reserved), F(temperature), F(top_k), F(top_p), F(min_p), F(uniform), F(token),
+         F(workspace), F(workspace_bytes), sizeof(fr_sample_desc)},
+#undef F
+#undef AT
+    };
+    PyObject* all = PyList_New(0);
+    for (const auto& s : structs)
+        for (long x : s) {
+            PyObject* y = all ? PyLong_FromLong(x) : nullptr;
+            if (!y || PyList_Append(all, y)) Py_CLEAR(all);
+            Py_XDECREF(y);
+        }
+    return all;
+}
+
 template <typename F> PyCFunction method(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f)); }
 
 PyMethodDef methods[] = {
+    {"layout", method(layout), METH_FASTCALL, nullptr},
     {"entries", method(entries), METH_FASTCALL, nullptr},
     {"kv_append", method(guarded<of_append, 11>), METH_FASTCALL, nullptr},
     {"attend_shared", method(guarded<of_attend, 15>), METH_FASTCALL, nullptr},

@@ -1,5 +1,6 @@
 """More of what the text-generation calls refuse and ask for, before anything touches a GPU."""
 import ctypes as C
+import os
 import random
 
 import pytest
@@ -54,3 +55,23 @@ def test_the_workspace_of_a_larger_call_is_enough_for_a_smaller_one():
     assert _need(16 * 300, 16, 300, 8192, 700)[1] <= _need(16 * 700, 16, 700, 8192, 700)[1]
     # a decoding step asks for some MB, not for what the largest possible cut would take
     assert _need(64, 64, 1, 16384, 1500)[1] < 64 << 20
+
+
+def test_a_module_built_from_another_header_is_not_loaded(monkeypatch, tmp_path):
+    pytest.importorskip("torch")
+    fr.binding._torch_calls()
+    other = type("fr_sample_desc", (C.Structure,), {"_fields_": list(reversed(fr.fr_sample_desc._fields_))})
+    assert C.sizeof(other) == C.sizeof(fr.fr_sample_desc)
+    monkeypatch.setattr(fr.binding, "_calls", None)
+    monkeypatch.setattr(fr.binding, "fr_sample_desc", other)
+    with pytest.raises(RuntimeError, match="another include/freeride.h"):
+        fr.binding._torch_calls()
+    # and an old one is built anew where only what is stale is built
+    build = fr.binding._build
+    module = tmp_path / "module.so"
+    monkeypatch.setattr(build, "TORCH_CALLS", str(module))
+    assert build.torch_calls_is_stale()
+    module.write_bytes(b"")
+    assert not build.torch_calls_is_stale() and build.build_torch_calls(force=False) == str(module)
+    os.utime(module, (1, 1))
+    assert build.torch_calls_is_stale()
