@@ -421,7 +421,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 const double all = __builtin_bit_cast(double, of_lane(__builtin_bit_cast(uint64_t, sum_up_to(in_wave)), 15));
                 __syncthreads();
                 const Sums held = scan_of(no, yes, 0, 0, (uint64_t)(fmaxf(n1 - n0, 0.0f) * w0 * 0x1p30f), (uint64_t)(fmaxf(n2 - n1, 0.0f) * w1 * 0x1p30f));
-                const uint64_t want = (uint64_t)(fmin((double)p * 1.05, 1.0 - 0.7 * (1.0 - (double)p)) * all * 0x1p30);
+                const uint64_t want = (uint64_t)fmax(fmin((double)p * 1.05, 1.0 - 0.7 * (1.0 - (double)p)) * all * 0x1p30, 1.0);     // (top_p may be 0 and below)
                 if (want <= held.all_m) {
                     last = min(last, find(held, true, want).digit + 4);
                     rank = V;

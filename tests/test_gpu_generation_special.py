@@ -322,3 +322,19 @@ def test_calls_without_a_stream_work_on_the_current_one():
         a, b = out.clone(), token.clone()
     side.synchronize()
     assert bool((a == 3.0).all()) and int(b) == 77
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_sample_shares_of_nothing_and_next_to_nothing(dt):
+    # top_p of 0, below 0 and too small for any share but the first entry's: the largest logit, the lowest index of equals
+    print("sample nothing", dt, flush=True)
+    V = 70001
+    p = [0.0, -0.0, -1.0, -math.inf, 1e-12, 1e-30, 1e-45, -1e-45]
+    g = torch.Generator().manual_seed(1)
+    logits = torch.randn((2 * len(p), V), generator=g).to(torch.bfloat16 if dt == "bf16" else torch.float32).cuda()
+    logits[:, 500:600] = 9.0
+    logits[len(p):, 600:60000] = 9.0                   # (many equal ones)
+    token = torch.full((2 * len(p),), -7, dtype=torch.int32, device="cuda")
+    fr.fr_sample(logits, torch.full((2 * len(p),), 0.99, device="cuda"), token, top_p=torch.tensor(p * 2, dtype=torch.float32, device="cuda"))
+    torch.cuda.synchronize()
+    assert token.tolist() == [500] * (2 * len(p))
