@@ -338,3 +338,64 @@ def test_sample_shares_of_nothing_and_next_to_nothing(dt):
     fr.fr_sample(logits, torch.full((2 * len(p),), 0.99, device="cuda"), token, top_p=torch.tensor(p * 2, dtype=torch.float32, device="cuda"))
     torch.cuda.synchronize()
     assert token.tolist() == [500] * (2 * len(p))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [4095, 4096, 4097])
+def test_sample_vocabularies_about_what_there_is_room_for(dt, V):
+    # 4096 entries have room, and up to 1740 of more are taken in one go; rows without and with equal entries
+    print("sample room", dt, V, flush=True)
+    rng = np.random.default_rng(V)
+    n = 24
+    x = 10.0 - 1.7 * np.log1p(np.stack([rng.permutation(V) for _ in range(n)])) + 0.5 * rng.standard_normal((n, V))
+    x[n // 2:] = np.round(x[n // 2:])
+    x[n - 1] = 3.0
+    types = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+    logits = torch.from_numpy(x).to(types[dt]).cuda()
+    x = _f64(logits)
+    for top_k, top_p in ((0, 1.0), (0, 0.95), (0, 0.5), (1739, 1.0), (1740, 1.0), (1741, 1.0), (1740, 0.9), (1741, 0.9), (V - 1, 1.0), (V - 1, 0.9), (V, 0.9)):
+        T, K, P, U, want = [], [], [], [], []
+        for r in range(n):
+            t = float(np.float32(rng.uniform(0.5, 1.5)))
+            w, y = oracle.weights(x[r], t)
+            order = np.argsort(-y, kind="stable")[: top_k or V]
+            run = np.cumsum(w[order])
+            p = 1.0
+            if top_p < 1:                              # the middle of an entry's share, so that roundings of 32 bits do not decide
+                j = int(np.searchsorted(run, top_p * run[-1]))
+                p = float(np.float32((run[j] - w[order][j] / 2) / run[-1]))
+            index, w = oracle.kept(x[r], t, top_k, p, 0.0)
+            run = np.cumsum(w[index])
+            big = np.flatnonzero(w[index] / run[-1] >= 2.0 ** -14)
+            j = int(rng.choice(big))
+            T.append(t), K.append(top_k), P.append(p), U.append(float((run[j] - w[index][j] / 2) / run[-1])), want.append(int(index[j]))
+        token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+        f = lambda y, kind=torch.float32: torch.tensor(y, dtype=kind, device="cuda")
+        fr.fr_sample(logits, f(U), token, temperature=f(T), top_k=f(K, torch.int32), top_p=f(P))
+        got = token.tolist()
+        assert got == want, (top_k, top_p, [r for r in range(n) if got[r] != want[r]])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_sample_counts_about_the_last_that_is_taken_in_one_go(dt):
+    # 1740 is the last; what is above the line that so many values of threads are above has room, or nearly
+    print("sample counts", dt, flush=True)
+    rng = np.random.default_rng(3)
+    types = {"bf16": torch.bfloat16, "f32": torch.float32}
+    for V in (4097, 5000, 20011, 131072):
+        K = [1023, 1024, 1025, 1738, 1739, 1740, 1741, 1742]
+        for spread in (0.01, 1.0, 30.0):
+            x = rng.standard_normal((len(K), V)) * spread
+            x[3] = np.sort(x[3])                       # the largest side by side, in few threads' shares
+            x[4] = np.sort(x[4])[::-1]
+            x[5, : V // 2] = x[5].max()
+            logits = torch.from_numpy(x).to(types[dt]).cuda()
+            y = _f64(logits)
+            for u in (0.0, 0.9999999):
+                token = torch.full((len(K),), -7, dtype=torch.int32, device="cuda")
+                f = lambda z, kind=torch.float32: torch.tensor(z, dtype=kind, device="cuda")
+                fr.fr_sample(logits, f([u] * len(K)), token, temperature=f([1e4] * len(K)), top_k=f(K, torch.int32))
+                got = token.tolist()
+                for r, k in enumerate(K):              # weights nearly equal: the first and the last of the kept indices
+                    index = np.sort(np.argsort(-y[r], kind="stable")[:k])
+                    assert got[r] == (index[0] if u == 0.0 else index[-1]), (V, spread, k, u)
