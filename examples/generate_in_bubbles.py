@@ -1,7 +1,7 @@
 """Text generation as a side task: a batch of sequences behind one shared prompt, a token each a step, in a stage's bubbles.
 
 A small decoder (random weights) on the library's own operators: fr_gemm_bf16 for the products, fr_kv_append (positions rotated,
-keys and values into pages), fr_attend_shared (the prompt's keys read once for the whole batch), fr_sample (the next token);
+keys and values into pages), fr_attend_shared (the prompt's keys lie there once for the whole batch), fr_sample (the next token);
 torch does the rest (norms, residual sums, table look-ups).  A step is one token of every sequence: short, of known length, and
 the state between two steps lies in device memory, so a bubble takes as many steps as fit and the next bubble goes on from there.
 A step is captured in a HIP graph once; run_step replays it on the side stream.

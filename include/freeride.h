@@ -640,7 +640,7 @@ int fr_kv_append(const fr_kv_append_desc* d, void* stream);
  * t sees the prefix_len shared keys and its first own_len[b] - t + 1 + i own ones (all of it counted from 0; with more
  * tokens than own keys the first tokens see the prefix only).  With scores x_j = scale <q, k_j> over the keys it sees,
  *     out = sum_j exp(x_j) v_j / sum_j exp(x_j),    lse = log sum_j exp(x_j);
- * a token that sees nothing gets zeros and -infinity.  Query head h reads key head h / (n_q_heads / n_kv_heads).  Slots
+ * a token that sees nothing, or only scores of -infinity, gets zeros and -infinity.  Query head h reads key head h / (n_q_heads / n_kv_heads).  Slots
  * behind a length are never used, whatever they hold; neither does a key that a token may not see change its result.
  * Scores, softmax and sums are held in 32 bits; the weights exp(x_j - max) are rounded to the cache's type for the
  * product with v (to its 8 or 11 significant bits; fp16 weights from 2^-21 down to fewer, below 2^-32 to 0), as is the result.

@@ -74,7 +74,7 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 template <int kLeft> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(kLeft) : "memory"); }
 // Global memory to LDS without passing through registers, 16 bytes (or 4) a lane: lane l's go to LDS address lds + 16 l (4 l).
 // Written as assembly so that the compiler does not wait for every load in flight before each read of LDS; which loads have to be
-// here is counted by hand.
+// here is counted by hand.  (m0 is reserved and cannot be named as overwritten; no instruction of these kernels but the two uses it.)
 __device__ __forceinline__ void load16_to_lds(uint32_t lds, const void* g)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory");

@@ -140,6 +140,45 @@ def test_values_that_only_later_tokens_see(D, G, P, t):
     c.check()
 
 
+@pytest.mark.parametrize("kind", range(len(KINDS)))
+def test_scores_of_infinity(kind):
+    # keys whose score is -infinity have no weight; a row that sees no others gets zeros and -infinity; +infinity makes NaN
+    Hq, Hk, D, page, P, own, new = KINDS[kind]
+    print("attend scores", *KINDS[kind][:5], len(own), flush=True)
+    c = _Batch("bf16", Hq, Hk, D, page, P, own, new, seed=kind)
+    c.q[:, :, 0] = 1.0
+    for b in range(len(own)):
+        for j in range(own[b]):                        # all own keys
+            at, slot = c.place(b, P + j)
+            c.k[at, :, slot, 0] = -math.inf
+    if P:
+        c.prepare()                                    # (every token sees the prefix, and that alone counts)
+        c.call()
+        torch.cuda.synchronize()
+        out, lse = _f64(c.out), _f64(c.lse)
+        k, v, q = _f64(c.k), _f64(c.v), _f64(c.q)
+        places = np.array([c.place(0, j) for j in range(P)])
+        for row in range(0, q.shape[0], max(1, q.shape[0] // 50)):
+            for h in range(0, Hq, 3):
+                o, l, a, x = oracle.attend_row(q[row, h], k[places[:, 0], h // (Hq // Hk), places[:, 1]], v[places[:, 0], h // (Hq // Hk), places[:, 1]], c.scale)
+                d = (D + 4) * 2.0 ** -24 * x + 2.0 ** -20
+                near = (UNIT["bf16"] + 2 * d + P * 2.0 ** -23) * a + UNIT["bf16"] * np.abs(o) * 1.01 + TINY["bf16"]
+                assert np.all(np.abs(out[row, h] - o) <= near) and abs(lse[row, h] - l) <= d + P * 2.0 ** -23 + 2.0 ** -20 * (1 + abs(l)), (row, h)
+    else:
+        c.prepare()
+        c.call()
+        torch.cuda.synchronize()
+        assert not c.out.any() and bool((c.lse == -math.inf).all())
+    if own[0]:
+        at, slot = c.place(0, 0)
+        c.k[at, :, slot, 0] = math.inf
+        c.prepare()
+        c.call()
+        torch.cuda.synchronize()
+        first = c.out[: new[0]] if not P else c.out
+        assert bool(torch.isnan(first.float()).all())
+
+
 def test_small_weights_of_many_keys_add_up():
     # one key far ahead of the others, whose weights of 2^-26 are too small for 16 bits by themselves but not together
     n, D = 2000, 64
