@@ -640,8 +640,9 @@ int fr_kv_append(const fr_kv_append_desc* d, void* stream);
  * t sees the prefix_len shared keys and its first own_len[b] - t + 1 + i own ones (all of it counted from 0; with more
  * tokens than own keys the first tokens see the prefix only).  With scores x_j = scale <q, k_j> over the keys it sees,
  *     out = sum_j exp(x_j) v_j / sum_j exp(x_j),    lse = log sum_j exp(x_j);
- * a token that sees nothing, or only scores of -infinity, gets zeros and -infinity.  Query head h reads key head h / (n_q_heads / n_kv_heads).  Slots
- * behind a length are never used, whatever they hold; neither does a key that a token may not see change its result.
+ * a token that sees nothing, or only scores of -infinity, gets zeros and -infinity.  Query head h reads key head
+ * h / (n_q_heads / n_kv_heads).  Slots behind a length are never used, whatever they hold; neither does a key that a token may
+ * not see change its result, while values that are not finite of keys that it sees show in it as the formula says.
  * Scores, softmax and sums are held in 32 bits; the weights exp(x_j - max) are rounded to the cache's type for the
  * product with v (to its 8 or 11 significant bits; fp16 weights from 2^-21 down to fewer, below 2^-32 to 0), as is the result.
  * Bounds on the device's numbers: a page id outside the cache counts as the nearest one inside, own_len is cut to
@@ -701,7 +702,7 @@ typedef struct fr_sample_desc {
     void*          workspace;      /* fr_sample_workspace_bytes of it, 256-byte aligned; NULL if that is 0    */
     uint64_t       workspace_bytes;
 } fr_sample_desc;
-/* Reads dtype, n_rows and n_vocab of d only. */
+/* Reads dtype, n_rows and n_vocab of d only.  0 for every size at present: a row is finished in LDS. */
 int fr_sample_workspace_bytes(const fr_sample_desc* d, uint64_t* bytes_out);
 int fr_sample(const fr_sample_desc* d, void* stream);
 

@@ -11,10 +11,10 @@
 // What bounds it:
 //   Decoding from long caches, the reading: 8 sequences of 20000 to 65536 tokens, 1.62 GB in 285 us, 5.7 TB/s (a kernel that only
 //     reads reaches 6.5).
-//   Prompts, the matrix cores: 16 questions of 300 to 700 tokens about 8192, 32 heads, 1.03 TFLOP in 1.05 ms, 0.98 PFLOP/s (a library
-//     product of 8192 x 8192 matrices 1.25); beside them the vector units make 2 exps and 5 other operations of every two weights.
-//   Decoding behind a prefix, neither: of 64 sequences behind 16384 keys (78 us) the prefix' products alone take 38 us, the own keys'
-//     reading alone 40, and the two kinds of workgroups slow one another down; then the parts are joined, 7 us.
+//   Prompts, the matrix cores: 16 questions of 300 to 700 tokens about 8192, 32 heads, 1.03 TFLOP in 1.04 to 1.08 ms, 0.95 to 0.99
+//     PFLOP/s (a library product of 8192 x 8192 matrices 1.25), 4 prompts of 4096 by themselves 0.55 in 0.62 ms; beside them the vector units make 2 exps and 5 other operations of every two weights.
+//   Decoding behind a prefix, neither: 64 sequences behind 16384 keys take 63 us in a kernel trace, the prefix' workgroups by
+//     themselves 33 and the own keys' 36: the two kinds slow one another down; then the parts are joined, 7 us.
 //   A few short sequences, the launch: 5 us.
 
 #include <algorithm>
@@ -497,8 +497,8 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
         // A weight of 0 for a key that a row does not see, times a value that is not finite, is not 0.  Keys from `hidden` on are not
         // seen by every row of the workgroup: where a result is not finite and one of them has such a value, the sums are made again,
         // with zeros for these values, and what they are to the rows that see them is added.  Fragments come straight from memory, V an
-        // element at a time, so that it takes the keys three times as long as the loop above, once; where all that is not finite is seen
-        // by every row, nothing is made again.
+        // element at a time, with a third of the pace: 4 questions of 300 tokens about 4096, 67 us, one NaN in a question 213; in the
+        // document, where every row sees it and nothing is made again, 68.
         const int hidden = w.seen_step ? max(w.k0, min(rows.seen(w.row0), w.k1)) : w.k1;
         auto place_of = [&](int j) {                        // (of a key behind the last: that of the last)
             j = min(j, w.k1 - 1);
@@ -766,8 +766,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void k_attend(AttendArgs
 }
 
 // Joins the parts of a row: twice four elements a thread, kLanes threads for every eight, each with every kLanes-th part.  Bound by
-// latency (the launch, the sequence's length, then all parts in one go): 33 sequences of up to 6 tokens with 15 heads 7 us of 22, 64
-// sequences with 32 heads and 22 parts, 23 MB, 7 of 72.  (With the parts' maxima first and then the parts, four at once, by 16 threads
+// latency (the launch, the sequence's length, then all parts in one go): 33 sequences of up to 6 tokens with 15 heads 5 us of 21, 64
+// sequences with 32 heads and 22 parts, 23 MB, 7 of 70.  (With the parts' maxima first and then the parts, four at once, by 16 threads
 // from 17 parts on, 1.5 to 2 us more.)
 template <typename T, int D, int kLanes>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, int row_blocks, int first_block)
@@ -1019,8 +1019,10 @@ Plan plan(const fr_attend_desc& d, int cus, bool whole = false)
             // Short caches: a wavefront an item.  By themselves, where each unit has four of up to 256 keys: 256 sequences of 64 keys with 8 key
             // heads 12 us, a workgroup an item 20, 128 of 200 17 and 19; of 400 50 either way, 64 of 200 12 and 10, of 800 28 and 25.
             // Behind a prefix, whose workgroups take half of a unit, items of 256 keys (128 where they are few, more where they are many),
-            // if there are enough, of up to 2048 keys, 512 where there are many: 16 of 1500 20 and 23, 64 of 400 25 and 27, 256 of 64 30
-            // and 38, of 512 with 64 heads 95 and 98; 256 of 800 137 and 130.  64 of up to 1500 behind 16384: 73.5; in parts of 512 77.1.
+            // if there are enough, of up to 2048 keys, 512 where there are many.  A wavefront and a workgroup an item, up to so many own keys
+            // behind 4096: 64 sequences, 32 heads: 300 24 and 26, 512 27 and 31, 1500 48 and 53, 2000 73 and 71; 128, 64 heads: 300 39 and 41,
+            // 512 43 and 46, 600 52 and 50, 1100 86 and 77; 256, 32 heads: 100 38 and 44, 400 60 either way, 512 71 either way, 600 93 and 86;
+            // 64 heads: 400 74 and 76, 512 86 and 88, 600 104 and 98.  64 of up to 1500 behind 16384: 73.5; in parts of 512 77.1.
             int64_t wave_len = base < cus ? 128 : 256;
             while (base * up(keys, wave_len) > (base < cus ? 4 : 16) * cus && wave_len < keys) wave_len *= 2;
             const bool enough = !whole && base >= cus / 2 && base * up(keys, wave_len) >= (base < cus ? 4 : 3) * cus / 2;
