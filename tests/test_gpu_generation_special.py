@@ -438,3 +438,26 @@ def test_sample_counts_about_the_last_that_is_taken_in_one_go(dt):
                 for r, k in enumerate(K):              # weights nearly equal: the first and the last of the kept indices
                     index = np.sort(np.argsort(-y[r], kind="stable")[:k])
                     assert got[r] == (index[0] if u == 0.0 else index[-1]), (V, spread, k, u)
+
+
+@pytest.mark.parametrize("P,own,T", [(0, 5000, 6000), (3000, 900, 4000)])
+def test_few_tokens_of_many_are_in_a_sequence(P, own, T):
+    # parts of all tokens' results would take more than the call has room for: it is made in one
+    print("attend few of many", P, own, T, flush=True)
+    c = _Batch("bf16", 8, 2, 128, 16, P, [own, own // 2, 3], [T, 0, 0], seed=P)
+    c.prepare()
+    begin = np.array([T // 2, T // 2 + 1, T // 2 + 2, T // 2 + 3], dtype=np.int32)
+    c.limits["max_q"] = 1
+    c.more["q_begin"] = torch.from_numpy(begin).cuda()
+    c.workspace = torch.empty(max(1, fr.fr_attend_shared_workspace_bytes(c.cache, c.gq, 3, **c.limits)), dtype=torch.uint8, device="cuda")
+    c.call()
+    torch.cuda.synchronize()
+    out, lse = c.out.clone(), c.lse.clone()
+    there = slice(T // 2, T // 2 + 3)
+    few = _Batch("bf16", 8, 2, 128, 16, P, [own, own // 2, 3], [1, 1, 1], seed=P)
+    few.k, few.v, few.prefix_pages, few.table, few.q = c.k, c.v, c.prefix_pages, c.table, c.q[there].contiguous()
+    few.check()
+    assert bool(((out[there].float() - few.out.float()).abs() <= 2.0 ** -7 * few.out.float().abs() + 2.0 ** -8).all())
+    assert bool(((lse[there] - few.lse).abs() <= 1e-4).all())
+    out[there], lse[there] = 9.0, 9.0
+    assert bool((out == 9.0).all()) and bool((lse == 9.0).all())
