@@ -12,7 +12,8 @@
 //   Decoding from long caches, the reading: 8 sequences of 20000 to 65536 tokens, 1.62 GB in 285 us, 5.7 TB/s (a kernel that only
 //     reads reaches 6.5).
 //   Prompts, the matrix cores: 16 questions of 300 to 700 tokens about 8192, 32 heads, 1.03 TFLOP in 1.04 to 1.08 ms, 0.95 to 0.99
-//     PFLOP/s (a library product of 8192 x 8192 matrices 1.25), 4 prompts of 4096 by themselves 0.55 in 0.62 ms; beside them the vector units make 2 exps and 5 other operations of every two weights.
+//     PFLOP/s (a library product of 8192 x 8192 matrices 1.25), 4 prompts of 4096 by themselves 0.55 in 0.62 ms; beside them the vector
+//     units make 2 exps and 5 other operations of every two weights.
 //   Decoding behind a prefix, neither: 64 sequences behind 16384 keys take 63 us in a kernel trace, the prefix' workgroups by
 //     themselves 33 and the own keys' 36: the two kinds slow one another down; then the parts are joined, 7 us.
 //   A few short sequences, the launch: 5 us.
@@ -527,11 +528,11 @@ __device__ __forceinline__ void attend(const AttendArgs& a, const Item& w, char*
 #pragma unroll
                 for (int i = 0; i < State::kInBlock; ++i) bad |= !(fabsf(x.o[d][i]) < INFINITY);
         }
-        if (__any(bad)) {
+        if (__builtin_expect(__any(bad), 0)) {
             bad = false;
             for (int j = hidden; j < w.k1; j += 64) bad |= spoilt(j) != 0;
         }
-        if (__any(bad)) {
+        if (__builtin_expect(__any(bad), 0)) {
             const float base = x.base(c);
             x.clear();
             constexpr int kBlocks = 32 / kCols, kInRow = 512 / kCols;       // blocks of 32 keys; keys of a fragment of weights
