@@ -706,6 +706,121 @@ typedef struct fr_sample_desc {
 int fr_sample_workspace_bytes(const fr_sample_desc* d, uint64_t* bytes_out);
 int fr_sample(const fr_sample_desc* d, void* stream);
 
+/* ------------------------------------------------------------------ a cache held in 8 bits */
+/*
+ * Of what a text-generation task books, its cache is most: held in 8 bits it is half of it, and so are the bytes of a step.  A number
+ * of the cache is a code of 8 bits, e4m3 (a sign, 4 bits of exponent, 3 of mantissa; the largest is 448, 0x7f and 0xff are NaN, there
+ * is no infinity), times the power of two that its block has: `block` consecutive slots of a page, of one head, have one scale byte s
+ * for K and one for V, which stands for 2^(s' - 127), s' being s cut to 10 .. 246 (FR_DTYPE_BF16) or 112 .. 134 (FR_DTYPE_F16).
+ * With these every number of the cache is one of the 16-bit type too, which is the type of queries, new keys, values and results.
+ * As above: asynchronous on `stream`, nothing allocated or kept, device pointers of the current device, numbers on the device bounded.
+ */
+/* Code (page, head, slot, i) of K lies at k[page * page_stride + head * head_stride + slot * slot_stride + i], of V likewise; the scale
+   byte of block j of a page at k_scale[page * scale_page_stride + head * scale_head_stride + j * scale_block_stride], of V likewise.
+   Strides are in bytes, from 0 to 2^31 - 1, those of codes multiples of 16; k and v are 16-byte aligned. */
+typedef struct fr_kv8_pages {
+    void*    k;
+    void*    v;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int64_t  n_pages;              /* 1 .. 2^31 - 1                                                           */
+    int64_t  page_stride, head_stride, slot_stride;
+    int64_t  scale_page_stride, scale_head_stride, scale_block_stride;
+    int32_t  n_kv_heads;           /* 1 .. 1024                                                               */
+    int32_t  head_dim;             /* 64 or 128                                                               */
+    int32_t  page_size;            /* a power of two, 1 .. 4096                                               */
+    int32_t  block;                /* slots of a scale: a power of two, 1 .. 128, page_size at most           */
+    int32_t  dtype;                /* FR_DTYPE_BF16 or FR_DTYPE_F16                                           */
+    int32_t  reserved;
+} fr_kv8_pages;
+
+/*
+ * fr_kv8_append: fr_kv_append into such a cache.  q_out is as there; rotated keys and values are not rounded to the 16-bit type but, from
+ * their exact values (a rotation's two products, their sum rounded to 53 bits), to codes: nearest, ties to even, at most 448 in magnitude; what
+ * is not finite becomes NaN.  A block's scale, of K or V, is the least with 448 * 2^(s - 127) >= the magnitude of every finite number
+ * that the call stores there, cut to the type's range.  If the block's first slot is not among the call's, the block goes on: its scale is
+ * no less than it was, and where it grows the codes of its other slots are rounded again to the new one (a power of two: exact, but for those
+ * that fall among or below the smallest codes).
+ * A block's tokens follow one another in the call, with rising slots (with block 1: in any order); where they do not, what its slots and
+ * scale hold is not defined.  Slots are distinct where not padding, as there.
+ */
+typedef struct fr_kv8_append_desc {
+    fr_kv8_pages cache;
+    const void* k;                 /* the rest as in fr_kv_append_desc                                        */
+    const void* v;
+    const void* q;
+    void*       q_out;
+    int64_t     k_stride, v_stride, q_stride, q_out_stride;
+    const int64_t* slot;
+    const int32_t* position;
+    const float*   rotary;
+    int32_t     n_positions, rotary_dim;
+    int32_t     style;
+    int32_t     n_tokens;
+    int32_t     n_q_heads;
+    int32_t     reserved;
+} fr_kv8_append_desc;
+int fr_kv8_append(const fr_kv8_append_desc* d, void* stream);
+
+/*
+ * fr_attend_kv8: attention to such a cache, to all of a sequence or to a window.  The sequences' tokens lie one after the other, those of
+ * sequence b at q_begin[b] .. q_begin[b + 1]; they are the last of its lens[b] keys.  Its token i of t has n = lens[b] - t + 1 + i keys up
+ * to and with its own, and sees key j < n if
+ *     window is 0, or j >= n - window, or j < sinks:
+ * the window last ones and the first few, which stay visible.  out and lse are as in fr_attend_shared, of scores and values that the
+ * codes and scales stand for; a token that sees nothing gets zeros and -infinity; keys that a token does not see do not change its result,
+ * whatever they hold, and NaN among those that it sees shows as the formula says.  Page ids of keys that no token of the call sees are not
+ * used: their pages may have been given to others.  A sequence's pages may also be another's: a prompt may lie there once for several.
+ * Bounds on the device's numbers: a page id outside the cache counts as the nearest one inside, lens is cut to 0 .. max_len, q_begin to
+ * 0 .. n_tokens, a sequence's tokens beyond max_q and tokens in no sequence are not computed.
+ */
+typedef struct fr_attend_kv8_desc {
+    fr_kv8_pages cache;
+    const void* q;                 /* [n_tokens][n_q_heads][head_dim] of the cache's 16-bit type              */
+    void*       out;               /* as q; not q itself                                                      */
+    float*      lse;               /* [n_tokens][n_q_heads], or NULL                                          */
+    int64_t     q_stride, out_stride;         /* elements from token to token, multiples of 8                 */
+    const int32_t* q_begin;        /* [n_seqs + 1] ascending; NULL: one token each (n_tokens = n_seqs)        */
+    const int32_t* pages;          /* [n_seqs], pages_stride apart: page ids; NULL if max_len is 0            */
+    const int32_t* lens;           /* [n_seqs]; NULL if max_len is 0                                          */
+    int64_t     pages_stride;      /* >= ceil(max_len / page_size)                                            */
+    int32_t     n_tokens, n_seqs;  /* 0: nothing to do                                                        */
+    int32_t     n_q_heads;         /* a multiple of n_kv_heads, up to 1024                                    */
+    int32_t     max_q;             /* upper bound of a sequence's tokens in this call, >= 1                   */
+    int32_t     max_len;           /* 0 .. 2^31 - 8192                                                        */
+    int32_t     window;            /* 0: all keys                                                             */
+    int32_t     sinks;             /* >= 0                                                                    */
+    float       scale;             /* positive and finite                                                     */
+    void*       workspace;         /* fr_attend_kv8_workspace_bytes of this or a larger call, 256-byte aligned;
+                                      free again when the call's work on the stream is done                   */
+    uint64_t    workspace_bytes;
+} fr_attend_kv8_desc;
+/* Reads the sizes of d only (no pointer).  A call of the same heads and head_dim with no larger n_tokens, n_seqs, max_q and max_len and any window
+   and sinks needs no more. */
+int fr_attend_kv8_workspace_bytes(const fr_attend_kv8_desc* d, uint64_t* bytes_out);
+int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream);
+
+/*
+ * fr_kv_copy_pages: page target[i] = page source[i] for pairs i < n_pairs, in every one of some caches (those of a model's layers), K, V and
+ * scales: what is left to do on the GPU when sequences fork (their last, partly filled page), when a cache is compacted, when pages come back.
+ * The caches may differ in everything but n_pages.  All pairs are carried out at once.  Left out are
+ *   pairs with a page id outside the cache (padding), pairs of a page with itself,
+ *   pairs whose target a later pair has as well (the last one counts),
+ *   pairs whose source is the target of another pair that is not padding (it would be read while it is written);
+ * copied[i] says of each pair whether it was carried out.
+ */
+typedef struct fr_kv_copy_desc {
+    const fr_kv_pages*  caches;    /* host, [n_caches], read during the call; NULL if there are none          */
+    const fr_kv8_pages* caches8;   /* host, [n_caches8], likewise                                             */
+    int32_t     n_caches, n_caches8;          /* 0 .. 4096                                                    */
+    const int32_t* source;         /* device, [n_pairs]                                                       */
+    const int32_t* target;
+    int32_t*    copied;            /* device, [n_pairs]: 1 or 0; or NULL                                      */
+    int32_t     n_pairs;           /* 0: nothing to do; up to 2^20                                            */
+    int32_t     reserved;
+} fr_kv_copy_desc;
+int fr_kv_copy_pages(const fr_kv_copy_desc* d, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

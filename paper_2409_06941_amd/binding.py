@@ -156,6 +156,29 @@ class fr_sample_desc(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
+class fr_kv8_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int64),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("slot_stride", C.c_int64), ("scale_page_stride", C.c_int64),
+                ("scale_head_stride", C.c_int64), ("scale_block_stride", C.c_int64), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("block", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class fr_kv8_append_desc(C.Structure):
+    _fields_ = [("cache", fr_kv8_pages)] + fr_kv_append_desc._fields_[1:]
+
+
+class fr_attend_kv8_desc(C.Structure):
+    _fields_ = [("cache", fr_kv8_pages), ("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("q_stride", C.c_int64),
+                ("out_stride", C.c_int64), ("q_begin", C.c_void_p), ("pages", C.c_void_p), ("lens", C.c_void_p), ("pages_stride", C.c_int64),
+                ("n_tokens", C.c_int32), ("n_seqs", C.c_int32), ("n_q_heads", C.c_int32), ("max_q", C.c_int32), ("max_len", C.c_int32),
+                ("window", C.c_int32), ("sinks", C.c_int32), ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class fr_kv_copy_desc(C.Structure):
+    _fields_ = [("caches", C.POINTER(fr_kv_pages)), ("caches8", C.POINTER(fr_kv8_pages)), ("n_caches", C.c_int32), ("n_caches8", C.c_int32),
+                ("source", C.c_void_p), ("target", C.c_void_p), ("copied", C.c_void_p), ("n_pairs", C.c_int32), ("reserved", C.c_int32)]
+
+
 # name -> (restype, argtypes); every symbol the header declares
 SIGNATURES = {
     "fr_create": (C.c_int, [C.POINTER(fr_config), C.POINTER(C.c_void_p)]),
@@ -213,6 +236,10 @@ SIGNATURES = {
     "fr_attend_shared": (C.c_int, [C.POINTER(fr_attend_desc), C.c_void_p]),
     "fr_sample_workspace_bytes": (C.c_int, [C.POINTER(fr_sample_desc), C.POINTER(C.c_uint64)]),
     "fr_sample": (C.c_int, [C.POINTER(fr_sample_desc), C.c_void_p]),
+    "fr_kv8_append": (C.c_int, [C.POINTER(fr_kv8_append_desc), C.c_void_p]),
+    "fr_attend_kv8_workspace_bytes": (C.c_int, [C.POINTER(fr_attend_kv8_desc), C.POINTER(C.c_uint64)]),
+    "fr_attend_kv8": (C.c_int, [C.POINTER(fr_attend_kv8_desc), C.c_void_p]),
+    "fr_kv_copy_pages": (C.c_int, [C.POINTER(fr_kv_copy_desc), C.c_void_p]),
 }
 
 _lib = None
@@ -575,11 +602,12 @@ def _torch_calls():
         loader = importlib.machinery.ExtensionFileLoader("_torch_calls", _build.TORCH_CALLS)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_torch_calls", loader))
         loader.exec_module(module)
-        want = [x for s in (fr_kv_pages, fr_kv_append_desc, fr_attend_desc, fr_sample_desc)
+        want = [x for s in (fr_kv_pages, fr_kv_append_desc, fr_attend_desc, fr_sample_desc, fr_kv8_pages, fr_kv8_append_desc, fr_attend_kv8_desc, fr_kv_copy_desc)
                 for x in [getattr(s, f[0]).offset for f in s._fields_] + [C.sizeof(s)]]
         if module.layout() != want:
             raise RuntimeError("%s was built from another include/freeride.h: build again" % _build.TORCH_CALLS)
-        module.entries(*(C.cast(f, C.c_void_p).value for f in (L.fr_kv_append, L.fr_attend_shared, L.fr_sample)), torch.cuda.current_stream)
+        module.entries(*(C.cast(f, C.c_void_p).value for f in (L.fr_kv_append, L.fr_attend_shared, L.fr_sample, L.fr_kv8_append, L.fr_attend_kv8,
+                                                               L.fr_kv_copy_pages)), torch.cuda.current_stream)
         _calls = module
     return _calls
 
@@ -640,3 +668,63 @@ def fr_sample_workspace_bytes(logits):
 
 def fr_sample(logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None, stream=None):
     return _check((_calls or _torch_calls()).sample(logits, uniform, token, temperature, top_k, top_p, min_p, workspace, stream), "fr_sample")
+
+
+class Kv8Pages:
+    """fr_kv8_pages of torch tensors: codes [n_pages, n_kv_heads, page_size, head_dim] with the same strides, uint8 or float8_e4m3fn, and
+    scale bytes [n_pages, n_kv_heads, page_size / block], uint8 (views are fine).  dtype: the 16-bit type of queries, keys, values, results.
+
+    The calls below take torch tensors, all on one GPU, and without a stream work on torch's current one there."""
+
+    def __init__(self, k, v, k_scale, v_scale, dtype):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v: [n_pages, n_kv_heads, page_size, head_dim], alike in shape, strides and type")
+        if str(k.dtype) not in ("torch.uint8", "torch.float8_e4m3fn"):
+            raise TypeError("k and v: uint8 or float8_e4m3fn, not %s" % k.dtype)
+        if k.stride(3) != 1:
+            raise ValueError("the elements of a head have to lie side by side")
+        if k_scale.dim() != 3 or k_scale.shape[:2] != k.shape[:2] or k_scale.shape != v_scale.shape or k_scale.stride() != v_scale.stride():
+            raise ValueError("k_scale and v_scale: [n_pages, n_kv_heads, page_size / block], alike in shape and strides")
+        if str(k_scale.dtype) != "torch.uint8" or k_scale.dtype != v_scale.dtype:
+            raise TypeError("k_scale and v_scale: uint8 is needed")
+        if k_scale.shape[2] < 1 or k.shape[2] % k_scale.shape[2]:
+            raise ValueError("k_scale: the blocks of a page have to be of one size")
+        name = str(dtype)[len("torch."):]
+        if name not in ("bfloat16", "float16"):
+            raise TypeError("%s: the library takes bfloat16 and float16 beside a cache of 8 bits" % dtype)
+        d = fr_kv8_pages()
+        d.k, d.v, d.k_scale, d.v_scale = _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale)
+        d.n_pages, d.n_kv_heads, d.page_size, d.head_dim = k.shape
+        d.page_stride, d.head_stride, d.slot_stride = k.stride()[:3]
+        d.scale_page_stride, d.scale_head_stride, d.scale_block_stride = k_scale.stride()
+        d.block, d.dtype = k.shape[2] // k_scale.shape[2], _DTYPE_OF[name]
+        self.desc = d
+        self._keep = (k, v, k_scale, v_scale)
+
+
+def fr_kv8_append(cache, k, v, slot, q=None, q_out=None, position=None, rotary=None, style=FR_ROTARY_HALVES, stream=None):
+    return _check((_calls or _torch_calls()).kv8_append(bytes(cache.desc), cache._keep, k, v, slot, q, q_out, position, rotary, style, stream), "fr_kv8_append")
+
+
+def fr_attend_kv8_workspace_bytes(cache, q, n_seqs, max_len, max_q=1, window=0, sinks=0):
+    """q: a tensor of the call's shape (only its shape is read)."""
+    d = fr_attend_kv8_desc(cache.desc, n_tokens=q.shape[0], n_seqs=n_seqs, n_q_heads=q.shape[1], max_q=max_q, max_len=max_len, window=window,
+                           sinks=sinks)
+    out = C.c_uint64()
+    _check(lib().fr_attend_kv8_workspace_bytes(C.byref(d), C.byref(out)), "fr_attend_kv8_workspace_bytes")
+    return out.value
+
+
+def fr_attend_kv8(cache, q, out, pages, lens, scale, max_len, q_begin=None, max_q=1, window=0, sinks=0, lse=None, workspace=None, stream=None):
+    return _check((_calls or _torch_calls()).attend_kv8(bytes(cache.desc), cache._keep, q, out, pages, lens, scale, max_len, q_begin, max_q, window, sinks,
+                                                        lse, workspace, stream), "fr_attend_kv8")
+
+
+def fr_kv_copy_pages(caches, source, target, copied=None, stream=None):
+    """caches: KvPages and Kv8Pages, one or a list of them."""
+    caches = [caches] if isinstance(caches, (KvPages, Kv8Pages)) else list(caches)
+    wide, narrow = [c for c in caches if isinstance(c, KvPages)], [c for c in caches if isinstance(c, Kv8Pages)]
+    if len(wide) + len(narrow) != len(caches):
+        raise TypeError("caches: KvPages and Kv8Pages are needed")
+    return _check((_calls or _torch_calls()).kv_copy_pages(b"".join(bytes(c.desc) for c in wide), b"".join(bytes(c.desc) for c in narrow),
+                                                           [x for c in wide + narrow for x in c._keep], source, target, copied, stream), "fr_kv_copy_pages")
