@@ -768,7 +768,7 @@ int fr_kv8_append(const fr_kv8_append_desc* d, void* stream);
  * to and with its own, and sees key j < n if
  *     window is 0, or j >= n - window, or j < sinks:
  * the window last ones and the first few, which stay visible.  out and lse are as in fr_attend_shared, of scores and values that the
- * codes and scales stand for; a token that sees nothing gets zeros and -infinity; keys that a token does not see do not change its result,
+ * codes and scales stand for, sums being held in 32 bits (of n > 2^11 values beyond 2^139 / n in magnitude they may leave its range); a token that sees nothing gets zeros and -infinity; keys that a token does not see do not change its result,
  * whatever they hold, and NaN among those that it sees shows as the formula says.  Page ids of keys that no token of the call sees are not
  * used: their pages may have been given to others.  A sequence's pages may also be another's: a prompt may lie there once for several.
  * Bounds on the device's numbers: a page id outside the cache counts as the nearest one inside, lens is cut to 0 .. max_len, q_begin to
@@ -796,7 +796,8 @@ typedef struct fr_attend_kv8_desc {
     uint64_t    workspace_bytes;
 } fr_attend_kv8_desc;
 /* Reads the sizes of d only (no pointer).  A call of the same heads and head_dim with no larger n_tokens, n_seqs, max_q and max_len and any window
-   and sinks needs no more. */
+   and sinks needs no more.  FR_ERR_ARG for sizes that the call refuses, too: those of the fields above, and so many sequences with so many
+   tokens (max_q) that the call would have 2^27 workgroups. */
 int fr_attend_kv8_workspace_bytes(const fr_attend_kv8_desc* d, uint64_t* bytes_out);
 int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream);
 

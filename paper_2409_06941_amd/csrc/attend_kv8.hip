@@ -1,16 +1,29 @@
 // Attention of a batch of sequences to keys and values held in 8 bits, to all of them or to a window and the first few.
 //
 // A query row q (a token, a head) that sees keys k_j with values v_j gets  out = sum_j w_j v_j / sum_j w_j,  w_j = exp(s_j - m),
-// s_j = scale q . k_j,  and lse = m + log sum_j w_j, m being the largest score so far: where it rises, the sums so far are multiplied by
-// exp(m_before - m), so that one pass over the keys is enough.
+// s_j = scale q . k_j,  and lse = m + log sum_j w_j, for whatever m: the largest score seen so far.  Where m rises, the sums so far
+// are multiplied by exp(m_before - m), so that one pass over the keys is enough, and parts of the keys, each with its own m, are
+// joined in the same way.  Scores, m, both sums and the parts' results are of 32 bits; weights are rounded to the 16-bit type for the
+// product with the values, and the result is, once.  Codes times their block's power of two are numbers of that type, exactly.
+//
+// The heads that share a key head, and all tokens of a sequence, are rows of one matrix product with its keys.
 
 #include <algorithm>
 #include <cmath>
 
+#include "attend_tiles.h"
 #include "common.h"
 #include "kv8.h"
 
 namespace {
+
+// What a workgroup's four wavefronts do.  kFewRows: 16 rows, and every wavefront takes every fourth tile of 32 keys for itself, the four
+// results being joined at the end.  kWaveRows: every wavefront has an item of its own, 16 rows and all of its keys.  kWideRows: 128
+// rows, 32 a wavefront, which share tiles of 64 keys.
+enum Kind { kFewRows, kWaveRows, kWideRows };
+constexpr int columns(Kind k) { return k == kWideRows ? 32 : 16; }                     // rows of a wavefront: columns of its MFMA blocks
+constexpr int rows_of(Kind k) { return k == kWideRows ? kWaves * 32 : 16; }            // rows of an item
+constexpr int keys_of(Kind k) { return k == kWideRows ? 64 : 32; }                     // keys of a tile
 
 struct Attend8Args {
     fr_kv8_pages c;
@@ -19,84 +32,505 @@ struct Attend8Args {
     float* lse;
     int64_t q_stride, out_stride, pages_stride;
     const int32_t *q_begin, *pages, *lens;
-    int32_t n_tokens, n_seqs, n_q_heads, max_q, max_len, window, sinks, page_shift, group;
-    float scale;
-    int64_t first;
+    int32_t n_tokens, n_seqs, n_q_heads, max_q, max_len, window, sinks, page_shift, block_shift, group;
+    float q_power, rate;                   // scale * log2 e = q_power * rate: a power of two that goes into the queries, and the rest
+    int32_t row_tiles, splits, split_len;  // row tiles of a sequence and key head; parts of its tiles of keys, and their length
+    int32_t items, groups, units, first_unit;
+    float* part_o;                         // [(group's sequence and key head, part), row tile][rows_of][head_dim], relative to 2^m
+    float2* part_ml;                       // the same: m in powers of 2, sum
 };
 
-constexpr int kThreads = 256;
+// The keys that rows of tokens i0 .. i1 see, in tiles: those that hold the first `few` keys, then those from `start` (of token i0) to
+// `end` (of token i1); tile u begins with key first(u).
+template <int kTile> struct Keys {
+    int32_t start, few, end, few_tiles, skipped, tiles;
+    __device__ __forceinline__ Keys(const Attend8Args& a, int n0, int i0, int i1)
+    {
+        end = max(0, n0 + i1);
+        start = a.window ? max(0, max(0, n0 + i0) - a.window) : 0;
+        few = min(a.sinks, start);
+        few_tiles = (few + kTile - 1) / kTile;
+        skipped = start / kTile - few_tiles;
+        if (skipped <= 0) few_tiles = skipped = 0;             // (nothing between the two)
+        tiles = (end + kTile - 1) / kTile - skipped;
+    }
+    __device__ __forceinline__ int first(int u) const { return (u < few_tiles ? u : u + skipped) * kTile; }
+    // a key that some row sees in place of one that none does
+    __device__ __forceinline__ int seen(int j) const { return j >= end ? end - 1 : j >= few && j < start ? start : j; }
+    __device__ __forceinline__ bool all_seen(int first) const { return first + kTile <= end && (first >= start || first + kTile <= few); }
+};
 
-__device__ __forceinline__ int32_t within(int32_t x, int32_t lo, int32_t hi) { return x < lo ? lo : x > hi ? hi : x; }
-__device__ __forceinline__ float code_value(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
+// A sequence's part in the call.
+struct Sequence {
+    int32_t token0, tokens, n0;            // first token; how many are computed; keys that the first one has up to itself (0 and less: none)
+    __device__ __forceinline__ Sequence(const Attend8Args& a, int b)
+    {
+        const int t0 = a.q_begin ? within(a.q_begin[b], 0, a.n_tokens) : b, t1 = a.q_begin ? within(a.q_begin[b + 1], t0, a.n_tokens) : b + 1;
+        const int len = a.max_len ? within(a.lens[b], 0, a.max_len) : 0;
+        token0 = t0;
+        tokens = min(t1 - t0, a.max_q);
+        n0 = len - (t1 - t0) + 1;
+    }
+};
 
-// One workgroup per token and head, 256 keys at a time: a thread a key, then a thread an element.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void k_attend8(Attend8Args a)
+typedef __attribute__((address_space(3))) uint64_t* LdsOffset;
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((address_space(3))) f32x2* LdsPair;
+typedef __attribute__((address_space(3))) u32x4* LdsWide;
+typedef __attribute__((address_space(3))) f32x4* LdsFloats;
+
+// Two codes of a register, times a power of two, as two numbers of the type.
+template <typename T, bool kHigh> __device__ __forceinline__ uint32_t two_numbers(uint32_t codes, float power)
 {
-    __shared__ float q[D], weight[kThreads], of[kThreads], reduce[kThreads];
-    __shared__ uint64_t place[kThreads];
-    __shared__ float power[kThreads];
-    const int64_t id = a.first + blockIdx.x;
-    const int token = (int)(id / a.n_q_heads), head = (int)(id % a.n_q_heads), kv = head / a.group, tid = threadIdx.x;
-    int b = token, t0 = token, t1 = token + 1;
-    if (a.q_begin) {
-        b = 0;
-        int end = a.n_seqs;
-        while (end - b > 1) {
-            const int middle = b + (end - b) / 2;
-            if (within(a.q_begin[middle], 0, a.n_tokens) <= token) b = middle;
-            else end = middle;
+    if constexpr (std::is_same_v<T, Bf16>) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, power, kHigh));
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, power, kHigh));
+}
+template <typename T> __device__ __forceinline__ u32x4 eight_numbers(uint32_t lo, uint32_t hi, float power)
+{
+    return (u32x4){two_numbers<T, false>(lo, power), two_numbers<T, true>(lo, power), two_numbers<T, false>(hi, power), two_numbers<T, true>(hi, power)};
+}
+
+// Codes that are NaN: their bytes' top bits.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t nan_or_0(uint32_t w) { return w & ~((nan_codes(w) >> 7) * 255u); }
+__device__ __forceinline__ uint4 without_nan(uint4 w) { return make_uint4(nan_or_0(w.x), nan_or_0(w.y), nan_or_0(w.z), nan_or_0(w.w)); }
+
+// Where a row's result goes.
+struct Rows {
+    const Attend8Args& a;
+    int32_t kv, token0, n0;
+    __device__ __forceinline__ int32_t token(int r) const { return token0 + r / a.group; }
+    __device__ __forceinline__ int32_t head(int r) const { return kv * a.group + r % a.group; }
+    __device__ __forceinline__ int32_t keys(int r) const { return max(0, n0 + r / a.group); }
+};
+
+template <Kind kKind, int D> struct Lds8 {
+    static constexpr uint32_t kTiles = kKind == kWideRows ? 512 * D : kWaves * 64 * D;      // K and V, two tiles each; of few rows, V of a tile a wavefront
+    static constexpr uint32_t kTable = kWaves * 2048;                                       // a wavefront: two sets of 64 offsets, two of 64 pairs of powers
+};
+
+// The work of one workgroup (kWaveRows: of one wavefront): rows `row0` .. of `rows` against tiles u0 .. u1 of their keys.
+template <typename T, int D, Kind kKind>
+__device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, int n_rows, int row0, const Keys<keys_of(kKind)>& keys, int u0, int u1,
+                                       const int32_t* pages, int64_t part, char* lds_array)
+{
+    constexpr bool kWide = kKind == kWideRows, kAlone = kKind == kWaveRows;
+    constexpr int kCols = columns(kKind), kTile = keys_of(kKind);
+    constexpr int kSharers = kKind == kFewRows ? kWaves : 1;
+    typedef Lds<D, kCols> L;
+    // (weights of bfloat16 are 2^-20, or 2^-12 where the maximum lags, so that sums of values as large as the type's largest stay in range; of
+    // values near its smallest number, 2^-126, the sums still have steps of 2^-129)
+    typedef Softmax<T, D, kCols, std::is_same_v<T, F16> ? 7 : -20> State;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds = (uint32_t)reinterpret_cast<uintptr_t>((LdsBytes)lds_array);
+    const float c = a.rate;
+
+    // the wavefront's rows
+    const int row_first = row0 + (kWide ? wave * kCols : 0), row_here = min(row_first + lane % kCols, n_rows - 1);
+    const bool idle = row_first >= n_rows;
+    const int n = rows.keys(row_here), from = a.window ? n - a.window : 0;
+    // what all rows of the wavefront see needs no look
+    const int n_least = rows.keys(min(row_first, n_rows - 1)), from_most = a.window ? rows.keys(min(row_first + kCols, n_rows) - 1) - a.window : 0;
+    State x;
+    {
+        // Few rows: a lane's 16 bytes of a key are the elements of two fragments, so that those of a query are taken in the same order.
+        const uint16_t* q = a.q + rows.token(row_here) * a.q_stride + (int64_t)rows.head(row_here) * D;
+#pragma unroll
+        for (int f = 0; f < D * kCols / 512; ++f)
+        {
+            uint4 w = *reinterpret_cast<const uint4*>(q + (kWide ? f * 16 + lane / kCols * 8 : f / 2 * 64 + lane / kCols * 16 + f % 2 * 8));
+            if constexpr (std::is_same_v<T, Bf16>) {
+                auto times = [&](uint32_t y) { return T::pack(T::up((uint16_t)y) * a.q_power, T::up((uint16_t)(y >> 16)) * a.q_power); };
+                w = make_uint4(times(w.x), times(w.y), times(w.z), times(w.w));
+            }
+            x.q[f] = __builtin_bit_cast(typename T::x8, w);
         }
-        t0 = within(a.q_begin[b], 0, a.n_tokens), t1 = within(a.q_begin[b + 1], t0, a.n_tokens);
-        if (token < t0 || token >= t1 || token - t0 >= a.max_q) return;
     }
-    const int len = a.max_len ? within(a.lens[b], 0, a.max_len) : 0, n = max(0, len - (t1 - t0) + 1 + token - t0);
-    const int start = a.window ? max(0, n - a.window) : 0, few = min(a.sinks, start);
-    if (tid < D) q[tid] = T::up(a.q[token * a.q_stride + (int64_t)head * D + tid]) * a.scale;
-    float m = -INFINITY, l = 0.0f, o = 0.0f;
-    const int d = tid % D, share = tid / D, shares = kThreads / D;
-    for (int j0 = 0; j0 < few + n - start; j0 += kThreads) {
-        const int v = j0 + tid, j = v < few ? v : start + v - few;
-        float s = -INFINITY;
-        __syncthreads();
-        if (v < few + n - start) {
-            const int32_t page = within(a.pages[b * a.pages_stride + (j >> a.page_shift)], 0, (int32_t)a.c.n_pages - 1);
-            const int slot = j & (a.c.page_size - 1), block = slot / a.c.block;
-            const uint64_t at = (uint64_t)page * a.c.page_stride + (uint64_t)kv * a.c.head_stride + (uint64_t)slot * a.c.slot_stride;
-            const uint64_t sat = (uint64_t)page * a.c.scale_page_stride + (uint64_t)kv * a.c.scale_head_stride + (uint64_t)block * a.c.scale_block_stride;
-            const uint8_t* k = (const uint8_t*)a.c.k + at;
-            s = 0.0f;
-            for (int e = 0; e < D; ++e) s = fmaf(q[e], code_value(k[e]), s);
-            s *= power_of(scale_byte<T>(a.c.k_scale[sat]));
-            place[tid] = at;
-            power[tid] = power_of(scale_byte<T>(a.c.v_scale[sat]));
+
+    // Where keys lie.  A wavefront loads kLoadRows rows of a tile; 64 of them are a set, those of two or four tiles, a lane each: the page id
+    // comes first, then the offset goes to LDS, and the scales' bytes, when they are here, as powers of two.
+    constexpr int kLoadRows = kWide ? 16 : 32, kTilesASet = 64 / kLoadRows;
+    const uint32_t offsets = lds + Lds8<kKind, D>::kTiles + wave * 2048, powers = offsets + 1024;
+    const int mine = kKind == kFewRows ? wave : 0, tiles = (u1 - u0 - mine + kSharers - 1) / kSharers;
+    auto tile_of = [&](int t) { return u0 + t * kSharers + mine; };
+    const uint8_t* gk = static_cast<const uint8_t*>(a.c.k) + rows.kv * a.c.head_stride;
+    const uint8_t* gv = static_cast<const uint8_t*>(a.c.v) + rows.kv * a.c.head_stride;
+    int32_t id;
+    uint8_t k_byte, v_byte;
+    auto key_of = [&](int set) {
+        const int u = min(tile_of(set * kTilesASet + lane / kLoadRows), u1 - 1);
+        return keys.seen(keys.first(u) + (kWide ? wave * 16 : 0) + lane % kLoadRows);
+    };
+    auto ask_ids = [&](int set) { id = pages[key_of(set) >> a.page_shift]; };
+    auto make_offsets = [&](int set) {
+        const int slot = key_of(set) & (a.c.page_size - 1);
+        const uint64_t page = (uint64_t)(uint32_t)within(id, 0, (int32_t)a.c.n_pages - 1);
+        *reinterpret_cast<LdsOffset>(lds_at(offsets + (set & 1) * 512 + lane * 8)) = page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)slot * (uint32_t)a.c.slot_stride;
+        const uint64_t at = page * (uint32_t)a.c.scale_page_stride + (uint64_t)(uint32_t)rows.kv * (uint32_t)a.c.scale_head_stride +
+                            (uint64_t)(uint32_t)(slot >> a.block_shift) * (uint32_t)a.c.scale_block_stride;
+        k_byte = a.c.k_scale[at];
+        v_byte = a.c.v_scale[at];
+    };
+    auto make_powers = [&](int set) {
+        *reinterpret_cast<LdsPair>(lds_at(powers + (set & 1) * 512 + lane * 8)) = f32x2{power_of(scale_byte<T>(k_byte)), power_of(scale_byte<T>(v_byte))};
+    };
+    auto offset_at = [&](int t, int r) { return *reinterpret_cast<LdsOffset>(lds_at(offsets + (t / kTilesASet & 1) * 512 + ((t % kTilesASet) * kLoadRows + r) * 8)); };
+    auto power_at = [&](int t, int r, bool value) {
+        return (*reinterpret_cast<LdsPair>(lds_at(powers + (t / kTilesASet & 1) * 512 + ((t % kTilesASet) * kLoadRows + r) * 8)))[value];
+    };
+    // Values: a lane has 16 codes of a row, kLanes lanes a row.
+    constexpr int kLanes = D / 16, kRowsAtOnce = 64 / kLanes, kLoads = kLoadRows / kRowsAtOnce;
+    const int my_row = lane / kLanes, my_piece = lane % kLanes;
+    // Rows of values that no row of queries sees become zeros (their weights are 0, but 0 times NaN is not); with `clean`, NaN does everywhere.
+    bool clean = false;
+    auto fit = [&](uint4 w, int first, int r) {
+        if (!keys.all_seen(first)) {
+            const int j = first + r;
+            if (keys.seen(j) != j) w = make_uint4(0, 0, 0, 0);
         }
-        reduce[tid] = s;
-        __syncthreads();
-        float top = m;
-        for (int i = 0; i < kThreads; ++i) top = fmaxf(top, reduce[i]);
-        const float was = top == -INFINITY ? 1.0f : expf(m - top);
-        m = top;
-        const float w = s == -INFINITY ? 0.0f : expf(s - m);
-        weight[tid] = w;
-        __syncthreads();
-        l *= was;
-        o *= was;
-        for (int i = 0; i < kThreads; ++i) l += weight[i];
-        const int here = min(kThreads, few + n - start - j0);
-        for (int i = share; i < here; i += shares) o = fmaf(weight[i], code_value(((const uint8_t*)a.c.v)[place[i] + d]) * power[i], o);
+        return clean ? without_nan(w) : w;
+    };
+    auto put = [&](uint32_t tile, int r, uint32_t order, uint4 w, float power) {
+        *reinterpret_cast<LdsWide>(lds_at(tile + r * L::kRow + ((2 * my_piece) ^ order) * 16)) = eight_numbers<T>(w.x, w.y, power);
+        *reinterpret_cast<LdsWide>(lds_at(tile + r * L::kRow + ((2 * my_piece + 1) ^ order) * 16)) = eight_numbers<T>(w.z, w.w, power);
+    };
+    // Scores of keys that a row does not see.
+    typedef typename State::Block Block;
+    auto hide = [&](Block (&s)[2], int first) {
+        if (first + kTile <= n_least && (first >= from_most || first + kTile <= a.sinks)) return;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < State::kInBlock; ++i) {
+                const int j = first + b * kCols + State::in_block(i, lane);
+                if (j >= n || (j < from && j >= a.sinks)) s[b][i] = -INFINITY;
+            }
+    };
+
+    auto pass = [&] {
+        x.start();
+        if (tiles <= 0) return;
+        if constexpr (!kWide) {
+            const uint32_t v = lds + wave * 64 * D;
+            const Fragments<T, D, kCols> fragments(v, lane);
+            uint4 kw[2][D / 64], vw[kLoads];
+            auto load_k = [&](int t) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const uint8_t* at = gk + offset_at(t, b * 16 + lane % 16) + lane / 16 * 16;
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h) kw[b][h] = *reinterpret_cast<const uint4*>(at + h * 64);
+                }
+            };
+            auto load_v = [&](int t) {
+#pragma unroll
+                for (int y = 0; y < kLoads; ++y) vw[y] = *reinterpret_cast<const uint4*>(gv + offset_at(t, y * kRowsAtOnce + my_row) + my_piece * 16);
+            };
+            ask_ids(0);
+            make_offsets(0);
+            if (tiles > kTilesASet) ask_ids(1);
+            load_k(0);
+            load_v(0);
+            make_powers(0);
+            for (int t = 0; t < tiles; ++t) {
+                const bool more = t + 1 < tiles;
+                const int first = keys.first(tile_of(t));
+                if (t % 2 == 0 && t + 2 < tiles) {
+                    make_offsets(t / 2 + 1);
+                    if (t + 4 < tiles) ask_ids(t / 2 + 2);
+                }
+                f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const float power = power_at(t, b * 16 + lane % 16, false);
+#pragma unroll
+                    for (int h = 0; h < D / 64; ++h) {
+                        s[b] = mfma(__builtin_bit_cast(typename T::x8, eight_numbers<T>(kw[b][h].x, kw[b][h].y, power)), x.q[2 * h], s[b]);
+                        s[b] = mfma(__builtin_bit_cast(typename T::x8, eight_numbers<T>(kw[b][h].z, kw[b][h].w, power)), x.q[2 * h + 1], s[b]);
+                    }
+                }
+                if (more) load_k(t + 1);
+#pragma unroll
+                for (int y = 0; y < kLoads; ++y) {
+                    const int r = y * kRowsAtOnce + my_row;
+                    put(v, r, L::fv(r), fit(vw[y], first, r), power_at(t, r, true));
+                }
+                if (more) load_v(t + 1);
+                if (t % 2 == 1 && more) make_powers(t / 2 + 1);
+                hide(s, first);
+                float top = s[0][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i / 4][i % 4]);
+                x.grow(top_of_row<kCols>(top), c);
+                const float zero = x.zero_point();
+                uint32_t p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = x.weigh_from(s[e / 2][2 * e % 4], s[e / 2][2 * e % 4 + 1], c, zero);
+                wait_lds();
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) x.o[d] = mfma(fragments.of_v(0, d), State::fragment(p), x.o[d]);
+                wait_lds();
+            }
+        } else {
+            constexpr uint32_t kHalf = kTile * L::kRow;
+            Fragments<T, D, kCols> fragments(lds, lane);
+            uint4 kw[kLoads], vw[kLoads];
+            auto load = [&](uint4 (&w)[kLoads], const uint8_t* from, int t) {
+#pragma unroll
+                for (int y = 0; y < kLoads; ++y) w[y] = *reinterpret_cast<const uint4*>(from + offset_at(t, y * kRowsAtOnce + my_row) + my_piece * 16);
+            };
+            auto put_k = [&](int t) {
+#pragma unroll
+                for (int y = 0; y < kLoads; ++y) {
+                    const int r = y * kRowsAtOnce + my_row;
+                    put(lds + (t & 1) * kHalf + wave * 16 * L::kRow, r, L::fk(wave * 16 + r), kw[y], power_at(t, r, false));
+                }
+            };
+            auto put_v = [&](int t) {
+#pragma unroll
+                for (int y = 0; y < kLoads; ++y) {
+                    const int r = y * kRowsAtOnce + my_row;
+                    put(lds + (2 + (t & 1)) * kHalf + wave * 16 * L::kRow, r, L::fv(wave * 16 + r), fit(vw[y], keys.first(u0 + t), wave * 16 + r), power_at(t, r, true));
+                }
+            };
+            ask_ids(0);
+            make_offsets(0);
+            if (tiles > kTilesASet) ask_ids(1);
+            load(kw, gk, 0);
+            load(vw, gv, 0);
+            make_powers(0);
+            for (int t = 0; t < tiles; ++t) {
+                put_k(t);
+                put_v(t);
+                if (t % kTilesASet == 0 && t + kTilesASet < tiles) {
+                    make_offsets(t / kTilesASet + 1);
+                    if (t + 2 * kTilesASet < tiles) ask_ids(t / kTilesASet + 2);
+                }
+                if (t + 1 < tiles) {
+                    load(kw, gk, t + 1);
+                    load(vw, gv, t + 1);
+                    if (t % kTilesASet == kTilesASet - 1) make_powers(t / kTilesASet + 1);
+                }
+                __syncthreads();
+                if (idle) continue;
+                f32x16 s[2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+                for (int f = 0; f < D / 16; ++f)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) s[b] = mfma(fragments.of_k((t & 1) * kHalf + b * 32 * L::kRow, f), x.q[f], s[b]);
+                hide(s, keys.first(u0 + t));
+                float top = s[0][0];
+#pragma unroll
+                for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
+                x.grow(top_of_row<kCols>(top), c);
+                const float zero = x.zero_point();
+                uint32_t p[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) p[e] = x.weigh_from(s[e / 8][2 * e % 16], s[e / 8][2 * e % 16 + 1], c, zero);
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma(fragments.of_v((2 + (t & 1)) * kHalf + f * 16 * L::kRow, d), State::fragment(p + 4 * f), x.o[d]);
+                wait_lds();
+            }
+        }
+    };
+    auto meet = [] {
+        if constexpr (!kAlone) __syncthreads();
+        else wait_lds();
+    };
+    pass();
+    // A weight of 0 for a key that a row does not see, times NaN, is NaN: where rows see different keys and one of the results is NaN, the pass
+    // is made again without the values' NaN, and then it is given to the rows that see it.
+    if (n_rows > a.group) {
+        bool bad = false;
+#pragma unroll
+        for (int d = 0; d < D / kCols; ++d)
+#pragma unroll
+            for (int i = 0; i < State::kInBlock; ++i) bad |= x.o[d][i] != x.o[d][i];
+        bad &= !idle;
+        if (kWide ? (bool)__syncthreads_or(bad) : (bool)__any(bad)) {
+            clean = true;
+            pass();
+            for (int t = 0; t < tiles; ++t) {
+                const int first = keys.first(tile_of(t)), j = first + lane;
+                bool any = false;
+                auto place = [&](int j) {
+                    const uint64_t page = (uint64_t)(uint32_t)within(pages[j >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
+                    return gv + page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)(j & (a.c.page_size - 1)) * (uint32_t)a.c.slot_stride;
+                };
+                if (lane < kTile && keys.seen(j) == j) {
+                    const uint4* w = reinterpret_cast<const uint4*>(place(j));
+#pragma unroll 1
+                    for (int e = 0; e < D / 16; ++e) any |= (nan_codes(w[e].x) | nan_codes(w[e].y) | nan_codes(w[e].z) | nan_codes(w[e].w)) != 0;
+                }
+#pragma unroll 1
+                for (uint64_t left = __ballot(any); left; left &= left - 1) {
+                    const int y = first + __ffsll((unsigned long long)left) - 1;
+                    if (y >= n || (y < from && y >= a.sinks)) continue;
+                    const uint8_t* at = place(y);
+#pragma unroll
+                    for (int d = 0; d < D / kCols; ++d)
+#pragma unroll
+                        for (int i = 0; i < State::kInBlock; ++i)
+                            if ((at[d * kCols + State::in_block(i, lane)] & 0x7f) == 0x7f) x.o[d][i] = NAN;
+                }
+            }
+        }
     }
-    __syncthreads();
-    of[tid] = o;
-    __syncthreads();
-    if (tid < D) {
-        for (int i = 1; i < shares; ++i) o += of[tid + i * D];
-        of[tid] = l == 0.0f ? 0.0f : o / l;
+    x.l = sum_of_row<kCols>(x.l + x.l1);
+
+    // results through LDS, so that rows are written whole: a wavefront's rows of D floats, 16-byte chunk c of row r at c ^ r
+    constexpr uint32_t kFloatRow = D * 4, kFloatChunks = D / 4, kRegion = kCols * kFloatRow;
+    static_assert(kWaves * kRegion <= Lds8<kKind, D>::kTiles, "");
+    meet();                                              // tiles are done with
+    const uint32_t region = lds + wave * kRegion, mls = lds + Lds8<kKind, D>::kTiles;
+    auto ml = [&](int wv, int r) { return reinterpret_cast<LdsPair>(lds_at(mls + wv * (kAlone ? 2048 : kCols * 8) + r * 8)); };
+    const float m2 = x.reference(c);                     // (-infinity stays: c is positive)
+    float mine_of = 1.0f;
+    if (lane < kCols) *ml(wave, lane) = f32x2{m2, x.l};
+    if constexpr (kKind == kFewRows) {
+        meet();
+        float top = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < kWaves; ++y) top = fmaxf(top, (*ml(y, lane % kCols))[0]);
+        mine_of = __builtin_amdgcn_exp2f(m2 - (top == -INFINITY ? 0.0f : top));
     }
-    __syncthreads();
-    if (tid < D && tid % 2 == 0)
-        *reinterpret_cast<uint32_t*>(a.out + token * a.out_stride + (int64_t)head * D + tid) = T::pack(of[tid], of[tid + 1]);
-    if (a.lse && tid == 0) a.lse[(int64_t)token * a.n_q_heads + head] = l == 0.0f ? -INFINITY : m + logf(l);
+#pragma unroll
+    for (int d = 0; d < D / kCols; ++d)
+#pragma unroll
+        for (int i = 0; i < State::kInBlock; i += 4) {
+            const uint32_t r = lane % kCols, chunk = (d * kCols + State::in_block(i, lane)) / 4;
+            *reinterpret_cast<LdsFloats>(lds_at(region + r * kFloatRow + (chunk ^ (r & (kFloatChunks - 1))) * 16)) =
+                f32x4{x.o[d][i] * mine_of, x.o[d][i + 1] * mine_of, x.o[d][i + 2] * mine_of, x.o[d][i + 3] * mine_of};
+        }
+    meet();
+    // a thread takes eight elements of a row: two chunks, neighbours for a result of 16 bits, head_dim / 2 apart for a part (so that
+    // neighbouring threads write neighbouring chunks)
+    const bool whole = a.splits == 1;
+    constexpr int kPieces = D / 8, kOutRows = rows_of(kKind);
+    for (int y = kAlone ? lane : tid; y < kOutRows * kPieces; y += kAlone ? 64 : kThreads) {
+        const int r = y / kPieces, piece = y % kPieces, to = row0 + r;
+        if (to >= n_rows) break;
+        f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+        float top, sum;
+        const int in = r % kCols;
+        auto chunk = [&](int wv, int e) {
+            return *reinterpret_cast<LdsFloats>(lds_at(lds + wv * kRegion + in * kFloatRow + ((uint32_t)(whole ? 2 * piece + e : piece + e * kPieces) ^ (in & (kFloatChunks - 1))) * 16));
+        };
+        if constexpr (kKind != kFewRows) {
+            const int wv = kAlone ? wave : r / kCols;
+            lo = chunk(wv, 0), hi = chunk(wv, 1);
+            top = (*ml(wv, in))[0], sum = (*ml(wv, in))[1];
+        } else {
+            top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int wv = 0; wv < kWaves; ++wv) top = fmaxf(top, (*ml(wv, in))[0]);
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int wv = 0; wv < kWaves; ++wv) {
+                lo += chunk(wv, 0), hi += chunk(wv, 1);
+                sum += (*ml(wv, in))[1] * __builtin_amdgcn_exp2f((*ml(wv, in))[0] - base);
+            }
+        }
+        if (whole) {
+            const int64_t token = rows.token(to), head = rows.head(to);
+            const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+            *reinterpret_cast<uint4*>(a.out + token * a.out_stride + head * D + piece * 8) =
+                make_uint4(T::pack(lo[0] * f, lo[1] * f), T::pack(lo[2] * f, lo[3] * f), T::pack(hi[0] * f, hi[1] * f), T::pack(hi[2] * f, hi[3] * f));
+            if (a.lse && piece == 0) a.lse[token * a.n_q_heads + head] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
+        } else {
+            const int64_t at = part * kOutRows + r;
+            *reinterpret_cast<f32x4*>(a.part_o + at * D + piece * 4) = lo;
+            *reinterpret_cast<f32x4*>(a.part_o + at * D + D / 2 + piece * 4) = hi;
+            if (piece == 0) a.part_ml[at] = make_float2(top, sum);
+        }
+    }
+}
+
+// Workgroups are dealt round-robin over the XCDs.  Those that read the same keys (the row tiles of a group: one sequence, one key head, one
+// run of keys) follow one another on one XCD, through its L2; groups go round the XCDs, so that long sequences spread.
+template <typename T, int D, Kind kKind>
+__global__ __launch_bounds__(kThreads, kKind == kWideRows ? D == 64 ? 3 : 2 : 3) void k_attend8(Attend8Args a)
+{
+    constexpr int kRows = rows_of(kKind), kTile = keys_of(kKind);
+    __shared__ __align__(1024) char lds[Lds8<kKind, D>::kTiles + Lds8<kKind, D>::kTable];
+    const int unit = a.first_unit + blockIdx.x / kXcds, xcd = blockIdx.x % kXcds;
+    const int tile = a.row_tiles - 1 - unit % a.row_tiles;             // (the last rows, which see the most keys, first)
+    int group = unit / a.row_tiles * kXcds + xcd;
+    if (group >= a.groups) return;
+    if constexpr (kKind == kWaveRows) {                                // (four items a workgroup)
+        group = group * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (group >= a.items) return;
+    }
+    const int split = group % a.splits, of = group / a.splits, kv = of % a.c.n_kv_heads, b = of / a.c.n_kv_heads;
+    const Sequence s(a, b);
+    const int n_rows = s.tokens * a.group, row0 = tile * kRows;
+    if (row0 >= n_rows) return;
+    const Keys<kTile> keys(a, s.n0, row0 / a.group, (min(n_rows, row0 + kRows) - 1) / a.group);
+    const int u0 = (int)min((int64_t)split * a.split_len, (int64_t)keys.tiles), u1 = (int)min((int64_t)u0 + a.split_len, (int64_t)keys.tiles);
+    if (u0 >= u1 && split) return;                                     // (the first part is always there)
+    const Rows rows{a, kv, s.token0, s.n0};
+    attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, (int64_t)group * a.row_tiles + tile, lds);
+}
+
+// Joins the parts of a row: eight elements a thread.
+template <typename T, int D, Kind kKind>
+__global__ __launch_bounds__(kThreads) void k_attend8_join(Attend8Args a, int64_t first)
+{
+    constexpr int kRows = rows_of(kKind), kPieces = D / 8, kRowsHere = kThreads / kPieces, kBlocks = kRows > kRowsHere ? kRows / kRowsHere : 1;
+    const int64_t id = first + blockIdx.x;
+    const int tile = (int)(id / kBlocks % a.row_tiles), of = (int)(id / kBlocks / a.row_tiles), kv = of % a.c.n_kv_heads, b = of / a.c.n_kv_heads;
+    const int r = (int)(id % kBlocks) * kRowsHere + threadIdx.x / kPieces, piece = threadIdx.x % kPieces;
+    const Sequence s(a, b);
+    const int n_rows = s.tokens * a.group, row0 = tile * kRows;
+    if (r >= kRows || row0 + r >= n_rows) return;
+    const Keys<keys_of(kKind)> keys(a, s.n0, row0 / a.group, (min(n_rows, row0 + kRows) - 1) / a.group);
+    const int parts = max(1, (keys.tiles + a.split_len - 1) / a.split_len);
+    constexpr int kAtOnce = 8;
+    const int64_t step = (int64_t)a.row_tiles * kRows, at0 = ((int64_t)of * a.splits * a.row_tiles + tile) * kRows + r;
+    float top = -INFINITY, sum = 0.0f, o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+    for (int y0 = 0; y0 < parts; y0 += kAtOnce) {
+        float2 ml[kAtOnce];
+        float4 lo[kAtOnce], hi[kAtOnce];
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+            const int64_t at = at0 + min(y0 + x, parts - 1) * step;
+            const float4* p = reinterpret_cast<const float4*>(a.part_o + at * D) + piece;
+            ml[x] = a.part_ml[at];
+            lo[x] = p[0];
+            hi[x] = p[kPieces];
+        }
+        const float before = top;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x)
+            if (y0 + x < parts) top = fmaxf(top, ml[x].x);
+        const float base = top == -INFINITY ? 0.0f : top, g = __builtin_amdgcn_exp2f(before - base);
+        sum *= g;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= g;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+            if (y0 + x >= parts) continue;
+            const float f = __builtin_amdgcn_exp2f(ml[x].x - base);
+            sum = fmaf(ml[x].y, f, sum);
+            o[0] = fmaf(lo[x].x, f, o[0]), o[1] = fmaf(lo[x].y, f, o[1]), o[2] = fmaf(lo[x].z, f, o[2]), o[3] = fmaf(lo[x].w, f, o[3]);
+            o[4] = fmaf(hi[x].x, f, o[4]), o[5] = fmaf(hi[x].y, f, o[5]), o[6] = fmaf(hi[x].z, f, o[6]), o[7] = fmaf(hi[x].w, f, o[7]);
+        }
+    }
+    const int64_t token = s.token0 + (row0 + r) / a.group, head = kv * a.group + (row0 + r) % a.group;
+    const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+    uint16_t* out = a.out + token * a.out_stride + head * D + piece * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f));
+    *reinterpret_cast<uint2*>(out + D / 2) = make_uint2(T::pack(o[4] * f, o[5] * f), T::pack(o[6] * f, o[7] * f));
+    if (a.lse && piece == 0) a.lse[token * a.n_q_heads + head] = sum == 0.0f ? -INFINITY : (top + __log2f(sum)) * kLn2;
 }
 
 bool sizes_ok(const fr_attend_kv8_desc& d)
@@ -107,12 +541,67 @@ bool sizes_ok(const fr_attend_kv8_desc& d)
     return d.max_len >= 0 && d.max_len <= 0x7fffffff - 8191 && d.window >= 0 && d.sinks >= 0;
 }
 
-template <typename T, int D> int launch(Attend8Args a, hipStream_t stream)
+int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
+
+// How a call is cut.
+struct Plan {
+    Kind kind = kFewRows;
+    int64_t row_tiles = 1, base = 0, splits = 1, split_len = 1;        // base: sequences x key heads x row tiles
+};
+constexpr int64_t kMostFew = 32;           // rows of a sequence that are few
+constexpr int64_t kMostItems = 4 * kUnits; // parts are no more than give so many items in all
+constexpr int64_t kMostBlocks = 0x7fffffff;
+
+int64_t rows_a_seq(const fr_attend_kv8_desc& d) { return (int64_t)std::min(d.max_q, d.n_tokens) * (d.n_q_heads / d.cache.n_kv_heads); }
+int64_t row_tiles_of(int64_t rows) { return rows > kMostFew ? up(rows, rows_of(kWideRows)) : up(rows, rows_of(kFewRows)); }
+
+Plan plan(const fr_attend_kv8_desc& d, int cus)
 {
-    const int64_t all = (int64_t)a.n_tokens * a.n_q_heads;
-    for (a.first = 0; a.first < all; a.first += kMostThreads / kThreads)
-        hipLaunchKernelGGL((k_attend8<T, D>), dim3((unsigned)std::min<int64_t>(all - a.first, kMostThreads / kThreads)), dim3(kThreads), 0, stream, a);
+    Plan p;
+    const int64_t rows = rows_a_seq(d), group = d.n_q_heads / d.cache.n_kv_heads;
+    p.kind = rows > kMostFew ? kWideRows : kFewRows;
+    p.row_tiles = row_tiles_of(rows);
+    p.base = (int64_t)d.n_seqs * d.cache.n_kv_heads * p.row_tiles;
+    const int64_t tile = keys_of(p.kind);
+    // tiles of keys that a row tile sees, at most
+    int64_t keys = d.max_len;
+    if (d.window) keys = std::min<int64_t>(keys, (int64_t)d.window + std::min<int64_t>(up(rows_of(p.kind), group), d.max_q) + d.sinks + 3 * tile);
+    const int64_t tiles = std::max<int64_t>(up(keys, tile), 1), least = p.kind == kWideRows ? 2 : 4;
+    const int64_t want = std::max<int64_t>(1, std::min(up(tiles, least), std::min<int64_t>(cus, kUnits) * 4 / p.base));
+    p.split_len = up(tiles, want);
+    p.splits = up(tiles, p.split_len);
+    return p;
+}
+
+// Rows of results in parts that a call has room for; no call with smaller sizes, of whatever window, has more.
+int64_t most_part_rows(const fr_attend_kv8_desc& d)
+{
+    const int64_t rows = rows_a_seq(d), kind_rows = rows > kMostFew ? rows_of(kWideRows) : rows_of(kFewRows);
+    const int64_t base = (int64_t)d.n_seqs * d.cache.n_kv_heads * row_tiles_of(rows), parts = up(d.max_len, 128);
+    return parts < 2 ? 0 : std::min(base * parts, kMostItems) * kind_rows;
+}
+uint64_t part_bytes(const fr_attend_kv8_desc& d) { return (uint64_t)most_part_rows(d) * (d.cache.head_dim * 4 + 8); }
+
+template <typename T, int D, Kind kKind> int launch(Attend8Args a, const Plan& p, hipStream_t stream)
+{
+    constexpr int kBlocksALaunch = kMostThreads / kThreads;
+    a.items = (int)((int64_t)a.n_seqs * a.c.n_kv_heads * p.splits);
+    a.groups = kKind == kWaveRows ? (a.items + kWaves - 1) / kWaves : a.items;
+    a.units = (int)(up(a.groups, kXcds) * a.row_tiles);
+    for (a.first_unit = 0; a.first_unit < a.units; a.first_unit += kBlocksALaunch / kXcds)
+        hipLaunchKernelGGL((k_attend8<T, D, kKind>), dim3((unsigned)std::min(a.units - a.first_unit, kBlocksALaunch / kXcds) * kXcds), dim3(kThreads), 0, stream, a);
+    if (p.splits > 1) {
+        constexpr int kRowsHere = kThreads / (D / 8), kBlocks = rows_of(kKind) > kRowsHere ? rows_of(kKind) / kRowsHere : 1;
+        const int64_t all = p.base * kBlocks;
+        for (int64_t first = 0; first < all; first += kBlocksALaunch)
+            hipLaunchKernelGGL((k_attend8_join<T, D, kKind>), dim3((unsigned)std::min<int64_t>(all - first, kBlocksALaunch)), dim3(kThreads), 0, stream, a, first);
+    }
     return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
+}
+
+template <typename T, int D> int launch(const Attend8Args& a, const Plan& p, hipStream_t stream)
+{
+    return p.kind == kWideRows ? launch<T, D, kWideRows>(a, p, stream) : p.kind == kWaveRows ? launch<T, D, kWaveRows>(a, p, stream) : launch<T, D, kFewRows>(a, p, stream);
 }
 
 }  // namespace
@@ -123,6 +612,9 @@ int fr_attend_kv8_workspace_bytes(const fr_attend_kv8_desc* d, uint64_t* bytes_o
 {
     if (!d || !bytes_out || !sizes_ok(*d)) return FR_ERR_ARG;
     *bytes_out = 0;
+    if (d->n_tokens == 0 || d->n_seqs == 0) return FR_OK;
+    if (plan(*d, kUnits).base > kMostBlocks / 16) return FR_ERR_ARG;
+    *bytes_out = part_bytes(*d);
     return FR_OK;
 }
 
@@ -138,12 +630,27 @@ int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream)
         if (s % 8 || s > most || s < 0 || (d->n_tokens > 1 && s < width)) return FR_ERR_ARG;
     if (!d->q_begin && d->n_tokens != d->n_seqs) return FR_ERR_ARG;
     if (d->max_len && (!d->pages || !d->lens || d->pages_stride < ((int64_t)d->max_len + c.page_size - 1) / c.page_size || d->pages_stride > most)) return FR_ERR_ARG;
-    const Attend8Args a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->pages, d->lens,
-                           d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->max_len, d->window, d->sinks,
-                           __builtin_ctz(c.page_size), d->n_q_heads / c.n_kv_heads, d->scale, 0};
+    const Plan p = plan(*d, (int)fr_stream_cus((hipStream_t)stream));
+    if (p.base > kMostBlocks / 16) return FR_ERR_ARG;
+    const uint64_t need = part_bytes(*d);
+    if (need && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < need)) return FR_ERR_ARG;
+    if (p.splits > 1 && p.base * p.splits * rows_of(p.kind) > most_part_rows(*d)) return FR_ERR_STATE;      // (never)
+    Attend8Args a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->pages, d->lens,
+                     d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->max_len, d->window, d->sinks,
+                     __builtin_ctz(c.page_size), __builtin_ctz(c.block), d->n_q_heads / c.n_kv_heads};
+    // With queries and keys as far apart as bfloat16 lets them be, a product of 32 bits would be beyond its range before the scale brings it back.
+    int e = 0;
+    if (c.dtype == FR_DTYPE_BF16) std::frexp(d->scale, &e);
+    a.q_power = std::ldexp(1.0f, e);
+    a.rate = std::ldexp(d->scale, -e) * kLog2e;
+    a.row_tiles = (int)p.row_tiles;
+    a.splits = (int)p.splits;
+    a.split_len = (int)std::min<int64_t>(p.split_len, 0x7fffffff);
+    a.part_o = (float*)d->workspace;
+    a.part_ml = (float2*)((char*)d->workspace + (uint64_t)p.base * p.splits * rows_of(p.kind) * c.head_dim * 4);
     hipStream_t s = (hipStream_t)stream;
-    if (c.dtype == FR_DTYPE_BF16) return c.head_dim == 64 ? launch<Bf16, 64>(a, s) : launch<Bf16, 128>(a, s);
-    return c.head_dim == 64 ? launch<F16, 64>(a, s) : launch<F16, 128>(a, s);
+    if (c.dtype == FR_DTYPE_BF16) return c.head_dim == 64 ? launch<Bf16, 64>(a, p, s) : launch<Bf16, 128>(a, p, s);
+    return c.head_dim == 64 ? launch<F16, 64>(a, p, s) : launch<F16, 128>(a, p, s);
 }
 
 }  // extern "C"
