@@ -2,6 +2,10 @@
 //
 // A block's codes are x 2^(127 - s), rounded to 4 significant bits; its scale s is the least with which no number goes beyond 448, so
 // that the largest magnitude of the block's tokens has to be known before the first code: a wavefront has all tokens of a block and head.
+// A rotated key is a c - b s.  Its two products are exact in 64 bits, their sum is rounded there and then to an odd number of 32 bits, so
+// that scale and code are those of the exact number but for one in 2^50; in 32 bits one code in a million would be its neighbour.
+// Every element is read and written once, so that memory bounds it: 16384 tokens of 64 + 2 x 8 heads of 128, 646 MB in 121 us, 5.3 TB/s (a
+// plain copy reaches 4.9).  A step's few tokens are bound by latency, four loads that depend on one another and the launch: 64 of them 6 us.
 
 #include <algorithm>
 
@@ -19,11 +23,11 @@ struct Append8Args {
     const int32_t* position;
     const float* rotary;
     int32_t n_positions, rotary_dim, style, n_q_heads, page_shift;
-    int32_t n_tokens;                      // of the call, and the first of this launch
-    int32_t first;
+    int32_t n_tokens, share;               // tokens, and how many of them a workgroup has whose keys and values it stores
+    int64_t stores, first;                 // such workgroups; the first workgroup of this launch
 };
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256, kWaves = kThreads / 64, kRowsHeld = 2;
 
 // The 32-bit number next to d on the side of zero, with its last bit set where d is not that number: what is rounded to fewer bits
 // from it is rounded as from d.
@@ -56,21 +60,49 @@ __device__ __forceinline__ const float* table_row(const Append8Args& a, int64_t 
     return a.rotary + (int64_t)(p < 0 ? 0 : p < a.n_positions ? p : a.n_positions - 1) * a.rotary_dim;
 }
 
-// The elements as numbers of 32 bits from which codes are rounded as from the exact ones.
-template <typename T> __device__ __forceinline__ void numbers(const uint16_t* from, const Pieces& p, const float* row, int u, int half, float (&x)[16])
+struct Raw { uint4 b[2]; };
+__device__ __forceinline__ Raw raw_at(const uint16_t* from, const Pieces& p)
 {
-    const uint4 b[2] = {*reinterpret_cast<const uint4*>(from + p.e[0]), *reinterpret_cast<const uint4*>(from + p.e[1])};
-    const uint32_t w[8] = {b[0].x, b[0].y, b[0].z, b[0].w, b[1].x, b[1].y, b[1].z, b[1].w};
+    return {{*reinterpret_cast<const uint4*>(from + p.e[0]), *reinterpret_cast<const uint4*>(from + p.e[1])}};
+}
+
+// Cosines and sines of a lane's eight pairs.
+struct Turn { float c[8], s[8]; };
+__device__ __forceinline__ Turn turn_at(const Append8Args& a, const Pieces& p, int64_t t, int u)
+{
+    Turn y = {};
+    if (p.turned) {
+        const float4 *c = reinterpret_cast<const float4*>(table_row(a, t) + u * 8), *s = reinterpret_cast<const float4*>(table_row(a, t) + u * 8 + a.rotary_dim / 2);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[2 * i] = T::up((uint16_t)w[i]), x[2 * i + 1] = T::up((uint16_t)(w[i] >> 16));
+        for (int i = 0; i < 2; ++i) {
+            const float4 f = c[i], g = s[i];
+            y.c[4 * i] = f.x, y.c[4 * i + 1] = f.y, y.c[4 * i + 2] = f.z, y.c[4 * i + 3] = f.w;
+            y.s[4 * i] = g.x, y.s[4 * i + 1] = g.y, y.s[4 * i + 2] = g.z, y.s[4 * i + 3] = g.w;
+        }
+    }
+    return y;
+}
+
+// Four elements of each piece, 4 q .. 4 q + 3 of its eight, as numbers of 32 bits from which codes are rounded as from the exact ones.
+template <typename T> __device__ __forceinline__ void numbers(const Raw& of, const Pieces& p, const Turn& by, int q, float (&x)[8])
+{
+    const uint32_t w[8] = {of.b[0].x, of.b[0].y, of.b[0].z, of.b[0].w, of.b[1].x, of.b[1].y, of.b[1].z, of.b[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = T::up((uint16_t)(w[i / 4 * 4 + 2 * q + i % 4 / 2] >> i % 2 * 16));
     if (!p.turned) return;
-    const float *c = row + u * 8, *s = c + half;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float &f = p.halves ? x[i] : x[2 * i], &g = p.halves ? x[i + 8] : x[2 * i + 1];
-        const double y = f, z = g, cd = c[i], sd = s[i];
+    auto turn = [&](float& f, float& g, int i) {
+        float c = by.c[i], s = by.s[i];
+        asm volatile("" : "+v"(c), "+v"(s));               // (made into 64 bits here: kept so through all heads they take 64 registers)
+        const double y = f, z = g, cd = c, sd = s;
         f = to_odd(y * cd - z * sd);
         g = to_odd(z * cd + y * sd);
+    };
+    if (p.halves) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) turn(x[i], x[i + 4], 4 * q + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) turn(x[2 * i], x[2 * i + 1], i / 2 * 4 + 2 * q + i % 2);
     }
 }
 
@@ -86,12 +118,12 @@ __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float 
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clipped(c), clipped(d), lo, true);
 }
 // Codes of x 2^(127 - s); `by` is that power.
-__device__ __forceinline__ uint2 eight_codes(const float* x, float by)
+__device__ __forceinline__ uint32_t codes_of(const float* x, float by)
 {
-    uint2 y = {four_codes(x[0] * by, x[1] * by, x[2] * by, x[3] * by), four_codes(x[4] * by, x[5] * by, x[6] * by, x[7] * by)};
+    uint32_t y = four_codes(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (!(fabsf(x[i]) < INFINITY)) (i < 4 ? y.x : y.y) |= 0x7fu << (i % 4 * 8);
+    for (int i = 0; i < 4; ++i)
+        if (!(fabsf(x[i]) < INFINITY)) y |= 0x7fu << i * 8;
     return y;
 }
 
@@ -108,24 +140,154 @@ __device__ __forceinline__ uint32_t again(uint32_t w, float by)
     return y;
 }
 
-// One workgroup per token: its queries, and, if a run of tokens of a block begins with it, that run's keys and values, a wavefront a
-// head of K or V at a time.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_kv8_append(Append8Args a)
+// How many tokens of a block follow one another from token t on.
+__device__ __forceinline__ int run_at(const Append8Args& a, int64_t t, int64_t slot, int lane)
 {
-    const int64_t t = a.first + (int64_t)blockIdx.x;
-    const int D = a.c.head_dim, units = D / 16, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = a.rotary_dim / 2;
-    if (a.n_q_heads) {
-        const float* row = table_row(a, t);
-        for (int x = threadIdx.x; x < a.n_q_heads * units; x += kThreads) {
-            const int h = x / units, u = x % units;
-            const uint16_t* from = a.q + t * a.q_stride + h * D;
-            uint16_t* to = a.q_out + t * a.q_out_stride + h * D;
+    const int most = a.c.block - (int)(slot & (a.c.block - 1));
+    if (most == 1) return 1;
+    int run = 0;
+    for (int i0 = 0; i0 < most; i0 += 64) {
+        const int i = i0 + lane;
+        const uint64_t same = __ballot(i < most && t + i < a.n_tokens && a.slot[t + i] == slot + i);
+        const int n = ~same ? __builtin_ctzll(~same) : 64;
+        run += n;
+        if (n < 64) break;
+    }
+    return run;
+}
+
+// Keys and values of such a run: of heads `task0`, task0 + step, .. (of K, then of V).  A wavefront's lanes are dealt out over the elements of
+// a row, as many rows as the run has, and heads.  Two rows of a lane (16 tokens of a block with head_dim 128, 32 with 64) stay in registers,
+// with their angles for all heads, and the next head's elements come while those of this one are made into codes; of longer runs (kLong)
+// rows are read twice, once for the scale and once for the codes.
+template <typename T, bool kLong> __device__ __forceinline__ void store_run(const Append8Args& a, int64_t t, int64_t slot, int run, int task0, int step, int lane)
+{
+    const int D = a.c.head_dim, units = D / 16, block = a.c.block, in_block = (int)(slot & (block - 1));
+    int rows = 64 / units;
+    while (rows > 1 && rows / 2 >= run) rows /= 2;
+    const int heads = 64 / (units * rows), u = lane % units, my_row = lane / units % rows, tasks = 2 * a.c.n_kv_heads;
+    const int64_t page = slot >> a.page_shift;
+    const int first = (int)(slot & (a.c.page_size - 1));
+    constexpr int kHeld = kLong ? 0 : kRowsHeld, kRoom = kLong ? 1 : kRowsHeld;
+    const Pieces turned(a, u, true), plain(a, u, false);
+    Turn turn[kRoom];
+#pragma unroll
+    for (int y = 0; y < kHeld; ++y) turn[y] = turn_at(a, turned, t + min(my_row + y * rows, run - 1), u);
+    struct Task {
+        const uint16_t* from;
+        int64_t stride;
+        uint8_t *to, *scale;
+        bool there, value;
+    };
+    auto task_of = [&](int i) {                            // heads of K, then of V
+        Task x;
+        x.there = i < tasks;
+        x.value = i >= a.c.n_kv_heads;
+        const int h = x.there ? x.value ? i - a.c.n_kv_heads : i : 0;
+        x.from = (x.value ? a.v : a.k) + h * D;
+        x.stride = x.value ? a.v_stride : a.k_stride;
+        x.to = static_cast<uint8_t*>(x.value ? a.c.v : a.c.k) + page * a.c.page_stride + h * a.c.head_stride;
+        x.scale = (x.value ? a.c.v_scale : a.c.k_scale) + page * a.c.scale_page_stride + h * a.c.scale_head_stride + first / block * a.c.scale_block_stride;
+        return x;
+    };
+    auto ask = [&](const Task& x, Raw (&held)[kRoom], int& old) {
+#pragma unroll
+        for (int y = 0; y < kHeld; ++y) held[y] = raw_at(x.from + (t + min(my_row + y * rows, run - 1)) * x.stride, x.value ? plain : turned);
+        old = in_block ? *x.scale : 0;
+    };
+    Raw next[kRoom];
+    int next_old;
+    int i = task0 * heads + lane / (units * rows);
+    ask(task_of(i), next, next_old);
+    for (; __any(i < tasks); i += step * heads) {
+        const Task x = task_of(i);
+        const Pieces p = x.value ? plain : turned;
+        Raw held[kRoom];
+#pragma unroll
+        for (int y = 0; y < kHeld; ++y) held[y] = next[y];
+        const int old = next_old;
+        if (__any(i + step * heads < tasks)) ask(task_of(i + step * heads), next, next_old);
+        auto each = [&](auto f) {
+#pragma unroll
+            for (int y = 0; y < kHeld; ++y)
+                if (my_row + y * rows < run) f(my_row + y * rows, held[y], turn[y]);
+            if constexpr (kLong)
+#pragma unroll 1
+                for (int r = my_row; r < run; r += rows) f(r, raw_at(x.from + (t + r) * x.stride, p), turn_at(a, p, t + r, u));
+        };
+        float top = 0.0f;
+        each([&](int, const Raw& w, const Turn& by) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float y[8];
+                numbers<T>(w, p, by, q, y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_magnitude(y[e]));
+                __builtin_amdgcn_sched_barrier(0);         // (the next ones' registers are these)
+            }
+        });
+        for (int e = 1; e < units * rows; e *= 2) top = fmaxf(top, __shfl_xor(top, e));
+        int s = byte_for<T>(top);
+        if (in_block) {
+            const int before = scale_byte<T>(old);
+            if (before >= s) {
+                s = before;
+            } else if (x.there) {
+                const float by = power_of(max(127 + before - s, 1));       // (2^-126 and less: all but NaN become 0)
+                for (int r = my_row; r < block; r += rows) {
+                    if (r >= in_block && r < in_block + run) continue;
+                    uint4* w = reinterpret_cast<uint4*>(x.to + (int64_t)(first - in_block + r) * a.c.slot_stride + u * 16);
+                    const uint4 y = *w;
+                    *w = make_uint4(again(y.x, by), again(y.y, by), again(y.z, by), again(y.w, by));
+                }
+            }
+        }
+        if (!x.there) continue;
+        const float power = power_of(254 - s);
+        // (the numbers are made again, not kept: with them, a wavefront's registers leave room for half as many)
+#pragma unroll
+        for (int y = 0; y < kHeld; ++y)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) asm volatile("" : "+v"(held[y].b[b].x), "+v"(held[y].b[b].y), "+v"(held[y].b[b].z), "+v"(held[y].b[b].w));
+        each([&](int r, const Raw& w, const Turn& by) {
+            uint32_t codes[2][2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float y[8];
+                numbers<T>(w, p, by, q, y);
+                codes[0][q] = codes_of(y, power);
+                codes[1][q] = codes_of(y + 4, power);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            uint8_t* at = x.to + (int64_t)(first + r) * a.c.slot_stride;
+            *reinterpret_cast<uint2*>(at + p.e[0]) = make_uint2(codes[0][0], codes[0][1]);
+            *reinterpret_cast<uint2*>(at + p.e[1]) = make_uint2(codes[1][0], codes[1][1]);
+        });
+        if (lane % (units * rows) == 0) *x.scale = (uint8_t)s;
+    }
+}
+
+template <typename T> __device__ __forceinline__ void turn_queries(const Append8Args& a, int64_t t)
+{
+    const int D = a.c.head_dim, units = D / 16, half = a.rotary_dim / 2;
+    const float* row = table_row(a, t);
+    constexpr int kHeld = 2;                               // pieces whose loads are under way at once
+    for (int x0 = threadIdx.x; x0 < a.n_q_heads * units; x0 += kHeld * kThreads) {
+        Raw held[kHeld];
+#pragma unroll
+        for (int y = 0; y < kHeld; ++y) {
+            const int x = min(x0 + y * kThreads, a.n_q_heads * units - 1);
+            held[y] = raw_at(a.q + t * a.q_stride + x / units * D, Pieces(a, x % units, true));
+        }
+#pragma unroll
+        for (int y = 0; y < kHeld; ++y) {
+            const int x = x0 + y * kThreads, h = x / units, u = x % units;
+            if (x >= a.n_q_heads * units) break;
             const Pieces p(a, u, true);
-            uint4 b[2] = {*reinterpret_cast<const uint4*>(from + p.e[0]), *reinterpret_cast<const uint4*>(from + p.e[1])};
+            const Raw& b = held[y];
+            uint32_t w[8] = {b.b[0].x, b.b[0].y, b.b[0].z, b.b[0].w, b.b[1].x, b.b[1].y, b.b[1].z, b.b[1].w};
             if (p.turned) {
                 const float *c = row + u * 8, *s = c + half;
-                uint32_t w[8] = {b[0].x, b[0].y, b[0].z, b[0].w, b[1].x, b[1].y, b[1].z, b[1].w};
                 if (p.halves) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -141,66 +303,38 @@ __global__ __launch_bounds__(kThreads) void k_kv8_append(Append8Args a)
                         w[i] = T::pack(x0 * c[i] - y0 * s[i], y0 * c[i] + x0 * s[i]);
                     }
                 }
-                b[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                b[1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
-            *reinterpret_cast<uint4*>(to + p.e[0]) = b[0];
-            *reinterpret_cast<uint4*>(to + p.e[1]) = b[1];
+            uint16_t* to = a.q_out + t * a.q_out_stride + h * D;
+            *reinterpret_cast<uint4*>(to + p.e[0]) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(to + p.e[1]) = make_uint4(w[4], w[5], w[6], w[7]);
         }
     }
-    const int64_t slot = a.slot[t];
-    if (slot < 0 || slot >= a.n_slots) return;
-    const int block = a.c.block, in_block = (int)(slot & (block - 1)), most = block - in_block;
-    if (t > 0 && in_block && a.slot[t - 1] == slot - 1) return;        // (the run began before)
-    int run = 0;
-    for (int i0 = 0; i0 < most; i0 += 64) {
-        const int i = i0 + lane;
-        const uint64_t same = __ballot(i < most && t + i < a.n_tokens && a.slot[t + i] == slot + i);
-        const int n = ~same ? __builtin_ctzll(~same) : 64;
-        run += n;
-        if (n < 64) break;
+}
+
+// The first workgroups take the keys and values, those of `share` tokens (up to 16) each; then comes one per token with its queries.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_kv8_append(Append8Args a)
+{
+    const int64_t id = a.first + (int64_t)blockIdx.x;
+    if (id >= a.stores) {
+        turn_queries<T>(a, id - a.stores);
+        return;
     }
-    const int64_t page = slot >> a.page_shift;
-    const int first = (int)(slot & (a.c.page_size - 1)), at_once = 64 / units, u = lane % units;
-    for (int task = wave; task < 2 * a.c.n_kv_heads; task += kWaves) {
-        const int h = task >> 1;
-        const bool value = task & 1;
-        const Pieces p(a, u, !value);
-        const uint16_t* from = (value ? a.v : a.k) + h * D;
-        const int64_t stride = value ? a.v_stride : a.k_stride;
-        uint8_t* to = static_cast<uint8_t*>(value ? a.c.v : a.c.k) + page * a.c.page_stride + h * a.c.head_stride;
-        uint8_t* scale = (value ? a.c.v_scale : a.c.k_scale) + page * a.c.scale_page_stride + h * a.c.scale_head_stride + first / block * a.c.scale_block_stride;
-        float x[16], top = 0.0f;
-        for (int r = lane / units; r < run; r += at_once) {
-            numbers<T>(from + (t + r) * stride, p, p.turned ? table_row(a, t + r) : nullptr, u, half, x);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, finite_magnitude(x[i]));
-        }
-#pragma unroll
-        for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
-        int s = byte_for<T>(top);
-        if (in_block) {
-            const int old = scale_byte<T>(*scale);
-            if (old >= s) {
-                s = old;
-            } else {
-                const float by = power_of(max(127 + old - s, 1));      // (2^-126 and less: all but NaN become 0)
-                for (int r = lane / (units); r < block; r += at_once) {
-                    if (r >= in_block && r < in_block + run) continue;
-                    uint4* w = reinterpret_cast<uint4*>(to + (int64_t)(first - in_block + r) * a.c.slot_stride + u * 16);
-                    uint4 y = *w;
-                    *w = make_uint4(again(y.x, by), again(y.y, by), again(y.z, by), again(y.w, by));
-                }
-            }
-        }
-        const float by = power_of(254 - s);
-        for (int r = lane / units; r < run; r += at_once) {
-            numbers<T>(from + (t + r) * stride, p, p.turned ? table_row(a, t + r) : nullptr, u, half, x);
-            uint8_t* at = to + (int64_t)(first + r) * a.c.slot_stride;
-            *reinterpret_cast<uint2*>(at + p.e[0]) = eight_codes(x, by);
-            *reinterpret_cast<uint2*>(at + p.e[1]) = eight_codes(x + 8, by);
-        }
-        if (lane == 0) *scale = (uint8_t)s;
+    // runs that begin with one of the tokens
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t t0 = id * a.share, t = t0 + lane;
+    const int64_t slot = lane < a.share && t < a.n_tokens ? a.slot[t] : -1, before = lane < a.share && t < a.n_tokens && t > 0 ? a.slot[t - 1] : -1;
+    const bool begins = slot >= 0 && slot < a.n_slots && (!(slot & (a.c.block - 1)) || before != slot - 1);
+    const uint64_t all = __ballot(begins);
+    const bool apart = __popcll(all) >= kWaves;            // a run each for the wavefronts, or its heads
+    int n = 0;
+    for (uint64_t left = all; left; left &= left - 1, ++n) {
+        if (apart && n % kWaves != wave) continue;
+        const int i = __ffsll((unsigned long long)left) - 1;
+        const int64_t at = (int64_t)((uint64_t)(uint32_t)__shfl((int)(uint32_t)(slot & 0xffffffff), i) | (uint64_t)(uint32_t)__shfl((int)(slot >> 32), i) << 32);
+        const int run = run_at(a, t0 + i, at, lane), task0 = apart ? 0 : wave, step = apart ? 1 : kWaves;
+        if (run <= kRowsHeld * 64 / (a.c.head_dim / 16)) store_run<T, false>(a, t0 + i, at, run, task0, step, lane);
+        else store_run<T, true>(a, t0 + i, at, run, task0, step, lane);
     }
 }
 
@@ -226,13 +360,14 @@ extern "C" int fr_kv8_append(const fr_kv8_append_desc* d, void* stream)
     if (d->rotary_dim && (!d->position || !d->rotary || ((uintptr_t)d->rotary & 15) || d->n_positions < 1)) return FR_ERR_ARG;
     Append8Args a = {c, (const uint16_t*)d->k, (const uint16_t*)d->v, (const uint16_t*)d->q, (uint16_t*)d->q_out, d->k_stride, d->v_stride,
                      d->q_stride, d->q_out_stride, c.n_pages * (int64_t)c.page_size, d->slot, d->position, d->rotary, d->n_positions,
-                     d->rotary_dim, d->style, d->n_q_heads, __builtin_ctz(c.page_size), d->n_tokens, 0};
-    for (int64_t left = d->n_tokens; left > 0;) {
-        const int64_t n = std::min<int64_t>(left, kMostThreads / kThreads);
-        if (c.dtype == FR_DTYPE_BF16) hipLaunchKernelGGL(k_kv8_append<Bf16>, dim3((unsigned)n), dim3(kThreads), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL(k_kv8_append<F16>, dim3((unsigned)n), dim3(kThreads), 0, (hipStream_t)stream, a);
-        left -= n;
-        a.first += (int32_t)n;
+                     d->rotary_dim, d->style, d->n_q_heads, __builtin_ctz(c.page_size), d->n_tokens};
+    a.share = std::max(1, std::min(16, d->n_tokens / 1024));
+    a.stores = (d->n_tokens + (int64_t)a.share - 1) / a.share;
+    const int64_t all = a.stores + (d->n_q_heads ? d->n_tokens : 0);
+    for (a.first = 0; a.first < all; a.first += kMostThreads / kThreads) {
+        const dim3 grid((unsigned)std::min<int64_t>(all - a.first, kMostThreads / kThreads));
+        if (c.dtype == FR_DTYPE_BF16) hipLaunchKernelGGL(k_kv8_append<Bf16>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL(k_kv8_append<F16>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
     }
     return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
 }
