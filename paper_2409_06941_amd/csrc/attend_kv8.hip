@@ -148,6 +148,8 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
         }
     }
 
+    // What a lane's places are is made anew from `anew()`: kept, they hold registers that the loop needs.
+    auto anew = [&] { int l = lane; asm volatile("" : "+v"(l)); return l; };
     // Where keys lie.  A wavefront loads kLoadRows rows of a tile; 64 of them are a set, those of two or four tiles, a lane each: the page id
     // comes first, then the offset goes to LDS, and the scales' bytes, when they are here, as powers of two.
     constexpr int kLoadRows = kWide ? 16 : 32, kTilesASet = 64 / kLoadRows;
@@ -159,21 +161,21 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
     int32_t id;
     uint8_t k_byte, v_byte;
     auto key_of = [&](int set) {
-        const int u = min(tile_of(set * kTilesASet + lane / kLoadRows), u1 - 1);
-        return keys.seen(keys.first(u) + (kWide ? wave * 16 : 0) + lane % kLoadRows);
+        const int l = anew(), u = min(tile_of(set * kTilesASet + l / kLoadRows), u1 - 1);
+        return keys.seen(keys.first(u) + (kWide ? wave * 16 : 0) + l % kLoadRows);
     };
     auto ask_ids = [&](int set) { id = pages[key_of(set) >> a.page_shift]; };
     auto make_offsets = [&](int set) {
         const int slot = key_of(set) & (a.c.page_size - 1);
         const uint64_t page = (uint64_t)(uint32_t)within(id, 0, (int32_t)a.c.n_pages - 1);
-        *reinterpret_cast<LdsOffset>(lds_at(offsets + (set & 1) * 512 + lane * 8)) = page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)slot * (uint32_t)a.c.slot_stride;
+        *reinterpret_cast<LdsOffset>(lds_at(offsets + (set & 1) * 512 + anew() * 8)) = page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)slot * (uint32_t)a.c.slot_stride;
         const uint64_t at = page * (uint32_t)a.c.scale_page_stride + (uint64_t)(uint32_t)rows.kv * (uint32_t)a.c.scale_head_stride +
                             (uint64_t)(uint32_t)(slot >> a.block_shift) * (uint32_t)a.c.scale_block_stride;
         k_byte = a.c.k_scale[at];
         v_byte = a.c.v_scale[at];
     };
     auto make_powers = [&](int set) {
-        *reinterpret_cast<LdsPair>(lds_at(powers + (set & 1) * 512 + lane * 8)) = f32x2{power_of(scale_byte<T>(k_byte)), power_of(scale_byte<T>(v_byte))};
+        *reinterpret_cast<LdsPair>(lds_at(powers + (set & 1) * 512 + anew() * 8)) = f32x2{power_of(scale_byte<T>(k_byte)), power_of(scale_byte<T>(v_byte))};
     };
     auto offset_at = [&](int t, int r) { return *reinterpret_cast<LdsOffset>(lds_at(offsets + (t / kTilesASet & 1) * 512 + ((t % kTilesASet) * kLoadRows + r) * 8)); };
     auto power_at = [&](int t, int r, bool value) {
@@ -181,7 +183,6 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
     };
     // Values: a lane has 16 codes of a row, kLanes lanes a row.
     constexpr int kLanes = D / 16, kRowsAtOnce = 64 / kLanes, kLoads = kLoadRows / kRowsAtOnce;
-    const int my_row = lane / kLanes, my_piece = lane % kLanes;
     // Rows of values that no row of queries sees become zeros (their weights are 0, but 0 times NaN is not); with `clean`, NaN does everywhere.
     bool clean = false;
     auto fit = [&](uint4 w, int first, int r) {
@@ -191,19 +192,21 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
         }
         return clean ? without_nan(w) : w;
     };
-    auto put = [&](uint32_t tile, int r, uint32_t order, uint4 w, float power) {
-        *reinterpret_cast<LdsWide>(lds_at(tile + r * L::kRow + ((2 * my_piece) ^ order) * 16)) = eight_numbers<T>(w.x, w.y, power);
-        *reinterpret_cast<LdsWide>(lds_at(tile + r * L::kRow + ((2 * my_piece + 1) ^ order) * 16)) = eight_numbers<T>(w.z, w.w, power);
+    auto put = [&](uint32_t tile, int r, int piece, uint32_t order, uint4 w, float power) {
+        const uint32_t at = tile + r * L::kRow + ((2 * piece) ^ order) * 16;
+        *reinterpret_cast<LdsWide>(lds_at(at)) = eight_numbers<T>(w.x, w.y, power);
+        *reinterpret_cast<LdsWide>(lds_at(at ^ 16)) = eight_numbers<T>(w.z, w.w, power);
     };
     // Scores of keys that a row does not see.
     typedef typename State::Block Block;
     auto hide = [&](Block (&s)[2], int first) {
         if (first + kTile <= n_least && (first >= from_most || first + kTile <= a.sinks)) return;
+        const int l = anew();
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < State::kInBlock; ++i) {
-                const int j = first + b * kCols + State::in_block(i, lane);
+                const int j = first + b * kCols + State::in_block(i, l);
                 if (j >= n || (j < from && j >= a.sinks)) s[b][i] = -INFINITY;
             }
     };
@@ -213,19 +216,21 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
         if (tiles <= 0) return;
         if constexpr (!kWide) {
             const uint32_t v = lds + wave * 64 * D;
-            const Fragments<T, D, kCols> fragments(v, lane);
+            Fragments<T, D, kCols> fragments(v, lane);
             uint4 kw[2][D / 64], vw[kLoads];
             auto load_k = [&](int t) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const uint8_t* at = gk + offset_at(t, b * 16 + lane % 16) + lane / 16 * 16;
+                    const int l = anew();
+                    const uint8_t* at = gk + offset_at(t, b * 16 + l % 16) + l / 16 * 16;
 #pragma unroll
                     for (int h = 0; h < D / 64; ++h) kw[b][h] = *reinterpret_cast<const uint4*>(at + h * 64);
                 }
             };
             auto load_v = [&](int t) {
+                const int l = anew();
 #pragma unroll
-                for (int y = 0; y < kLoads; ++y) vw[y] = *reinterpret_cast<const uint4*>(gv + offset_at(t, y * kRowsAtOnce + my_row) + my_piece * 16);
+                for (int y = 0; y < kLoads; ++y) vw[y] = *reinterpret_cast<const uint4*>(gv + offset_at(t, y * kRowsAtOnce + l / kLanes) + l % kLanes * 16);
             };
             ask_ids(0);
             make_offsets(0);
@@ -243,18 +248,21 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
                 f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const float power = power_at(t, b * 16 + lane % 16, false);
+                    const float power = power_at(t, b * 16 + anew() % 16, false);
 #pragma unroll
                     for (int h = 0; h < D / 64; ++h) {
                         s[b] = mfma(__builtin_bit_cast(typename T::x8, eight_numbers<T>(kw[b][h].x, kw[b][h].y, power)), x.q[2 * h], s[b]);
                         s[b] = mfma(__builtin_bit_cast(typename T::x8, eight_numbers<T>(kw[b][h].z, kw[b][h].w, power)), x.q[2 * h + 1], s[b]);
+                        keep_order();                      // (a fragment's registers, not all fragments': four workgroups a unit)
                     }
                 }
                 if (more) load_k(t + 1);
+                const int l = anew();
 #pragma unroll
                 for (int y = 0; y < kLoads; ++y) {
-                    const int r = y * kRowsAtOnce + my_row;
-                    put(v, r, L::fv(r), fit(vw[y], first, r), power_at(t, r, true));
+                    const int r = y * kRowsAtOnce + l / kLanes;
+                    put(v, r, l % kLanes, L::fv(r), fit(vw[y], first, r), power_at(t, r, true));
+                    keep_order();
                 }
                 if (more) load_v(t + 1);
                 if (t % 2 == 1 && more) make_powers(t / 2 + 1);
@@ -268,8 +276,12 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[e] = x.weigh_from(s[e / 2][2 * e % 4], s[e / 2][2 * e % 4 + 1], c, zero);
                 wait_lds();
+                asm volatile("" : "+v"(fragments.v));
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) x.o[d] = mfma(fragments.of_v(0, d), State::fragment(p), x.o[d]);
+                for (int d = 0; d < D / 16; ++d) {
+                    x.o[d] = mfma(fragments.of_v(0, d), State::fragment(p), x.o[d]);
+                    if (d % 4 == 3) keep_order();
+                }
                 wait_lds();
             }
         } else {
@@ -277,21 +289,24 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
             Fragments<T, D, kCols> fragments(lds, lane);
             uint4 kw[kLoads], vw[kLoads];
             auto load = [&](uint4 (&w)[kLoads], const uint8_t* from, int t) {
+                const int l = anew();
 #pragma unroll
-                for (int y = 0; y < kLoads; ++y) w[y] = *reinterpret_cast<const uint4*>(from + offset_at(t, y * kRowsAtOnce + my_row) + my_piece * 16);
+                for (int y = 0; y < kLoads; ++y) w[y] = *reinterpret_cast<const uint4*>(from + offset_at(t, y * kRowsAtOnce + l / kLanes) + l % kLanes * 16);
             };
             auto put_k = [&](int t) {
+                const int l = anew();
 #pragma unroll
                 for (int y = 0; y < kLoads; ++y) {
-                    const int r = y * kRowsAtOnce + my_row;
-                    put(lds + (t & 1) * kHalf + wave * 16 * L::kRow, r, L::fk(wave * 16 + r), kw[y], power_at(t, r, false));
+                    const int r = y * kRowsAtOnce + l / kLanes;
+                    put(lds + (t & 1) * kHalf + wave * 16 * L::kRow, r, l % kLanes, L::fk(wave * 16 + r), kw[y], power_at(t, r, false));
                 }
             };
             auto put_v = [&](int t) {
+                const int l = anew();
 #pragma unroll
                 for (int y = 0; y < kLoads; ++y) {
-                    const int r = y * kRowsAtOnce + my_row;
-                    put(lds + (2 + (t & 1)) * kHalf + wave * 16 * L::kRow, r, L::fv(wave * 16 + r), fit(vw[y], keys.first(u0 + t), wave * 16 + r), power_at(t, r, true));
+                    const int r = y * kRowsAtOnce + l / kLanes;
+                    put(lds + (2 + (t & 1)) * kHalf + wave * 16 * L::kRow, r, l % kLanes, L::fv(wave * 16 + r), fit(vw[y], keys.first(u0 + t), wave * 16 + r), power_at(t, r, true));
                 }
             };
             ask_ids(0);
@@ -344,42 +359,43 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
         if constexpr (!kAlone) __syncthreads();
         else wait_lds();
     };
-    pass();
     // A weight of 0 for a key that a row does not see, times NaN, is NaN: where rows see different keys and one of the results is NaN, the pass
     // is made again without the values' NaN, and then it is given to the rows that see it.
-    if (n_rows > a.group) {
+    for (;;) {
+        pass();
+        if (clean || n_rows <= a.group) break;
         bool bad = false;
 #pragma unroll
         for (int d = 0; d < D / kCols; ++d)
 #pragma unroll
             for (int i = 0; i < State::kInBlock; ++i) bad |= x.o[d][i] != x.o[d][i];
         bad &= !idle;
-        if (kWide ? (bool)__syncthreads_or(bad) : (bool)__any(bad)) {
-            clean = true;
-            pass();
-            for (int t = 0; t < tiles; ++t) {
-                const int first = keys.first(tile_of(t)), j = first + lane;
-                bool any = false;
-                auto place = [&](int j) {
-                    const uint64_t page = (uint64_t)(uint32_t)within(pages[j >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
-                    return gv + page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)(j & (a.c.page_size - 1)) * (uint32_t)a.c.slot_stride;
-                };
-                if (lane < kTile && keys.seen(j) == j) {
-                    const uint4* w = reinterpret_cast<const uint4*>(place(j));
+        clean = kWide ? (bool)__syncthreads_or(bad) : (bool)__any(bad);
+        if (!clean) break;
+    }
+    if (__builtin_expect(clean, 0)) {
+        for (int t = 0; t < tiles; ++t) {
+            const int first = keys.first(tile_of(t)), j = first + lane;
+            bool any = false;
+            auto place = [&](int j) {
+                const uint64_t page = (uint64_t)(uint32_t)within(pages[j >> a.page_shift], 0, (int32_t)a.c.n_pages - 1);
+                return gv + page * (uint32_t)a.c.page_stride + (uint64_t)(uint32_t)(j & (a.c.page_size - 1)) * (uint32_t)a.c.slot_stride;
+            };
+            if (lane < kTile && keys.seen(j) == j) {
+                const uint4* w = reinterpret_cast<const uint4*>(place(j));
 #pragma unroll 1
-                    for (int e = 0; e < D / 16; ++e) any |= (nan_codes(w[e].x) | nan_codes(w[e].y) | nan_codes(w[e].z) | nan_codes(w[e].w)) != 0;
-                }
+                for (int e = 0; e < D / 16; ++e) any |= (nan_codes(w[e].x) | nan_codes(w[e].y) | nan_codes(w[e].z) | nan_codes(w[e].w)) != 0;
+            }
 #pragma unroll 1
-                for (uint64_t left = __ballot(any); left; left &= left - 1) {
-                    const int y = first + __ffsll((unsigned long long)left) - 1;
-                    if (y >= n || (y < from && y >= a.sinks)) continue;
-                    const uint8_t* at = place(y);
+            for (uint64_t left = __ballot(any); left; left &= left - 1) {
+                const int y = first + __ffsll((unsigned long long)left) - 1;
+                if (y >= n || (y < from && y >= a.sinks)) continue;
+                const uint8_t* at = place(y);
 #pragma unroll
-                    for (int d = 0; d < D / kCols; ++d)
+                for (int d = 0; d < D / kCols; ++d)
 #pragma unroll
-                        for (int i = 0; i < State::kInBlock; ++i)
-                            if ((at[d * kCols + State::in_block(i, lane)] & 0x7f) == 0x7f) x.o[d][i] = NAN;
-                }
+                    for (int i = 0; i < State::kInBlock; ++i)
+                        if ((at[d * kCols + State::in_block(i, lane)] & 0x7f) == 0x7f) x.o[d][i] = NAN;
             }
         }
     }
@@ -454,9 +470,10 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
 }
 
 // Workgroups are dealt round-robin over the XCDs.  Those that read the same keys (the row tiles of a group: one sequence, one key head, one
-// run of keys) follow one another on one XCD, through its L2; groups go round the XCDs, so that long sequences spread.
+// run of keys) follow one another on one XCD, through its L2; groups go round the XCDs, the first parts of all sequences before the second
+// ones, so that every XCD has the same mixture of sequences and of parts that short ones do not have.
 template <typename T, int D, Kind kKind>
-__global__ __launch_bounds__(kThreads, kKind == kWideRows ? D == 64 ? 3 : 2 : 3) void k_attend8(Attend8Args a)
+__global__ __launch_bounds__(kThreads, kKind == kWideRows ? D == 64 ? 3 : 2 : 4) void k_attend8(Attend8Args a)
 {
     constexpr int kRows = rows_of(kKind), kTile = keys_of(kKind);
     __shared__ __align__(1024) char lds[Lds8<kKind, D>::kTiles + Lds8<kKind, D>::kTable];
@@ -468,7 +485,7 @@ __global__ __launch_bounds__(kThreads, kKind == kWideRows ? D == 64 ? 3 : 2 : 3)
         group = group * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if (group >= a.items) return;
     }
-    const int split = group % a.splits, of = group / a.splits, kv = of % a.c.n_kv_heads, b = of / a.c.n_kv_heads;
+    const int whole = a.n_seqs * a.c.n_kv_heads, split = group / whole, of = group % whole, kv = of % a.c.n_kv_heads, b = of / a.c.n_kv_heads;
     const Sequence s(a, b);
     const int n_rows = s.tokens * a.group, row0 = tile * kRows;
     if (row0 >= n_rows) return;
@@ -476,7 +493,7 @@ __global__ __launch_bounds__(kThreads, kKind == kWideRows ? D == 64 ? 3 : 2 : 3)
     const int u0 = (int)min((int64_t)split * a.split_len, (int64_t)keys.tiles), u1 = (int)min((int64_t)u0 + a.split_len, (int64_t)keys.tiles);
     if (u0 >= u1 && split) return;                                     // (the first part is always there)
     const Rows rows{a, kv, s.token0, s.n0};
-    attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, (int64_t)group * a.row_tiles + tile, lds);
+    attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, ((int64_t)of * a.splits + split) * a.row_tiles + tile, lds);
 }
 
 // Joins the parts of a row: eight elements a thread.
