@@ -285,73 +285,186 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
                 wait_lds();
             }
         } else {
+            // While tile t's scores become weights (vector unit), the matrix cores make those of tile t + 1, and the codes of K of t + 2 and V of
+            // t + 1 become numbers in LDS; those of K of t + 3 and V of t + 2 are asked for behind that.  Scores are made less the maximum: the
+            // products' sum starts with it.
             constexpr uint32_t kHalf = kTile * L::kRow;
+            constexpr int kSteps = D / 8;                   // MFMAs of the scores, and as many with the values
+            constexpr int kAhead = 4;                       // fragments read ahead of their MFMA
+            constexpr int kPairsBeside = D == 128 ? 10 : 8; // of 16 pairs of weights, those beside the scores' MFMAs; the rest are beside the first half of the values'
             Fragments<T, D, kCols> fragments(lds, lane);
-            uint4 kw[kLoads], vw[kLoads];
-            auto load = [&](uint4 (&w)[kLoads], const uint8_t* from, int t) {
-                const int l = anew();
+            typename T::x8 ahead[kAhead];
+            auto k_of = [&](auto odd, int y) { return fragments.of_k(odd * kHalf + y % 2 * 32 * L::kRow, y / 2); };
+            auto v_of = [&](auto odd, int y) { return fragments.of_v((2 + odd) * kHalf + y / (D / 32) * 16 * L::kRow, y % (D / 32)); };
+            u32x4 kw[kLoads], vw[kLoads];
+            auto load = [&](u32x4 (&w)[kLoads], const uint8_t* from, int t) {
+                const int l = anew(), to = min(t, tiles - 1);
 #pragma unroll
-                for (int y = 0; y < kLoads; ++y) w[y] = *reinterpret_cast<const uint4*>(from + offset_at(t, y * kRowsAtOnce + l / kLanes) + l % kLanes * 16);
+                for (int y = 0; y < kLoads; ++y) w[y] = *reinterpret_cast<const u32x4*>(from + offset_at(to, y * kRowsAtOnce + l / kLanes) + l % kLanes * 16);
             };
-            auto put_k = [&](int t) {
-                const int l = anew();
+            // powers of two of the lane's rows of tile t; half a lane's codes of a row into tile `odd` of K (V)
+            auto powers_of = [&](float (&w)[kLoads], int t, bool value) {
+                const int l = anew(), of = min(t, tiles - 1);
 #pragma unroll
-                for (int y = 0; y < kLoads; ++y) {
-                    const int r = y * kRowsAtOnce + l / kLanes;
-                    put(lds + (t & 1) * kHalf + wave * 16 * L::kRow, r, l % kLanes, L::fk(wave * 16 + r), kw[y], power_at(t, r, false));
+                for (int y = 0; y < kLoads; ++y) w[y] = power_at(of, y * kRowsAtOnce + l / kLanes, value);
+            };
+            float kp[kLoads], vp[kLoads];
+            // (rows y kRowsAtOnce further down have another order of pieces, in bits that the lane's own leave alone)
+            const uint32_t my_row = wave * 16 + lane / kLanes;
+            uint32_t k_at = lds + my_row * L::kRow + ((2 * (lane % kLanes)) ^ L::fk(my_row)) * 16, v_at = lds + 2 * kHalf + my_row * L::kRow + ((2 * (lane % kLanes)) ^ L::fv(my_row)) * 16;
+            auto made_here = [&](uint32_t lo, uint32_t hi, float power) {       // (not where the codes come: the numbers take twice their registers)
+                asm volatile("" : "+v"(lo), "+v"(hi));
+                return eight_numbers<T>(lo, hi, power);
+            };
+            auto put_k = [&](uint32_t odd, int e) {
+                const int y = e / 2;
+                *reinterpret_cast<LdsWide>(lds_at(k_at ^ ((L::fk(y * kRowsAtOnce) ^ e % 2) * 16)) + odd * kHalf + y * kRowsAtOnce * L::kRow) =
+                    made_here(kw[y][e % 2 * 2], kw[y][e % 2 * 2 + 1], kp[y]);
+            };
+            auto put_v = [&](uint32_t odd, int e) {
+                const int y = e / 2;
+                *reinterpret_cast<LdsWide>(lds_at(v_at ^ ((L::fv(y * kRowsAtOnce) ^ e % 2) * 16)) + odd * kHalf + y * kRowsAtOnce * L::kRow) =
+                    made_here(vw[y][e % 2 * 2], vw[y][e % 2 * 2 + 1], vp[y]);
+            };
+            auto fit_v = [&](int t) {
+                const int first = keys.first(u0 + t);
+                if (!keys.all_seen(first) || clean) {
+#pragma unroll
+                    for (int y = 0; y < kLoads; ++y) vw[y] = __builtin_bit_cast(u32x4, fit(__builtin_bit_cast(uint4, vw[y]), first, wave * 16 + y * kRowsAtOnce + anew() / kLanes));
                 }
             };
-            auto put_v = [&](int t) {
-                const int l = anew();
+            f32x16 minus;
 #pragma unroll
-                for (int y = 0; y < kLoads; ++y) {
-                    const int r = y * kRowsAtOnce + l / kLanes;
-                    put(lds + (2 + (t & 1)) * kHalf + wave * 16 * L::kRow, r, l % kLanes, L::fv(wave * 16 + r), fit(vw[y], keys.first(u0 + t), wave * 16 + r), power_at(t, r, true));
+            for (int i = 0; i < 16; ++i) minus[i] = 0.0f;
+            float top = -INFINITY;
+            auto tops = [&](const f32x16 (&s)[2], int e) { top = fmaxf(top, s[e / 16][e % 16]); };
+            auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2], int t, auto here, auto other) {      // (here: t modulo 2)
+                __syncthreads();                            // K of t + 1 and V of t are here; K of t and V of t - 1 are done with
+                powers_of(kp, t + 2, false);
+                powers_of(vp, t + 1, true);
+                fit_v(t + 1);
+                if (idle) {
+#pragma unroll
+                    for (int e = 0; e < 2 * kLoads; ++e) put_k(here, e), put_v(other, e);
+                } else {
+                    asm volatile("" : "+v"(fragments.k), "+v"(fragments.v), "+v"(k_at), "+v"(v_at));        // (one register each, not one for every fragment)
+#pragma unroll
+                    for (int y = 0; y < kAhead; ++y) ahead[y] = k_of(other, y);
+                    // a larger maximum, if the one in use lags behind by more than kSlack, or there has been none
+                    if (__any((x.m == -INFINITY ? top + INFINITY : top * c) > kSlack)) {
+                        // (exactly as much as the tile's scores exceed it: the maximum may be off by half an ulp then, which the next tile's scores show)
+                        const bool none = x.m == -INFINITY;
+                        const float more = none ? top == -INFINITY ? 0.0f : top : fmaxf(top, 0.0f), old = __builtin_amdgcn_exp2f(-more * c);
+                        x.l *= none ? 1.0f : old;
+                        x.l1 *= none ? 1.0f : old;
+#pragma unroll
+                        for (int d = 0; d < D / kCols; ++d)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x.o[d][i] *= none ? 1.0f : old;
+                        x.m = none ? top : x.m + more;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            now[0][i] -= more;
+                            now[1][i] -= more;
+                            minus[i] = -x.zero_point();
+                        }
+                    }
+                    uint32_t p[16];
+                    auto pair = [&](int e) {
+                        p[e] = x.weigh_from(now[e / 8][2 * e % 16], now[e / 8][2 * e % 16 + 1], c, 0.0f);
+                        asm volatile("" : "+v"(p[e]), "+v"(x.l), "+v"(x.l1));             // (made here, not where they are used)
+                    };
+                    keep_order();
+#pragma unroll
+                    for (int y = 0; y < kSteps; ++y) {          // (behind the last tile: of what lies there, not used)
+                        next[y % 2] = mfma(ahead[y % kAhead], x.q[y / 2], y < 2 ? minus : next[y % 2]);
+                        ahead[y % kAhead] = y + kAhead < kSteps ? k_of(other, y + kAhead) : v_of(here, y + kAhead - kSteps);
+#pragma unroll
+                        for (int e = y * kPairsBeside / kSteps; e < (y + 1) * kPairsBeside / kSteps; ++e) pair(e);
+                        if (y % 2 == 0) {
+                            if (y / 2 < 2 * kLoads) put_k(here, y / 2);
+                            else put_v(other, y / 2 - 2 * kLoads);
+                        }
+                        keep_order();
+                    }
+                    hide(next, keys.first(u0 + t + 1));
+                    top = -INFINITY;
+                    keep_order();
+                    // (in front of the tiles' loads: the compiler waits for those behind a load that may not have been asked for)
+                    if (t % kTilesASet == 0) {
+                        make_offsets(t / kTilesASet + 1);
+                        ask_ids(t / kTilesASet + 2);
+                    } else if (t % kTilesASet == 1) {
+                        make_powers(t / kTilesASet + 1);
+                    }
+                    load(kw, gk, t + 3);
+                    load(vw, gv, t + 2);
+                    keep_order();
+                    __builtin_amdgcn_s_setprio(1);              // (first to the matrix cores: the other workgroup's wavefront has weights to make)
+#pragma unroll
+                    for (int y = 0; y < kSteps; ++y) {
+                        constexpr int kFirst = kSteps / 2, kRest = 16 - kPairsBeside;
+                        const int f = y / (D / 32), d = y % (D / 32);
+                        x.o[d] = mfma(ahead[y % kAhead], State::fragment(p + 4 * f), x.o[d]);
+                        if (y + kAhead < kSteps) ahead[y % kAhead] = v_of(here, y + kAhead);
+                        if (y < kFirst) {
+#pragma unroll
+                            for (int e = y * kRest / kFirst; e < (y + 1) * kRest / kFirst; ++e) pair(kPairsBeside + e);
+                        } else {
+#pragma unroll
+                            for (int e = (y - kFirst) * 32 / kFirst; e < (y - kFirst + 1) * 32 / kFirst; ++e) tops(next, e);
+                        }
+                        keep_order();
+                    }
+                    __builtin_amdgcn_s_setprio(0);
+                    top = top_of_row<kCols>(top);
+                    return;
                 }
+                if (t % kTilesASet == 0) {
+                    make_offsets(t / kTilesASet + 1);
+                    ask_ids(t / kTilesASet + 2);
+                } else if (t % kTilesASet == 1) {
+                    make_powers(t / kTilesASet + 1);
+                }
+                load(kw, gk, t + 3);
+                load(vw, gv, t + 2);
             };
+            const std::integral_constant<uint32_t, 0> even{};
+            const std::integral_constant<uint32_t, 1> odd{};
             ask_ids(0);
             make_offsets(0);
-            if (tiles > kTilesASet) ask_ids(1);
+            ask_ids(1);
             load(kw, gk, 0);
             load(vw, gv, 0);
             make_powers(0);
-            for (int t = 0; t < tiles; ++t) {
-                put_k(t);
-                put_v(t);
-                if (t % kTilesASet == 0 && t + kTilesASet < tiles) {
-                    make_offsets(t / kTilesASet + 1);
-                    if (t + 2 * kTilesASet < tiles) ask_ids(t / kTilesASet + 2);
-                }
-                if (t + 1 < tiles) {
-                    load(kw, gk, t + 1);
-                    load(vw, gv, t + 1);
-                    if (t % kTilesASet == kTilesASet - 1) make_powers(t / kTilesASet + 1);
-                }
-                __syncthreads();
-                if (idle) continue;
-                f32x16 s[2];
+            powers_of(kp, 0, false);
+            powers_of(vp, 0, true);
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+            for (int e = 0; e < 2 * kLoads; ++e) put_k(even, e);
+            load(kw, gk, 1);
+            powers_of(kp, 1, false);
+            fit_v(0);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+            for (int e = 0; e < 2 * kLoads; ++e) put_v(even, e);
+            load(vw, gv, 1);
 #pragma unroll
-                for (int f = 0; f < D / 16; ++f)
+            for (int e = 0; e < 2 * kLoads; ++e) put_k(odd, e);
+            load(kw, gk, 2);
+            __syncthreads();
+            f32x16 s0[2], s1[2];
+            if (!idle) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) s[b] = mfma(fragments.of_k((t & 1) * kHalf + b * 32 * L::kRow, f), x.q[f], s[b]);
-                hide(s, keys.first(u0 + t));
-                float top = s[0][0];
+                for (int y = 0; y < kSteps; ++y) s0[y % 2] = mfma(k_of(even, y), x.q[y / 2], y < 2 ? minus : s0[y % 2]);
+                hide(s0, keys.first(u0));
 #pragma unroll
-                for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
-                x.grow(top_of_row<kCols>(top), c);
-                const float zero = x.zero_point();
-                uint32_t p[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) p[e] = x.weigh_from(s[e / 8][2 * e % 16], s[e / 8][2 * e % 16 + 1], c, zero);
-#pragma unroll
-                for (int f = 0; f < 4; ++f)
-#pragma unroll
-                    for (int d = 0; d < D / 32; ++d) x.o[d] = mfma(fragments.of_v((2 + (t & 1)) * kHalf + f * 16 * L::kRow, d), State::fragment(p + 4 * f), x.o[d]);
-                wait_lds();
+                for (int e = 0; e < 32; ++e) tops(s0, e);
+                top = top_of_row<kCols>(top);
+            }
+            for (int t = 0;; t += 2) {
+                step(s0, s1, t, even, odd);
+                if (t + 1 >= tiles) break;
+                step(s1, s0, t + 1, odd, even);
+                if (t + 2 >= tiles) break;
             }
         }
     };
@@ -473,7 +586,7 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
 // run of keys) follow one another on one XCD, through its L2; groups go round the XCDs, the first parts of all sequences before the second
 // ones, so that every XCD has the same mixture of sequences and of parts that short ones do not have.
 template <typename T, int D, Kind kKind>
-__global__ __launch_bounds__(kThreads, kKind == kWideRows ? D == 64 ? 3 : 2 : 4) void k_attend8(Attend8Args a)
+__global__ __launch_bounds__(kThreads, kKind == kWideRows ? 2 : 4) void k_attend8(Attend8Args a)
 {
     constexpr int kRows = rows_of(kKind), kTile = keys_of(kKind);
     __shared__ __align__(1024) char lds[Lds8<kKind, D>::kTiles + Lds8<kKind, D>::kTable];
