@@ -34,11 +34,13 @@ template <typename X> __device__ __forceinline__ void copy_rows(char* base, cons
     const char* x = base + from * s.page_stride;
     char* y = base + to * s.page_stride;
     const int a_row = s.row / (int)sizeof(X), all = s.n0 * s.n1 * a_row;
-    for (int i = threadIdx.x; i < all; i += kThreads) {
+    const bool whole = s.n0 * s.n1 == 1;                   // (rows that lie side by side are one: no division)
+    auto place = [&](int i) {
+        if (whole) return (int64_t)i * (int)sizeof(X);
         const int r = i / a_row;
-        const int64_t at = (int64_t)(r / s.n1) * s.s0 + (int64_t)(r % s.n1) * s.s1 + (int64_t)(i % a_row) * (int)sizeof(X);
-        *reinterpret_cast<X*>(y + at) = *reinterpret_cast<const X*>(x + at);
-    }
+        return (int64_t)(r / s.n1) * s.s0 + (int64_t)(r % s.n1) * s.s1 + (int64_t)(i % a_row) * (int)sizeof(X);
+    };
+    for (int i = threadIdx.x; i < all; i += kThreads) *reinterpret_cast<X*>(y + place(i)) = *reinterpret_cast<const X*>(x + place(i));
 }
 
 __device__ __forceinline__ void copy_array(char* base, const Shape& s, int64_t from, int64_t to)
@@ -47,10 +49,11 @@ __device__ __forceinline__ void copy_array(char* base, const Shape& s, int64_t f
     else copy_rows<uint8_t>(base, s, from, to);
 }
 
-// One workgroup per pair and cache.  Whether the pair is carried out is found by a look at all others.
+// Two workgroups per pair and cache, for K and for V.  Whether the pair is carried out is found by a look at all others.
 __global__ __launch_bounds__(kThreads) void k_copy_pages(CopyArgs a)
 {
-    const int i = blockIdx.x % a.n_pairs, c = blockIdx.x / a.n_pairs;
+    const int i = blockIdx.x % a.n_pairs, of = blockIdx.x / a.n_pairs, c = of >> 1;
+    const bool value = of & 1;
     const int32_t from = a.source[i], to = a.target[i];
     bool out = from < 0 || to < 0 || from >= a.n_pages || to >= a.n_pages || from == to;
     if (!out) {
@@ -64,14 +67,10 @@ __global__ __launch_bounds__(kThreads) void k_copy_pages(CopyArgs a)
         }
         out = __syncthreads_or(hit);
     }
-    if (a.copied && c == 0 && threadIdx.x == 0) a.copied[i] = !out;
+    if (a.copied && of == 0 && threadIdx.x == 0) a.copied[i] = !out;
     if (out) return;
-    copy_array(a.k[c], a.codes, from, to);
-    copy_array(a.v[c], a.codes, from, to);
-    if (a.scales.row) {
-        copy_array(a.ks[c], a.scales, from, to);
-        copy_array(a.vs[c], a.scales, from, to);
-    }
+    copy_array(value ? a.v[c] : a.k[c], a.codes, from, to);
+    if (a.scales.row) copy_array(value ? a.vs[c] : a.ks[c], a.scales, from, to);
 }
 
 // Rows that lie side by side become one; the largest piece that all addresses are multiples of.
@@ -113,12 +112,12 @@ extern "C" int fr_kv_copy_pages(const fr_kv_copy_desc* d, void* stream)
     a.n_pages = n_pages;
     a.source = d->source, a.target = d->target, a.copied = d->copied, a.n_pairs = d->n_pairs;
     auto go = [&] {
-        const int at_once = (int)std::max<int64_t>(1, kMostThreads / kThreads / a.n_pairs);
+        const int at_once = (int)std::max<int64_t>(1, kMostThreads / kThreads / 2 / a.n_pairs);
         for (int done = 0; done < a.n_caches; done += at_once) {
             CopyArgs x = a;
             x.n_caches = std::min(at_once, a.n_caches - done);
             for (int c = 0; c < x.n_caches; ++c) x.k[c] = a.k[done + c], x.v[c] = a.v[done + c], x.ks[c] = a.ks[done + c], x.vs[c] = a.vs[done + c];
-            hipLaunchKernelGGL(k_copy_pages, dim3((unsigned)x.n_caches * a.n_pairs), dim3(kThreads), 0, (hipStream_t)stream, x);
+            hipLaunchKernelGGL(k_copy_pages, dim3((unsigned)x.n_caches * a.n_pairs * 2), dim3(kThreads), 0, (hipStream_t)stream, x);
         }
         a.n_caches = 0;
         a.copied = nullptr;
