@@ -535,3 +535,169 @@ def test_copy_many_pairs():
     rng = np.random.default_rng(5)
     source = rng.integers(-2, 25, 1500)
     _copy_case(ONE + [(8, 2, 16, 64, 8, "slots")], source.tolist(), rng.integers(-2, 25, 1500).tolist(), 10)
+
+
+# ---------------------------------------------------------------- together
+
+def test_a_prompt_that_forks_and_goes_on():
+    # a prompt in two pieces, three sequences that go on from it in pages of their own, a window; every code and every row against the oracle
+    dt, Hq, Hk, D, page, block, pages = "bf16", 8, 2, 128, 16, 8, 30
+    rng = np.random.default_rng(3)
+    oracle = [np.zeros((pages, Hk, page, D), np.uint8), np.zeros((pages, Hk, page, D), np.uint8)] + [np.zeros((pages, Hk, page // block), np.uint8) for _ in range(2)]
+    gpu = [torch.from_numpy(x.copy()).cuda() for x in oracle]
+    cache = fr.Kv8Pages(*gpu, DT[dt])
+    order = rng.permutation(pages)
+    tables = np.tile(order[:4], (3, 1)).astype(np.int32)                 # the prompt's pages stand in all tables ...
+    tables = np.concatenate([tables, order[4:4 + 9].reshape(3, 3).astype(np.int32)], 1)
+    angle = rng.random((200, 32)) * 6.3
+    table = torch.from_numpy(np.concatenate([np.cos(angle), np.sin(angle)], 1)).float()
+
+    def run(new, lens, tables, window, sinks):
+        """new tokens of every sequence, the last of its lens keys: appended and attended to"""
+        T = sum(new)
+        q, k, v = (torch.from_numpy(rng.normal(0, 1, (T, h, D)) * 2.0 ** rng.integers(-3, 4, (T, 1, 1))).to(DT[dt]) for h in (Hq, Hk, Hk))
+        where = np.concatenate([np.arange(n - t, n) for n, t in zip(lens, new)])
+        seq = np.repeat(np.arange(len(new)), new)
+        slot = (tables[seq, where // page] * page + where % page).astype(np.int64)
+        begin = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        qg, out, lse = q.cuda(), torch.full((T, Hq, D), 9.0, dtype=DT[dt], device="cuda"), torch.zeros(T, Hq, device="cuda")
+        fr.fr_kv8_append(cache, k.cuda(), v.cuda(), torch.from_numpy(slot).cuda(), q=qg, q_out=qg, position=torch.from_numpy(where.astype(np.int32)).cuda(), rotary=table.cuda())
+        lim = dict(max_len=max(lens), max_q=max(new), window=window, sinks=sinks)
+        ws = torch.empty(max(1, fr.fr_attend_kv8_workspace_bytes(cache, qg, len(new), **lim)), dtype=torch.uint8, device="cuda")
+        fr.fr_attend_kv8(cache, qg, out, torch.from_numpy(np.ascontiguousarray(tables)).cuda(), torch.tensor(lens, dtype=I32, device="cuda"), D ** -0.5,
+                         q_begin=torch.from_numpy(begin).cuda(), lse=lse, workspace=ws, **lim)
+        torch.cuda.synchronize()
+        cache8.append(*oracle, _f64(k), _f64(v), slot, block, dt, _f64(table)[where, :32], _f64(table)[where, 32:], 64, False)
+        for a, b in zip(gpu, oracle):
+            assert np.array_equal(a.cpu().numpy(), b)
+        K, V = cache8.numbers(oracle[0], oracle[2], block, dt), cache8.numbers(oracle[1], oracle[3], block, dt)
+        _check_attend(dt, qg, K, V, [t for t in tables], page, lens, begin, window, sinks, D ** -0.5, out, lse)
+
+    run([33], [33], tables[:1], 0, 0)
+    run([26], [59], tables[:1], 20, 2)                                   # (59 tokens: the fourth page is not full)
+    source, target = np.full(2, order[3]), tables[1:, 4]
+    copied = torch.zeros(2, dtype=I32, device="cuda")
+    fr.fr_kv_copy_pages([cache], torch.from_numpy(source.astype(np.int32)).cuda(), torch.from_numpy(np.ascontiguousarray(target)).cuda(), copied=copied)
+    for x in oracle:
+        x[target] = x[source]
+    assert copied.tolist() == [1, 1]
+    tables[1:, 3] = target                                               # ... but for the last one, of which the others have copies
+    tables[:, 4:6] = np.stack([tables[0, 4:6], tables[1, 5:7], tables[2, 5:7]])
+    lens = [59, 59, 59]
+    for new in ([1, 1, 1], [1, 1, 1], [5, 1, 7], [1, 0, 1], [20, 3, 11]):
+        lens = [n + t for n, t in zip(lens, new)]
+        run(new, lens, tables, 24, 3)
+        if new[0] == 5:
+            run([0, 1, 0], [lens[0], lens[1] + 1, lens[2]], tables, 0, 0)
+            lens[1] += 1
+
+
+def _step(dt=torch.bfloat16, seqs=6, Hq=8, Hk=2, D=64, page=16, block=16, longest=900, window=0, seed=0):
+    """A step that reads from the device where it stands: append, then attend; and what it works on."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = longest // page
+    codes = [torch.randint(0, 120, (seqs * n, Hk, page, D), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    scale = [torch.full((seqs * n, Hk, page // block), 118, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    s = dict(cache=fr.Kv8Pages(*codes, *scale, dt), tensors=codes + scale, pages=torch.randperm(seqs * n, generator=g, device="cuda").to(I32).view(seqs, n),
+             at=torch.arange(seqs, device="cuda") * 131 % (longest - 40), row=torch.randn((seqs, Hq + 2 * Hk, D), generator=g, device="cuda").to(dt),
+             out=torch.zeros((seqs, Hq, D), dtype=dt, device="cuda"), lse=torch.zeros(seqs, Hq, device="cuda"), rows=torch.arange(seqs, device="cuda"))
+    lim = dict(max_len=n * page, window=window, sinks=2 if window else 0)
+    s["workspace"] = torch.empty(max(1, fr.fr_attend_kv8_workspace_bytes(s["cache"], s["out"], seqs, **lim)), dtype=torch.uint8, device="cuda")
+
+    def step(stream=None):
+        q, k, v = s["row"].split([Hq, Hk, Hk], 1)
+        slot = s["pages"][s["rows"], s["at"] // page].long() * page + s["at"] % page
+        fr.fr_kv8_append(s["cache"], k, v, slot, stream=stream)
+        s["at"].add_(1)
+        fr.fr_attend_kv8(s["cache"], q.contiguous(), s["out"], s["pages"], s["at"].int(), D ** -0.5, lse=s["lse"], workspace=s["workspace"], stream=stream, **lim)
+        s["row"].copy_(s["row"].roll(1, 0) * 1.01)
+    return s, step
+
+
+def test_captured_steps_replay_beside_one_another():
+    # two graphs that share a workspace, replayed in turn with eager work and other calls between: the bits of eager steps
+    make = lambda: [_step(seed=1), _step(seed=2, window=100)]
+    want, steps = [], make()
+    steps[1][0]["workspace"] = steps[0][0]["workspace"] = max((s["workspace"] for s, _ in steps), key=lambda w: w.numel())
+    for _ in range(8):
+        for s, step in steps:
+            step()
+            want.append((s["out"].clone(), s["lse"].clone(), [x.clone() for x in s["tensors"]]))
+    steps = make()
+    steps[1][0]["workspace"] = steps[0][0]["workspace"] = max((s["workspace"] for s, _ in steps), key=lambda w: w.numel())
+    graphs = []
+    for s, step in steps:
+        keep = {k: s[k].clone() for k in ("at", "row")}
+        tensors = [x.clone() for x in s["tensors"]]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        for k, x in keep.items():
+            s[k].copy_(x)
+        for a, b in zip(s["tensors"], tensors):
+            a.copy_(b)
+        graphs.append(graph)
+    other = _step(seed=9)[1]
+    for i in range(8):
+        for j, (s, _) in enumerate(steps):
+            graphs[j].replay()
+            if i % 3 == 1:
+                other()
+            if i % 2:
+                torch.cuda.synchronize()
+            out, lse, tensors = want[2 * i + j]
+            assert torch.equal(s["out"], out) and torch.equal(s["lse"], lse), (i, j)
+            assert all(torch.equal(a, b) for a, b in zip(s["tensors"], tensors)), (i, j)
+
+
+def test_calls_on_streams_of_their_own_side_by_side():
+    alone = []
+    for seed in (4, 5):
+        s, step = _step(seed=seed, seqs=40, longest=1600)
+        for _ in range(6):
+            step()
+        torch.cuda.synchronize()
+        alone.append((s["out"].clone(), s["tensors"][0].clone()))
+    pairs, streams = [_step(seed=seed, seqs=40, longest=1600) for seed in (4, 5)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for (s, step), stream in zip(pairs, streams):
+            with torch.cuda.stream(stream):
+                step()                                 # (without a stream: torch's current one)
+    torch.cuda.synchronize()
+    for (s, _), (out, codes) in zip(pairs, alone):
+        assert torch.equal(s["out"], out) and torch.equal(s["tensors"][0], codes)
+
+
+def test_a_masked_stream_gives_the_same_result():
+    # fewer units: keys are cut in other parts, results are those of the definition all the same
+    ctx = fr.Context(device_id=0, cu_count=16)
+    for lens, new in (([2000, 1, 300], [1, 1, 1]), ([400, 90], [200, 90])):
+        _attend_case("bf16", 8, 2, 128, 16, 16, lens, new, 31, stream=ctx.fr_side_stream(), rows=200)
+        _attend_case("f16", 8, 2, 64, 16, 4, lens, new, 32, 128, 2, stream=ctx.fr_side_stream(), rows=200)
+    ctx.fr_destroy()
+
+
+@pytest.mark.parametrize("window,sinks,prompt", [(0, 0, 500), (64, 4, 512), (300, 1, 250)])
+def test_the_example_in_8_bits(window, sinks, prompt):
+    from examples import generate_in_bubbles as example
+    make = lambda: example.Decoder(prompt=prompt, new=20, seed=6, cache_bits=8, window=window, sinks=sinks)
+    model = make()
+    model.prefill()
+    for _ in range(20):
+        model.step()
+    torch.cuda.synchronize()
+    want = model.tokens.clone()
+    assert int(want.min()) >= 0 and len(set(want[:, 0].tolist())) > 1 and bool(torch.isfinite(model.logits.float()).all())
+    model = make()
+    model.prefill()
+    model.capture()
+    got, step_ns = example.standalone(model)
+    assert torch.equal(got, want)
+    again, progress, bubble_ns = example.harvest(model, step_ns, epochs=10)
+    assert progress.steps == 20 and bubble_ns > 0 and torch.equal(again, want)
