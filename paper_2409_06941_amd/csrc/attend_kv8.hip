@@ -609,30 +609,31 @@ __global__ __launch_bounds__(kThreads, kKind == kWideRows ? 2 : 4) void k_attend
     attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, ((int64_t)of * a.splits + split) * a.row_tiles + tile, lds);
 }
 
-// Joins the parts of a row: eight elements a thread.
-template <typename T, int D, Kind kKind>
+// Joins the parts of a row: twice four elements a thread, kLanes threads for every eight, each with every kLanes-th part, eight of them in one
+// go.  Bound by latency: the launch, the sequence's length, then all parts.
+template <typename T, int D, Kind kKind, int kLanes>
 __global__ __launch_bounds__(kThreads) void k_attend8_join(Attend8Args a, int64_t first)
 {
-    constexpr int kRows = rows_of(kKind), kPieces = D / 8, kRowsHere = kThreads / kPieces, kBlocks = kRows > kRowsHere ? kRows / kRowsHere : 1;
+    constexpr int kRows = rows_of(kKind), kPieces = D / 8, kRowsHere = kThreads / kPieces / kLanes, kBlocks = (kRows + kRowsHere - 1) / kRowsHere;
     const int64_t id = first + blockIdx.x;
     const int tile = (int)(id / kBlocks % a.row_tiles), of = (int)(id / kBlocks / a.row_tiles), kv = of % a.c.n_kv_heads, b = of / a.c.n_kv_heads;
-    const int r = (int)(id % kBlocks) * kRowsHere + threadIdx.x / kPieces, piece = threadIdx.x % kPieces;
+    const int r = (int)(id % kBlocks) * kRowsHere + threadIdx.x / kPieces / kLanes, mine = threadIdx.x / kPieces % kLanes, piece = threadIdx.x % kPieces;
     const Sequence s(a, b);
     const int n_rows = s.tokens * a.group, row0 = tile * kRows;
-    if (r >= kRows || row0 + r >= n_rows) return;
-    const Keys<keys_of(kKind)> keys(a, s.n0, row0 / a.group, (min(n_rows, row0 + kRows) - 1) / a.group);
-    const int parts = max(1, (keys.tiles + a.split_len - 1) / a.split_len);
+    const bool there = r < kRows && row0 + r < n_rows;
+    const Keys<keys_of(kKind)> keys(a, s.n0, row0 / a.group, max(0, min(n_rows, row0 + kRows) - 1) / a.group);
+    const int parts = there ? max(1, (keys.tiles + a.split_len - 1) / a.split_len) : 0;
     constexpr int kAtOnce = 8;
     const int64_t step = (int64_t)a.row_tiles * kRows, at0 = ((int64_t)of * a.splits * a.row_tiles + tile) * kRows + r;
-    float top = -INFINITY, sum = 0.0f, o[8];
+    float top = -INFINITY, base, sum = 0.0f, o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-    for (int y0 = 0; y0 < parts; y0 += kAtOnce) {
+    for (int y0 = mine; y0 < parts; y0 += kAtOnce * kLanes) {
         float2 ml[kAtOnce];
         float4 lo[kAtOnce], hi[kAtOnce];
 #pragma unroll
         for (int x = 0; x < kAtOnce; ++x) {
-            const int64_t at = at0 + min(y0 + x, parts - 1) * step;
+            const int64_t at = at0 + min(y0 + x * kLanes, parts - 1) * step;
             const float4* p = reinterpret_cast<const float4*>(a.part_o + at * D) + piece;
             ml[x] = a.part_ml[at];
             lo[x] = p[0];
@@ -641,20 +642,43 @@ __global__ __launch_bounds__(kThreads) void k_attend8_join(Attend8Args a, int64_
         const float before = top;
 #pragma unroll
         for (int x = 0; x < kAtOnce; ++x)
-            if (y0 + x < parts) top = fmaxf(top, ml[x].x);
-        const float base = top == -INFINITY ? 0.0f : top, g = __builtin_amdgcn_exp2f(before - base);
+            if (y0 + x * kLanes < parts) top = fmaxf(top, ml[x].x);
+        base = top == -INFINITY ? 0.0f : top;
+        const float g = __builtin_amdgcn_exp2f(before - base);
         sum *= g;
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] *= g;
 #pragma unroll
         for (int x = 0; x < kAtOnce; ++x) {
-            if (y0 + x >= parts) continue;
+            if (y0 + x * kLanes >= parts) continue;
             const float f = __builtin_amdgcn_exp2f(ml[x].x - base);
             sum = fmaf(ml[x].y, f, sum);
             o[0] = fmaf(lo[x].x, f, o[0]), o[1] = fmaf(lo[x].y, f, o[1]), o[2] = fmaf(lo[x].z, f, o[2]), o[3] = fmaf(lo[x].w, f, o[3]);
             o[4] = fmaf(hi[x].x, f, o[4]), o[5] = fmaf(hi[x].y, f, o[5]), o[6] = fmaf(hi[x].z, f, o[6]), o[7] = fmaf(hi[x].w, f, o[7]);
         }
     }
+    if constexpr (kLanes > 1) {
+        __shared__ float all[10][kThreads];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) all[e][threadIdx.x] = o[e];
+        all[8][threadIdx.x] = sum;
+        all[9][threadIdx.x] = top;
+        __syncthreads();
+        if (mine) return;
+        for (int y = 1; y < kLanes; ++y) top = fmaxf(top, all[9][threadIdx.x + y * kPieces]);
+        base = top == -INFINITY ? 0.0f : top;
+        sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+        for (int y = 0; y < kLanes; ++y) {
+            const int x = threadIdx.x + y * kPieces;
+            const float f = __builtin_amdgcn_exp2f(all[9][x] - base);
+            sum = fmaf(all[8][x], f, sum);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(all[e][x], f, o[e]);
+        }
+    }
+    if (!there) return;
     const int64_t token = s.token0 + (row0 + r) / a.group, head = kv * a.group + (row0 + r) % a.group;
     const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
     uint16_t* out = a.out + token * a.out_stride + head * D + piece * 4;
@@ -679,8 +703,13 @@ struct Plan {
     int64_t row_tiles = 1, base = 0, splits = 1, split_len = 1;        // base: sequences x key heads x row tiles
 };
 constexpr int64_t kMostFew = 32;           // rows of a sequence that are few
-constexpr int64_t kMostItems = 4 * kUnits; // parts are no more than give so many items in all
+constexpr int64_t kMostParts = 128;        // of a row: what the join reads in one go
 constexpr int64_t kMostBlocks = 0x7fffffff;
+
+// Parts are no more than give so many items in all: four a unit, which are on it at once.  Of few rows three times as many, where there are few sequences
+// and heads: they even out lengths that differ (8 sequences of up to 65536 tokens with 8 key heads 125 -> 114 us; with more sequences than that there is
+// no gain, and of equal lengths they begin and end more often: 128 of 4096 tokens 185 us in one part, 197 in two).
+int64_t most_items(Kind k, int64_t base, int64_t cus) { return (k == kFewRows && 2 * base <= cus ? 12 : 4) * cus; }
 
 int64_t rows_a_seq(const fr_attend_kv8_desc& d) { return (int64_t)std::min(d.max_q, d.n_tokens) * (d.n_q_heads / d.cache.n_kv_heads); }
 int64_t row_tiles_of(int64_t rows) { return rows > kMostFew ? up(rows, rows_of(kWideRows)) : up(rows, rows_of(kFewRows)); }
@@ -696,8 +725,8 @@ Plan plan(const fr_attend_kv8_desc& d, int cus)
     // tiles of keys that a row tile sees, at most
     int64_t keys = d.max_len;
     if (d.window) keys = std::min<int64_t>(keys, (int64_t)d.window + std::min<int64_t>(up(rows_of(p.kind), group), d.max_q) + d.sinks + 3 * tile);
-    const int64_t tiles = std::max<int64_t>(up(keys, tile), 1), least = p.kind == kWideRows ? 2 : 4;
-    const int64_t want = std::max<int64_t>(1, std::min(up(tiles, least), std::min<int64_t>(cus, kUnits) * 4 / p.base));
+    const int64_t tiles = std::max<int64_t>(up(keys, tile), 1), least = p.kind == kWideRows ? 2 : 8;
+    const int64_t want = std::max<int64_t>(1, std::min({up(tiles, least), most_items(p.kind, p.base, std::min(cus, kUnits)) / p.base, kMostParts}));
     p.split_len = up(tiles, want);
     p.splits = up(tiles, p.split_len);
     return p;
@@ -706,9 +735,9 @@ Plan plan(const fr_attend_kv8_desc& d, int cus)
 // Rows of results in parts that a call has room for; no call with smaller sizes, of whatever window, has more.
 int64_t most_part_rows(const fr_attend_kv8_desc& d)
 {
-    const int64_t rows = rows_a_seq(d), kind_rows = rows > kMostFew ? rows_of(kWideRows) : rows_of(kFewRows);
+    const int64_t rows = rows_a_seq(d), kind_rows = rows > kMostFew ? rows_of(kWideRows) : rows_of(kFewRows), most = most_items(rows > kMostFew ? kWideRows : kFewRows, 1, kUnits);
     const int64_t base = (int64_t)d.n_seqs * d.cache.n_kv_heads * row_tiles_of(rows), parts = up(d.max_len, 128);
-    return parts < 2 ? 0 : std::min(base * parts, kMostItems) * kind_rows;
+    return parts < 2 ? 0 : std::min(base * parts, most) * kind_rows;
 }
 uint64_t part_bytes(const fr_attend_kv8_desc& d) { return (uint64_t)most_part_rows(d) * (d.cache.head_dim * 4 + 8); }
 
@@ -720,12 +749,15 @@ template <typename T, int D, Kind kKind> int launch(Attend8Args a, const Plan& p
     a.units = (int)(up(a.groups, kXcds) * a.row_tiles);
     for (a.first_unit = 0; a.first_unit < a.units; a.first_unit += kBlocksALaunch / kXcds)
         hipLaunchKernelGGL((k_attend8<T, D, kKind>), dim3((unsigned)std::min(a.units - a.first_unit, kBlocksALaunch / kXcds) * kXcds), dim3(kThreads), 0, stream, a);
-    if (p.splits > 1) {
-        constexpr int kRowsHere = kThreads / (D / 8), kBlocks = rows_of(kKind) > kRowsHere ? rows_of(kKind) / kRowsHere : 1;
+    auto join = [&](auto lanes) {
+        constexpr int kRowsHere = kThreads / (D / 8) / lanes, kBlocks = (rows_of(kKind) + kRowsHere - 1) / kRowsHere;
         const int64_t all = p.base * kBlocks;
         for (int64_t first = 0; first < all; first += kBlocksALaunch)
-            hipLaunchKernelGGL((k_attend8_join<T, D, kKind>), dim3((unsigned)std::min<int64_t>(all - first, kBlocksALaunch)), dim3(kThreads), 0, stream, a, first);
-    }
+            hipLaunchKernelGGL((k_attend8_join<T, D, kKind, lanes>), dim3((unsigned)std::min<int64_t>(all - first, kBlocksALaunch)), dim3(kThreads), 0, stream, a, first);
+    };
+    if (p.splits > 32) join(std::integral_constant<int, 16>{});
+    else if (p.splits > 8) join(std::integral_constant<int, 4>{});
+    else if (p.splits > 1) join(std::integral_constant<int, 1>{});
     return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
 }
 
