@@ -36,6 +36,7 @@ struct Attend8Args {
     float q_power, rate;                   // scale * log2 e = q_power * rate: a power of two that goes into the queries, and the rest
     int32_t row_tiles, splits, split_len;  // row tiles of a sequence and key head; parts of its tiles of keys, and their length
     int32_t items, groups, units, first_unit;
+    int32_t workers;                       // of a key head, among which its tiles of keys are dealt out evenly
     float* part_o;                         // [(group's sequence and key head, part), row tile][rows_of][head_dim], relative to 2^m
     float2* part_ml;                       // the same: m in powers of 2, sum
 };
@@ -113,7 +114,7 @@ template <Kind kKind, int D> struct Lds8 {
 // The work of one workgroup (kWaveRows: of one wavefront): rows `row0` .. of `rows` against tiles u0 .. u1 of their keys.
 template <typename T, int D, Kind kKind>
 __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, int n_rows, int row0, const Keys<keys_of(kKind)>& keys, int u0, int u1,
-                                       const int32_t* pages, int64_t part, char* lds_array)
+                                       const int32_t* pages, bool whole, int64_t part, char* lds_array)
 {
     constexpr bool kWide = kKind == kWideRows, kAlone = kKind == kWaveRows;
     constexpr int kCols = columns(kKind), kTile = keys_of(kKind);
@@ -122,7 +123,9 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
     // (weights of bfloat16 are 2^-20, or 2^-12 where the maximum lags, so that sums of values as large as the type's largest stay in range; of
     // values near its smallest number, 2^-126, the sums still have steps of 2^-129)
     typedef Softmax<T, D, kCols, std::is_same_v<T, F16> ? 7 : -20> State;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                        // (what is made of it is made for every item, not kept from one to the next)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t lds = (uint32_t)reinterpret_cast<uintptr_t>((LdsBytes)lds_array);
     const float c = a.rate;
 
@@ -541,7 +544,6 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
     meet();
     // a thread takes eight elements of a row: two chunks, neighbours for a result of 16 bits, head_dim / 2 apart for a part (so that
     // neighbouring threads write neighbouring chunks)
-    const bool whole = a.splits == 1;
     constexpr int kPieces = D / 8, kOutRows = rows_of(kKind);
     for (int y = kAlone ? lane : tid; y < kOutRows * kPieces; y += kAlone ? 64 : kThreads) {
         const int r = y / kPieces, piece = y % kPieces, to = row0 + r;
@@ -606,7 +608,88 @@ __global__ __launch_bounds__(kThreads, kKind == kWideRows ? 2 : 4) void k_attend
     const int u0 = (int)min((int64_t)split * a.split_len, (int64_t)keys.tiles), u1 = (int)min((int64_t)u0 + a.split_len, (int64_t)keys.tiles);
     if (u0 >= u1 && split) return;                                     // (the first part is always there)
     const Rows rows{a, kv, s.token0, s.n0};
-    attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, ((int64_t)of * a.splits + split) * a.row_tiles + tile, lds);
+    attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, a.splits == 1, ((int64_t)of * a.splits + split) * a.row_tiles + tile, lds);
+}
+
+// How the tiles of a key head's items (a sequence, 16 of its rows) are dealt out among workers: all items one behind the other, `length` tiles each.
+// Where the items are about as long as that, by whole items: nothing has to be joined then.  An item's weight is its tiles, 1 if it has rows that see
+// nothing.  Every wavefront finds this out for itself, 64 items at a time.
+struct Share {
+    int32_t length, before, weight;        // tiles of a worker; tiles before an item, and its own
+    int32_t item;
+    bool by_items;
+    static __device__ __forceinline__ int weigh(const Attend8Args& a, int item)
+    {
+        const Sequence s(a, item / a.row_tiles);
+        const int n_rows = s.tokens * a.group, row0 = item % a.row_tiles * rows_of(kFewRows);
+        if (row0 >= n_rows) return 0;
+        return max(1, Keys<keys_of(kFewRows)>(a, s.n0, row0 / a.group, (min(n_rows, row0 + rows_of(kFewRows)) - 1) / a.group).tiles);
+    }
+    // of an item, or (item < 0) of the one in which worker ~item begins
+    __device__ __forceinline__ Share(const Attend8Args& a, int lane, int of)
+    {
+        const int items = a.n_seqs * a.row_tiles;
+        int all = 0, most = 0;
+        for (int i0 = 0; i0 < items; i0 += 64) {
+            const int w = i0 + lane < items ? weigh(a, i0 + lane) : 0;
+            int sum = w, top = w;
+#pragma unroll
+            for (int e = 1; e < 64; e *= 2) sum += __shfl_xor(sum, e), top = max(top, __shfl_xor(top, e));
+            all += sum;
+            most = max(most, top);
+        }
+        length = max((all + a.workers - 1) / a.workers, 8);
+        by_items = (int64_t)most * ((items + a.workers - 1) / a.workers) * 8 <= (int64_t)length * 9;
+        item = items, before = all, weight = 0;
+        const int64_t from = of < 0 ? (int64_t)~of * length : 0;
+        int at = 0;
+        for (int i0 = 0; i0 < items; i0 += 64) {
+            const int w = i0 + lane < items ? weigh(a, i0 + lane) : 0;
+            int sum = w;
+#pragma unroll
+            for (int e = 1; e < 64; e *= 2) {
+                const int y = __shfl_up(sum, e);
+                if (lane >= e) sum += y;
+            }
+            const uint64_t found = __ballot(of < 0 ? at + sum > from : i0 + lane == of);
+            if (found) {
+                const int l = __ffsll((unsigned long long)found) - 1;
+                weight = __shfl(w, l);
+                before = at + __shfl(sum, l) - weight;
+                item = i0 + l;
+                return;
+            }
+            at += __shfl(sum, 63);
+        }
+    }
+};
+
+// A worker goes through its tiles, item by item: results of whole items go where they belong, of others they are parts, at most two a worker.
+template <typename T, int D> __global__ __launch_bounds__(kThreads, 4) void k_attend8_dealt(Attend8Args a)
+{
+    constexpr int kRows = rows_of(kFewRows);
+    __shared__ __align__(1024) char lds[Lds8<kFewRows, D>::kTiles + Lds8<kFewRows, D>::kTable];
+    const int kv = blockIdx.x % a.c.n_kv_heads, worker = blockIdx.x / a.c.n_kv_heads, items = a.n_seqs * a.row_tiles;
+    const Share share(a, threadIdx.x & 63, ~worker);
+    const bool by_items = __builtin_amdgcn_readfirstlane(share.by_items);
+    int item = __builtin_amdgcn_readfirstlane(by_items ? worker : share.item);
+    int u0 = __builtin_amdgcn_readfirstlane(by_items ? 0 : worker * share.length - share.before);
+    int left = __builtin_amdgcn_readfirstlane(by_items ? 0x7fffffff : share.length);
+    for (bool first = true; item < items && left > 0; first = false) {
+        const int tile = item % a.row_tiles, b = item / a.row_tiles;
+        const Sequence s(a, b);
+        const int n_rows = s.tokens * a.group, row0 = tile * kRows;
+        if (row0 < n_rows) {
+            const Keys<keys_of(kFewRows)> keys(a, s.n0, row0 / a.group, (min(n_rows, row0 + kRows) - 1) / a.group);
+            const int u1 = min(keys.tiles, u0 + min(left, keys.tiles));
+            if (!first) __syncthreads();                   // (the results before are out of LDS)
+            attend<T, D, kFewRows>(a, Rows{a, kv, s.token0, s.n0}, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, u0 == 0 && u1 == keys.tiles,
+                                   ((int64_t)kv * a.workers + worker) * 2 + !first, lds);
+            if (!by_items) left -= max(u1 - u0, 1);
+        }
+        item += by_items ? a.workers : 1;
+        u0 = 0;
+    }
 }
 
 // Joins the parts of a row: twice four elements a thread, kLanes threads for every eight, each with every kLanes-th part, eight of them in one
@@ -620,11 +703,22 @@ __global__ __launch_bounds__(kThreads) void k_attend8_join(Attend8Args a, int64_
     const int r = (int)(id % kBlocks) * kRowsHere + threadIdx.x / kPieces / kLanes, mine = threadIdx.x / kPieces % kLanes, piece = threadIdx.x % kPieces;
     const Sequence s(a, b);
     const int n_rows = s.tokens * a.group, row0 = tile * kRows;
-    const bool there = r < kRows && row0 + r < n_rows;
+    bool there = r < kRows && row0 + r < n_rows;
     const Keys<keys_of(kKind)> keys(a, s.n0, row0 / a.group, max(0, min(n_rows, row0 + kRows) - 1) / a.group);
-    const int parts = there ? max(1, (keys.tiles + a.split_len - 1) / a.split_len) : 0;
+    int parts = there ? max(1, (keys.tiles + a.split_len - 1) / a.split_len) : 0;
     constexpr int kAtOnce = 8;
-    const int64_t step = (int64_t)a.row_tiles * kRows, at0 = ((int64_t)of * a.splits * a.row_tiles + tile) * kRows + r;
+    int64_t step = (int64_t)a.row_tiles * kRows, at0 = ((int64_t)of * a.splits * a.row_tiles + tile) * kRows + r, at_first = 0;
+    if constexpr (kKind == kFewRows) {
+        if (a.workers) {
+            const Share share(a, threadIdx.x & 63, b * a.row_tiles + tile);
+            const int w0 = share.before / share.length, w1 = (share.before + max(share.weight, 1) - 1) / share.length;
+            if (share.by_items || w0 == w1) there = false;     // (nothing to join)
+            parts = there ? w1 - w0 + 1 : 0;
+            step = 2 * kRows;
+            at0 = ((int64_t)kv * a.workers + w0) * 2 * kRows + r;
+            at_first = share.before % share.length ? kRows : 0;        // the first part's, if it is not the first of its worker
+        }
+    }
     float top = -INFINITY, base, sum = 0.0f, o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = 0.0f;
@@ -633,7 +727,8 @@ __global__ __launch_bounds__(kThreads) void k_attend8_join(Attend8Args a, int64_
         float4 lo[kAtOnce], hi[kAtOnce];
 #pragma unroll
         for (int x = 0; x < kAtOnce; ++x) {
-            const int64_t at = at0 + min(y0 + x * kLanes, parts - 1) * step;
+            const int y = min(y0 + x * kLanes, parts - 1);
+            const int64_t at = at0 + y * step + (y ? 0 : at_first);
             const float4* p = reinterpret_cast<const float4*>(a.part_o + at * D) + piece;
             ml[x] = a.part_ml[at];
             lo[x] = p[0];
@@ -701,8 +796,10 @@ int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 struct Plan {
     Kind kind = kFewRows;
     int64_t row_tiles = 1, base = 0, splits = 1, split_len = 1;        // base: sequences x key heads x row tiles
+    int64_t workers = 0;                   // of a key head; 0: every item has the same number of parts
 };
 constexpr int64_t kMostFew = 32;           // rows of a sequence that are few
+constexpr int64_t kMostDealt = 512;        // items of a key head that are dealt out evenly: each worker looks at all of them
 constexpr int64_t kMostParts = 128;        // of a row: what the join reads in one go
 constexpr int64_t kMostBlocks = 0x7fffffff;
 
@@ -717,6 +814,7 @@ int64_t row_tiles_of(int64_t rows) { return rows > kMostFew ? up(rows, rows_of(k
 Plan plan(const fr_attend_kv8_desc& d, int cus)
 {
     Plan p;
+    cus = std::min(cus, kUnits);
     const int64_t rows = rows_a_seq(d), group = d.n_q_heads / d.cache.n_kv_heads;
     p.kind = rows > kMostFew ? kWideRows : kFewRows;
     p.row_tiles = row_tiles_of(rows);
@@ -726,9 +824,15 @@ Plan plan(const fr_attend_kv8_desc& d, int cus)
     int64_t keys = d.max_len;
     if (d.window) keys = std::min<int64_t>(keys, (int64_t)d.window + std::min<int64_t>(up(rows_of(p.kind), group), d.max_q) + d.sinks + 3 * tile);
     const int64_t tiles = std::max<int64_t>(up(keys, tile), 1), least = p.kind == kWideRows ? 2 : 8;
-    const int64_t want = std::max<int64_t>(1, std::min({up(tiles, least), most_items(p.kind, p.base, std::min(cus, kUnits)) / p.base, kMostParts}));
+    const int64_t want = std::max<int64_t>(1, std::min({up(tiles, least), most_items(p.kind, p.base, cus) / p.base, kMostParts}));
     p.split_len = up(tiles, want);
     p.splits = up(tiles, p.split_len);
+    // Some long sequences: tiles dealt out evenly.  Against parts of one length, 8 key heads, lengths up to these: 4 sequences of 65536 88 -> 78 us, 8
+    // 164 -> 151, 16 of 32768 134 -> 126, of equal lengths 206 -> 204; with more items the units even themselves out better (32 of 8000 equal ones
+    // 103, dealt out 114), with fewer there are enough parts (2 of 65536 57 and 60).
+    if (p.kind == kFewRows && d.n_seqs > 1 && d.n_seqs * p.row_tiles <= kMostDealt && 8 * p.base >= cus && 2 * p.base <= cus && p.base * tiles >= 128 * (int64_t)cus &&
+        d.n_seqs * p.row_tiles * tiles < 1 << 30)
+        p.workers = 4 * cus / d.cache.n_kv_heads;
     return p;
 }
 
@@ -747,7 +851,10 @@ template <typename T, int D, Kind kKind> int launch(Attend8Args a, const Plan& p
     a.items = (int)((int64_t)a.n_seqs * a.c.n_kv_heads * p.splits);
     a.groups = kKind == kWaveRows ? (a.items + kWaves - 1) / kWaves : a.items;
     a.units = (int)(up(a.groups, kXcds) * a.row_tiles);
-    for (a.first_unit = 0; a.first_unit < a.units; a.first_unit += kBlocksALaunch / kXcds)
+    if (p.workers) {
+        if constexpr (kKind == kFewRows)
+            hipLaunchKernelGGL((k_attend8_dealt<T, D>), dim3((unsigned)(p.workers * a.c.n_kv_heads)), dim3(kThreads), 0, stream, a);
+    } else for (a.first_unit = 0; a.first_unit < a.units; a.first_unit += kBlocksALaunch / kXcds)
         hipLaunchKernelGGL((k_attend8<T, D, kKind>), dim3((unsigned)std::min(a.units - a.first_unit, kBlocksALaunch / kXcds) * kXcds), dim3(kThreads), 0, stream, a);
     auto join = [&](auto lanes) {
         constexpr int kRowsHere = kThreads / (D / 8) / lanes, kBlocks = (rows_of(kKind) + kRowsHere - 1) / kRowsHere;
@@ -755,8 +862,8 @@ template <typename T, int D, Kind kKind> int launch(Attend8Args a, const Plan& p
         for (int64_t first = 0; first < all; first += kBlocksALaunch)
             hipLaunchKernelGGL((k_attend8_join<T, D, kKind, lanes>), dim3((unsigned)std::min<int64_t>(all - first, kBlocksALaunch)), dim3(kThreads), 0, stream, a, first);
     };
-    if (p.splits > 32) join(std::integral_constant<int, 16>{});
-    else if (p.splits > 8) join(std::integral_constant<int, 4>{});
+    if (p.workers || (p.splits > 8 && p.splits <= 32)) join(std::integral_constant<int, 4>{});
+    else if (p.splits > 32) join(std::integral_constant<int, 16>{});
     else if (p.splits > 1) join(std::integral_constant<int, 1>{});
     return hipGetLastError() == hipSuccess ? FR_OK : FR_ERR_HIP;
 }
@@ -796,7 +903,8 @@ int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream)
     if (p.base > kMostBlocks / 16) return FR_ERR_ARG;
     const uint64_t need = part_bytes(*d);
     if (need && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < need)) return FR_ERR_ARG;
-    if (p.splits > 1 && p.base * p.splits * rows_of(p.kind) > most_part_rows(*d)) return FR_ERR_STATE;      // (never)
+    const int64_t part_rows = p.workers ? p.workers * c.n_kv_heads * 2 * rows_of(p.kind) : p.splits > 1 ? p.base * p.splits * rows_of(p.kind) : 0;
+    if (part_rows > most_part_rows(*d)) return FR_ERR_STATE;      // (never)
     Attend8Args a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->pages, d->lens,
                      d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->max_len, d->window, d->sinks,
                      __builtin_ctz(c.page_size), __builtin_ctz(c.block), d->n_q_heads / c.n_kv_heads};
@@ -809,7 +917,8 @@ int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream)
     a.splits = (int)p.splits;
     a.split_len = (int)std::min<int64_t>(p.split_len, 0x7fffffff);
     a.part_o = (float*)d->workspace;
-    a.part_ml = (float2*)((char*)d->workspace + (uint64_t)p.base * p.splits * rows_of(p.kind) * c.head_dim * 4);
+    a.part_ml = (float2*)((char*)d->workspace + (uint64_t)part_rows * c.head_dim * 4);
+    a.workers = (int)p.workers;
     hipStream_t s = (hipStream_t)stream;
     if (c.dtype == FR_DTYPE_BF16) return c.head_dim == 64 ? launch<Bf16, 64>(a, p, s) : launch<Bf16, 128>(a, p, s);
     return c.head_dim == 64 ? launch<F16, 64>(a, p, s) : launch<F16, 128>(a, p, s);

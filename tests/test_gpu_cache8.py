@@ -219,7 +219,8 @@ def _attend_case(dt, Hq, Hk, D, page, block, lens, new, seed, window=0, sinks=0,
     order = rng.permutation(pages)
     table = np.full((n, width), 1 << 30, dtype=np.int32)               # ids of pages that are not seen lead nowhere
     used = np.zeros((pages, page), dtype=bool)
-    ck, cv = (cache8.encode(rng.normal(0, 100, (pages, Hk, page, D))) for _ in range(2))
+    draws = cache8.encode(rng.normal(0, 100, 1 << 16))
+    ck, cv = (draws[rng.integers(0, 1 << 16, (pages, Hk, page, D), dtype=np.uint16)] for _ in range(2))
     sk, sv = (rng.integers(scales[0], scales[1] + 1, (pages, Hk, page // block)).astype(np.uint8) for _ in range(2))
     at = 0
     place = []
@@ -255,9 +256,19 @@ def _attend_case(dt, Hq, Hk, D, page, block, lens, new, seed, window=0, sinks=0,
     fr.fr_attend_kv8(cache, q, out, torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=I32, device="cuda"), scale,
                      q_begin=torch.from_numpy(begin).cuda() if q_begin else None, lse=lse, workspace=ws, stream=stream or torch.cuda.current_stream(), **lim)
     torch.cuda.synchronize()
-    K, V = cache8.numbers(ck, sk, block, dt), cache8.numbers(cv, sv, block, dt)
-    _check_attend(dt, q, K, V, place, page, lens, begin, window, sinks, scale, out, lse, rows)
+    _check_attend(dt, q, Numbers(ck, sk, block, dt), Numbers(cv, sv, block, dt), place, page, lens, begin, window, sinks, scale, out, lse, rows)
     return out, lse
+
+
+class Numbers:
+    """What codes and scales stand for, made where they are asked for: [pages, a head, slots]."""
+
+    def __init__(self, codes, scale, block, dt):
+        self.codes, self.scale, self.block, self.dt, self.shape = codes, scale, block, dt, codes.shape
+
+    def __getitem__(self, at):
+        p, h, o = at
+        return cache8.VALUES[self.codes[p, h, o]] * cache8.scale_of(self.scale[p, h, o // self.block], self.dt)[:, None]
 
 
 def _check_attend(dt, q, K, V, place, page, lens, begin, window, sinks, scale, out, lse, rows=None):
@@ -348,6 +359,46 @@ def test_attend_many_short_sequences(dt, D, window, new):
     lens = [int(x) for x in rng.integers(0, 40, 66)] + [0, 1, 31, 32, 33, 255, 256, 257, 600]
     t = [min(x, int(rng.integers(1, new + 1))) if new > 1 else 1 for x in lens]
     _attend_case(dt, 16, 8, D, 16, 8, lens, t, window + D, window, 2)
+
+
+def _ragged(kind, seqs, most, rng):
+    if kind == "any":
+        return [int(x) for x in rng.integers(0, most, seqs - 3)] + [0, 1, most]
+    if kind == "equal":
+        return [most - int(x) for x in rng.integers(0, 40, seqs)]
+    if kind == "one":
+        return [0, 3] * (seqs // 2 - 1) + [most, 17]
+    return [32 * int(x) for x in rng.integers(0, most // 32, seqs - 1)] + [most]          # whole tiles: items that end where a worker's share does
+
+
+@pytest.mark.parametrize("dt,D", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("kind,seqs,most,Hq,Hk,new,window", [
+    ("any", 16, 8400, 8, 8, 1, 0), ("equal", 16, 8300, 8, 8, 1, 0), ("whole", 16, 8320, 16, 8, 1, 0), ("one", 10, 17000, 20, 5, 1, 0), ("any", 8, 17000, 16, 4, 6, 0),
+    ("any", 16, 20000, 8, 8, 1, 9000), ("any", 70, 2100, 12, 4, 7, 0)])
+def test_attend_lengths_that_are_dealt_out_evenly(dt, D, kind, seqs, most, Hq, Hk, new, window):
+    # many keys in sequences that differ: workers go through several items, and items through several workers
+    print("attend dealt", dt, D, kind, seqs, most, Hq, Hk, new, window, flush=True)
+    rng = np.random.default_rng(seqs + most)
+    lens = _ragged(kind, seqs, most, rng)
+    t = [min(n, int(rng.integers(0, new + 1))) if new > 1 else 1 for n in lens]
+    _attend_case(dt, Hq, Hk, D, 16, 8, lens, t, most, window, 5 if window else 0, rows=160)
+
+
+def test_attend_lengths_dealt_out_among_few_units():
+    ctx = fr.Context(device_id=0, cu_count=16)
+    rng = np.random.default_rng(1)
+    for kind, seqs, most, Hq, Hk, new in (("any", 4, 8300, 4, 2, 1), ("any", 3, 17000, 16, 2, 3), ("whole", 4, 8320, 2, 2, 1), ("one", 8, 8300, 3, 1, 1), ("equal", 4, 9000, 2, 2, 1)):
+        lens = _ragged(kind, seqs, most, rng)
+        t = [min(n, int(rng.integers(0, new + 1))) if new > 1 else 1 for n in lens]
+        _attend_case("bf16", Hq, Hk, 64, 16, 16, lens, t, most, stream=ctx.fr_side_stream(), rows=100)
+        _attend_case("f16", Hq, Hk, 128, 32, 1, lens, t, most, 8250, 40, stream=ctx.fr_side_stream(), rows=100, nan_at=[(len(lens) - 1, lens[-1] - 1, 3, True)])
+    for kind, seqs, most, Hq, Hk, new in (("any", 11, 700, 8, 4, 1), ("any", 40, 300, 6, 3, 5), ("one", 30, 2000, 2, 2, 1)):
+        lens = _ragged(kind, seqs, most, rng)
+        t = [min(n, int(rng.integers(0, new + 1))) if new > 1 else 1 for n in lens]
+        _attend_case("bf16", Hq, Hk, 64, 16, 16, lens, t, most, stream=ctx.fr_side_stream(), rows=400)
+        _attend_case("f16", Hq, Hk, 128, 32, 1, lens, t, most, 250, 40, stream=ctx.fr_side_stream(), rows=400)
+        _attend_case("bf16", Hq, Hk, 128, 16, 16, lens, t, most, stream=ctx.fr_side_stream(), rows=400, nan_at=[(len(lens) - 1, 2, 3, True)])
+    ctx.fr_destroy()
 
 
 @pytest.mark.parametrize("layout", ["slots", "joined"])
