@@ -7,6 +7,13 @@
 // product with the values, and the result is, once.  Codes times their block's power of two are numbers of that type, exactly.
 //
 // The heads that share a key head, and all tokens of a sequence, are rows of one matrix product with its keys.
+// What bounds it:
+//   Decoding from long caches, the reading: 128 sequences of 4096 keys each with 8 key heads, 1.07 GB, 190 us, 5.6 TB/s (the same loads without a
+//     product 5.9; a kernel that only reads one array from end to end 6.5).  Where lengths differ, units that have nothing left: 8 of 20000 to 65536
+//     131 us, 4.9 TB/s, 64 of up to 4000 75 us, 3.6.
+//   Prompts, the vector units beside the matrix cores (2 exps and 5 other operations of every two weights, and half a conversion of a code):
+//     8 sequences of 2048 tokens behind 6144, 32 heads, 1.92 TFLOP in 2.0 ms, 0.96 PFLOP/s.
+//   A few short sequences, the launch: 6 us.
 
 #include <algorithm>
 #include <cmath>
@@ -18,9 +25,8 @@
 namespace {
 
 // What a workgroup's four wavefronts do.  kFewRows: 16 rows, and every wavefront takes every fourth tile of 32 keys for itself, the four
-// results being joined at the end.  kWaveRows: every wavefront has an item of its own, 16 rows and all of its keys.  kWideRows: 128
-// rows, 32 a wavefront, which share tiles of 64 keys.
-enum Kind { kFewRows, kWaveRows, kWideRows };
+// results being joined at the end.  kWideRows: 128 rows, 32 a wavefront, which share tiles of 64 keys.
+enum Kind { kFewRows, kWideRows };
 constexpr int columns(Kind k) { return k == kWideRows ? 32 : 16; }                     // rows of a wavefront: columns of its MFMA blocks
 constexpr int rows_of(Kind k) { return k == kWideRows ? kWaves * 32 : 16; }            // rows of an item
 constexpr int keys_of(Kind k) { return k == kWideRows ? 64 : 32; }                     // keys of a tile
@@ -35,7 +41,7 @@ struct Attend8Args {
     int32_t n_tokens, n_seqs, n_q_heads, max_q, max_len, window, sinks, page_shift, block_shift, group;
     float q_power, rate;                   // scale * log2 e = q_power * rate: a power of two that goes into the queries, and the rest
     int32_t row_tiles, splits, split_len;  // row tiles of a sequence and key head; parts of its tiles of keys, and their length
-    int32_t items, groups, units, first_unit;
+    int32_t groups, units, first_unit;
     int32_t workers;                       // of a key head, among which its tiles of keys are dealt out evenly
     float* part_o;                         // [(group's sequence and key head, part), row tile][rows_of][head_dim], relative to 2^m
     float2* part_ml;                       // the same: m in powers of 2, sum
@@ -111,12 +117,21 @@ template <Kind kKind, int D> struct Lds8 {
     static constexpr uint32_t kTable = kWaves * 2048;                                       // a wavefront: two sets of 64 offsets, two of 64 pairs of powers
 };
 
-// The work of one workgroup (kWaveRows: of one wavefront): rows `row0` .. of `rows` against tiles u0 .. u1 of their keys.
+// The work of one workgroup: rows `row0` .. of `rows` against tiles u0 .. u1 of their keys.
+//
+// kFewRows: 16 rows, blocks of 16 x 16 x 32.  Codes come to registers, a tile ahead, 8 KB a wavefront at head_dim 128; with what a lane's
+// places are made anew where they are used, its registers leave room for four workgroups a unit (166 -> 120; 128 sequences of 4096 keys, 64 heads,
+// 207 -> 185 us).  A lane's 16 bytes of a key are two fragments; values are made into numbers on the way into LDS, where they are transposed.
+//
+// kWideRows: a wavefront's 32 rows are the columns of 32 x 32 x 16 blocks; weights go from the one product to the next without passing
+// through LDS.  A wavefront makes a quarter of every tile's codes into numbers, which all four then read: 32 conversions beside 32 MFMAs.
+// 8 ragged sequences of up to 2048 tokens: scores, weights and values of a tile one after another 776 us, the next tile's scores beside this one's weights
+// 744; with places in LDS worked out for every piece 820, conversions where the codes come instead of between the MFMAs 756.
 template <typename T, int D, Kind kKind>
 __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, int n_rows, int row0, const Keys<keys_of(kKind)>& keys, int u0, int u1,
                                        const int32_t* pages, bool whole, int64_t part, char* lds_array)
 {
-    constexpr bool kWide = kKind == kWideRows, kAlone = kKind == kWaveRows;
+    constexpr bool kWide = kKind == kWideRows;
     constexpr int kCols = columns(kKind), kTile = keys_of(kKind);
     constexpr int kSharers = kKind == kFewRows ? kWaves : 1;
     typedef Lds<D, kCols> L;
@@ -471,10 +486,6 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
             }
         }
     };
-    auto meet = [] {
-        if constexpr (!kAlone) __syncthreads();
-        else wait_lds();
-    };
     // A weight of 0 for a key that a row does not see, times NaN, is NaN: where rows see different keys and one of the results is NaN, the pass
     // is made again without the values' NaN, and then it is given to the rows that see it.
     for (;;) {
@@ -520,14 +531,14 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
     // results through LDS, so that rows are written whole: a wavefront's rows of D floats, 16-byte chunk c of row r at c ^ r
     constexpr uint32_t kFloatRow = D * 4, kFloatChunks = D / 4, kRegion = kCols * kFloatRow;
     static_assert(kWaves * kRegion <= Lds8<kKind, D>::kTiles, "");
-    meet();                                              // tiles are done with
+    __syncthreads();                                              // tiles are done with
     const uint32_t region = lds + wave * kRegion, mls = lds + Lds8<kKind, D>::kTiles;
-    auto ml = [&](int wv, int r) { return reinterpret_cast<LdsPair>(lds_at(mls + wv * (kAlone ? 2048 : kCols * 8) + r * 8)); };
+    auto ml = [&](int wv, int r) { return reinterpret_cast<LdsPair>(lds_at(mls + (wv * kCols + r) * 8)); };
     const float m2 = x.reference(c);                     // (-infinity stays: c is positive)
     float mine_of = 1.0f;
     if (lane < kCols) *ml(wave, lane) = f32x2{m2, x.l};
     if constexpr (kKind == kFewRows) {
-        meet();
+        __syncthreads();
         float top = -INFINITY;
 #pragma unroll
         for (int y = 0; y < kWaves; ++y) top = fmaxf(top, (*ml(y, lane % kCols))[0]);
@@ -541,11 +552,11 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
             *reinterpret_cast<LdsFloats>(lds_at(region + r * kFloatRow + (chunk ^ (r & (kFloatChunks - 1))) * 16)) =
                 f32x4{x.o[d][i] * mine_of, x.o[d][i + 1] * mine_of, x.o[d][i + 2] * mine_of, x.o[d][i + 3] * mine_of};
         }
-    meet();
+    __syncthreads();
     // a thread takes eight elements of a row: two chunks, neighbours for a result of 16 bits, head_dim / 2 apart for a part (so that
     // neighbouring threads write neighbouring chunks)
     constexpr int kPieces = D / 8, kOutRows = rows_of(kKind);
-    for (int y = kAlone ? lane : tid; y < kOutRows * kPieces; y += kAlone ? 64 : kThreads) {
+    for (int y = tid; y < kOutRows * kPieces; y += kThreads) {
         const int r = y / kPieces, piece = y % kPieces, to = row0 + r;
         if (to >= n_rows) break;
         f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
@@ -555,7 +566,7 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
             return *reinterpret_cast<LdsFloats>(lds_at(lds + wv * kRegion + in * kFloatRow + ((uint32_t)(whole ? 2 * piece + e : piece + e * kPieces) ^ (in & (kFloatChunks - 1))) * 16));
         };
         if constexpr (kKind != kFewRows) {
-            const int wv = kAlone ? wave : r / kCols;
+            const int wv = r / kCols;
             lo = chunk(wv, 0), hi = chunk(wv, 1);
             top = (*ml(wv, in))[0], sum = (*ml(wv, in))[1];
         } else {
@@ -584,6 +595,18 @@ __device__ __forceinline__ void attend(const Attend8Args& a, const Rows& rows, i
     }
 }
 
+// The sequence that comes at a place in the order of falling lengths (64 sequences at most; equal ones in their own order).
+__device__ __forceinline__ int by_length(const Attend8Args& a, int place, int lane)
+{
+    const int len = lane < a.n_seqs && a.max_len ? within(a.lens[lane], 0, a.max_len) : -1;
+    int longer = 0;
+    for (int e = 0; e < a.n_seqs; ++e) {
+        const int y = __builtin_amdgcn_readlane(len, e);
+        longer += y > len || (y == len && e < lane);
+    }
+    return __ffsll((unsigned long long)__ballot(lane < a.n_seqs && longer == place)) - 1;
+}
+
 // Workgroups are dealt round-robin over the XCDs.  Those that read the same keys (the row tiles of a group: one sequence, one key head, one
 // run of keys) follow one another on one XCD, through its L2; groups go round the XCDs, the first parts of all sequences before the second
 // ones, so that every XCD has the same mixture of sequences and of parts that short ones do not have.
@@ -594,13 +617,12 @@ __global__ __launch_bounds__(kThreads, kKind == kWideRows ? 2 : 4) void k_attend
     __shared__ __align__(1024) char lds[Lds8<kKind, D>::kTiles + Lds8<kKind, D>::kTable];
     const int unit = a.first_unit + blockIdx.x / kXcds, xcd = blockIdx.x % kXcds;
     const int tile = a.row_tiles - 1 - unit % a.row_tiles;             // (the last rows, which see the most keys, first)
-    int group = unit / a.row_tiles * kXcds + xcd;
+    const int group = unit / a.row_tiles * kXcds + xcd;
     if (group >= a.groups) return;
-    if constexpr (kKind == kWaveRows) {                                // (four items a workgroup)
-        group = group * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (group >= a.items) return;
-    }
-    const int whole = a.n_seqs * a.c.n_kv_heads, split = group / whole, of = group % whole, kv = of % a.c.n_kv_heads, b = of / a.c.n_kv_heads;
+    const int whole = a.n_seqs * a.c.n_kv_heads, split = group / whole, of = group % whole, kv = of % a.c.n_kv_heads;
+    int b = of / a.c.n_kv_heads;
+    // Many rows: the longest sequences first, so that what runs last is short.
+    if (kKind == kWideRows && a.n_seqs > 1 && a.n_seqs <= 64) b = by_length(a, b, threadIdx.x & 63);
     const Sequence s(a, b);
     const int n_rows = s.tokens * a.group, row0 = tile * kRows;
     if (row0 >= n_rows) return;
@@ -608,7 +630,7 @@ __global__ __launch_bounds__(kThreads, kKind == kWideRows ? 2 : 4) void k_attend
     const int u0 = (int)min((int64_t)split * a.split_len, (int64_t)keys.tiles), u1 = (int)min((int64_t)u0 + a.split_len, (int64_t)keys.tiles);
     if (u0 >= u1 && split) return;                                     // (the first part is always there)
     const Rows rows{a, kv, s.token0, s.n0};
-    attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, a.splits == 1, ((int64_t)of * a.splits + split) * a.row_tiles + tile, lds);
+    attend<T, D, kKind>(a, rows, n_rows, row0, keys, u0, u1, a.pages + b * a.pages_stride, a.splits == 1, (((int64_t)b * a.c.n_kv_heads + kv) * a.splits + split) * a.row_tiles + tile, lds);
 }
 
 // How the tiles of a key head's items (a sequence, 16 of its rows) are dealt out among workers: all items one behind the other, `length` tiles each.
@@ -848,8 +870,7 @@ uint64_t part_bytes(const fr_attend_kv8_desc& d) { return (uint64_t)most_part_ro
 template <typename T, int D, Kind kKind> int launch(Attend8Args a, const Plan& p, hipStream_t stream)
 {
     constexpr int kBlocksALaunch = kMostThreads / kThreads;
-    a.items = (int)((int64_t)a.n_seqs * a.c.n_kv_heads * p.splits);
-    a.groups = kKind == kWaveRows ? (a.items + kWaves - 1) / kWaves : a.items;
+    a.groups = (int)((int64_t)a.n_seqs * a.c.n_kv_heads * p.splits);
     a.units = (int)(up(a.groups, kXcds) * a.row_tiles);
     if (p.workers) {
         if constexpr (kKind == kFewRows)
@@ -870,7 +891,7 @@ template <typename T, int D, Kind kKind> int launch(Attend8Args a, const Plan& p
 
 template <typename T, int D> int launch(const Attend8Args& a, const Plan& p, hipStream_t stream)
 {
-    return p.kind == kWideRows ? launch<T, D, kWideRows>(a, p, stream) : p.kind == kWaveRows ? launch<T, D, kWaveRows>(a, p, stream) : launch<T, D, kFewRows>(a, p, stream);
+    return p.kind == kWideRows ? launch<T, D, kWideRows>(a, p, stream) : launch<T, D, kFewRows>(a, p, stream);
 }
 
 }  // namespace
