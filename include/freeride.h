@@ -817,7 +817,7 @@ typedef struct fr_kv_copy_desc {
     const int32_t* source;         /* device, [n_pairs]                                                       */
     const int32_t* target;
     int32_t*    copied;            /* device, [n_pairs]: 1 or 0; or NULL                                      */
-    int32_t     n_pairs;           /* 0: nothing to do; up to 2^20                                            */
+    int32_t     n_pairs;           /* 0: nothing to do; up to 2^16 (each looks at all others)                 */
     int32_t     reserved;
 } fr_kv_copy_desc;
 int fr_kv_copy_pages(const fr_kv_copy_desc* d, void* stream);

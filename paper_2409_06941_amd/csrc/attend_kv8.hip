@@ -925,7 +925,7 @@ int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream)
     const uint64_t need = part_bytes(*d);
     if (need && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < need)) return FR_ERR_ARG;
     const int64_t part_rows = p.workers ? p.workers * c.n_kv_heads * 2 * rows_of(p.kind) : p.splits > 1 ? p.base * p.splits * rows_of(p.kind) : 0;
-    if (part_rows > most_part_rows(*d)) return FR_ERR_STATE;      // (never)
+    if (part_rows > most_part_rows(*d)) return FR_ERR_ARG;        // (the plan keeps to it)
     Attend8Args a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->pages, d->lens,
                      d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->max_len, d->window, d->sinks,
                      __builtin_ctz(c.page_size), __builtin_ctz(c.block), d->n_q_heads / c.n_kv_heads};

@@ -24,7 +24,7 @@ struct CopyArgs {
     int64_t n_pages;
     const int32_t *source, *target;
     int32_t* copied;
-    int32_t n_pairs, n_caches;
+    int32_t n_pairs, n_caches, share;      // share: caches of a workgroup
     char* k[kCachesALaunch];
     char* v[kCachesALaunch];
     char* ks[kCachesALaunch];
@@ -51,10 +51,10 @@ __device__ __forceinline__ void copy_array(char* base, const Shape& s, int64_t f
     else copy_rows<uint8_t>(base, s, from, to);
 }
 
-// Two workgroups per pair and cache, for K and for V.  Whether the pair is carried out is found by a look at all others.
+// Two workgroups per pair and share of the caches, for K and for V.  Whether the pair is carried out is found by a look at all others.
 __global__ __launch_bounds__(kThreads) void k_copy_pages(CopyArgs a)
 {
-    const int i = blockIdx.x % a.n_pairs, of = blockIdx.x / a.n_pairs, c = of >> 1;
+    const int i = blockIdx.x % a.n_pairs, of = blockIdx.x / a.n_pairs;
     const bool value = of & 1;
     const int32_t from = a.source[i], to = a.target[i];
     bool out = from < 0 || to < 0 || from >= a.n_pages || to >= a.n_pages || from == to;
@@ -71,8 +71,10 @@ __global__ __launch_bounds__(kThreads) void k_copy_pages(CopyArgs a)
     }
     if (a.copied && of == 0 && threadIdx.x == 0) a.copied[i] = !out;
     if (out) return;
-    copy_array(value ? a.v[c] : a.k[c], a.codes, from, to);
-    if (a.scales.row) copy_array(value ? a.vs[c] : a.ks[c], a.scales, from, to);
+    for (int c = (of >> 1) * a.share, end = min(c + a.share, a.n_caches); c < end; ++c) {
+        copy_array(value ? a.v[c] : a.k[c], a.codes, from, to);
+        if (a.scales.row) copy_array(value ? a.vs[c] : a.ks[c], a.scales, from, to);
+    }
 }
 
 // Rows that lie side by side become one; the largest piece that all addresses are multiples of.
@@ -97,7 +99,7 @@ bool same(const Shape& a, const Shape& b)
 
 extern "C" int fr_kv_copy_pages(const fr_kv_copy_desc* d, void* stream)
 {
-    if (!d || d->n_caches < 0 || d->n_caches8 < 0 || d->n_caches > 4096 || d->n_caches8 > 4096 || d->n_pairs < 0 || d->n_pairs > 1 << 20) return FR_ERR_ARG;
+    if (!d || d->n_caches < 0 || d->n_caches8 < 0 || d->n_caches > 4096 || d->n_caches8 > 4096 || d->n_pairs < 0 || d->n_pairs > 1 << 16) return FR_ERR_ARG;
     if ((d->n_caches && !d->caches) || (d->n_caches8 && !d->caches8)) return FR_ERR_ARG;
     int64_t n_pages = 0;
     for (int i = 0; i < d->n_caches; ++i) {
@@ -113,13 +115,16 @@ extern "C" int fr_kv_copy_pages(const fr_kv_copy_desc* d, void* stream)
     CopyArgs a = {};
     a.n_pages = n_pages;
     a.source = d->source, a.target = d->target, a.copied = d->copied, a.n_pairs = d->n_pairs;
+    // one cache a workgroup, more where there are so many pairs that looking at them takes as long as copying a page
+    a.share = std::max(1, d->n_pairs / 1024);
     auto go = [&] {
-        const int at_once = (int)std::max<int64_t>(1, kMostThreads / kThreads / 2 / a.n_pairs);
-        for (int done = 0; done < a.n_caches; done += at_once) {
+        const int shares = (a.n_caches + a.share - 1) / a.share;          // (2^23 / 2 pairs a launch are at least 64 of the most that a call has)
+        for (int done = 0; done < shares; done += kMostThreads / kThreads / 2 / a.n_pairs) {
             CopyArgs x = a;
-            x.n_caches = std::min(at_once, a.n_caches - done);
-            for (int c = 0; c < x.n_caches; ++c) x.k[c] = a.k[done + c], x.v[c] = a.v[done + c], x.ks[c] = a.ks[done + c], x.vs[c] = a.vs[done + c];
-            hipLaunchKernelGGL(k_copy_pages, dim3((unsigned)x.n_caches * a.n_pairs * 2), dim3(kThreads), 0, (hipStream_t)stream, x);
+            const int first = done * a.share, n = (int)std::min<int64_t>(a.n_caches - first, kMostThreads / kThreads / 2 / a.n_pairs * a.share);
+            x.n_caches = n;
+            for (int c = 0; c < n; ++c) x.k[c] = a.k[first + c], x.v[c] = a.v[first + c], x.ks[c] = a.ks[first + c], x.vs[c] = a.vs[first + c];
+            hipLaunchKernelGGL(k_copy_pages, dim3((unsigned)((n + a.share - 1) / a.share) * a.n_pairs * 2), dim3(kThreads), 0, (hipStream_t)stream, x);
         }
         a.n_caches = 0;
         a.copied = nullptr;

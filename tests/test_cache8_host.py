@@ -142,7 +142,7 @@ def _copy(**change):
 
 
 @pytest.mark.parametrize("change", [dict(source=None), dict(target=None), dict(n_caches=-1), dict(n_caches8=-1), dict(n_caches=4097), dict(caches=None),
-                                    dict(caches8=None), dict(n_pairs=-1), dict(n_pairs=(1 << 20) + 1), dict(wide=dict(n_pages=11)), dict(narrow=dict(n_pages=9)),
+                                    dict(caches8=None), dict(n_pairs=-1), dict(n_pairs=(1 << 16) + 1), dict(wide=dict(n_pages=11)), dict(narrow=dict(n_pages=9)),
                                     dict(wide=dict(k=None)), dict(wide=dict(head_dim=96))] + [dict(narrow=p) for p in BAD_PAGES])
 def test_copy_refuses(change):
     assert _copy(**change) == fr.FR_ERR_ARG

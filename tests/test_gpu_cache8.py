@@ -586,6 +586,29 @@ def test_copy_many_pairs():
     rng = np.random.default_rng(5)
     source = rng.integers(-2, 25, 1500)
     _copy_case(ONE + [(8, 2, 16, 64, 8, "slots")], source.tolist(), rng.integers(-2, 25, 1500).tolist(), 10)
+    # so many that a workgroup has several caches: padding but for a few
+    for n in (2100, 5000):
+        source, target = np.full(n, -1), np.full(n, 3)
+        source[[5, n // 2, n - 1]], target[[5, n // 2, n - 1]] = [1, 2, 2], [7, 8, 9]
+        _copy_case([(8, 2, 16, 64, 8, "heads")] * 7 + [(16, 1, 4, 64, 1, "heads")] * 3, source.tolist(), target.tolist(), n)
+
+
+def test_attend_of_nothing_at_all_gives_zeros():
+    cache = fr.Kv8Pages(*(torch.zeros(1, 1, 1, 64, dtype=torch.uint8, device="cuda") for _ in range(2)), *(torch.zeros(1, 1, 1, dtype=torch.uint8, device="cuda") for _ in range(2)),
+                        torch.float16)
+    for t in (1, 40):
+        q = torch.ones(3 * t, 2, 64, dtype=torch.float16, device="cuda")
+        out, lse = torch.full_like(q, 3.0), torch.zeros(3 * t, 2, device="cuda")
+        fr.fr_attend_kv8(cache, q, out, None, None, 0.125, max_len=0, max_q=t, q_begin=torch.arange(0, 3 * t + 1, t, dtype=I32, device="cuda"), lse=lse)
+        torch.cuda.synchronize()
+        assert not bool(out.any()) and bool(torch.isneginf(lse).all())
+
+
+@pytest.mark.parametrize("Hq,t", [(1024, 1), (300, 2)])
+def test_attend_hundreds_of_heads_to_a_key_head(Hq, t):
+    # rows of one token are many: tiles of 128 rows that all see the same keys
+    _attend_case("bf16", Hq, 1, 64, 16, 4, [100, 0, 70], [t, 0, t], Hq, 30, 3, rows=300)
+    _attend_case("f16", Hq, 1, 128, 16, 16, [300], [t], Hq + 1, rows=300)
 
 
 # ---------------------------------------------------------------- together
