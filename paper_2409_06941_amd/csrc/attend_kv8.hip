@@ -39,7 +39,7 @@ struct Attend8Args {
     int64_t q_stride, out_stride, pages_stride;
     const int32_t *q_begin, *pages, *lens;
     int32_t n_tokens, n_seqs, n_q_heads, max_q, max_len, window, sinks, page_shift, block_shift, group;
-    float q_power, rate;                   // scale * log2 e = q_power * rate: a power of two that goes into the queries, and the rest
+    float q_power, rate;                   // scale * log2 e = q_power * rate: a power of two, 1 at most, that goes into the queries, and the rest
     int32_t row_tiles, splits, split_len;  // row tiles of a sequence and key head; parts of its tiles of keys, and their length
     int32_t groups, units, first_unit;
     int32_t workers;                       // of a key head, among which its tiles of keys are dealt out evenly
@@ -911,7 +911,7 @@ int fr_attend_kv8_workspace_bytes(const fr_attend_kv8_desc* d, uint64_t* bytes_o
 int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream)
 {
     if (!d || !sizes_ok(*d) || !kv8_pages_ok(d->cache)) return FR_ERR_ARG;
-    if (!(d->scale > 0.0f) || std::isinf(d->scale)) return FR_ERR_ARG;
+    if (!(d->scale > 0.0f && d->scale <= 0x1p120f)) return FR_ERR_ARG;
     if (d->n_tokens == 0 || d->n_seqs == 0) return FR_OK;
     const fr_kv8_pages& c = d->cache;
     const int64_t width = (int64_t)d->n_q_heads * c.head_dim, most = (int64_t)1 << 45;
@@ -929,9 +929,14 @@ int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream)
     Attend8Args a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->pages, d->lens,
                      d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->max_len, d->window, d->sinks,
                      __builtin_ctz(c.page_size), __builtin_ctz(c.block), d->n_q_heads / c.n_kv_heads};
-    // With queries and keys as far apart as bfloat16 lets them be, a product of 32 bits would be beyond its range before the scale brings it back.
+    // With queries and keys as far apart as bfloat16 lets them be, a product of 32 bits would be beyond its range before a scale below 1 brings it back.
+    // Not more of it than 2^-64 goes into the queries: those down to 2^-62 lose nothing then, and sums up to 2^192 are in range.  A scale above 1 makes
+    // scores larger than the products, which need no help; into the queries it could take them beyond the type's range.
     int e = 0;
-    if (c.dtype == FR_DTYPE_BF16) std::frexp(d->scale, &e);
+    if (c.dtype == FR_DTYPE_BF16) {
+        std::frexp(d->scale, &e);
+        e = std::max(-64, std::min(0, e));
+    }
     a.q_power = std::ldexp(1.0f, e);
     a.rate = std::ldexp(d->scale, -e) * kLog2e;
     a.row_tiles = (int)p.row_tiles;
