@@ -1,4 +1,5 @@
 """The ends of what fr_attend_kv8 takes, the scale's among them, against the fp64 oracle or exact results."""
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -6,6 +7,8 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import paper_2409_06941_amd as fr                 # noqa: E402
+import test_gpu_cache8 as cases                   # noqa: E402
+from oracle import cache8, generation             # noqa: E402
 from test_gpu_cache8 import DT, I32, _attend_case          # noqa: E402
 
 SHAPES = [([40, 3, 190], [1, 1, 1]), ([190, 77], [100, 77])]           # few rows; many
@@ -70,3 +73,52 @@ def test_attend_scores_in_range_whatever_makes_them(dt, q, scale, byte, t):
         unit = 2.0 ** -8 if dt == "bf16" else 2.0 ** -11
         assert bool(((out[i, 0].double() - want).abs() <= (2 * unit + 2.0 ** -16) * (w @ v[:seen].abs()) + 2.0 ** -20).all()), i
         assert abs(float(lse[i, 0]) - float(torch.logsumexp(score, 0))) <= 2.0 ** -20 * (1 + abs(float(torch.logsumexp(score, 0)))), i
+
+
+class _Uncut(cases.Numbers):
+    """What codes and scale bytes would stand for if one end of the range did not cut the bytes."""
+
+    def __init__(self, end, *of):
+        super().__init__(*of)
+        self.end = end
+
+    def __getitem__(self, at):
+        p, h, o = at
+        lo, hi = cache8.RANGE[self.dt]
+        byte = np.clip(self.scale[p, h, o // self.block].astype(np.int64), -1000 if self.end == "lo" else lo, 1000 if self.end == "hi" else hi)
+        return cache8.VALUES[self.codes[p, h, o]] * (2.0 ** (byte - 127))[:, None]
+
+
+# Most blocks' bytes lie beyond the cut, the others next to it; scores are of order one.
+@pytest.mark.parametrize("dt,end,scales,std,scale", [
+    ("bf16", "lo", (0, 11), 2.0 ** -12, 2.0 ** 119), ("bf16", "hi", (245, 255), 2.0 ** -20, 2.0 ** -109),
+    ("f16", "lo", (100, 113), 1.0, 2.0 ** 5), ("f16", "hi", (133, 145), 2.0 ** -8, 2.0 ** -9)])
+def test_attend_scale_bytes_are_cut(monkeypatch, dt, end, scales, std, scale):
+    print("attend cut", dt, end, flush=True)
+    spread, row, plain = [], generation.attend_row, cases.Numbers
+
+    def noting(q, k, v, scale):
+        if len(k):
+            spread.append(float(scale * np.abs(k @ q).max()))
+        return row(q, k, v, scale)
+    monkeypatch.setattr(generation, "attend_row", noting)
+
+    def call(lens, new):
+        _attend_case(dt, 4, 2, 128, 16, 1, lens, new, 15, scales=scales, scale=scale, std=std)
+        _attend_case(dt, 4, 2, 64, 16, 16, lens, new, 16, 50, 3, scales=scales, scale=scale, std=std)
+    for lens, new in SHAPES:
+        call(lens, new)
+    # (the bound of the comparison grows with 2^-17 of the largest score: nothing beside the type's rounding)
+    assert 1 < max(spread) < 16
+    # and the comparison sees a cut that is missing, of K's bytes alone and of V's alone
+    for wrong in (0, 1):
+        for lens, new in SHAPES:
+            made = []
+
+            def numbers(*of):
+                made.append(len(made))
+                return _Uncut(end, *of) if made[-1] % 2 == wrong else plain(*of)
+            monkeypatch.setattr(cases, "Numbers", numbers)
+            with np.errstate(all="ignore"), pytest.raises(AssertionError):
+                call(lens, new)
+            monkeypatch.setattr(cases, "Numbers", plain)
