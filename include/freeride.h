@@ -767,12 +767,14 @@ int fr_kv8_append(const fr_kv8_append_desc* d, void* stream);
  * sequence b at q_begin[b] .. q_begin[b + 1]; they are the last of its lens[b] keys.  Its token i of t has n = lens[b] - t + 1 + i keys up
  * to and with its own, and sees key j < n if
  *     window is 0, or j >= n - window, or j < sinks:
- * the window last ones and the first few, which stay visible.  out and lse are as in fr_attend_shared, of scores and values that the
- * codes and scales stand for, sums being held in 32 bits (of n > 2^11 values beyond 2^139 / n in magnitude they may leave its range).  With FR_DTYPE_BF16 the
- * power of two that a scale below 1 has, 2^-64 at least, goes into the queries first, so that a product is in range where its score is: elements of q
- * times it lose bits below 2^-126, those from 2^-62 on never do.  A token that sees nothing gets zeros and -infinity; keys that a token does not see do not change its result,
- * whatever they hold, and NaN among those that it sees shows as the formula says.  Page ids of keys that no token of the call sees are not
- * used: their pages may have been given to others.  A sequence's pages may also be another's: a prompt may lie there once for several.
+ * the window last ones and the first few, which stay visible.  out and lse are as in fr_attend_shared, of scores and values that the codes and
+ * scales stand for, sums being held in 32 bits.  A token that sees nothing gets zeros and -infinity; keys that a token does not see do not
+ * change its result, whatever they hold, and NaN among those that it sees shows as the formula says.  With FR_DTYPE_BF16
+ *     the power of two that a scale below 1 has, 2^-64 at least, goes into the queries first, so that a product is in range where its score is:
+ *     elements of q times it lose bits below 2^-126, those from 2^-62 on never do;
+ *     sums of n > 2^11 values beyond 2^139 / n in magnitude may leave the range, and values are added up in steps of 2^-129.
+ * Page ids of keys that no token of the call sees are not used: their pages may have been given to others.  A sequence's pages may also be
+ * another's: a prompt may lie there once for several.
  * Bounds on the device's numbers: a page id outside the cache counts as the nearest one inside, lens is cut to 0 .. max_len, q_begin to
  * 0 .. n_tokens, a sequence's tokens beyond max_q and tokens in no sequence are not computed.
  */

@@ -122,3 +122,45 @@ def test_attend_scale_bytes_are_cut(monkeypatch, dt, end, scales, std, scale):
             with np.errstate(all="ignore"), pytest.raises(AssertionError):
                 call(lens, new)
             monkeypatch.setattr(cases, "Numbers", plain)
+
+
+@pytest.mark.parametrize("t", [1, 40])
+@pytest.mark.parametrize("Hq,n", [(1, 20), (4, 2048)])
+def test_attend_largest_and_smallest_values(t, Hq, n):
+    # bfloat16: 2^11 values of the largest magnitude, all of one sign; and values of some 2^-126 .. 2^-118
+    print("attend values", t, Hq, n, flush=True)
+    D, page = 64, 16
+    pages = -(-n // page)
+    g = torch.Generator(device="cuda").manual_seed(n + t)
+    codes = lambda lo, hi: torch.randint(lo, hi, (pages, 1, page, D), generator=g, device="cuda", dtype=torch.uint8)
+    byte = lambda x: torch.full((pages, 1, 1), x, device="cuda", dtype=torch.uint8)
+    q = torch.randn((t, Hq, D), generator=g, device="cuda").to(torch.bfloat16)
+    i32 = lambda x: torch.tensor(x, dtype=I32, device="cuda")
+
+    def call(ck, cv, v_byte):
+        cache, out = fr.Kv8Pages(ck, cv, byte(119), byte(v_byte), torch.bfloat16), torch.full_like(q, 9.0)
+        lim = dict(max_len=n, max_q=t)
+        ws = torch.empty(max(1, fr.fr_attend_kv8_workspace_bytes(cache, q, 1, **lim)), dtype=torch.uint8, device="cuda")
+        fr.fr_attend_kv8(cache, q, out, torch.arange(pages, dtype=I32, device="cuda").view(1, -1), i32([n]), D ** -0.5, q_begin=i32([0, t]), workspace=ws, **lim)
+        torch.cuda.synchronize()
+        return out.double().cpu().numpy()
+    ck = codes(0, 256) & 0xbf                          # (below 2: scores of some units)
+    top = call(ck, torch.full_like(ck, 0x7e), 250)
+    # equal values: off by the weights' rounding and the result's
+    assert not top[: max(0, t - n)].any()              # (they see nothing)
+    top = top[max(0, t - n):]
+    assert np.all(np.abs(top / (448 * 2.0 ** 119) - 1) <= 2 * 2.0 ** -8 + 2.0 ** -16)
+    cv = codes(0, 17)
+    got = call(ck, cv, 3)
+    K = cache8.VALUES[ck.cpu().numpy()].transpose(0, 2, 1, 3).reshape(-1, D) * 2.0 ** (119 - 127)
+    V = cache8.VALUES[cv.cpu().numpy()].transpose(0, 2, 1, 3).reshape(-1, D) * 2.0 ** -117
+    q = q.double().cpu().numpy()
+    for i in range(t):
+        for h in range(Hq):
+            seen = n - t + 1 + i
+            o, _, a, x = generation.attend_row(q[i, h], K[:seen], V[:seen], D ** -0.5)
+            if seen > 0:
+                # the bound of ordinary values; and sums of weights 2^-20 times theirs, the largest one 1 at least, whose steps are 2^-149: half a
+                # step for every eight keys or fewer that are added at once, for every time that the maximum rises, and for every part that is joined
+                near = (2.0 ** -8 + 2 * ((D + 4) * 2.0 ** -24 * x + 2.0 ** -20) + n * 2.0 ** -23) * a + 2.0 ** -8 * np.abs(o) + 2.0 ** -134 + (n / 8 + 64) * 2.0 ** -130
+                assert np.all(np.abs(got[i, h] - o) <= near), (i, h)
