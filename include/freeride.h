@@ -790,7 +790,7 @@ typedef struct fr_attend_kv8_desc {
     int64_t     pages_stride;      /* >= ceil(max_len / page_size)                                            */
     int32_t     n_tokens, n_seqs;  /* 0: nothing to do                                                        */
     int32_t     n_q_heads;         /* a multiple of n_kv_heads, up to 1024                                    */
-    int32_t     max_q;             /* upper bound of a sequence's tokens in this call, >= 1                   */
+    int32_t     max_q;             /* upper bound of a sequence's tokens in this call, >= 1; without q_begin 1 */
     int32_t     max_len;           /* 0 .. 2^31 - 8192                                                        */
     int32_t     window;            /* 0: all keys                                                             */
     int32_t     sinks;             /* >= 0                                                                    */

@@ -920,14 +920,16 @@ int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream)
         if (s % 8 || s > most || s < 0 || (d->n_tokens > 1 && s < width)) return FR_ERR_ARG;
     if (!d->q_begin && d->n_tokens != d->n_seqs) return FR_ERR_ARG;
     if (d->max_len && (!d->pages || !d->lens || d->pages_stride < ((int64_t)d->max_len + c.page_size - 1) / c.page_size || d->pages_stride > most)) return FR_ERR_ARG;
-    const Plan p = plan(*d, (int)fr_stream_cus((hipStream_t)stream));
+    fr_attend_kv8_desc sizes = *d;
+    if (!d->q_begin) sizes.max_q = 1;                              // (a token each, whatever a program's other calls have)
+    const Plan p = plan(sizes, (int)fr_stream_cus((hipStream_t)stream));
     if (p.base > kMostBlocks / 16) return FR_ERR_ARG;
-    const uint64_t need = part_bytes(*d);
+    const uint64_t need = part_bytes(sizes);
     if (need && (!d->workspace || ((uintptr_t)d->workspace & 255) || d->workspace_bytes < need)) return FR_ERR_ARG;
     const int64_t part_rows = p.workers ? p.workers * c.n_kv_heads * 2 * rows_of(p.kind) : p.splits > 1 ? p.base * p.splits * rows_of(p.kind) : 0;
-    if (part_rows > most_part_rows(*d)) return FR_ERR_ARG;        // (the plan keeps to it)
+    if (part_rows > most_part_rows(sizes)) return FR_ERR_ARG;        // (the plan keeps to it)
     Attend8Args a = {c, (const uint16_t*)d->q, (uint16_t*)d->out, d->lse, d->q_stride, d->out_stride, d->pages_stride, d->q_begin, d->pages, d->lens,
-                     d->n_tokens, d->n_seqs, d->n_q_heads, d->q_begin ? d->max_q : 1, d->max_len, d->window, d->sinks,
+                     d->n_tokens, d->n_seqs, d->n_q_heads, sizes.max_q, d->max_len, d->window, d->sinks,
                      __builtin_ctz(c.page_size), __builtin_ctz(c.block), d->n_q_heads / c.n_kv_heads};
     // With queries and keys as far apart as bfloat16 lets them be, a product of 32 bits would be beyond its range before a scale below 1 brings it back.
     // Not more of it than 2^-64 goes into the queries: those down to 2^-62 lose nothing then, and sums up to 2^192 are in range.  A scale above 1 makes

@@ -1,0 +1,36 @@
+"""Calls of the operators of a cache held in 8 bits that go another way than their sizes alone would say."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import paper_2409_06941_amd as fr              # noqa: E402
+from test_gpu_cache8 import DT, I32, _attend_case          # noqa: E402
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("Hq,Hk,longest", [(16, 2, 300), (8, 8, 20), (8, 1, 5000)])
+def test_one_token_a_sequence_whatever_max_q(dt, Hq, Hk, longest):
+    # without q_begin every sequence has one token: a larger max_q, that of a program's other calls, changes neither result nor kernel
+    print("attend max_q", dt, Hq, Hk, longest, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(longest)
+    n, D, page = 9, 64, 16
+    width = -(-longest // page)
+    codes = [torch.randint(0, 120, (n * width, Hk, page, D), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    scale = [torch.full((n * width, Hk, 1), 118, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    cache = fr.Kv8Pages(*codes, *scale, DT[dt])
+    q = torch.randn((n, Hq, D), generator=g, device="cuda").to(DT[dt])
+    table = torch.randperm(n * width, generator=g, device="cuda").to(I32).view(n, width)
+    lens = torch.randint(1, longest, (n,), generator=g, device="cuda").to(I32)
+    lens[0], lens[1] = longest, 0
+    results = []
+    for max_q in (1, 8, 64, 1 << 20):
+        out, lse = torch.full_like(q, 9.0), torch.full((n, Hq), 9.0, device="cuda")
+        ws = torch.full((max(1, fr.fr_attend_kv8_workspace_bytes(cache, q, n, max_len=longest)),), 255, dtype=torch.uint8, device="cuda")
+        fr.fr_attend_kv8(cache, q, out, table, lens, 0.125, max_len=longest, max_q=max_q, lse=lse, workspace=ws)
+        torch.cuda.synchronize()
+        results.append((out, lse))
+    for out, lse in results[1:]:
+        assert torch.equal(out, results[0][0]) and torch.equal(lse, results[0][1])
