@@ -812,7 +812,7 @@ int fr_attend_kv8(const fr_attend_kv8_desc* d, void* stream);
  *   pairs with a page id outside the cache (padding), pairs of a page with itself,
  *   pairs whose target a later pair has as well (the last one counts),
  *   pairs whose source is the target of another pair that is not padding (it would be read while it is written);
- * copied[i] says of each pair whether it was carried out.
+ * copied[i] says of each pair whether it was carried out.  A call without caches does nothing: it does not write copied either.
  */
 typedef struct fr_kv_copy_desc {
     const fr_kv_pages*  caches;    /* host, [n_caches], read during the call; NULL if there are none          */

@@ -34,3 +34,10 @@ def test_one_token_a_sequence_whatever_max_q(dt, Hq, Hk, longest):
         results.append((out, lse))
     for out, lse in results[1:]:
         assert torch.equal(out, results[0][0]) and torch.equal(lse, results[0][1])
+
+
+def test_copy_without_caches_touches_nothing():
+    source, copied = torch.arange(3, dtype=I32, device="cuda"), torch.full((3,), 7, dtype=I32, device="cuda")
+    fr.fr_kv_copy_pages([], source, source + 3, copied=copied)
+    torch.cuda.synchronize()
+    assert copied.tolist() == [7, 7, 7]
