@@ -41,3 +41,15 @@ def test_copy_without_caches_touches_nothing():
     fr.fr_kv_copy_pages([], source, source + 3, copied=copied)
     torch.cuda.synchronize()
     assert copied.tolist() == [7, 7, 7]
+
+
+@pytest.mark.parametrize("dt,Hq,Hk,D", [("bf16", 8, 1, 64), ("f16", 12, 2, 128)])
+@pytest.mark.parametrize("seqs,window", [(64, 0), (65, 0), (130, 50)])
+def test_attend_many_rows_of_many_sequences(dt, Hq, Hk, D, seqs, window):
+    # 128 rows a workgroup; up to 64 sequences go by falling lengths, more of them in their own order
+    print("attend many rows", dt, Hq, Hk, D, seqs, window, flush=True)
+    rng = np.random.default_rng(seqs)
+    new = [int(x) for x in rng.integers(0, 10, seqs)]
+    lens = [int(x) for x in rng.integers(0, 150, seqs)]
+    new[3], new[-1], lens[-1] = 40, 9, 333
+    _attend_case(dt, Hq, Hk, D, 16, 8, lens, new, seqs, window, 3 if window else 0)
