@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import paper_2409_06941_amd as fr              # noqa: E402
-from test_gpu_cache8 import DT, I32, _attend_case          # noqa: E402
+from test_gpu_cache8 import DT, I32, _append_case, _attend_case          # noqa: E402
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
@@ -53,3 +53,18 @@ def test_attend_many_rows_of_many_sequences(dt, Hq, Hk, D, seqs, window):
     lens = [int(x) for x in rng.integers(0, 150, seqs)]
     new[3], new[-1], lens[-1] = 40, 9, 333
     _attend_case(dt, Hq, Hk, D, 16, 8, lens, new, seqs, window, 3 if window else 0)
+
+
+@pytest.mark.parametrize("T", [767, 768, 1023, 2047, 2048, 2560, 8192])
+@pytest.mark.parametrize("block", [1, 16])
+def test_append_tokens_of_a_workgroup(T, block):
+    # how many tokens' keys and values a workgroup has goes by their number: runs that begin and end at its border and elsewhere, padding
+    print("append", T, block, flush=True)
+    rng = np.random.default_rng(T)
+    slot, at = [], 0
+    while len(slot) < T:
+        n = int(rng.integers(1, 40))
+        begin = at * 16 + int(rng.integers(0, 16))
+        slot += [begin + i for i in range(n)] if n < 30 else [-1] * (n - 29)
+        at += 4
+    _append_case("bf16", T, 2, 1, 64, 16, block, 64, 0, T, slot=slot[:T], pages=at)
