@@ -820,7 +820,16 @@ struct Plan {
     int64_t row_tiles = 1, base = 0, splits = 1, split_len = 1;        // base: sequences x key heads x row tiles
     int64_t workers = 0;                   // of a key head; 0: every item has the same number of parts
 };
-constexpr int64_t kMostFew = 32;           // rows of a sequence that are few
+// Rows of a sequence and key head that are few: up to three items of 16, each of which goes through the keys, against 128 rows of which some are none.
+// us by items of 16 and by 128 rows, head_dim 128, sequences x key heads:
+//                                  24 rows        32        40        48        64        96
+//   64 x 8, up to 4000 keys       92   114   99   116  111  111  119  121  131  121  179  135
+//   8 x 8, up to 4000             26    46   26    45   30   50   32   50   35   46   43   53
+//   33 x 5, window 1000           24    48   24    49   26   51   26   50   28   54   33   55
+//   128 x 8, up to 500            31    51   30    49   43   56   42   55   49   55   66   58
+//   1 x 8, 40000                  35    50   36    51   46   55   48   56   54   58   64   63
+//   8 x 8, up to 40000           135   155  151   158  177  173  176  167  235  171  341  189
+constexpr int64_t kMostFew = 48;
 constexpr int64_t kMostDealt = 512;        // items of a key head that are dealt out evenly: each worker looks at all of them
 constexpr int64_t kMostParts = 128;        // of a row: what the join reads in one go
 constexpr int64_t kMostBlocks = 0x7fffffff;

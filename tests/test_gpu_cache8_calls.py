@@ -68,3 +68,22 @@ def test_append_tokens_of_a_workgroup(T, block):
         slot += [begin + i for i in range(n)] if n < 30 else [-1] * (n - 29)
         at += 4
     _append_case("bf16", T, 2, 1, 64, 16, block, 64, 0, T, slot=slot[:T], pages=at)
+
+
+@pytest.mark.parametrize("dt,D", [("bf16", 128), ("f16", 64)])
+@pytest.mark.parametrize("Hq,Hk,new", [(8, 1, 4), (11, 1, 3), (16, 2, 5), (10, 2, 9), (24, 3, 6), (7, 1, 7)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_attend_about_as_many_rows_as_are_few(dt, D, Hq, Hk, new, window, sinks):
+    # 32 to 49 rows of a sequence and key head: two, three tiles of 16, and the first that go by 128
+    print("attend rows", dt, D, Hq, Hk, new, window, flush=True)
+    lens = [0, 1, new, 31, 33, 130, 700, 257]
+    _attend_case(dt, Hq, Hk, D, 16, 8, lens, [min(n, new) for n in lens], Hq + new, window, sinks, rows=400)
+    _attend_case(dt, Hq, Hk, D, 16, 1, [90, 40], [new, new - 1], Hq + new, window, sinks, nan_at=[(0, 89, 3, True), (0, 30, 8, True), (1, 37, 0, False)])
+
+
+@pytest.mark.parametrize("dt,D", [("bf16", 128), ("f16", 64)])
+def test_attend_three_tiles_of_rows_dealt_out_evenly(dt, D):
+    rng = np.random.default_rng(3)
+    lens = [int(x) for x in rng.integers(0, 17000, 5)]
+    lens[0], lens[3] = 17000, 4
+    _attend_case(dt, 56, 8, D, 16, 8, lens, [6, 5, 0, 4, 6], 9, rows=150)
