@@ -634,8 +634,11 @@ __global__ __launch_bounds__(kThreads, kKind == kWideRows ? 2 : 4) void k_attend
 }
 
 // How the tiles of a key head's items (a sequence, 16 of its rows) are dealt out among workers: all items one behind the other, `length` tiles each.
-// Where the items are about as long as that, by whole items: nothing has to be joined then.  An item's weight is its tiles, 1 if it has rows that see
-// nothing.  Every wavefront finds this out for itself, 64 items at a time.
+// Where no item has more than twice that, by whole items: nothing has to be joined then.  It is so where a call has room for long sequences (max_len) and
+// they are short: with 16 sequences of up to 65536 tokens, all of which have up to 450, 25 -> 18 us, equal ones of 450 21 -> 18, of 512 17.4 -> 18.4.
+// Eight tiles at least, two a wavefront: 4 cost such sequences of up to 200 and 400 tokens 24 and 20 us instead of 15 and 18, 16 those of up to 1000 27
+// instead of 22; long ones do not care.  An item's weight is its tiles, 1 if it has rows that see nothing.  Every wavefront finds this out for itself,
+// 64 items at a time.
 struct Share {
     int32_t length, before, weight;        // tiles of a worker; tiles before an item, and its own
     int32_t item;
@@ -661,7 +664,7 @@ struct Share {
             most = max(most, top);
         }
         length = max((all + a.workers - 1) / a.workers, 8);
-        by_items = (int64_t)most * ((items + a.workers - 1) / a.workers) * 8 <= (int64_t)length * 9;
+        by_items = (int64_t)most * ((items + a.workers - 1) / a.workers) <= (int64_t)length * 2;
         item = items, before = all, weight = 0;
         const int64_t from = of < 0 ? (int64_t)~of * length : 0;
         int at = 0;

@@ -87,3 +87,14 @@ def test_attend_three_tiles_of_rows_dealt_out_evenly(dt, D):
     lens = [int(x) for x in rng.integers(0, 17000, 5)]
     lens[0], lens[3] = 17000, 4
     _attend_case(dt, 56, 8, D, 16, 8, lens, [6, 5, 0, 4, 6], 9, rows=150)
+
+
+@pytest.mark.parametrize("longest", [1, 250, 288, 300, 511, 512, 513, 600, 1000])
+@pytest.mark.parametrize("kind", ["equal", "any"])
+def test_attend_short_sequences_with_room_for_long_ones(longest, kind):
+    # tiles are dealt out evenly among workers, by whole sequences where all of them are short
+    print("attend short", longest, kind, flush=True)
+    rng = np.random.default_rng(longest)
+    lens = [longest] * 16 if kind == "equal" else [int(x) for x in rng.integers(0, longest + 1, 15)] + [longest]
+    _attend_case("bf16", 16, 8, 64, 16, 8, lens, [1] * 16, longest, max_len=40000)
+    _attend_case("f16", 6, 2, 128, 16, 8, lens, [1] * 16, longest, max_len=140000)
