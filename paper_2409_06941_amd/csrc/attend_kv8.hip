@@ -834,7 +834,9 @@ struct Plan {
 //   8 x 8, up to 40000           135   155  151   158  177  173  176  167  235  171  341  189
 constexpr int64_t kMostFew = 48;
 constexpr int64_t kMostDealt = 512;        // items of a key head that are dealt out evenly: each worker looks at all of them
-constexpr int64_t kMostParts = 128;        // of a row: what the join reads in one go
+// Parts of a row, at most: what the join's threads read in one go (32, 64, 128 and 256: two sequences of 30000 keys with one key head 22, 16, 13.3, 13.3 us, one of
+// 60000 33, 22, 16, 14.5, one of 60000 with 8 key heads 35, 29, 30, 32).
+constexpr int64_t kMostParts = 128;
 constexpr int64_t kMostBlocks = 0x7fffffff;
 
 // Parts are no more than give so many items in all: four a unit, which are on it at once.  Of few rows three times as many, where there are few sequences
@@ -857,6 +859,10 @@ Plan plan(const fr_attend_kv8_desc& d, int cus)
     // tiles of keys that a row tile sees, at most
     int64_t keys = d.max_len;
     if (d.window) keys = std::min<int64_t>(keys, (int64_t)d.window + std::min<int64_t>(up(rows_of(p.kind), group), d.max_q) + d.sinks + 3 * tile);
+    // A part has two tiles a wavefront at least where rows are few, and two tiles of 128 rows.  Few rows, 4 and 8 tiles, 32 heads, 8 key heads of 128: 8 sequences of
+    // 4000 keys 24.9, 20.6 us, 16 of 2000 23.3, 20.4, 3 of up to 9000 19.5, 17.8, 4 of 3000 15.0, 15.2, one of 1000 10.1, 11.7 (16 tiles 14.0), two of 700 9.8, 12.1.
+    // Many, 1, 2, 4 and 8 tiles: 300 tokens behind as many 47, 34, 30, 30, 300 alone 29, 24, 25, 20, 2 x 64 behind 2000 50, 35, 34, 32, 20 behind 1000 with 16 heads of
+    // 64 16.2, 16.5, 18, 22.
     const int64_t tiles = std::max<int64_t>(up(keys, tile), 1), least = p.kind == kWideRows ? 2 : 8;
     const int64_t want = std::max<int64_t>(1, std::min({up(tiles, least), most_items(p.kind, p.base, cus) / p.base, kMostParts}));
     p.split_len = up(tiles, want);
@@ -895,6 +901,8 @@ template <typename T, int D, Kind kKind> int launch(Attend8Args a, const Plan& p
         for (int64_t first = 0; first < all; first += kBlocksALaunch)
             hipLaunchKernelGGL((k_attend8_join<T, D, kKind, lanes>), dim3((unsigned)std::min<int64_t>(all - first, kBlocksALaunch)), dim3(kThreads), 0, stream, a, first);
     };
+    // Threads of the join for every eight elements, 1, 4 and 16: one sequence of 60000 keys, 128 parts, 45, 33, 30 us, two of 8000, 32 parts, 18.1, 15.5, 15.9, 4 of
+    // 3000, 12 parts, 14.2, 14.7, 15.5, 64 of up to 4000, 2 parts, 73, 79, 90; dealt out, 8 of up to 65536, 131, 128, 130.
     if (p.workers || (p.splits > 8 && p.splits <= 32)) join(std::integral_constant<int, 4>{});
     else if (p.splits > 32) join(std::integral_constant<int, 16>{});
     else if (p.splits > 1) join(std::integral_constant<int, 1>{});
