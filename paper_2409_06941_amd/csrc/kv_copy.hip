@@ -115,8 +115,10 @@ extern "C" int fr_kv_copy_pages(const fr_kv_copy_desc* d, void* stream)
     CopyArgs a = {};
     a.n_pages = n_pages;
     a.source = d->source, a.target = d->target, a.copied = d->copied, a.n_pairs = d->n_pairs;
-    // one cache a workgroup, more where there are so many pairs that looking at them takes as long as copying a page
-    a.share = std::max(1, d->n_pairs / 1024);
+    // One cache a workgroup, more where there are so many pairs that looking at them takes as long as copying a page.  16 caches, one for every 256, 512, 1024 pairs
+    // and one always: pages of 2 KB, 1024 pairs 33, 46, 71, 71 us, 2048 54, 68, 104, 176, 16384 1001, 1001, 1001, 5630; of 16 KB 202, 199, 197, 197, 419, 407, 400,
+    // 428, 3472, 3472, 3469, 8796.
+    a.share = std::max(1, d->n_pairs / 512);
     auto go = [&] {
         const int shares = (a.n_caches + a.share - 1) / a.share;          // (2^23 / 2 pairs a launch are at least 64 of the most that a call has)
         for (int done = 0; done < shares; done += kMostThreads / kThreads / 2 / a.n_pairs) {

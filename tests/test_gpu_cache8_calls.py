@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import paper_2409_06941_amd as fr              # noqa: E402
-from test_gpu_cache8 import DT, I32, _append_case, _attend_case          # noqa: E402
+from test_gpu_cache8 import DT, I32, _append_case, _attend_case, _copy_case          # noqa: E402
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
@@ -98,3 +98,12 @@ def test_attend_short_sequences_with_room_for_long_ones(longest, kind):
     lens = [longest] * 16 if kind == "equal" else [int(x) for x in rng.integers(0, longest + 1, 15)] + [longest]
     _attend_case("bf16", 16, 8, 64, 16, 8, lens, [1] * 16, longest, max_len=40000)
     _attend_case("f16", 6, 2, 128, 16, 8, lens, [1] * 16, longest, max_len=140000)
+
+
+@pytest.mark.parametrize("n", [511, 512, 1023, 1024, 1537])
+def test_copy_caches_of_a_workgroup(n):
+    rng = np.random.default_rng(n)
+    source, target = np.full(n, -1), rng.integers(0, 23, n)
+    for i, (a, b) in zip((0, n // 3, n // 2, n - 1), ((1, 2), (1, 7), (4, 5), (6, 2))):
+        source[i], target[i] = a, b
+    _copy_case([(8, 3, 8, 64, 4, "slots")] * 5 + [(16, 2, 4, 128, 1, "heads")], source.tolist(), target.tolist(), n)
