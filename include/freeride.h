@@ -774,7 +774,8 @@ int fr_kv8_append(const fr_kv8_append_desc* d, void* stream);
  *     elements of q times it lose bits below 2^-126, those from 2^-62 on never do;
  *     sums of n > 2^11 values beyond 2^139 / n in magnitude may leave the range, and values are added up in steps of 2^-129.
  * Page ids of keys that no token of the call sees are not used: their pages may have been given to others.  A sequence's pages may also be
- * another's: a prompt may lie there once for several.
+ * another's: a prompt may lie there once for several.  How a call is cut follows max_q and max_len: a long prompt and many single tokens take
+ * several times as long in one call as in two.
  * Bounds on the device's numbers: a page id outside the cache counts as the nearest one inside, lens is cut to 0 .. max_len, q_begin to
  * 0 .. n_tokens, a sequence's tokens beyond max_q and tokens in no sequence are not computed.
  */

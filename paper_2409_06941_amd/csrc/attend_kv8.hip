@@ -8,9 +8,9 @@
 //
 // The heads that share a key head, and all tokens of a sequence, are rows of one matrix product with its keys.
 // What bounds it:
-//   Decoding from long caches, the reading: 128 sequences of 4096 keys each with 8 key heads, 1.07 GB, 190 us, 5.6 TB/s (the same loads without a
+//   Decoding from long caches, the reading: 128 sequences of 4096 keys each with 8 key heads, 1.07 GB, 192 us, 5.6 TB/s (the same loads without a
 //     product 5.9; a kernel that only reads one array from end to end 6.5).  Where lengths differ, units that have nothing left: 8 of 20000 to 65536
-//     131 us, 4.9 TB/s, 64 of up to 4000 75 us, 3.6.
+//     131 us, 4.9 TB/s, 64 of up to 4000 76 us, 3.6.
 //   Prompts, the vector units beside the matrix cores (2 exps and 5 other operations of every two weights, and half a conversion of a code):
 //     8 sequences of 2048 tokens behind 6144, 32 heads, 1.92 TFLOP in 2.0 ms, 0.96 PFLOP/s.
 //   A few short sequences, the launch: 6 us.
@@ -120,8 +120,9 @@ template <Kind kKind, int D> struct Lds8 {
 // The work of one workgroup: rows `row0` .. of `rows` against tiles u0 .. u1 of their keys.
 //
 // kFewRows: 16 rows, blocks of 16 x 16 x 32.  Codes come to registers, a tile ahead, 8 KB a wavefront at head_dim 128; with what a lane's
-// places are made anew where they are used, its registers leave room for four workgroups a unit (166 -> 120; 128 sequences of 4096 keys, 64 heads,
-// 207 -> 185 us).  A lane's 16 bytes of a key are two fragments; values are made into numbers on the way into LDS, where they are transposed.
+// places are made anew where they are used, its registers leave room for four workgroups a unit (166 -> 123, 127 where tiles are dealt out evenly, of 128 that
+// four have; 128 sequences' windows of 4096 keys, fp16, 64 heads, 207 -> 185 us).  A lane's 16 bytes of a key are two fragments; values are made into numbers on the way
+// into LDS, where they are transposed.
 //
 // kWideRows: a wavefront's 32 rows are the columns of 32 x 32 x 16 blocks; weights go from the one product to the next without passing
 // through LDS.  A wavefront makes a quarter of every tile's codes into numbers, which all four then read: 32 conversions beside 32 MFMAs.
@@ -841,7 +842,7 @@ constexpr int64_t kMostBlocks = 0x7fffffff;
 
 // Parts are no more than give so many items in all: four a unit, which are on it at once.  Of few rows three times as many, where there are few sequences
 // and heads: they even out lengths that differ (8 sequences of up to 65536 tokens with 8 key heads 125 -> 114 us; with more sequences than that there is
-// no gain, and of equal lengths they begin and end more often: 128 of 4096 tokens 185 us in one part, 197 in two).
+// no gain, and of equal lengths they begin and end more often: 128 windows of 4096 tokens 185 us in one part, 197 in two).
 int64_t most_items(Kind k, int64_t base, int64_t cus) { return (k == kFewRows && 2 * base <= cus ? 12 : 4) * cus; }
 
 int64_t rows_a_seq(const fr_attend_kv8_desc& d) { return (int64_t)std::min(d.max_q, d.n_tokens) * (d.n_q_heads / d.cache.n_kv_heads); }
