@@ -363,11 +363,11 @@ extern "C" int fr_kv8_append(const fr_kv8_append_desc* d, void* stream)
                      d->q_stride, d->q_out_stride, c.n_pages * (int64_t)c.page_size, d->slot, d->position, d->rotary, d->n_positions,
                      d->rotary_dim, d->style, d->n_q_heads, __builtin_ctz(c.page_size), d->n_tokens};
     // A block's tokens are stored by the workgroup that has its first one, so that with blocks of 16 and a token a workgroup 15 of 16 only look; tokens in
-    // blocks of their own are one after another where a workgroup has more than four.  32 + 2 x 8 heads of 128, by 1, 4, 8 and 16 tokens a workgroup:
-    //   prompts, blocks of 16: 512 tokens 19.4, 15.5, 14.8, 14.8 us, 1024 32, 16, 15, 16, 2048 55, 22, 17, 17, 4096 109, 39, 27, 21, 8192 224, 81, 56, 44
-    //   a token a sequence: 512 7.4, 8.1, 12.6, 22 us, 768 8.7, 8.9, 13.5, 23, 1024 11.6, 9.4, 14.3, 24, 2048 20, 13, 15, 25
-    // and 20 + 2 x 5 heads of 64 with blocks of 1: 2048 12.0, 8.4, 9.3, 15.2, 4096 21, 13.8, 13.2, 16.1, 8192 39, 25, 24, 24.  (Two tokens: slower than four.)
-    a.share = d->n_tokens < 768 ? 1 : std::max(4, std::min(16, d->n_tokens / 512));
+    // blocks of their own are one after another where a workgroup has more than four.  32 + 2 x 8 heads of 128, blocks of 16, by 1, 4, 8 and 16 tokens a workgroup:
+    //   prompts: 1024 tokens 32, 16, 15, 16 us, 2048 55, 22, 17, 17, 4096 109, 39, 27, 21, 8192 224, 81, 56, 44; of 300 each, 3000 31, 24, 25, 29, 6000 54, 37, 35, 37
+    //   a token a sequence: 512 7.4, 8.1, 12.6, 22, 1024 11.6, 9.4, 14.3, 24, 2048 20, 13, 15, 25;  two: 1022 12.5, 14.2, 19.5, 28, 2044 22, 17, 21, 29, 4100 44, 30, 26, 33
+    // and 20 + 2 x 5 heads of 64 with blocks of 1: 2048 12.0, 8.4, 9.3, 15.2, 4096 21, 13.8, 13.2, 16.1, 8192 39, 25, 24, 24.  (Other numbers are no faster than these.)
+    a.share = d->n_tokens < 1024 ? 1 : d->n_tokens < 4096 ? 4 : d->n_tokens < 8192 ? 8 : 16;
     a.stores = (d->n_tokens + (int64_t)a.share - 1) / a.share;
     const int64_t all = a.stores + (d->n_q_heads ? d->n_tokens : 0);
     for (a.first = 0; a.first < all; a.first += kMostThreads / kThreads) {

@@ -55,7 +55,7 @@ def test_attend_many_rows_of_many_sequences(dt, Hq, Hk, D, seqs, window):
     _attend_case(dt, Hq, Hk, D, 16, 8, lens, new, seqs, window, 3 if window else 0)
 
 
-@pytest.mark.parametrize("T", [767, 768, 1023, 2047, 2048, 2560, 8192])
+@pytest.mark.parametrize("T", [767, 1023, 1024, 2047, 4095, 4096, 8192])
 @pytest.mark.parametrize("block", [1, 16])
 def test_append_tokens_of_a_workgroup(T, block):
     # how many tokens' keys and values a workgroup has goes by their number: runs that begin and end at its border and elsewhere, padding
